@@ -352,6 +352,39 @@ int moe_layer_fwd(const moe_layer* layer, const char** where, hipStream_t stream
 int moe_layer_bwd(const moe_layer* layer, const char** where, hipStream_t stream);
 
 /*
+ * Layer norm, the layer's pre-norm (the residual stream x enters the layer as
+ * its norm; the layer's output is added to x by the caller):
+ *   mean[t] = (1/d) sum_c x[t,c];  rstd[t] = 1 / sqrt((1/d) sum_c (x[t,c] - mean[t])^2 + eps)
+ *   y[t,c]  = (x[t,c] - mean[t]) rstd[t] weight[c] + bias[c]
+ * x, y [T,d] dtype (y may be x); weight [d] fp32, bias [d] fp32 or NULL (none);
+ * mean, rstd [T] fp32 (the backward reads them).  eps must be finite and >= 0;
+ * a row of equal values needs eps > 0.
+ * Limits: d % 8 == 0, d <= 16384, T >= 0, every array 16-byte aligned except mean
+ * and rstd (4).
+ */
+int moe_layernorm_fwd(const void* x, const float* weight, const float* bias, int dtype, int T,
+                      int d, float eps, void* y, float* mean, float* rstd, hipStream_t stream);
+
+/*
+ * Backward of moe_layernorm_fwd, with xh = (x - mean) rstd and g = dy * weight:
+ *   dx[t,:] = dres[t,:] + rstd[t] (g - mean_c(g) - xh mean_c(g xh))
+ *   dw[c]  (+)= sum_t dy[t,c] xh[t,c];   db[c] (+)= sum_t dy[t,c]
+ * dy, x, dx [T,d] dtype; dres [T,d] dtype or NULL: the gradient that reaches x
+ * past the norm (the residual stream's); dx may be dy or dres.  dw [d] fp32, db
+ * [d] fp32 or NULL; they are added to when accumulate_dw != 0, else overwritten
+ * (zeros when T = 0).
+ * ws: device workspace (16-byte aligned) of at least
+ * moe_layernorm_bwd_workspace_size(T, d, dtype) bytes (which depends on the
+ * current device's compute-unit count); its contents on entry are ignored.
+ * Limits as for the forward.  The sums over t are taken in a fixed order.
+ */
+size_t moe_layernorm_bwd_workspace_size(int T, int d, int dtype);
+int moe_layernorm_bwd(const void* dy, const void* x, const float* weight, const float* mean,
+                      const float* rstd, int dtype, int T, int d, const void* dres, void* dx,
+                      float* dw, float* db, int accumulate_dw, void* ws, size_t ws_bytes,
+                      hipStream_t stream);
+
+/*
  * Round boundary: expert-wise pseudo-gradient of the resident experts and its
  * average over the expert's replica group (Alg. 2, aggregation of the sparse
  * parameters within expert replica groups; Sec. 3.4 "Round structure").

@@ -26,6 +26,7 @@ EXPORTS = [
     "moe_grouped_ffn_fwd_sets",
     "moe_grouped_ffn_bwd_workspace_size", "moe_grouped_ffn_bwd_sets", "moe_combine_fwd",
     "moe_combine_bwd", "moe_layer_fwd", "moe_layer_bwd",
+    "moe_layernorm_fwd", "moe_layernorm_bwd_workspace_size", "moe_layernorm_bwd",
     "moe_expert_delta", "moe_adamw_step", "moe_outer_nesterov", "moe_replica_mean",
     "moe_gen_placement", "moe_migration_map", "moe_copy_expert_rows", "moe_warmup_lr",
     "moe_adamw_step_rows", "moe_timing_enable", "moe_timing_collect",
@@ -67,6 +68,9 @@ _SIGS = {
     "moe_combine_bwd": (_I, [_P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P]),
     "moe_layer_fwd": (_I, [_P, C.POINTER(C.c_char_p), _P]),
     "moe_layer_bwd": (_I, [_P, C.POINTER(C.c_char_p), _P]),
+    "moe_layernorm_fwd": (_I, [_P, _P, _P, _I, _I, _I, _F, _P, _P, _P, _P]),
+    "moe_layernorm_bwd_workspace_size": (_Z, [_I, _I, _I]),
+    "moe_layernorm_bwd": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _Z, _P]),
     "moe_expert_delta": (_I, [_P, _P, C.POINTER(C.c_void_p), _I, _Z, _P, _P, _P]),
     "moe_adamw_step": (_I, [_P, _P, _P, _P, _Z, _I, _F, _F, _F, _F, _F, _P, _P]),
     "moe_outer_nesterov": (_I, [_P, _P, _P, _P, _Z, _F, _F, _P, _P]),
@@ -286,6 +290,23 @@ def moe_layer_fwd(layer, stream=None):
 
 def moe_layer_bwd(layer, stream=None):
     return _layer_call(lib().moe_layer_bwd, layer, stream)
+
+
+def moe_layernorm_fwd(x, weight, bias, dtype, T, d, eps, y, mean, rstd, stream=None):
+    return _check("moe_layernorm_fwd", lib().moe_layernorm_fwd(
+        _ptr(x), _ptr(weight), _ptr(bias), dtype, T, d, eps, _ptr(y), _ptr(mean), _ptr(rstd),
+        _stream(stream)))
+
+
+def moe_layernorm_bwd_workspace_size(T, d, dtype) -> int:
+    return lib().moe_layernorm_bwd_workspace_size(T, d, dtype)
+
+
+def moe_layernorm_bwd(dy, x, weight, mean, rstd, dtype, T, d, dres, dx, dw, db, accumulate_dw, ws,
+                      ws_bytes, stream=None):
+    return _check("moe_layernorm_bwd", lib().moe_layernorm_bwd(
+        _ptr(dy), _ptr(x), _ptr(weight), _ptr(mean), _ptr(rstd), dtype, T, d, _ptr(dres), _ptr(dx),
+        _ptr(dw), _ptr(db), accumulate_dw, _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def moe_expert_delta(theta_start, theta_now, peers, n_peers, n_params, delta_local, delta_avg,

@@ -469,6 +469,55 @@ int moe_layer_bwd(const moe_layer* l, const char** where, hipStream_t stream) {
   return ok();
 }
 
+namespace {
+int check_norm(int dtype, int T, int d) {
+  int r;
+  if ((r = check_dtype(dtype)) != MOE_OK) return r;
+  REQUIRE(T >= 0 && d >= 1, "bad sizes T = %d, d = %d", T, d);
+  SUPPORT(d % 8 == 0, "d = %d must be a multiple of 8", d);
+  SUPPORT(d <= moe::kMaxNormWidth, "d = %d: at most %d", d, moe::kMaxNormWidth);
+  return MOE_OK;
+}
+}  // namespace
+
+int moe_layernorm_fwd(const void* x, const float* weight, const float* bias, int dtype, int T,
+                      int d, float eps, void* y, float* mean, float* rstd, hipStream_t stream) {
+  int r;
+  if ((r = check_norm(dtype, T, d)) != MOE_OK) return r;
+  REQUIRE(std::isfinite(eps) && eps >= 0.f, "eps must be finite and >= 0");
+  REQUIRE(weight, "weight must not be NULL");
+  REQUIRE(T == 0 || (x && y && mean && rstd), "x, y, mean and rstd must not be NULL");
+  for (const void* p : {x, (const void*)weight, (const void*)bias, (const void*)y})
+    SUPPORT(p == nullptr || aligned16(p), "arrays must be 16-byte aligned");
+  return hip_status(moe::launch_norm_fwd(x, weight, bias, dtype == MOE_BF16, T, d, eps, y, mean,
+                                         rstd, stream),
+                    "moe_layernorm_fwd");
+}
+
+size_t moe_layernorm_bwd_workspace_size(int T, int d, int dtype) {
+  if (T < 0 || d < 1) return 0;
+  return moe::norm_bwd_ws_bytes(T, d, dtype == MOE_BF16);
+}
+
+int moe_layernorm_bwd(const void* dy, const void* x, const float* weight, const float* mean,
+                      const float* rstd, int dtype, int T, int d, const void* dres, void* dx,
+                      float* dw, float* db, int accumulate_dw, void* ws, size_t ws_bytes,
+                      hipStream_t stream) {
+  int r;
+  if ((r = check_norm(dtype, T, d)) != MOE_OK) return r;
+  REQUIRE(weight && dw, "weight and dw must not be NULL");
+  REQUIRE(T == 0 || (dy && x && mean && rstd && dx), "dy, x, mean, rstd and dx must not be NULL");
+  const size_t need = moe::norm_bwd_ws_bytes(T, d, dtype == MOE_BF16);
+  REQUIRE(need == 0 || (ws && ws_bytes >= need), "workspace of %zu bytes needed (got %zu)", need,
+          ws_bytes);
+  for (const void* p : {dy, x, (const void*)weight, dres, (const void*)dx, (const void*)dw,
+                        (const void*)db, (const void*)ws})
+    SUPPORT(p == nullptr || aligned16(p), "arrays must be 16-byte aligned");
+  return hip_status(moe::launch_norm_bwd(dy, x, weight, mean, rstd, dtype == MOE_BF16, T, d, dres,
+                                         dx, dw, db, accumulate_dw, ws, stream),
+                    "moe_layernorm_bwd");
+}
+
 int moe_expert_delta(const float* theta_start, const float* theta_now,
                      const float* const* peers, int n_peers, size_t n_params, float* delta_local,
                      float* delta_avg, hipStream_t stream) {

@@ -103,6 +103,16 @@ hipError_t launch_outer_nesterov(float* start, float* now, const float* delta, f
 hipError_t launch_replica_mean(const float* local, const float* const* peers, int n_peers,
                                size_t n, float* out, hipStream_t s);
 
+// Layer norm (norm.hip), the MoE layer's pre-norm.  The backward's ws holds one partial
+// row of dw and db per block (norm_bwd_ws_bytes()); its contents on entry are ignored.
+constexpr int kMaxNormWidth = 16384;
+hipError_t launch_norm_fwd(const void* x, const float* w, const float* b, int bf16, int T, int d,
+                           float eps, void* y, float* mean, float* rstd, hipStream_t s);
+size_t norm_bwd_ws_bytes(int T, int d, int bf16);
+hipError_t launch_norm_bwd(const void* dy, const void* x, const float* w, const float* mean,
+                           const float* rstd, int bf16, int T, int d, const void* dres, void* dx,
+                           float* dw, float* db, int accumulate, void* ws, hipStream_t s);
+
 // Placement and migration (placement.hip).  gen_placement: false when the
 // constraints cannot be met.  launch_copy_expert_rows: src_row / dst_row are
 // host arrays of n_rows <= 256 entries (dst_row NULL = 0..n_rows-1).

@@ -23,6 +23,31 @@ import torch
 from . import binding as B
 
 
+def _check_tensor(name, t, shape, dtype, device, owner):
+    """Raise ValueError unless t is a contiguous tensor with this shape, dtype and device."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and t.device == device and t.is_contiguous()):
+        return
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor, got {type(t).__name__}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the {owner} on {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _check_current(device, owner):
+    """Raise ValueError unless device is the current one: kernels are launched on the current
+    device's stream."""
+    if device.type == "cuda" and torch.cuda.current_device() != device.index:
+        raise ValueError(f"the {owner} is on {device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+
+
 class ResidentMoELayer:
     def __init__(self, T, d, E, k, H, resident, dtype=torch.bfloat16, n_shared_hidden=0,
                  gate="softmax_topk", inv_tau=1.0, device="cuda", partitioned=False,
@@ -123,19 +148,7 @@ class ResidentMoELayer:
         """Raise ValueError unless t is a contiguous tensor on this layer's
         device with the given shape and dtype (the layer's own by default)."""
         dtype = self.dtype if dtype is None else dtype
-        if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
-                and t.device == self.resident.device and t.is_contiguous()):
-            return
-        if not isinstance(t, torch.Tensor):
-            raise ValueError(f"{name} must be a tensor, got {type(t).__name__}")
-        if t.device != self.resident.device:
-            raise ValueError(f"{name} is on {t.device}, the layer on {self.resident.device}")
-        if t.dtype != dtype:
-            raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
+        _check_tensor(name, t, shape, dtype, self.resident.device, "layer")
 
     def _check_weights(self, x, w_router, w_gate_up, w_down, shared_gate_up, shared_down):
         r1 = 2 if self.act == B.MOE_ACT_SWIGLU else 1
@@ -238,6 +251,86 @@ class ResidentMoELayer:
                         self.topk_w, self.logits, self.dtopk_w, self.dz, self.dw_router,
                         self.d_bias, self.dx, 1, self.ws_route, self.ws_route_bytes, stream)
         return self.dx
+
+
+class LayerNorm:
+    """The layer's pre-norm over [T, d] activations: moe_layernorm_fwd / _bwd on buffers of its
+    own (y, mean, rstd; dx, dw, db from the first backward on)."""
+
+    def __init__(self, T, d, dtype=torch.bfloat16, bias=True, eps=1e-5, device="cuda"):
+        self.T, self.d, self.eps, self.bias = int(T), int(d), float(eps), bool(bias)
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"unsupported dtype {dtype}")
+        self.dtype = dtype
+        self.dt = B.MOE_BF16 if dtype == torch.bfloat16 else B.MOE_F32
+        self.y = torch.empty(self.T, self.d, dtype=dtype, device=device)
+        self.mean, self.rstd = (torch.empty(self.T, dtype=torch.float32, device=device)
+                                for _ in range(2))
+        self.device = self.y.device
+        self.dx = self.dw = self.db = self.ws = None
+        self.ws_bytes = 0
+
+    def _check(self, name, t, shape, dtype):
+        _check_tensor(name, t, shape, dtype, self.device, "norm")
+
+    def forward(self, x, weight, bias=None, stream=None):
+        _check_current(self.device, "norm")
+        self._check("x", x, (self.T, self.d), self.dtype)
+        self._check("weight", weight, (self.d,), torch.float32)
+        if self.bias:
+            self._check("bias", bias, (self.d,), torch.float32)
+        elif bias is not None:
+            raise ValueError("a bias given to a norm built without one")
+        B.moe_layernorm_fwd(x, weight, bias, self.dt, self.T, self.d, self.eps, self.y, self.mean,
+                            self.rstd, stream)
+        return self.y
+
+    def backward(self, dy, x, weight, dres=None, mean=None, rstd=None, accumulate_dw=0,
+                 stream=None):
+        """dx (+ dres, the residual stream's gradient), with dw and db beside it.  mean and
+        rstd: of this x, where they are not those of the last forward."""
+        _check_current(self.device, "norm")
+        mean = self.mean if mean is None else mean
+        rstd = self.rstd if rstd is None else rstd
+        for name, t in (("dy", dy), ("x", x)) + ((("dres", dres),) if dres is not None else ()):
+            self._check(name, t, (self.T, self.d), self.dtype)
+        self._check("weight", weight, (self.d,), torch.float32)
+        self._check("mean", mean, (self.T,), torch.float32)
+        self._check("rstd", rstd, (self.T,), torch.float32)
+        if self.ws is None:
+            self.dx = torch.empty_like(self.y)
+            # zeros: the first backward may add to them
+            self.dw = torch.zeros(self.d, dtype=torch.float32, device=self.device)
+            self.db = torch.zeros_like(self.dw) if self.bias else None
+            self.ws_bytes = B.moe_layernorm_bwd_workspace_size(self.T, self.d, self.dt)
+            self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+        B.moe_layernorm_bwd(dy, x, weight, mean, rstd, self.dt, self.T, self.d, dres, self.dx,
+                            self.dw, self.db, accumulate_dw, self.ws, self.ws_bytes, stream)
+        return self.dx
+
+
+class PreNormMoELayer:
+    """ResidentMoELayer behind its pre-norm, as a transformer block has it: out = x + moe(norm(x)).
+
+    forward returns moe(norm(x)), which the caller adds to x; backward takes the gradient of
+    out and returns that of x, the residual's share included.  ``layer`` and ``norm`` hold the
+    outputs and gradients of the two."""
+
+    def __init__(self, T, d, E, k, H, resident, dtype=torch.bfloat16, norm_bias=True, eps=1e-5,
+                 device="cuda", **kw):
+        self.layer = ResidentMoELayer(T, d, E, k, H, resident, dtype=dtype, device=device, **kw)
+        self.norm = LayerNorm(T, d, dtype=dtype, bias=norm_bias, eps=eps, device=device)
+
+    def forward(self, x, norm_weight, norm_bias, w_router, w_gate_up, w_down, stream=None, **kw):
+        h = self.norm.forward(x, norm_weight, norm_bias, stream=stream)
+        return self.layer.forward(h, w_router, w_gate_up, w_down, stream=stream, **kw)
+
+    def backward(self, dout, x, norm_weight, w_router, w_gate_up, w_down, accumulate_dw=0,
+                 stream=None, **kw):
+        dh = self.layer.backward(dout, self.norm.y, w_router, w_gate_up, w_down,
+                                 accumulate_dw=accumulate_dw, stream=stream, **kw)
+        return self.norm.backward(dh, x, norm_weight, dres=dout, accumulate_dw=accumulate_dw,
+                                  stream=stream)
 
 
 def expert_delta(theta_start, theta_now, peers, delta_local=None, delta_avg=None, stream=None):
