@@ -385,6 +385,31 @@ int moe_layernorm_bwd(const void* dy, const void* x, const float* weight, const 
                       hipStream_t stream);
 
 /*
+ * MXFP4 (microscaled 4-bit floating point): every 32 consecutive values of a row are
+ * a block with one E8M0 scale byte s, standing for 2^(s - 127), and an E2M1 code
+ * each (sign in bit 3; magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6).
+ *   s = max(0, floor(log2 max|x|) - 2 + 127) over the block (0 for a block of zeros)
+ *   code = x / 2^(s - 127) rounded to the nearest value (ties to the even code);
+ *          past 6 it stays 6
+ * so the block's largest magnitude lands in [4, 8) of which (6, 8) saturates.  A
+ * block that holds an infinity or a NaN gets s = 255, which makes all of it NaN.
+ * codes  [rows, cols / 2] uint8: value 2i of a row in the low nibble of byte i.
+ * scales [rows, moe_mxfp4_scale_stride(cols)] uint8: a row's cols / 32 scales, padded
+ *        with zero bytes to whole words of four.
+ * x [rows, cols] dtype.  n_rows: device int32, only the first *n_rows rows are
+ * converted and the others left as they are (rows that a dispatch has filled:
+ * offsets + n_groups); NULL converts all.
+ * Limits: cols % 32 == 0, rows >= 0, rows * cols / 8 below 2^40; x and codes 16-byte aligned.
+ */
+int moe_mxfp4_scale_stride(int cols);
+int moe_mxfp4_quantize(const void* x, int dtype, int rows, int cols, const int32_t* n_rows,
+                       uint8_t* codes, uint8_t* scales, hipStream_t stream);
+/* The values that codes and scales stand for, rounded to dtype (every value of a
+ * scale that moe_mxfp4_quantize writes is exact in bf16 and fp32). */
+int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, int rows,
+                         int cols, const int32_t* n_rows, void* x, hipStream_t stream);
+
+/*
  * Round boundary: expert-wise pseudo-gradient of the resident experts and its
  * average over the expert's replica group (Alg. 2, aggregation of the sparse
  * parameters within expert replica groups; Sec. 3.4 "Round structure").

@@ -27,6 +27,7 @@ EXPORTS = [
     "moe_grouped_ffn_bwd_workspace_size", "moe_grouped_ffn_bwd_sets", "moe_combine_fwd",
     "moe_combine_bwd", "moe_layer_fwd", "moe_layer_bwd",
     "moe_layernorm_fwd", "moe_layernorm_bwd_workspace_size", "moe_layernorm_bwd",
+    "moe_mxfp4_scale_stride", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
     "moe_expert_delta", "moe_adamw_step", "moe_outer_nesterov", "moe_replica_mean",
     "moe_gen_placement", "moe_migration_map", "moe_copy_expert_rows", "moe_warmup_lr",
     "moe_adamw_step_rows", "moe_timing_enable", "moe_timing_collect",
@@ -71,6 +72,9 @@ _SIGS = {
     "moe_layernorm_fwd": (_I, [_P, _P, _P, _I, _I, _I, _F, _P, _P, _P, _P]),
     "moe_layernorm_bwd_workspace_size": (_Z, [_I, _I, _I]),
     "moe_layernorm_bwd": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _Z, _P]),
+    "moe_mxfp4_scale_stride": (_I, [_I]),
+    "moe_mxfp4_quantize": (_I, [_P, _I, _I, _I, _P, _P, _P, _P]),
+    "moe_mxfp4_dequantize": (_I, [_P, _P, _I, _I, _I, _P, _P, _P]),
     "moe_expert_delta": (_I, [_P, _P, C.POINTER(C.c_void_p), _I, _Z, _P, _P, _P]),
     "moe_adamw_step": (_I, [_P, _P, _P, _P, _Z, _I, _F, _F, _F, _F, _F, _P, _P]),
     "moe_outer_nesterov": (_I, [_P, _P, _P, _P, _Z, _F, _F, _P, _P]),
@@ -307,6 +311,20 @@ def moe_layernorm_bwd(dy, x, weight, mean, rstd, dtype, T, d, dres, dx, dw, db, 
     return _check("moe_layernorm_bwd", lib().moe_layernorm_bwd(
         _ptr(dy), _ptr(x), _ptr(weight), _ptr(mean), _ptr(rstd), dtype, T, d, _ptr(dres), _ptr(dx),
         _ptr(dw), _ptr(db), accumulate_dw, _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_mxfp4_scale_stride(cols) -> int:
+    return lib().moe_mxfp4_scale_stride(cols)
+
+
+def moe_mxfp4_quantize(x, dtype, rows, cols, n_rows, codes, scales, stream=None):
+    return _check("moe_mxfp4_quantize", lib().moe_mxfp4_quantize(
+        _ptr(x), dtype, rows, cols, _ptr(n_rows), _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+def moe_mxfp4_dequantize(codes, scales, dtype, rows, cols, n_rows, x, stream=None):
+    return _check("moe_mxfp4_dequantize", lib().moe_mxfp4_dequantize(
+        _ptr(codes), _ptr(scales), dtype, rows, cols, _ptr(n_rows), _ptr(x), _stream(stream)))
 
 
 def moe_expert_delta(theta_start, theta_now, peers, n_peers, n_params, delta_local, delta_avg,

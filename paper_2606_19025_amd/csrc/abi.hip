@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "mx.h"
 #include "moe_resident.h"
 #include "timing.h"
 
@@ -516,6 +517,41 @@ int moe_layernorm_bwd(const void* dy, const void* x, const float* weight, const 
   return hip_status(moe::launch_norm_bwd(dy, x, weight, mean, rstd, dtype == MOE_BF16, T, d, dres,
                                          dx, dw, db, accumulate_dw, ws, stream),
                     "moe_layernorm_bwd");
+}
+
+namespace {
+int check_mx(int dtype, int rows, int cols, const void* x, const uint8_t* codes,
+             const uint8_t* scales) {
+  int r;
+  if ((r = check_dtype(dtype)) != MOE_OK) return r;
+  REQUIRE(rows >= 0 && cols >= 1, "bad sizes rows = %d, cols = %d", rows, cols);
+  SUPPORT(cols % moe::MX_BLOCK == 0, "cols = %d must be a multiple of 32", cols);
+  SUPPORT((int64_t)rows * (cols / 8) < (int64_t)1 << 40, "rows = %d of cols = %d are too many", rows,
+          cols);
+  REQUIRE(rows == 0 || (x && codes && scales), "x, codes and scales must not be NULL");
+  SUPPORT(aligned16(x) && aligned16(codes), "x and codes must be 16-byte aligned");
+  return MOE_OK;
+}
+}  // namespace
+
+int moe_mxfp4_scale_stride(int cols) { return cols < 1 ? 0 : moe::mx_stride(cols); }
+
+int moe_mxfp4_quantize(const void* x, int dtype, int rows, int cols, const int32_t* n_rows,
+                       uint8_t* codes, uint8_t* scales, hipStream_t stream) {
+  const int r = check_mx(dtype, rows, cols, x, codes, scales);
+  if (r != MOE_OK) return r;
+  return hip_status(
+      moe::launch_mx_quantize(x, dtype == MOE_BF16, rows, cols, n_rows, codes, scales, stream),
+      "moe_mxfp4_quantize");
+}
+
+int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype, int rows,
+                         int cols, const int32_t* n_rows, void* x, hipStream_t stream) {
+  const int r = check_mx(dtype, rows, cols, x, codes, scales);
+  if (r != MOE_OK) return r;
+  return hip_status(
+      moe::launch_mx_dequantize(codes, scales, dtype == MOE_BF16, rows, cols, n_rows, x, stream),
+      "moe_mxfp4_dequantize");
 }
 
 int moe_expert_delta(const float* theta_start, const float* theta_now,

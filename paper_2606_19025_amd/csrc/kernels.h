@@ -113,6 +113,12 @@ hipError_t launch_norm_bwd(const void* dy, const void* x, const float* w, const 
                            const float* rstd, int bf16, int T, int d, const void* dres, void* dx,
                            float* dw, float* db, int accumulate, void* ws, hipStream_t s);
 
+// MXFP4 rows (mx.hip); n_rows: device count of the rows to convert, or NULL (all).
+hipError_t launch_mx_quantize(const void* x, int bf16, int rows, int cols, const int32_t* n_rows,
+                              uint8_t* codes, uint8_t* scales, hipStream_t s);
+hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int bf16, int rows,
+                                int cols, const int32_t* n_rows, void* x, hipStream_t s);
+
 // Placement and migration (placement.hip).  gen_placement: false when the
 // constraints cannot be met.  launch_copy_expert_rows: src_row / dst_row are
 // host arrays of n_rows <= 256 entries (dst_row NULL = 0..n_rows-1).

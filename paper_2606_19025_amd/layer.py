@@ -41,9 +41,11 @@ def _check_tensor(name, t, shape, dtype, device, owner):
 
 
 def _check_current(device, owner):
-    """Raise ValueError unless device is the current one: kernels are launched on the current
+    """Raise ValueError unless device is the current GPU: kernels are launched on the current
     device's stream."""
-    if device.type == "cuda" and torch.cuda.current_device() != device.index:
+    if device.type != "cuda":
+        raise ValueError(f"the {owner} is on {device}, not on a GPU")
+    if torch.cuda.current_device() != device.index:
         raise ValueError(f"the {owner} is on {device}, the current device is "
                          f"cuda:{torch.cuda.current_device()}")
 
@@ -331,6 +333,51 @@ class PreNormMoELayer:
                                  accumulate_dw=accumulate_dw, stream=stream, **kw)
         return self.norm.backward(dh, x, norm_weight, dres=dout, accumulate_dw=accumulate_dw,
                                   stream=stream)
+
+
+def _mx_cols(x):
+    if not isinstance(x, torch.Tensor) or x.dim() < 2:
+        raise ValueError("MXFP4 takes tensors of rows: [..., rows, cols]")
+    return x.shape[-1]
+
+
+def mxfp4_quantize(x, out=None, n_rows=None, stream=None):
+    """(codes, scales) of x [..., rows, cols] in MXFP4: uint8 [..., rows, cols / 2] and
+    [..., rows, moe_mxfp4_scale_stride(cols)].  out: such a pair to write to; n_rows: device
+    int32, how many rows to convert (None: all)."""
+    cols = _mx_cols(x)
+    _check_current(x.device, "tensor")
+    rows = x.numel() // cols if cols else 0
+    if out is None:
+        out = (torch.empty(*x.shape[:-1], cols // 2, dtype=torch.uint8, device=x.device),
+               torch.empty(*x.shape[:-1], B.moe_mxfp4_scale_stride(cols), dtype=torch.uint8,
+                           device=x.device))
+    codes, scales = out
+    _check_tensor("x", x, x.shape, x.dtype, x.device, "tensor")
+    _check_tensor("codes", codes, (*x.shape[:-1], cols // 2), torch.uint8, x.device, "tensor")
+    _check_tensor("scales", scales, (*x.shape[:-1], B.moe_mxfp4_scale_stride(cols)), torch.uint8,
+                  x.device, "tensor")
+    if n_rows is not None:
+        _check_tensor("n_rows", n_rows, n_rows.shape, torch.int32, x.device, "tensor")
+    B.moe_mxfp4_quantize(x, B.dtype_code(x), rows, cols, n_rows, codes, scales, stream)
+    return out
+
+
+def mxfp4_dequantize(codes, scales, dtype=torch.bfloat16, out=None, n_rows=None, stream=None):
+    """The values [..., rows, cols] that codes and scales stand for."""
+    cols = 2 * _mx_cols(codes)
+    _check_current(codes.device, "tensor")
+    rows = 2 * codes.numel() // cols if cols else 0
+    if out is None:
+        out = torch.empty(*codes.shape[:-1], cols, dtype=dtype, device=codes.device)
+    _check_tensor("codes", codes, codes.shape, torch.uint8, codes.device, "tensor")
+    _check_tensor("scales", scales, (*codes.shape[:-1], B.moe_mxfp4_scale_stride(cols)), torch.uint8,
+                  codes.device, "tensor")
+    _check_tensor("out", out, (*codes.shape[:-1], cols), dtype, codes.device, "tensor")
+    if n_rows is not None:
+        _check_tensor("n_rows", n_rows, n_rows.shape, torch.int32, codes.device, "tensor")
+    B.moe_mxfp4_dequantize(codes, scales, B.dtype_code(out), rows, cols, n_rows, out, stream)
+    return out
 
 
 def expert_delta(theta_start, theta_now, peers, delta_local=None, delta_avg=None, stream=None):
