@@ -410,6 +410,65 @@ int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype,
                          int cols, const int32_t* n_rows, void* x, hipStream_t stream);
 
 /*
+ * The whole layer's forward for a few tokens (evaluation on a handful of tokens,
+ * generation), where moe_layer_fwd's time is that of its many launches and of
+ * rows that it moves: three launches, each active expert's weights read once.
+ *
+ *   the routing of moe_route_mask, bit for bit (logits, topk_idx, topk_w, topk_local)
+ *   h[t,j,:] = s_j(x_t) act(Wgu_e x_t)         (e: the expert of the resident route j of t)
+ *   y[t,:]   = sum_j Wd_e h[t,j,:] + Wd_s act(Wgu_s x_t)      (s: the shared experts, if any)
+ *
+ * with act the SwiGLU or SiLU form of moe_ffn_set.  h is rounded once to dtype, y
+ * once from an fp32 sum over all experts (moe_layer_fwd also rounds each route's
+ * output).  A token whose routes are all ghosts gets the shared experts' output alone
+ * (exactly 0 without them).
+ *
+ * weights: MOE_W_PLAIN - every expert matrix in dtype, in the layouts of moe_ffn_set.
+ * MOE_W_MXFP4 (dtype MOE_BF16) - the same matrices [rows, cols] as the codes [rows,
+ * cols / 2] of moe_mxfp4_quantize, with their scales in the *_scales fields; they are
+ * widened to bf16 (exactly: their values have two significant bits) and multiplied
+ * with bf16 activations.  Router weights and x are always dtype.
+ * x, y [T,d] dtype; w_router [E,d]; router_bias [E] fp32 or NULL; resident [E] uint8
+ * with E_r nonzero entries; w_gate_up [E_r, 2H (SiLU: H), d], w_down [E_r, d, H];
+ * shared_gate_up [2 Hs (Hs), d], shared_down [d, Hs], Hs = 0: no shared experts.
+ * logits [T,E] fp32, topk_idx, topk_local [T,k] int32, topk_w [T,k] fp32: outputs, each
+ * may be NULL.
+ * ws: device workspace (256-byte aligned) of at least moe_few_fwd_workspace_size(f) bytes
+ * (which depends on the sizes, on whether logits is NULL, and on the current device's
+ * compute-unit count); its contents on entry are ignored, and two calls may share it
+ * only if they are ordered on a stream.
+ * Limits: 0 <= T <= 64, 1 <= k <= 8, k <= E <= 256, d % 64 == 0, H % 64 == 0, Hs % 64 == 0;
+ * x, y, the weights and codes 16-byte aligned.
+ */
+enum { MOE_W_PLAIN = 0, MOE_W_MXFP4 = 1 };
+typedef struct moe_few {
+  int dtype, weights, activation, gate;
+  int T, d, E, k, E_r, H, Hs;
+  float inv_tau;
+  const void* x;
+  const void* w_router;
+  const float* router_bias;
+  const uint8_t* resident;
+  const void* w_gate_up;
+  const void* w_down;
+  const void* shared_gate_up;
+  const void* shared_down;
+  const uint8_t* w_gate_up_scales; /* MOE_W_MXFP4 */
+  const uint8_t* w_down_scales;
+  const uint8_t* shared_gate_up_scales;
+  const uint8_t* shared_down_scales;
+  float* logits;
+  int32_t* topk_idx;
+  float* topk_w;
+  int32_t* topk_local;
+  void* y;
+  void* ws;
+  size_t ws_bytes;
+} moe_few;
+size_t moe_few_fwd_workspace_size(const moe_few* f);
+int moe_few_fwd(const moe_few* f, hipStream_t stream);
+
+/*
  * Round boundary: expert-wise pseudo-gradient of the resident experts and its
  * average over the expert's replica group (Alg. 2, aggregation of the sparse
  * parameters within expert replica groups; Sec. 3.4 "Round structure").

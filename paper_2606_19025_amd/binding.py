@@ -28,6 +28,7 @@ EXPORTS = [
     "moe_combine_bwd", "moe_layer_fwd", "moe_layer_bwd",
     "moe_layernorm_fwd", "moe_layernorm_bwd_workspace_size", "moe_layernorm_bwd",
     "moe_mxfp4_scale_stride", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
+    "moe_few_fwd_workspace_size", "moe_few_fwd",
     "moe_expert_delta", "moe_adamw_step", "moe_outer_nesterov", "moe_replica_mean",
     "moe_gen_placement", "moe_migration_map", "moe_copy_expert_rows", "moe_warmup_lr",
     "moe_adamw_step_rows", "moe_timing_enable", "moe_timing_collect",
@@ -75,6 +76,8 @@ _SIGS = {
     "moe_mxfp4_scale_stride": (_I, [_I]),
     "moe_mxfp4_quantize": (_I, [_P, _I, _I, _I, _P, _P, _P, _P]),
     "moe_mxfp4_dequantize": (_I, [_P, _P, _I, _I, _I, _P, _P, _P]),
+    "moe_few_fwd_workspace_size": (_Z, [_P]),
+    "moe_few_fwd": (_I, [_P, _P]),
     "moe_expert_delta": (_I, [_P, _P, C.POINTER(C.c_void_p), _I, _Z, _P, _P, _P]),
     "moe_adamw_step": (_I, [_P, _P, _P, _P, _Z, _I, _F, _F, _F, _F, _F, _P, _P]),
     "moe_outer_nesterov": (_I, [_P, _P, _P, _P, _Z, _F, _F, _P, _P]),
@@ -116,6 +119,19 @@ class moe_layer(C.Structure):
     _fields_ += [("ws_route_bytes", _Z), ("sets", moe_ffn_set * 2)]
 
 
+class moe_few(C.Structure):
+    """The few-token layer's arguments (struct moe_few of include/moe_resident.h)."""
+    _fields_ = [(n, _I) for n in ("dtype", "weights", "activation", "gate", "T", "d", "E", "k", "E_r",
+                                  "H", "Hs")]
+    _fields_ += [("inv_tau", _F)]
+    _fields_ += [(n, _P) for n in ("x", "w_router", "router_bias", "resident", "w_gate_up", "w_down",
+                                   "shared_gate_up", "shared_down", "w_gate_up_scales",
+                                   "w_down_scales", "shared_gate_up_scales", "shared_down_scales",
+                                   "logits", "topk_idx", "topk_w", "topk_local", "y", "ws")]
+    _fields_ += [("ws_bytes", _Z)]
+
+
+MOE_W_PLAIN, MOE_W_MXFP4 = 0, 1
 MOE_ACT_SWIGLU, MOE_ACT_SILU = 0, 1
 ACTIVATIONS = {"swiglu": MOE_ACT_SWIGLU, "silu": MOE_ACT_SILU}
 
@@ -325,6 +341,15 @@ def moe_mxfp4_quantize(x, dtype, rows, cols, n_rows, codes, scales, stream=None)
 def moe_mxfp4_dequantize(codes, scales, dtype, rows, cols, n_rows, x, stream=None):
     return _check("moe_mxfp4_dequantize", lib().moe_mxfp4_dequantize(
         _ptr(codes), _ptr(scales), dtype, rows, cols, _ptr(n_rows), _ptr(x), _stream(stream)))
+
+
+def moe_few_fwd_workspace_size(few) -> int:
+    return lib().moe_few_fwd_workspace_size(C.byref(few))
+
+
+def moe_few_fwd(few, stream=None):
+    """few: a moe_few."""
+    return _check("moe_few_fwd", lib().moe_few_fwd(C.byref(few), _stream(stream)))
 
 
 def moe_expert_delta(theta_start, theta_now, peers, n_peers, n_params, delta_local, delta_avg,

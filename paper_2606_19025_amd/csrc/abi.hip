@@ -554,6 +554,57 @@ int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype,
       "moe_mxfp4_dequantize");
 }
 
+namespace {
+// Everything of a moe_few but its pointers.
+int check_few_sizes(const moe_few* f) {
+  int r;
+  REQUIRE(f != nullptr, "the arguments must not be NULL");
+  if ((r = check_dtype(f->dtype)) != MOE_OK) return r;
+  REQUIRE(f->weights == MOE_W_PLAIN || f->weights == MOE_W_MXFP4, "unknown weights %d", f->weights);
+  REQUIRE(f->activation == MOE_ACT_SWIGLU || f->activation == MOE_ACT_SILU,
+          "activation = %d is not an expert form", f->activation);
+  REQUIRE(f->gate >= MOE_GATE_SOFTMAX_TOPK && f->gate <= MOE_GATE_SIGMOID, "unknown gate %d", f->gate);
+  SUPPORT(f->weights == MOE_W_PLAIN || f->dtype == MOE_BF16, "MXFP4 weights need dtype MOE_BF16");
+  REQUIRE(f->T >= 0 && f->d >= 1 && f->H >= 1 && f->Hs >= 0, "bad sizes T = %d, d = %d, H = %d, Hs = %d",
+          f->T, f->d, f->H, f->Hs);
+  SUPPORT(f->T <= moe::kFewTokens, "T = %d: at most %d tokens (moe_layer_fwd takes more)", f->T,
+          moe::kFewTokens);
+  REQUIRE(f->E >= 1 && f->E <= 256, "E = %d must be in [1, 256]", f->E);
+  REQUIRE(f->k >= 1 && f->k <= f->E, "k = %d must be in [1, E = %d]", f->k, f->E);
+  SUPPORT(f->k <= moe::kFewRoutes, "k = %d: at most %d routes", f->k, moe::kFewRoutes);
+  REQUIRE(f->E_r >= 0 && f->E_r <= f->E, "E_r = %d must be in [0, E = %d]", f->E_r, f->E);
+  REQUIRE(std::isfinite(f->inv_tau) && f->inv_tau > 0.f, "inv_tau must be finite and > 0");
+  SUPPORT(f->d % 64 == 0 && f->H % 64 == 0 && f->Hs % 64 == 0,
+          "d = %d, H = %d and Hs = %d must be multiples of 64", f->d, f->H, f->Hs);
+  return MOE_OK;
+}
+}  // namespace
+
+size_t moe_few_fwd_workspace_size(const moe_few* f) {
+  return check_few_sizes(f) == MOE_OK ? moe::few_ws_bytes(f) : 0;
+}
+
+int moe_few_fwd(const moe_few* f, hipStream_t stream) {
+  int r;
+  if ((r = check_few_sizes(f)) != MOE_OK) return r;
+  const bool mx = f->weights == MOE_W_MXFP4;
+  REQUIRE(f->w_router && f->resident, "w_router and resident must not be NULL");
+  REQUIRE(f->T == 0 || (f->x && f->y), "x and y must not be NULL");
+  REQUIRE(f->E_r == 0 || (f->w_gate_up && f->w_down), "the experts' weights must not be NULL");
+  REQUIRE(f->Hs == 0 || (f->shared_gate_up && f->shared_down),
+          "the shared experts' weights must not be NULL");
+  REQUIRE(!mx || ((f->E_r == 0 || (f->w_gate_up_scales && f->w_down_scales)) &&
+                  (f->Hs == 0 || (f->shared_gate_up_scales && f->shared_down_scales))),
+          "MXFP4 weights need their scales");
+  for (const void* p : {f->x, f->w_router, f->w_gate_up, f->w_down, f->shared_gate_up,
+                        f->shared_down, (const void*)f->y})
+    SUPPORT(p == nullptr || aligned16(p), "x, y and the weights must be 16-byte aligned");
+  const size_t need = moe::few_ws_bytes(f);
+  REQUIRE(f->ws && f->ws_bytes >= need, "workspace of %zu bytes needed (got %zu)", need, f->ws_bytes);
+  SUPPORT((reinterpret_cast<uintptr_t>(f->ws) & 255u) == 0, "the workspace must be 256-byte aligned");
+  return hip_status(moe::launch_few(f, stream), "moe_few_fwd");
+}
+
 int moe_expert_delta(const float* theta_start, const float* theta_now,
                      const float* const* peers, int n_peers, size_t n_params, float* delta_local,
                      float* delta_avg, hipStream_t stream) {

@@ -113,6 +113,11 @@ hipError_t launch_norm_bwd(const void* dy, const void* x, const float* w, const 
                            const float* rstd, int bf16, int T, int d, const void* dres, void* dx,
                            float* dw, float* db, int accumulate, void* ws, hipStream_t s);
 
+// The whole layer for a few tokens (few.hip).
+constexpr int kFewTokens = 64, kFewRoutes = 8;
+size_t few_ws_bytes(const moe_few* f);
+hipError_t launch_few(const moe_few* f, hipStream_t s);
+
 // MXFP4 rows (mx.hip); n_rows: device count of the rows to convert, or NULL (all).
 hipError_t launch_mx_quantize(const void* x, int bf16, int rows, int cols, const int32_t* n_rows,
                               uint8_t* codes, uint8_t* scales, hipStream_t s);

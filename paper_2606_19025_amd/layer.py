@@ -380,6 +380,106 @@ def mxfp4_dequantize(codes, scales, dtype=torch.bfloat16, out=None, n_rows=None,
     return out
 
 
+class InferenceMoELayer:
+    """The layer's forward for few tokens on weights that stay: evaluation and generation.
+
+    The weights are given once (they are read where they lie, so later in-place updates are
+    seen): ``w_gate_up`` [E_r, 2H, d] and ``w_down`` [E_r, d, H] (SiLU experts: [E_r, H, d]) of
+    the router's dtype, or each a (codes, scales) pair of ``mxfp4_quantize``; the shared
+    experts' likewise, [1, ...].  ``few`` takes up to 64 tokens; the outputs of its last call
+    are y, logits, topk_idx, topk_w and topk_local, in buffers that the next call reuses (two
+    calls on different streams need a layer each)."""
+
+    MAX_TOKENS = 64
+
+    def __init__(self, k, resident, w_router, w_gate_up, w_down, router_bias=None,
+                 shared_gate_up=None, shared_down=None, gate="softmax_topk", inv_tau=1.0,
+                 expert="swiglu"):
+        dev, dt = w_router.device, w_router.dtype
+        self.device, self.dtype = dev, dt
+        E, d = w_router.shape
+        mx = isinstance(w_gate_up, (tuple, list))
+        r1 = 2 if B.ACTIVATIONS[expert] == B.MOE_ACT_SWIGLU else 1
+        res = torch.as_tensor(resident, dtype=torch.uint8).reshape(-1).to(dev)
+        if res.numel() != E:
+            raise ValueError(f"resident has {res.numel()} entries, the router {E} experts")
+        E_r = int((res != 0).sum().item())
+
+        def inner(w):
+            # hidden units of a second projection [n, d, H]
+            if isinstance(w, (tuple, list)) != mx:
+                raise ValueError("all expert weights are plain, or all are MXFP4 pairs")
+            return w[0].shape[-1] * 2 if mx else w.shape[-1]
+
+        H = inner(w_down)
+        Hs = inner(shared_down) if shared_down is not None else 0
+        if (shared_gate_up is None) != (shared_down is None):
+            raise ValueError("shared experts need both shared_gate_up and shared_down")
+
+        def check(name, w, n, rows, cols):
+            if isinstance(w, (tuple, list)) != mx:
+                raise ValueError(f"{name}: all expert weights are plain, or all are MXFP4 pairs")
+            if not mx:
+                _check_tensor(name, w, (n, rows, cols), dt, dev, "layer")
+                return w, None
+            codes, scales = w
+            _check_tensor(name + " codes", codes, (n, rows, cols // 2), torch.uint8, dev, "layer")
+            _check_tensor(name + " scales", scales, (n, rows, B.moe_mxfp4_scale_stride(cols)),
+                          torch.uint8, dev, "layer")
+            return codes, scales
+
+        _check_tensor("w_router", w_router, (E, d), dt, dev, "layer")
+        if router_bias is not None:
+            _check_tensor("router_bias", router_bias, (E,), torch.float32, dev, "layer")
+        gu, gu_s = check("w_gate_up", w_gate_up, E_r, r1 * H, d)
+        dn, dn_s = check("w_down", w_down, E_r, d, H)
+        sgu = sgu_s = sd = sd_s = None
+        if Hs:
+            sgu, sgu_s = check("shared_gate_up", shared_gate_up, 1, r1 * Hs, d)
+            sd, sd_s = check("shared_down", shared_down, 1, d, Hs)
+        # (held here: the library keeps addresses only)
+        self._held = (w_router, router_bias, res, gu, gu_s, dn, dn_s, sgu, sgu_s, sd, sd_s)
+        p = B._ptr
+        self.T, self.d, self.E, self.k, self.E_r, self.H, self.Hs = 0, d, E, int(k), E_r, H, Hs
+        self._few = B.moe_few(
+            dtype=B.dtype_code(w_router), weights=B.MOE_W_MXFP4 if mx else B.MOE_W_PLAIN,
+            activation=B.ACTIVATIONS[expert],
+            gate=B.GATES[gate] if isinstance(gate, str) else int(gate), d=d, E=E, k=self.k,
+            E_r=E_r, H=H, Hs=Hs, inv_tau=float(inv_tau), w_router=p(w_router),
+            router_bias=p(router_bias), resident=p(res), w_gate_up=p(gu), w_down=p(dn),
+            shared_gate_up=p(sgu), shared_down=p(sd), w_gate_up_scales=p(gu_s),
+            w_down_scales=p(dn_s), shared_gate_up_scales=p(sgu_s), shared_down_scales=p(sd_s))
+        self.y = self.logits = self.topk_idx = self.topk_w = self.topk_local = self._ws = None
+
+    def _size(self, T):
+        """Buffers and arguments for T tokens (kept until T changes)."""
+        if not 0 <= T <= self.MAX_TOKENS:
+            raise ValueError(f"few takes up to {self.MAX_TOKENS} tokens, got {T}")
+        f, dev = self._few, self.device
+        self.y = torch.empty(T, self.d, dtype=self.dtype, device=dev)
+        self.logits = torch.empty(T, self.E, dtype=torch.float32, device=dev)
+        self.topk_w = torch.empty(T, self.k, dtype=torch.float32, device=dev)
+        self.topk_idx, self.topk_local = (torch.empty(T, self.k, dtype=torch.int32, device=dev)
+                                          for _ in range(2))
+        f.T = T
+        for name in ("y", "logits", "topk_w", "topk_idx", "topk_local"):
+            setattr(f, name, getattr(self, name).data_ptr())
+        f.ws_bytes = B.moe_few_fwd_workspace_size(f)
+        self._ws = torch.empty(max(f.ws_bytes, 1), dtype=torch.uint8, device=dev)
+        f.ws = self._ws.data_ptr()
+        self.T = T
+
+    def few(self, x, stream=None):
+        """y [T, d] of up to 64 tokens x [T, d], by moe_few_fwd."""
+        _check_current(self.device, "layer")
+        if self.y is None or x.shape[0] != self.T:
+            self._size(x.shape[0])
+        _check_tensor("x", x, (self.T, self.d), self.dtype, self.device, "layer")
+        self._few.x = x.data_ptr()
+        B.moe_few_fwd(self._few, stream)
+        return self.y
+
+
 def expert_delta(theta_start, theta_now, peers, delta_local=None, delta_avg=None, stream=None):
     """Round-boundary pseudo-gradient of the resident experts and its replica-group average."""
     n = theta_start.numel()

@@ -84,7 +84,8 @@ _SYMBOLS = [
     (r"outer_nesterov_kernel", lambda m: "outer_nesterov"),
     (r"replica_mean_kernel", lambda m: "replica_mean"),
     (r"copy_expert_rows_kernel", lambda m: "copy_expert_rows"),
-    (r"(norm_fwd|norm_bwd|norm_dw|mx_quantize|mx_dequantize)_kernel", lambda m: m.group(1)),
+    (r"few_logits_(?:bf16|f32)_kernel", lambda m: "few_logits"),
+    (r"(norm_fwd|norm_bwd|norm_dw|mx_quantize|mx_dequantize|few_gu|few_down)_kernel", lambda m: m.group(1)),
 ]
 
 # timing name prefix -> source file that holds the kernel
@@ -92,7 +93,8 @@ _SOURCES = [("gemm_", "gemm.hip"), ("splitk_", "gemm.hip"), ("zero_counters", "g
             ("combine_", "dispatch.hip"), ("unpermute", "dispatch.hip"),
             ("expert_delta", "dispatch.hip"), ("adamw", "optim.hip"), ("outer_", "optim.hip"),
             ("replica_", "optim.hip"),
-            ("copy_expert_rows", "placement.hip"), ("norm_", "norm.hip"), ("mx_", "mx.hip")]
+            ("copy_expert_rows", "placement.hip"), ("norm_", "norm.hip"), ("mx_", "mx.hip"),
+            ("few_", "few.hip")]
 
 
 def timing_name(symbol: str) -> str | None:
