@@ -600,7 +600,8 @@ int moe_few_fwd(const moe_few* f, hipStream_t stream) {
                         f->shared_down, (const void*)f->y})
     SUPPORT(p == nullptr || aligned16(p), "x, y and the weights must be 16-byte aligned");
   const size_t need = moe::few_ws_bytes(f);
-  REQUIRE(f->ws && f->ws_bytes >= need, "workspace of %zu bytes needed (got %zu)", need, f->ws_bytes);
+  REQUIRE(need == 0 || (f->ws && f->ws_bytes >= need), "workspace of %zu bytes needed (got %zu)", need,
+          f->ws_bytes);
   SUPPORT((reinterpret_cast<uintptr_t>(f->ws) & 255u) == 0, "the workspace must be 256-byte aligned");
   return hip_status(moe::launch_few(f, stream), "moe_few_fwd");
 }

@@ -17,6 +17,8 @@
 // Weights go from HBM to registers in the order of the instruction's operand: a lane
 // takes a row's consecutive bytes, the four lanes of a row 64 or 128 of them.  (The
 // order of k within an instruction is free as long as both operands have the same.)
+#include <type_traits>
+
 #include "kernels.h"
 #include "mx.h"
 #include "route_select.h"
@@ -25,8 +27,7 @@
 namespace moe {
 namespace {
 
-constexpr int FW = 8;             // waves per block
-constexpr int FT = 64 * FW;       // threads
+constexpr int LW = 8;              // waves of few_logits_bf16_kernel: the router's shares of d
 constexpr int FEW_T = kFewTokens;  // tokens at most
 constexpr int FEW_K = RT_KSEL;     // routes of a token at most
 
@@ -43,13 +44,10 @@ struct FewArgs {
   int32_t* local;
   void* y;
   // workspace
-  int* counters;   // [d / 16]
-  float* w_gate;   // [T k]
   int32_t* w_local;  // [T k]
   void* h;         // [T k, H], rows of resident routes
   void* hs;        // [T, Hs]
-  float* part;     // [parts][d / 16][T][16]
-  int T, d, E, k, E_r, H, Hs, gate, parts, n_slices;
+  int T, d, E, k, E_r, H, Hs, gate;
   float inv_tau;
 };
 
@@ -59,15 +57,13 @@ struct FewArgs {
 // sixteen k in each, and the waves' sums are added in order.  Few experts per block, so
 // that a single token's logits come from many CUs.
 constexpr int LE = 8;
-__global__ __launch_bounds__(FT) void few_logits_bf16_kernel(FewArgs a) {
-  __shared__ float part[FW][32 * LE];
+__global__ __launch_bounds__(64 * LW) void few_logits_bf16_kernel(FewArgs a) {
+  __shared__ float part[LW][32 * LE];
   const bf16_t* x = static_cast<const bf16_t*>(a.x);
   const bf16_t* w = static_cast<const bf16_t*>(a.w_router);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane & 31, half = lane >> 5;
   const int e0 = blockIdx.x * LE, t0 = blockIdx.y * 32;
-  if (blockIdx.x == 0 && blockIdx.y == 0)
-    for (int i = threadIdx.x; i < a.n_slices; i += FT) a.counters[i] = 0;
   const int n = (a.d + 63) / 64;
   const bool has_t = t0 + row < a.T, has_e = row < LE && e0 + row < a.E;
   const bf16_t* xr = x + (size_t)(has_t ? t0 + row : 0) * a.d;
@@ -75,13 +71,13 @@ __global__ __launch_bounds__(FT) void few_logits_bf16_kernel(FewArgs a) {
   f32x16_t acc = {};
   const bf16x8_t zero = {};
   constexpr int U = 4;
-  for (int s0 = wave; s0 < n; s0 += U * FW) {
+  for (int s0 = wave; s0 < n; s0 += U * LW) {
     bf16x8_t xv[U][4], wv[U][4];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int c = (s0 + u * FW) * 64 + half * 32 + q * 8;
+        const int c = (s0 + u * LW) * 64 + half * 32 + q * 8;
         xv[u][q] = has_t && c < a.d ? *reinterpret_cast<const bf16x8_t*>(xr + c) : zero;
         wv[u][q] = has_e && c < a.d ? *reinterpret_cast<const bf16x8_t*>(wr + c) : zero;
       }
@@ -102,7 +98,7 @@ __global__ __launch_bounds__(FT) void few_logits_bf16_kernel(FewArgs a) {
     const int t = t0 + threadIdx.x / LE, e = e0 + threadIdx.x % LE;
     float v = part[0][threadIdx.x];
 #pragma unroll
-    for (int q = 1; q < FW; ++q) v += part[q][threadIdx.x];
+    for (int q = 1; q < LW; ++q) v += part[q][threadIdx.x];
     if (t < a.T && e < a.E) {
       if (a.bias) v += a.bias[e];
       a.logits[(size_t)t * a.E + e] = v * a.inv_tau;
@@ -119,8 +115,6 @@ __global__ __launch_bounds__(256) void few_logits_f32_kernel(FewArgs a) {
   const float* x = static_cast<const float*>(a.x);
   const float* w = static_cast<const float*>(a.w_router);
   const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
-  if (blockIdx.x == 0 && blockIdx.y == 0)
-    for (int i = threadIdx.x; i < a.n_slices; i += 256) a.counters[i] = 0;
   const int lr = threadIdx.x >> 4, lc = (threadIdx.x & 15) * 4;  // the thread's 16 bytes of a chunk
   const float* xp = x + (size_t)min(t0 + lr, a.T - 1) * a.d;
   const float* wp = w + (size_t)min(e0 + lr, a.E - 1) * a.d;
@@ -217,7 +211,6 @@ DEVI void few_select(const FewArgs& a, FewTables& tb, int t, bool publish) {
     tb.gate[o] = g;
     tb.local[o] = (int16_t)l;
     if (publish) {
-      a.w_gate[o] = g;
       a.w_local[o] = l;
       if (a.idx) a.idx[o] = my_id;
       if (a.tw) a.tw[o] = g;
@@ -334,40 +327,28 @@ template <> struct Op<bf16_t, true> {
 // An item is 16 hidden units of one expert (32 rows of a SwiGLU expert's matrix, 16 of a
 // SiLU one's); its k is dealt over the block's waves in steps, and the waves' sums are
 // added in order through LDS.
+//
+// The shared experts' items come first and need no routing; every block makes the routes'
+// tables itself when it comes to its first routed item (a launch of its own for them would
+// take longer than their two microseconds).
+constexpr int gu_waves(int NT) { return NT == 1 ? 4 : 8; }
+
 template <class E, bool MX, int ACT, int NT>
-__global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
+__global__ __launch_bounds__(64 * gu_waves(NT), NT == 1 ? 4 : 2) void few_gu_kernel(FewArgs a) {
   using O = Op<E, MX>;
+  constexpr int FW = gu_waves(NT), FT = 64 * FW;
   constexpr int KL = O::KL, KS = 4 * KL;
   constexpr int R = ACT == MOE_ACT_SWIGLU ? 2 : 1;
-  constexpr int U = NT == 1 ? 4 : 2;  // steps whose loads are issued together
+  constexpr int U = NT == 1 && !MX ? 4 : 2;  // steps whose loads are issued together
   __shared__ FewTables tb;
   __shared__ f32x4_t red[FW][R][NT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int l16 = lane & 15, q4 = lane >> 4;
-  if (wave == 0) build_local_map(a.resident, a.E, tb.lmap);
-  if (threadIdx.x < 256) tb.slot[threadIdx.x] = 0;
-  __syncthreads();
-  for (int t = wave * 4 + q4; t - q4 < a.T; t += FW * 4) {
-    if (a.E <= 64) few_select<4>(a, tb, t, blockIdx.x == 0);
-    else few_select<16>(a, tb, t, blockIdx.x == 0);
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.T * a.k; i += FT)
-    if (tb.local[i] >= 0) tb.slot[tb.local[i]] = 1;
-  __syncthreads();
-  if (wave == 0) few_active(a, tb);
-  __syncthreads();
-  const int n_s = a.Hs / 16, n_r = a.H / 16;
-  const int n_items = n_s + tb.n_active * n_r;
   const E* x = static_cast<const E*>(a.x);
-  for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
-    const bool shared = item < n_s;
-    const int act = shared ? 0 : (item - n_s) / n_r;
-    const int h0 = (shared ? item : (item - n_s) % n_r) * 16;
-    const int r = shared ? 0 : tb.expert[act];
+
+  // hidden units h0 .. h0 + 15 of one expert; my_p: the row of h for lane t's token, or -1
+  auto item = [&](bool shared, int r, int h0, int my_p) {
     const int H = shared ? a.Hs : a.H;
-    // lane t's route, and the tiles that hold a token of this expert
-    const int my_p = shared ? (lane < a.T ? lane : -1) : route_to(a, tb, lane, r);
     const uint64_t who = __ballot(my_p >= 0);
     const void* W = shared ? a.sgu : a.wgu;
     const uint8_t* S = shared ? a.sgu_s : a.wgu_s;
@@ -397,6 +378,7 @@ __global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) acc[g][n] = O::mma(w[u][g], xv[u][n], acc[g][n]);
     }
+    __syncthreads();  // the previous item's sums have been read
 #pragma unroll
     for (int g = 0; g < R; ++g)
 #pragma unroll
@@ -423,104 +405,134 @@ __global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
         }
       }
     }
-    __syncthreads();
+  };
+
+  const int n_s = a.Hs / 16, n_r = a.H / 16;
+  int it = blockIdx.x;
+  for (; it < n_s; it += gridDim.x) item(true, 0, it * 16, lane < a.T ? lane : -1);
+
+  if (wave == 0) build_local_map(a.resident, a.E, tb.lmap);
+  for (int i = threadIdx.x; i < 256; i += FT) tb.slot[i] = 0;
+  __syncthreads();
+  for (int t = wave * 4 + q4; t - q4 < a.T; t += FW * 4) {
+    if (a.E <= 64) few_select<4>(a, tb, t, blockIdx.x == 0);
+    else if (a.E <= 128) few_select<8>(a, tb, t, blockIdx.x == 0);
+    else few_select<16>(a, tb, t, blockIdx.x == 0);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.T * a.k; i += FT)
+    if (tb.local[i] >= 0) tb.slot[tb.local[i]] = 1;
+  __syncthreads();
+  if (wave == 0) few_active(a, tb);
+  __syncthreads();
+  for (; it < n_s + tb.n_active * n_r; it += gridDim.x) {
+    const int r = tb.expert[(it - n_s) / n_r];
+    item(false, r, (it - n_s) % n_r * 16, route_to(a, tb, lane, r));
   }
 }
 
 // ------------------------------------------------------------------ second projections
-// A block is 16 columns of y (rows of W_d) and one of `parts` shares of the reduction: all
-// active experts' hidden units, then the shared experts', in steps.  Waves take consecutive
-// steps.  With several parts the last block of a slice to finish adds their fp32 sums, in
-// order of the parts.
-template <class E, bool MX, int NT>
-__global__ __launch_bounds__(FT) void few_down_kernel(FewArgs a) {
+// A block is RB columns of y (rows of W_d; the matrix instruction's other rows are empty)
+// and the whole reduction: the shared experts' hidden units, then all active experts', in
+// steps of which each wave takes consecutive ones.  Sums run on over experts; the waves'
+// are added in order through LDS.  RB is 16, or less where that would leave CUs without a
+// block: cutting the reduction into parts instead, added by the last block to finish, took
+// three times as long (the fences write back each XCD's whole L2).
+constexpr int DW = 16;  // waves
+
+template <class E, bool MX, int NT, int RB>
+__global__ __launch_bounds__(64 * DW) void few_down_kernel(FewArgs a) {
   using O = Op<E, MX>;
   constexpr int KL = O::KL, KS = 4 * KL;
-  constexpr int U = NT == 1 ? 4 : 2;
+  constexpr int U = NT == 1 && !MX ? 2 : 1;  // steps in a stage; two stages' loads in flight
   __shared__ FewTables tb;
-  __shared__ f32x4_t red[FW][NT][64];
-  __shared__ int last;
+  __shared__ f32x4_t red[DW][NT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int l16 = lane & 15, q4 = lane >> 4;
-  if (threadIdx.x < 256) tb.slot[threadIdx.x] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.T * a.k; i += FT) {
-    const int l = a.w_local[i];
-    tb.local[i] = (int16_t)l;
-    if (l >= 0) tb.slot[l] = 1;
-  }
-  __syncthreads();
-  if (wave == 0) few_active(a, tb);
-  __syncthreads();
-  const int slice = blockIdx.x % a.n_slices, part = blockIdx.x / a.n_slices;
-  const int n_h = ceil_div(a.H, KS), n_routed = tb.n_active * n_h;
-  const int steps = n_routed + ceil_div(a.Hs, KS);
-  const int share = part * FW + wave, shares = a.parts * FW;
-  const int s0 = (int)((int64_t)steps * share / shares), s1 = (int)((int64_t)steps * (share + 1) / shares);
-  const int row = slice * 16 + l16;
+  for (int i = threadIdx.x; i < a.T * a.k; i += 64 * DW) tb.local[i] = (int16_t)a.w_local[i];
+  for (int i = threadIdx.x; i < 256; i += 64 * DW) tb.slot[i] = 0;
+  const int row = blockIdx.x * RB + l16;
+  const bool has_row = l16 < RB;
   f32x4_t acc[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  int cur = -1, my_p = -1, r = 0;  // the active expert at hand and lane t's route to it
-  for (int s = s0; s < s1; s += U) {
+
+  struct Stage {
     typename O::W w[U];
-    typename O::X xv[U][NT];
+    typename O::X x[U][NT];
+  };
+  int cur = -1, my_p = -1, r = 0;  // the active expert at hand and lane t's route to it
+  // the steps [s0, s1) of n_h to an expert; the shared ones if SH
+  auto run = [&](auto SH, int s0, int s1, int n_h) {
+    constexpr bool shared = decltype(SH)::value;
+    const int H = shared ? a.Hs : a.H;
+    const void* W = shared ? a.sd : a.wd;
+    const uint8_t* S = shared ? a.sd_s : a.wd_s;
+    const E* h = static_cast<const E*>(shared ? a.hs : a.h);
+    auto load = [&](Stage& g, int s) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int st = s + u;
-      const bool on = st < s1, shared = st >= n_routed;
-      const int act = shared ? 256 : st / n_h;
-      if (on && act != cur) {
-        cur = act;
-        r = shared ? 0 : tb.expert[act];
-        my_p = shared ? (lane < a.T ? lane : -1) : route_to(a, tb, lane, r);
-      }
-      const int H = shared ? a.Hs : a.H;
-      const int k = (shared ? st - n_routed : st - act * n_h) * KS + q4 * KL;
-      const bool ok = on && k < H;
-      O::load(w[u], shared ? a.sd : a.wd, shared ? a.sd_s : a.wd_s, (size_t)r * a.d + row, H, k, ok);
-      const E* h = static_cast<const E*>(shared ? a.hs : a.h);
+      for (int u = 0; u < U; ++u) {
+        const int st = s + u;
+        const bool on = st < s1;
+        int k = st;
+        if constexpr (!shared) {
+          const int act = st / n_h;
+          k -= act * n_h;
+          if (on && act != cur) {
+            cur = act;
+            r = tb.expert[act];
+            my_p = route_to(a, tb, lane, r);
+          }
+        }
+        k = k * KS + q4 * KL;
+        const bool ok = on && k < H;
+        O::load(g.w[u], W, S, (size_t)r * a.d + row, H, k, ok && has_row);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const int p = __shfl(my_p, 16 * n + l16, 64);
-        O::load_x(xv[u][n], h + (size_t)(p < 0 ? 0 : p) * H + k, ok && p >= 0);
+        for (int n = 0; n < NT; ++n) {
+          const int p = __shfl(my_p, 16 * n + l16, 64);
+          O::load_x(g.x[u][n], h + (size_t)(p < 0 ? 0 : p) * H + k, ok && p >= 0);
+        }
       }
+    };
+    auto mma = [&](const Stage& g) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n] = O::mma(g.w[u], g.x[u][n], acc[n]);
+    };
+    if (s0 >= s1) return;
+    Stage g0, g1;
+    load(g0, s0);
+    for (int s = s0; s < s1; s += 2 * U) {
+      load(g1, s + U);
+      mma(g0);
+      load(g0, s + 2 * U);
+      mma(g1);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) acc[n] = O::mma(w[u], xv[u][n], acc[n]);
+  };
+  if (a.Hs) {
+    my_p = lane < a.T ? lane : -1;
+    const int n = ceil_div(a.Hs, KS);
+    run(std::true_type{}, n * wave / DW, n * (wave + 1) / DW, n);
   }
-#pragma unroll
-  for (int n = 0; n < NT; ++n) red[wave][n][lane] = acc[n];
   __syncthreads();
-  // token t of tile `wave`, columns 16 slice + 4 q4 ..
-  const int t = 16 * wave + l16;
-  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-  if (wave < NT) {
-    v = red[0][wave][lane];
+  for (int i = threadIdx.x; i < a.T * a.k; i += 64 * DW)
+    if (tb.local[i] >= 0) tb.slot[tb.local[i]] = 1;
+  __syncthreads();
+  if (wave == 0) few_active(a, tb);
+  __syncthreads();
+  const int n_h = ceil_div(a.H, KS), n = tb.n_active * n_h;
+  run(std::false_type{}, n * wave / DW, n * (wave + 1) / DW, n_h);
 #pragma unroll
-    for (int q = 1; q < FW; ++q) v += red[q][wave][lane];
-  }
-  if (a.parts > 1) {
-    float* mine = a.part + (((size_t)part * a.n_slices + slice) * a.T) * 16;
-    if (wave < NT) {
-      if (t < a.T) *reinterpret_cast<f32x4_t*>(mine + t * 16 + 4 * q4) = v;
-      __threadfence();  // each writing wave's sums, before the block counts itself
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(a.counters + slice, 1) == a.parts - 1;
-    __syncthreads();
-    if (!last || wave >= NT) return;
-    __threadfence();
-    if (t < a.T) {
-      v = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      for (int q = 0; q < a.parts; ++q)
-        v += *reinterpret_cast<const f32x4_t*>(a.part + (((size_t)q * a.n_slices + slice) * a.T + t) * 16 + 4 * q4);
-    }
-  }
-  if (wave < NT && t < a.T) {
-    E* y = static_cast<E*>(a.y) + (size_t)t * a.d + slice * 16 + 4 * q4;
+  for (int q = 0; q < NT; ++q) red[wave][q][lane] = acc[q];
+  __syncthreads();
+  // token t of tile `wave`, columns RB blockIdx.x + 4 q4 ..
+  const int t = 16 * wave + l16;
+  if (wave < NT && t < a.T && 4 * q4 < RB) {
+    f32x4_t v = red[0][wave][lane];
+#pragma unroll
+    for (int q = 1; q < DW; ++q) v += red[q][wave][lane];
+    E* y = static_cast<E*>(a.y) + (size_t)t * a.d + blockIdx.x * RB + 4 * q4;
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = from_f32<E>(v[i]);
   }
@@ -528,48 +540,41 @@ __global__ __launch_bounds__(FT) void few_down_kernel(FewArgs a) {
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Steps of the second projections' reduction at most, and the parts they are cut into: so
-// many that the blocks fill the GPU twice over, but a step at least for every wave.
-int few_parts(const moe_few* f) {
-  const int ks = f->weights == MOE_W_MXFP4 ? 128 : f->dtype == MOE_BF16 ? 64 : 32;
-  const int experts = (int)std::min<int64_t>(f->E_r, (int64_t)f->T * f->k);
-  const int64_t steps = (int64_t)experts * ceil_div(f->H, ks) + ceil_div(f->Hs, ks);
-  const int want = ceil_div(2 * num_cus(), f->d / 16);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(want, steps / FW));
-}
-
 struct FewLayout {
-  size_t counters, gate, local, logits, h, hs, part, bytes;
-  int parts;
+  size_t local, logits, h, hs, bytes;
 };
 FewLayout few_layout(const moe_few* f) {
   FewLayout l;
   const size_t e = f->dtype == MOE_BF16 ? 2 : 4, T = f->T;
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at += up256(n); return o; };
-  l.parts = few_parts(f);
-  l.counters = take((size_t)(f->d / 16) * 4);
-  l.gate = take(T * f->k * 4);
   l.local = take(T * f->k * 4);
   l.logits = take(f->logits ? 0 : T * f->E * 4);
   l.h = take(T * f->k * f->H * e);
   l.hs = take(T * f->Hs * e);
-  l.part = take(l.parts > 1 ? (size_t)l.parts * T * f->d * 4 : 0);
   l.bytes = at;
   return l;
 }
 
 template <class E, bool MX, int ACT, int NT>
-void few_launch(const FewArgs& a, int gu_blocks, hipStream_t s) {
-  MOE_TIMED("few_gu", s, few_gu_kernel<E, MX, ACT, NT><<<gu_blocks, FT, 0, s>>>(a));
-  MOE_TIMED("few_down", s, few_down_kernel<E, MX, NT><<<a.n_slices * a.parts, FT, 0, s>>>(a));
+void few_launch(const FewArgs& a, hipStream_t s) {
+  const int64_t items = std::min<int64_t>(a.E_r, (int64_t)a.T * a.k) * (a.H / 16) + a.Hs / 16;
+  const int most = (NT == 1 ? 4 : 2) * num_cus();  // as many as are resident at once
+  MOE_TIMED("few_gu", s, few_gu_kernel<E, MX, ACT, NT>
+            <<<(int)std::max<int64_t>(1, std::min<int64_t>(items, most)), 64 * gu_waves(NT), 0, s>>>(a));
+#define FEW_DOWN(RB) \
+  MOE_TIMED("few_down", s, few_down_kernel<E, MX, NT, RB><<<a.d / RB, 64 * DW, 0, s>>>(a))
+  if (a.d / 16 >= num_cus()) FEW_DOWN(16);
+  else if (a.d / 8 >= num_cus()) FEW_DOWN(8);
+  else FEW_DOWN(4);
+#undef FEW_DOWN
 }
 template <class E, bool MX, int ACT>
-void few_tiles(const FewArgs& a, int gu_blocks, hipStream_t s) {
-  if (a.T <= 16) few_launch<E, MX, ACT, 1>(a, gu_blocks, s);
-  else if (a.T <= 32) few_launch<E, MX, ACT, 2>(a, gu_blocks, s);
-  else if (a.T <= 48) few_launch<E, MX, ACT, 3>(a, gu_blocks, s);
-  else few_launch<E, MX, ACT, 4>(a, gu_blocks, s);
+void few_tiles(const FewArgs& a, hipStream_t s) {
+  if (a.T <= 16) few_launch<E, MX, ACT, 1>(a, s);
+  else if (a.T <= 32) few_launch<E, MX, ACT, 2>(a, s);
+  else if (a.T <= 48) few_launch<E, MX, ACT, 3>(a, s);
+  else few_launch<E, MX, ACT, 4>(a, s);
 }
 
 }  // namespace
@@ -587,31 +592,24 @@ hipError_t launch_few(const moe_few* f, hipStream_t s) {
   a.sgu_s = f->shared_gate_up_scales; a.sd_s = f->shared_down_scales;
   a.logits = f->logits ? f->logits : reinterpret_cast<float*>(ws + l.logits);
   a.idx = f->topk_idx; a.tw = f->topk_w; a.local = f->topk_local; a.y = f->y;
-  a.counters = reinterpret_cast<int*>(ws + l.counters);
-  a.w_gate = reinterpret_cast<float*>(ws + l.gate);
   a.w_local = reinterpret_cast<int32_t*>(ws + l.local);
   a.h = ws + l.h;
   a.hs = ws + l.hs;
-  a.part = reinterpret_cast<float*>(ws + l.part);
   a.T = f->T; a.d = f->d; a.E = f->E; a.k = f->k; a.E_r = f->E_r; a.H = f->H; a.Hs = f->Hs;
   a.gate = f->gate; a.inv_tau = f->inv_tau;
-  a.n_slices = f->d / 16;
-  a.parts = l.parts;
   if (f->dtype == MOE_BF16)
     MOE_TIMED("few_logits", s, few_logits_bf16_kernel<<<dim3(ceil_div(f->E, LE), ceil_div(f->T, 32)),
-                                                        FT, 0, s>>>(a));
+                                                        64 * LW, 0, s>>>(a));
   else
     MOE_TIMED("few_logits", s, few_logits_f32_kernel<<<dim3(ceil_div(f->E, 16), ceil_div(f->T, 16)),
                                                        256, 0, s>>>(a));
-  const int64_t items = std::min<int64_t>(f->E_r, (int64_t)f->T * f->k) * (f->H / 16) + f->Hs / 16;
-  const int gu = (int)std::max<int64_t>(1, std::min<int64_t>(items, 2 * num_cus()));
   const bool swiglu = f->activation == MOE_ACT_SWIGLU;
   if (f->weights == MOE_W_MXFP4)
-    swiglu ? few_tiles<bf16_t, true, MOE_ACT_SWIGLU>(a, gu, s) : few_tiles<bf16_t, true, MOE_ACT_SILU>(a, gu, s);
+    swiglu ? few_tiles<bf16_t, true, MOE_ACT_SWIGLU>(a, s) : few_tiles<bf16_t, true, MOE_ACT_SILU>(a, s);
   else if (f->dtype == MOE_BF16)
-    swiglu ? few_tiles<bf16_t, false, MOE_ACT_SWIGLU>(a, gu, s) : few_tiles<bf16_t, false, MOE_ACT_SILU>(a, gu, s);
+    swiglu ? few_tiles<bf16_t, false, MOE_ACT_SWIGLU>(a, s) : few_tiles<bf16_t, false, MOE_ACT_SILU>(a, s);
   else
-    swiglu ? few_tiles<float, false, MOE_ACT_SWIGLU>(a, gu, s) : few_tiles<float, false, MOE_ACT_SILU>(a, gu, s);
+    swiglu ? few_tiles<float, false, MOE_ACT_SWIGLU>(a, s) : few_tiles<float, false, MOE_ACT_SILU>(a, s);
   return hipGetLastError();
 }
 
