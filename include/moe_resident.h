@@ -437,7 +437,8 @@ int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype,
  * (which depends on the sizes, on whether logits is NULL, and on the current device's
  * compute-unit count); its contents on entry are ignored, and two calls may share it
  * only if they are ordered on a stream.
- * Limits: 0 <= T <= 64, 1 <= k <= 8, k <= E <= 256, d % 64 == 0, H % 64 == 0, Hs % 64 == 0;
+ * Limits: 0 <= T <= 64, 1 <= k <= 8, k <= E <= 256, d % 64 == 0, H % 64 == 0, Hs % 64 == 0,
+ * 2 max(H, Hs) d below 2^31;
  * x, y, the weights and codes 16-byte aligned.
  */
 enum { MOE_W_PLAIN = 0, MOE_W_MXFP4 = 1 };

@@ -576,6 +576,7 @@ int check_few_sizes(const moe_few* f) {
   REQUIRE(std::isfinite(f->inv_tau) && f->inv_tau > 0.f, "inv_tau must be finite and > 0");
   SUPPORT(f->d % 64 == 0 && f->H % 64 == 0 && f->Hs % 64 == 0,
           "d = %d, H = %d and Hs = %d must be multiples of 64", f->d, f->H, f->Hs);
+  SUPPORT(2L * std::max(f->H, f->Hs) * f->d < 1L << 31, "an expert's matrix must stay below 2^31 elements");
   return MOE_OK;
 }
 }  // namespace

@@ -8,15 +8,8 @@
 // Three launches: the logits (few_logits_*), the first projections (few_gu_kernel) and the
 // second ones with the sum over experts (few_down_kernel).  No rows are moved: the weights
 // are the matrix instruction's first operand (16 rows of an expert's matrix) and the tokens
-// its second (16 columns, all of the batch's tokens in up to four tiles; a tile that no
-// token of an expert falls in is skipped).  Columns of tokens that are not routed to the
-// expert cost nothing that counts: in few_gu_kernel they are not stored, in
-// few_down_kernel they are zeros.  So the second kernel's accumulators run on from expert
-// to expert, with the gate already in h.
-//
-// Weights go from HBM to registers in the order of the instruction's operand: a lane
-// takes a row's consecutive bytes, the four lanes of a row 64 or 128 of them.  (The
-// order of k within an instruction is free as long as both operands have the same.)
+// its second (16 columns).  The gate is in h, so that the second projections are plain sums.
+// (The order of k within a matrix instruction is free as long as both operands have the same.)
 #include <type_traits>
 
 #include "kernels.h"
@@ -45,13 +38,24 @@ struct FewArgs {
   void* y;
   // workspace
   int32_t* w_local;  // [T k]
-  void* h;         // [T k, H], rows of resident routes
-  void* hs;        // [T, Hs]
+  void* h;         // [T k + 1, H]: rows of resident routes; zeros
+  void* hs;        // [T + 1, Hs]; zeros
   int T, d, E, k, E_r, H, Hs, gate;
   float inv_tau;
 };
 
 // ------------------------------------------------------------------ logits
+// The rows of zeros behind h and hs, which few_down_kernel reads for tokens that are not
+// routed to an expert.
+template <class E>
+DEVI void few_zero_rows(const FewArgs& a) {
+  if (blockIdx.x || blockIdx.y) return;
+  E* h = static_cast<E*>(a.h) + (size_t)a.T * a.k * a.H;
+  E* hs = static_cast<E*>(a.hs) + (size_t)a.T * a.Hs;
+  for (int i = threadIdx.x; i < a.H; i += blockDim.x) h[i] = from_f32<E>(0.f);
+  for (int i = threadIdx.x; i < a.Hs; i += blockDim.x) hs[i] = from_f32<E>(0.f);
+}
+
 // bf16: 32 tokens by LE experts per block.  The sums are the router's, to the bit: wave w
 // takes the 64-wide slices w, w + 8, ... of d on v_mfma_f32_32x32x16_bf16 with the same
 // sixteen k in each, and the waves' sums are added in order.  Few experts per block, so
@@ -64,6 +68,7 @@ __global__ __launch_bounds__(64 * LW) void few_logits_bf16_kernel(FewArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane & 31, half = lane >> 5;
   const int e0 = blockIdx.x * LE, t0 = blockIdx.y * 32;
+  few_zero_rows<bf16_t>(a);
   const int n = (a.d + 63) / 64;
   const bool has_t = t0 + row < a.T, has_e = row < LE && e0 + row < a.E;
   const bf16_t* xr = x + (size_t)(has_t ? t0 + row : 0) * a.d;
@@ -115,6 +120,7 @@ __global__ __launch_bounds__(256) void few_logits_f32_kernel(FewArgs a) {
   const float* x = static_cast<const float*>(a.x);
   const float* w = static_cast<const float*>(a.w_router);
   const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
+  few_zero_rows<float>(a);
   const int lr = threadIdx.x >> 4, lc = (threadIdx.x & 15) * 4;  // the thread's 16 bytes of a chunk
   const float* xp = x + (size_t)min(t0 + lr, a.T - 1) * a.d;
   const float* wp = w + (size_t)min(e0 + lr, a.E - 1) * a.d;
@@ -146,15 +152,15 @@ __global__ __launch_bounds__(256) void few_logits_f32_kernel(FewArgs a) {
 }
 
 // ------------------------------------------------------------------ routes
-// The block's tables: each route's gate and local expert, the experts that any token is
-// routed to (in order), and for each of those the route of every token (or -1).
+// The block's tables: each route's gate and local expert, and the experts that any token is
+// routed to.
 struct FewTables {
   float gate[FEW_T * FEW_K];
   int16_t local[FEW_T * FEW_K];
   int16_t expert[256];        // active expert -> local id
-  int16_t slot[256];          // local id -> active expert, or -1
+  int slot[256];              // tokens of a local expert
   int lmap[256];
-  int n_active;
+  int n_active, n_small;      // active experts, and those with up to 16 tokens
 };
 
 // Top-k, gates and local ids of token t, by 16 lanes (the router's selection on logits in
@@ -219,20 +225,29 @@ DEVI void few_select(const FewArgs& a, FewTables& tb, int t, bool publish) {
   }
 }
 
-// The active experts in ascending order (one wave; slot[] holds 1 for an expert with a route).
+// The active experts, those with up to 16 tokens first, each class in ascending order.  All
+// threads call it, with slot[] zero and the routes in local[]; it ends with a barrier.
 DEVI void few_active(const FewArgs& a, FewTables& tb) {
-  const int lane = threadIdx.x & 63;
-  int n = 0;
-  for (int r0 = 0; r0 < a.E_r; r0 += 64) {
-    const int r = r0 + lane;
-    const bool on = r < a.E_r && tb.slot[r] != 0;
-    const uint64_t m = __ballot(on);
-    const int s = n + __popcll(m & ((1ull << lane) - 1ull));
-    if (r < a.E_r) tb.slot[r] = (int16_t)(on ? s : -1);
-    if (on) tb.expert[s] = (int16_t)r;
-    n += __popcll(m);
+  for (int i = threadIdx.x; i < a.T * a.k; i += blockDim.x)
+    if (tb.local[i] >= 0) atomicAdd(&tb.slot[tb.local[i]], 1);
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    int n = 0;
+    for (int big = 0; big < 2; ++big) {
+      for (int r0 = 0; r0 < a.E_r; r0 += 64) {
+        const int r = r0 + lane;
+        const int c = r < a.E_r ? tb.slot[r] : 0;
+        const bool on = c > 0 && (c > 16) == (big == 1);
+        const uint64_t m = __ballot(on);
+        if (on) tb.expert[n + __popcll(m & ((1ull << lane) - 1ull))] = (int16_t)r;
+        n += __popcll(m);
+      }
+      if (big == 0 && lane == 0) tb.n_small = n;
+    }
+    if (lane == 0) tb.n_active = n;
   }
-  if (lane == 0) tb.n_active = n;
+  __syncthreads();
 }
 
 // Route (t k + j) of token t to local expert r, or -1.
@@ -245,296 +260,483 @@ DEVI int route_to(const FewArgs& a, const FewTables& tb, int t, int r) {
 }
 
 // ------------------------------------------------------------------ operands
-// One step of a wave: 16 weight rows by KS of k.  Lane (r, q) = (lane % 16, lane / 16)
-// holds the KL = KS / 4 values of row r from k0 + q KL on, and of token r likewise.
-//   bf16   KL 16 (32 bytes), two v_mfma_f32_16x16x32_bf16
-//   fp32   KL 8 (32 bytes), eight v_mfma_f32_16x16x4_f32
-//   MXFP4  KL 32 (16 bytes and one scale), widened to bf16 (exactly, a value has two
-//          significant bits): four v_mfma_f32_16x16x32_bf16 on bf16 activations
-template <class E, bool MX> struct Op;
-template <> struct Op<bf16_t, false> {
-  static constexpr int KL = 16;
-  struct W { bf16x8_t v[2]; };
-  struct X { bf16x8_t v[2]; };
-  DEVI static void load(W& w, const void* p, const uint8_t*, size_t row, int K, int k, bool ok) {
-    const bf16_t* q = static_cast<const bf16_t*>(p) + row * K + k;
-    const bf16x8_t z = {};
-    w.v[0] = ok ? *reinterpret_cast<const bf16x8_t*>(q) : z;
-    w.v[1] = ok ? *reinterpret_cast<const bf16x8_t*>(q + 8) : z;
-  }
-  DEVI static void load_x(X& x, const bf16_t* q, bool ok) {
-    const bf16x8_t z = {};
-    x.v[0] = ok ? *reinterpret_cast<const bf16x8_t*>(q) : z;
-    x.v[1] = ok ? *reinterpret_cast<const bf16x8_t*>(q + 8) : z;
-  }
-  DEVI static f32x4_t mma(const W& w, const X& x, f32x4_t c) {
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[0], x.v[0], c, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[1], x.v[1], c, 0, 0, 0);
-  }
+// One step of a wave: tiles of 16 weight rows and of 16 tokens by KS of k, brought to the
+// wave's own ring in LDS by DMA, whole row pieces of WROW (weights) and XROW (activations)
+// bytes, and read from there as operands: lane (r, q) = (lane % 16, lane / 16) holds row r.
+//   bf16   KS 64, two v_mfma_f32_16x16x32_bf16 per pair of tiles
+//   fp32   KS 32, eight v_mfma_f32_16x16x4_f32
+//   MXFP4  KS 128 (and a word of four scales per row), widened to bf16 (exactly, a value
+//          has two significant bits): four v_mfma_f32_16x16x32_bf16 on bf16 activations
+// (Loaded in operand order instead, straight to registers, a load instruction touches 16
+// rows and a CU's address unit was the bound: 2.3 to 3.1 TB/s over the GPU.)
+template <class E, bool MX> struct Fmt;
+template <> struct Fmt<bf16_t, false> { static constexpr int KS = 64, WROW = 128, XROW = 128; };
+template <> struct Fmt<float, false> { static constexpr int KS = 32, WROW = 128, XROW = 128; };
+template <> struct Fmt<bf16_t, true> { static constexpr int KS = 128, WROW = 64, XROW = 256; };
+
+// 16 bytes per lane from base + off (base uniform) to LDS at lds + 16 lane.  The asm sets m0
+// and leaves the one wait state an LDS DMA needs after it.
+DEVI void few_dma16(uint64_t base, unsigned off, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds)
+               : "m0", "memory");
+}
+// 4 bytes per lane, to lds + 4 lane.
+DEVI void few_dma4(uint64_t base, unsigned off, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds)
+               : "m0", "memory");
+}
+DEVI uint64_t uniform64(const void* p) {
+  const uint64_t v = (uint64_t)(uintptr_t)p;
+  const uint64_t lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)v);
+  const uint64_t hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(v >> 32));
+  return hi << 32 | lo;
+}
+
+// Row pieces of B bytes as a DMA instruction brings them: part p holds the rows
+// p * RPI + lane / LPR of a tile, and 16-byte chunk c of row r sits at chunk c ^ swz(r), so
+// that the 16 lanes of an operand read (16 rows, one chunk) are free of bank conflicts.
+template <int B>
+struct Piece {
+  static constexpr int LPR = B / 16, RPI = 64 / LPR, PARTS = 16 / RPI;
+  DEVI static int swz(int r) { return LPR == 4 ? (r >> 2) & 3 : LPR == 8 ? (r >> 1) & 7 : r & 15; }
+  DEVI static int row(int part) { return part * RPI + (int)(threadIdx.x & 63) / LPR; }
+  DEVI static int chunk(int part) { return ((int)(threadIdx.x & 63) % LPR) ^ swz(row(part)); }
+  DEVI static const char* at(const char* tile, int r, int c) { return tile + r * B + ((c ^ swz(r)) << 4); }
 };
-template <> struct Op<float, false> {
-  static constexpr int KL = 8;
-  struct W { f32x4_t v[2]; };
-  struct X { f32x4_t v[2]; };
-  DEVI static void load(W& w, const void* p, const uint8_t*, size_t row, int K, int k, bool ok) {
-    load_x(w, static_cast<const float*>(p) + row * K + k, ok);
-  }
-  template <class V> DEVI static void load_x(V& x, const float* q, bool ok) {
-    const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
-    x.v[0] = ok ? *reinterpret_cast<const f32x4_t*>(q) : z;
-    x.v[1] = ok ? *reinterpret_cast<const f32x4_t*>(q + 4) : z;
-  }
-  DEVI static f32x4_t mma(const W& w, const X& x, f32x4_t c) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      c = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[i >> 2][i & 3], x.v[i >> 2][i & 3], c, 0, 0, 0);
-    return c;
-  }
-};
+
 typedef __bf16 bf16x2_v __attribute__((ext_vector_type(2)));
-template <> struct Op<bf16_t, true> {
-  static constexpr int KL = 32;
-  struct W { u32x4_t c; unsigned s; };
-  struct X { bf16x8_t v[4]; };
-  DEVI static void load(W& w, const void* p, const uint8_t* s, size_t row, int K, int k, bool ok) {
-    const u32x4_t z = {0u, 0u, 0u, 0u};
-    w.c = ok ? *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(p) + (row * K + k) / 2) : z;
-    w.s = ok ? s[row * mx_stride(K) + k / MX_BLOCK] : 0u;
+DEVI bf16x8_t mx_widen8(unsigned c, float s) {
+  const bf16x2_v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0);
+  const bf16x2_v b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1);
+  const bf16x2_v d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2);
+  const bf16x2_v e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
+  const bf16x8_t v = {a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
+  return v;
+}
+
+constexpr int FW = 4;             // waves of few_gu_kernel and few_down_kernel, one block per CU
+constexpr int FT = 64 * FW;
+// Bytes of a wave's ring: what a CU's 160 KB leave beside the sums and tables.
+constexpr int GU_RING = 28 * 1024;
+constexpr int down_ring(int NT) { return NT <= 2 ? 36 * 1024 : 32 * 1024; }
+
+// A wave's stream of steps: RT tiles of weights and N of activations each.  WP: DMA parts of
+// a weight tile (fewer than all where only its first rows count).
+template <class E, bool MX, int RT, int N, int WP, int RING>
+struct Stream {
+  using F = Fmt<E, MX>;
+  using PW = Piece<F::WROW>;
+  using PX = Piece<F::XROW>;
+  static constexpr int W_TILE = WP * 1024, X_TILE = 16 * F::XROW;
+  static constexpr int STAGE = RT * W_TILE + N * X_TILE + (MX ? 256 : 0);
+  static constexpr int PER = RT * WP + N * PX::PARTS + (MX ? 1 : 0);  // DMA instructions of a step
+  static constexpr int D0 = RING / STAGE, D = D0 > 12 ? 12 : D0;        // steps in flight
+  static_assert(D >= 2 && D * PER <= 63, "a ring of two steps, counted by vmcnt");
+
+  // lane offsets, and what a lane past the end of a cut MXFP4 step (K % 128 == 64, its last
+  // two of four chunks) goes back to stay in the row
+  unsigned woff[WP], xoff[N][PX::PARTS], soff;
+  unsigned wback, xback;
+  char* ring;
+  unsigned ring_lds;
+  int K;
+
+  DEVI Stream(char* wave_ring, int k) : ring(wave_ring), K(k) {
+    ring_lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void_t*)wave_ring);
+    wback = xback = soff = 0;
   }
-  DEVI static void load_x(X& x, const bf16_t* q, bool ok) {
-    const bf16x8_t z = {};
+  // line: bytes of a weight row; rows: those of the matrix tile that exist (16, or fewer)
+  DEVI void weights(unsigned line, int rows) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[i] = ok ? *reinterpret_cast<const bf16x8_t*>(q + 8 * i) : z;
+    for (int p = 0; p < WP; ++p) woff[p] = min(PW::row(p), rows - 1) * line + PW::chunk(p) * 16;
+    // (one part: the lane's chunk is the same in every tile)
+    wback = MX && PW::chunk(0) >= 2 ? 32 : 0;
   }
-  DEVI static bf16x8_t widen(unsigned c, float s) {
-    const bf16x2_v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0);
-    const bf16x2_v b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1);
-    const bf16x2_v d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2);
-    const bf16x2_v e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
-    const bf16x8_t v = {a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
-    return v;
-  }
-  DEVI static f32x4_t mma(const W& w, const X& x, f32x4_t c) {
-    const float s = mx_scale_f32(w.s);
+  // the row of activations of each column of tile n, by column
+  DEVI void column(int n, int row_of_lane16) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w.c[i], s), x.v[i], c, 0, 0, 0);
-    return c;
+    for (int p = 0; p < PX::PARTS; ++p) {
+      const int row = __shfl(row_of_lane16, PX::row(p), 64);
+      xoff[n][p] = (unsigned)row * (unsigned)(K * sizeof(E)) + PX::chunk(p) * 16;
+    }
+  }
+  DEVI bool cut(int st) const { return MX && (st + 1) * F::KS > K; }
+
+  // w[i], scales: uniform addresses of the tiles' first row and of the scales at step 0
+  DEVI void issue(int slot, int st, const uint64_t* w, uint64_t scales, uint64_t x) const {
+    const unsigned at = ring_lds + slot * STAGE;
+    const bool c = cut(st);
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int p = 0; p < WP; ++p)
+        few_dma16(w[i] + (uint64_t)st * F::WROW, MX && c ? woff[p] - wback : woff[p], at + i * W_TILE + p * 1024);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int p = 0; p < PX::PARTS; ++p) {
+        unsigned o = xoff[n][p];
+        if (MX && c && PX::chunk(p) >= 8) o -= 128;
+        few_dma16(x + (uint64_t)st * F::XROW, o, at + RT * W_TILE + n * X_TILE + p * 1024);
+      }
+    if constexpr (MX) few_dma4(scales + (uint64_t)st * 4, soff, at + RT * W_TILE + N * X_TILE);
+  }
+
+  // Operands of one step, in registers.
+  struct Frags {
+    u32x4_t w[RT][MX ? 1 : 2];
+    u32x4_t x[N][MX ? 4 : 2];
+    unsigned s[RT];
+  };
+  DEVI void read(Frags& f, int slot, int st) const {
+    const char* at = ring + slot * STAGE;
+    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int p = 0; p < (MX ? 1 : 2); ++p)
+        f.w[i][p] = *reinterpret_cast<const u32x4_t*>(PW::at(at + i * W_TILE, r, 4 * p + q));
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int p = 0; p < (MX ? 4 : 2); ++p)
+        f.x[n][p] = *reinterpret_cast<const u32x4_t*>(PX::at(at + RT * W_TILE + n * X_TILE, r, MX ? 4 * q + p : 4 * p + q));
+    if constexpr (MX) {
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+        f.s[i] = *reinterpret_cast<const unsigned*>(at + RT * W_TILE + N * X_TILE + (16 * i + r) * 4) >> (8 * q) & 255u;
+      if (cut(st) && q >= 2)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) f.w[i][0] = u32x4_t{0u, 0u, 0u, 0u};
+    }
+  }
+  DEVI static void mma(const Frags& f, f32x4_t (&acc)[RT][N]) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      if constexpr (MX) {
+        const float s = mx_scale_f32(f.s[i]);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const bf16x8_t w = mx_widen8(f.w[i][0][p], s);
+#pragma unroll
+          for (int n = 0; n < N; ++n)
+            acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8_t, f.x[n][p]), acc[i][n], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int n = 0; n < N; ++n) {
+            if constexpr (sizeof(E) == 2) {
+              acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  __builtin_bit_cast(bf16x8_t, f.w[i][p]), __builtin_bit_cast(bf16x8_t, f.x[n][p]), acc[i][n], 0, 0, 0);
+            } else {
+              const f32x4_t a = __builtin_bit_cast(f32x4_t, f.w[i][p]), b = __builtin_bit_cast(f32x4_t, f.x[n][p]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], acc[i][n], 0, 0, 0);
+            }
+          }
+      }
+    }
   }
 };
+
+// Row of activations of each column of a wave's N tiles, from my_row (lane l: token l's, or
+// -1): the column's token t and its row.  compact: the tokens that have a row are moved to
+// the front (at most 16 of them); otherwise token first + 16 n + column.
+template <int N>
+struct Cols {
+  int t[N], row[N];
+  DEVI Cols(int my_row, bool compact, int first) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15;
+    int who = lane;
+    if (compact) {
+      const uint64_t on = __ballot(my_row >= 0), below = (1ull << lane) - 1ull;
+      const int to = my_row >= 0 ? __popcll(on & below) : __popcll(on) + __popcll(~on & below);
+      who = __builtin_amdgcn_ds_permute(to * 4, lane);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      t[n] = __shfl(who, (first + 16 * n + l16) & 63, 64);
+      row[n] = __shfl(my_row, t[n], 64);
+    }
+  }
+};
+
+// Tiles that a pass over an expert's weights takes, and passes over all of a batch's NT tiles.
+// (MXFP4 activations take 4 KB of a stage per tile: more than two would leave no ring.)
+constexpr int pass_tiles(bool MX, int NT) { return MX && NT > 2 ? 2 : NT; }
+constexpr int passes(bool MX, int NT) { return MX && NT > 2 ? 2 : 1; }
 
 // ------------------------------------------------------------------ first projections
-// An item is 16 hidden units of one expert (32 rows of a SwiGLU expert's matrix, 16 of a
-// SiLU one's); its k is dealt over the block's waves in steps, and the waves' sums are
-// added in order through LDS.
+// An item is 16 HG hidden units of one expert (for SwiGLU as many rows of W_g and of W_u);
+// its k is cut into a consecutive part for each wave, and the waves' sums are added in order
+// through LDS.  A wave's stream of steps runs on over the block's items: the next item's
+// loads are in flight while this one's sums are added.
 //
-// The shared experts' items come first and need no routing; every block makes the routes'
-// tables itself when it comes to its first routed item (a launch of its own for them would
-// take longer than their two microseconds).
-constexpr int gu_waves(int NT) { return NT == 1 ? 4 : 8; }
+// The shared experts' items come first: their loads are issued before the routes' tables are
+// made, which every block does for itself (a launch of its own for them would take longer
+// than their two microseconds).  Then the experts with up to 16 tokens, in one tile, and
+// those with more.
+constexpr int gu_groups(bool MX) { return MX ? 2 : 1; }
 
 template <class E, bool MX, int ACT, int NT>
-__global__ __launch_bounds__(64 * gu_waves(NT), NT == 1 ? 4 : 2) void few_gu_kernel(FewArgs a) {
-  using O = Op<E, MX>;
-  constexpr int FW = gu_waves(NT), FT = 64 * FW;
-  constexpr int KL = O::KL, KS = 4 * KL;
-  constexpr int R = ACT == MOE_ACT_SWIGLU ? 2 : 1;
-  constexpr int U = NT == 1 && !MX ? 4 : 2;  // steps whose loads are issued together
+__global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
+  using F = Fmt<E, MX>;
+  constexpr int HG = gu_groups(MX), R = ACT == MOE_ACT_SWIGLU ? 2 : 1, RT = R * HG;
+  constexpr int HB = 16 * HG, NP = pass_tiles(MX, NT), PASS = passes(MX, NT);
+  __shared__ __attribute__((aligned(1024))) char rings[FW][GU_RING];
+  __shared__ f32x4_t red[FW][RT][NP][64];
   __shared__ FewTables tb;
-  __shared__ f32x4_t red[FW][R][NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int l16 = lane & 15, q4 = lane >> 4;
-  const E* x = static_cast<const E*>(a.x);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int q4 = lane >> 4;
+  const int steps = ceil_div(a.d, F::KS);
+  const int s_lo = steps * wave / FW, n = steps * (wave + 1) / FW - s_lo;
 
-  // hidden units h0 .. h0 + 15 of one expert; my_p: the row of h for lane t's token, or -1
-  auto item = [&](bool shared, int r, int h0, int my_p) {
-    const int H = shared ? a.Hs : a.H;
-    const uint64_t who = __ballot(my_p >= 0);
-    const void* W = shared ? a.sgu : a.wgu;
-    const uint8_t* S = shared ? a.sgu_s : a.wgu_s;
-    const size_t row0 = (size_t)r * R * H + h0 + l16;
-    f32x4_t acc[R][NT];
-#pragma unroll
-    for (int g = 0; g < R; ++g)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) acc[g][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = wave * KS; k0 < a.d; k0 += U * FW * KS) {
-      typename O::W w[U][R];
-      typename O::X xv[U][NT];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = k0 + u * FW * KS + q4 * KL;
-        const bool ok = k < a.d;
-#pragma unroll
-        for (int g = 0; g < R; ++g) O::load(w[u][g], W, S, row0 + (size_t)g * H, a.d, k, ok);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-          O::load_x(xv[u][n], x + (size_t)(16 * n + l16) * a.d + k, ok && (who >> (16 * n + l16) & 1));
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int g = 0; g < R; ++g)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) acc[g][n] = O::mma(w[u][g], xv[u][n], acc[g][n]);
-    }
-    __syncthreads();  // the previous item's sums have been read
-#pragma unroll
-    for (int g = 0; g < R; ++g)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) red[wave][g][n][lane] = acc[g][n];
+  auto tables = [&]() {
+    if (wave == 0) build_local_map(a.resident, a.E, tb.lmap);
+    for (int i = threadIdx.x; i < 256; i += FT) tb.slot[i] = 0;
     __syncthreads();
-    if (wave < NT) {
-      // this wave's tile: token 16 wave + l16, hidden units h0 + 4 q4 ..
-      const int t = 16 * wave + l16;
-      f32x4_t v[R];
+    for (int t = wave * 4 + q4; t - q4 < a.T; t += FW * 4) {
+      if (a.E <= 64) few_select<4>(a, tb, t, blockIdx.x == 0);
+      else if (a.E <= 128) few_select<8>(a, tb, t, blockIdx.x == 0);
+      else few_select<16>(a, tb, t, blockIdx.x == 0);
+    }
+    __syncthreads();
+    few_active(a, tb);
+  };
+
+  // The block's items lo + i gridDim < hi, each (expert of the class, pass, hidden units).
+  auto stream = [&](auto tiles, bool shared, int first, int lo, int hi, auto&& between) {
+    constexpr int N = decltype(tiles)::value;
+    const bool compact = !shared && N < NT && PASS * N < NT;
+    const int H = shared ? a.Hs : a.H, per = H / HB * (compact ? 1 : PASS);
+    const unsigned line = MX ? (unsigned)a.d / 2 : (unsigned)a.d * sizeof(E), sline = mx_stride(a.d);
+    const char* W = static_cast<const char*>(shared ? a.sgu : a.wgu);
+    const uint8_t* S = shared ? a.sgu_s : a.wgu_s;
+    Stream<E, MX, RT, N, Piece<F::WROW>::PARTS, GU_RING> st(rings[wave], a.d);
+    using ST = decltype(st);
+    st.weights(line, 16);
+    if constexpr (MX) {
+      const int tile = min(lane >> 4, RT - 1);  // (tiles g HG + hg)
+      st.soff = (unsigned)((tile / HG) * H + (tile % HG) * 16 + (lane & 15)) * sline;
+    }
+    const int items = hi > lo ? (hi - lo + (int)gridDim.x - 1) / (int)gridDim.x : 0, total = items * n;
+    // what item `it` is
+    auto expert = [&](int it) {
+      return shared ? 0 : __builtin_amdgcn_readfirstlane((int)tb.expert[first + it / per]);
+    };
+    auto cols = [&](int it, int r) {
+      const int my = lane >= a.T ? -1 : shared ? lane : route_to(a, tb, lane, r);
+      return Cols<N>(my, compact, compact ? 0 : it % per / (H / HB) * 16 * N);
+    };
+    int issued = 0, l_it = lo, l_s = 0;
+    uint64_t w[RT], sc = 0;
+    const uint64_t x = uniform64(a.x);
+    auto issue = [&]() {
+      if (l_s == 0) {
+        const int r = expert(l_it), h0 = l_it % (H / HB) * HB;
+        const Cols<N> c = cols(l_it, r);
 #pragma unroll
-      for (int g = 0; g < R; ++g) {
-        v[g] = red[0][g][wave][lane];
+        for (int i = 0; i < N; ++i) st.column(i, c.row[i] >= 0 ? c.t[i] : 0);
 #pragma unroll
-        for (int q = 1; q < FW; ++q) v[g] += red[q][g][wave][lane];
+        for (int i = 0; i < RT; ++i)
+          w[i] = uniform64(W + ((size_t)r * R * H + (size_t)(i / HG) * H + h0 + i % HG * 16) * line);
+        if constexpr (MX) sc = uniform64(S + ((size_t)r * R * H + h0) * sline);
       }
-      const int p = __shfl(my_p, t & 63, 64);
-      if (t < a.T && p >= 0) {
-        const float gate = shared ? 1.0f : tb.gate[p];
-        E* out = static_cast<E*>(shared ? a.hs : a.h) + (size_t)p * H + h0 + 4 * q4;
+      st.issue(issued % ST::D, s_lo + l_s, w, sc, x);
+      ++issued;
+      if (++l_s == n) {
+        l_s = 0;
+        l_it += gridDim.x;
+      }
+    };
+    for (int i = 0; i < ST::D; ++i)
+      if (issued < total) issue();
+    between();
+    int done = 0;
+    for (int it = lo; it < hi; it += gridDim.x) {
+      f32x4_t acc[RT][N];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float s = gate * silu_f(v[0][i]);
-          out[i] = from_f32<E>(R == 2 ? s * v[R - 1][i] : s);
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int m = 0; m < N; ++m) acc[i][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int s = 0; s < n; ++s) {
+        wait_vm_groups<ST::PER, ST::D - 1>(issued - done - 1);
+        typename ST::Frags f;
+        st.read(f, done % ST::D, s_lo + s);
+        WAIT_LGKMCNT(0);  // the operands are in registers: their place may be refilled
+        if (issued < total) issue();
+        ST::mma(f, acc);
+        ++done;
+      }
+      __syncthreads();  // the previous item's sums have been read
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int m = 0; m < N; ++m) red[wave][i][m][lane] = acc[i][m];
+      __syncthreads();
+      const int r = expert(it), h0 = it % (H / HB) * HB;
+      const Cols<N> c = cols(it, r);
+#pragma unroll
+      for (int m = 0; m < N; ++m)
+#pragma unroll
+        for (int g = 0; g < HG; ++g) {
+          // tile m of hidden group g by one wave: hidden units h0 + 16 g + 4 q4 ..
+          if (wave != (m * HG + g) % FW) continue;
+          f32x4_t v[R];
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            v[i] = red[0][i * HG + g][m][lane];
+#pragma unroll
+            for (int q = 1; q < FW; ++q) v[i] += red[q][i * HG + g][m][lane];
+          }
+          if (c.row[m] >= 0) {
+            const float gate = shared ? 1.0f : tb.gate[c.row[m]];
+            E* out = static_cast<E*>(shared ? a.hs : a.h) + (size_t)c.row[m] * H + h0 + 16 * g + 4 * q4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float s = gate * silu_f(v[0][i]);
+              out[i] = from_f32<E>(R == 2 ? s * v[R - 1][i] : s);
+            }
+          }
         }
-      }
     }
   };
 
-  const int n_s = a.Hs / 16, n_r = a.H / 16;
-  int it = blockIdx.x;
-  for (; it < n_s; it += gridDim.x) item(true, 0, it * 16, lane < a.T ? lane : -1);
-
-  if (wave == 0) build_local_map(a.resident, a.E, tb.lmap);
-  for (int i = threadIdx.x; i < 256; i += FT) tb.slot[i] = 0;
-  __syncthreads();
-  for (int t = wave * 4 + q4; t - q4 < a.T; t += FW * 4) {
-    if (a.E <= 64) few_select<4>(a, tb, t, blockIdx.x == 0);
-    else if (a.E <= 128) few_select<8>(a, tb, t, blockIdx.x == 0);
-    else few_select<16>(a, tb, t, blockIdx.x == 0);
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.T * a.k; i += FT)
-    if (tb.local[i] >= 0) tb.slot[tb.local[i]] = 1;
-  __syncthreads();
-  if (wave == 0) few_active(a, tb);
-  __syncthreads();
-  for (; it < n_s + tb.n_active * n_r; it += gridDim.x) {
-    const int r = tb.expert[(it - n_s) / n_r];
-    item(false, r, (it - n_s) % n_r * 16, route_to(a, tb, lane, r));
+  typedef std::integral_constant<int, 1> One;
+  typedef std::integral_constant<int, NP> All;
+  const int n_s = a.Hs / HB * PASS, n_r = a.H / HB;
+  stream(All{}, true, 0, blockIdx.x, n_s, tables);
+  // the first of this block's numbers from `from` on
+  auto next = [&](int from) {
+    const int m = (from - (int)blockIdx.x) % (int)gridDim.x;
+    return from + (m > 0 ? (int)gridDim.x - m : -m);
+  };
+  auto nothing = [] {};
+  const int e1 = tb.n_small * n_r, e2 = e1 + (tb.n_active - tb.n_small) * n_r * PASS;
+  if constexpr (NT == 1) {
+    stream(One{}, false, 0, next(n_s) - n_s, e1, nothing);
+  } else {
+    stream(One{}, false, 0, next(n_s) - n_s, e1, nothing);
+    stream(All{}, false, tb.n_small, next(n_s + e1) - n_s - e1, e2 - e1, nothing);
   }
 }
 
 // ------------------------------------------------------------------ second projections
-// A block is RB columns of y (rows of W_d; the matrix instruction's other rows are empty)
-// and the whole reduction: the shared experts' hidden units, then all active experts', in
-// steps of which each wave takes consecutive ones.  Sums run on over experts; the waves'
-// are added in order through LDS.  RB is 16, or less where that would leave CUs without a
-// block: cutting the reduction into parts instead, added by the last block to finish, took
-// three times as long (the fences write back each XCD's whole L2).
-constexpr int DW = 16;  // waves
-
+// A block is RB columns of y (rows of W_d; the matrix instruction's other rows repeat the
+// last one) and the whole reduction: the shared experts' hidden units, then all active
+// experts', in steps of which each wave takes consecutive ones, its stream running on from
+// expert to expert.  RB is 16, or less where that would leave CUs without a block: cutting the
+// reduction into parts instead, added by the last block to finish, took three times as long
+// (the fences write back each XCD's whole L2).
+//
+// Up to 16 tokens (NT 1) the accumulators run on too, every token in its own column (rows of
+// zeros for those not routed to the expert).  With more, an expert's tokens are moved
+// together into one tile if they fit, and its sums are added to the wave's own rows of y
+// in LDS.
 template <class E, bool MX, int NT, int RB>
-__global__ __launch_bounds__(64 * DW) void few_down_kernel(FewArgs a) {
-  using O = Op<E, MX>;
-  constexpr int KL = O::KL, KS = 4 * KL;
-  constexpr int U = NT == 1 && !MX ? 2 : 1;  // steps in a stage; two stages' loads in flight
+__global__ __launch_bounds__(FT) void few_down_kernel(FewArgs a) {
+  using F = Fmt<E, MX>;
+  constexpr int NP = pass_tiles(MX, NT), PASS = passes(MX, NT);
+  constexpr int WP = RB < 16 && Piece<F::WROW>::PARTS == 2 ? 1 : Piece<F::WROW>::PARTS;
+  __shared__ __attribute__((aligned(1024))) char rings[FW][down_ring(NT)];
+  __shared__ f32x4_t red[FW][16 * NT][RB / 4];
   __shared__ FewTables tb;
-  __shared__ f32x4_t red[DW][NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, q4 = lane >> 4;
-  for (int i = threadIdx.x; i < a.T * a.k; i += 64 * DW) tb.local[i] = (int16_t)a.w_local[i];
-  for (int i = threadIdx.x; i < 256; i += 64 * DW) tb.slot[i] = 0;
-  const int row = blockIdx.x * RB + l16;
-  const bool has_row = l16 < RB;
-  f32x4_t acc[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) acc[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int i = lane; i < 16 * NT * (RB / 4); i += 64) (&red[wave][0][0])[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  struct Stage {
-    typename O::W w[U];
-    typename O::X x[U][NT];
+  auto tables = [&]() {
+    for (int i = threadIdx.x; i < a.T * a.k; i += FT) tb.local[i] = (int16_t)a.w_local[i];
+    for (int i = threadIdx.x; i < 256; i += FT) tb.slot[i] = 0;
+    __syncthreads();
+    few_active(a, tb);
   };
-  int cur = -1, my_p = -1, r = 0;  // the active expert at hand and lane t's route to it
-  // the steps [s0, s1) of n_h to an expert; the shared ones if SH
-  auto run = [&](auto SH, int s0, int s1, int n_h) {
-    constexpr bool shared = decltype(SH)::value;
-    const int H = shared ? a.Hs : a.H;
-    const void* W = shared ? a.sd : a.wd;
-    const uint8_t* S = shared ? a.sd_s : a.wd_s;
-    const E* h = static_cast<const E*>(shared ? a.hs : a.h);
-    auto load = [&](Stage& g, int s) {
+
+  // The wave's share of the steps of `experts` experts (PASS passes over each if not compact).
+  auto stream = [&](auto tiles, bool shared, int first, int experts, auto&& between) {
+    constexpr int N = decltype(tiles)::value;
+    const bool compact = !shared && N < NT && PASS * N < NT;
+    const int H = shared ? a.Hs : a.H, n_h = ceil_div(H, F::KS), n_p = compact ? 1 : PASS;
+    const int64_t all = (int64_t)experts * n_p * n_h;
+    const int s_lo = (int)(all * wave / FW), s_hi = (int)(all * (wave + 1) / FW);
+    const unsigned line = MX ? (unsigned)H / 2 : (unsigned)H * sizeof(E), sline = mx_stride(H);
+    const char* W = static_cast<const char*>(shared ? a.sd : a.wd) + (size_t)blockIdx.x * RB * line;
+    const uint8_t* S = (shared ? a.sd_s : a.wd_s) + (size_t)blockIdx.x * RB * sline;
+    Stream<E, MX, 1, N, WP, down_ring(NT)> st(rings[wave], H);
+    using ST = decltype(st);
+    st.weights(line, RB);
+    st.soff = (unsigned)min(l16, RB - 1) * sline;
+    const int zero_row = shared ? a.T : a.T * a.k;
+    auto expert = [&](int s) {
+      return shared ? 0 : __builtin_amdgcn_readfirstlane((int)tb.expert[first + s / (n_h * n_p)]);
+    };
+    auto cols = [&](int s, int r) {
+      const int my = lane >= a.T ? -1 : shared ? lane : route_to(a, tb, lane, r);
+      return Cols<N>(my, compact, compact ? 0 : s / n_h % n_p * 16 * N);
+    };
+    int issued = s_lo;
+    uint64_t w = 0, sc = 0;
+    const uint64_t x = uniform64(shared ? a.hs : a.h);
+    auto issue = [&]() {
+      const int s = issued % n_h;
+      if (issued == s_lo || s == 0) {
+        const int r = expert(issued);
+        const Cols<N> c = cols(issued, r);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int st = s + u;
-        const bool on = st < s1;
-        int k = st;
-        if constexpr (!shared) {
-          const int act = st / n_h;
-          k -= act * n_h;
-          if (on && act != cur) {
-            cur = act;
-            r = tb.expert[act];
-            my_p = route_to(a, tb, lane, r);
-          }
-        }
-        k = k * KS + q4 * KL;
-        const bool ok = on && k < H;
-        O::load(g.w[u], W, S, (size_t)r * a.d + row, H, k, ok && has_row);
+        for (int i = 0; i < N; ++i) st.column(i, c.row[i] >= 0 ? c.row[i] : zero_row);
+        w = uniform64(W + (size_t)r * a.d * line);
+        if constexpr (MX) sc = uniform64(S + (size_t)r * a.d * sline);
+      }
+      st.issue((issued - s_lo) % ST::D, s, &w, sc, x);
+      ++issued;
+    };
+    for (int i = 0; i < ST::D; ++i)
+      if (issued < s_hi) issue();
+    between();
+    f32x4_t acc[1][N];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const int p = __shfl(my_p, 16 * n + l16, 64);
-          O::load_x(g.x[u][n], h + (size_t)(p < 0 ? 0 : p) * H + k, ok && p >= 0);
+    for (int i = 0; i < N; ++i) acc[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int s = s_lo; s < s_hi; ++s) {
+      wait_vm_groups<ST::PER, ST::D - 1>(issued - s - 1);
+      typename ST::Frags f;
+      st.read(f, (s - s_lo) % ST::D, s % n_h);
+      WAIT_LGKMCNT(0);  // the operands are in registers: their place may be refilled
+      if (issued < s_hi) issue();
+      ST::mma(f, acc);
+      // the end of the wave's steps, or (every token its own column: only there) of an expert
+      if (s + 1 == s_hi || ((NT > 1 || PASS > 1) && (s + 1) % n_h == 0)) {
+        const Cols<N> c = cols(s, expert(s));
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int t = NT == 1 ? l16 : c.t[i];
+          if ((NT == 1 || c.row[i] >= 0) && 4 * q4 < RB) red[wave][t][q4] += acc[0][i];
+          acc[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
       }
-    };
-    auto mma = [&](const Stage& g) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n] = O::mma(g.w[u], g.x[u][n], acc[n]);
-    };
-    if (s0 >= s1) return;
-    Stage g0, g1;
-    load(g0, s0);
-    for (int s = s0; s < s1; s += 2 * U) {
-      load(g1, s + U);
-      mma(g0);
-      load(g0, s + 2 * U);
-      mma(g1);
     }
   };
-  if (a.Hs) {
-    my_p = lane < a.T ? lane : -1;
-    const int n = ceil_div(a.Hs, KS);
-    run(std::true_type{}, n * wave / DW, n * (wave + 1) / DW, n);
+  typedef std::integral_constant<int, 1> One;
+  typedef std::integral_constant<int, NP> All;
+  stream(All{}, true, 0, a.Hs ? 1 : 0, tables);
+  auto nothing = [] {};
+  if constexpr (NT == 1) {
+    stream(One{}, false, 0, tb.n_active, nothing);
+  } else {
+    stream(One{}, false, 0, tb.n_small, nothing);
+    stream(All{}, false, tb.n_small, tb.n_active - tb.n_small, nothing);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < a.T * a.k; i += 64 * DW)
-    if (tb.local[i] >= 0) tb.slot[tb.local[i]] = 1;
-  __syncthreads();
-  if (wave == 0) few_active(a, tb);
-  __syncthreads();
-  const int n_h = ceil_div(a.H, KS), n = tb.n_active * n_h;
-  run(std::false_type{}, n * wave / DW, n * (wave + 1) / DW, n_h);
+  for (int i = threadIdx.x; i < a.T * (RB / 4); i += FT) {
+    const int t = i / (RB / 4), c = i % (RB / 4);
+    f32x4_t v = red[0][t][c];
 #pragma unroll
-  for (int q = 0; q < NT; ++q) red[wave][q][lane] = acc[q];
-  __syncthreads();
-  // token t of tile `wave`, columns RB blockIdx.x + 4 q4 ..
-  const int t = 16 * wave + l16;
-  if (wave < NT && t < a.T && 4 * q4 < RB) {
-    f32x4_t v = red[0][wave][lane];
+    for (int q = 1; q < FW; ++q) v += red[q][t][c];
+    E* y = static_cast<E*>(a.y) + (size_t)t * a.d + blockIdx.x * RB + 4 * c;
 #pragma unroll
-    for (int q = 1; q < DW; ++q) v += red[q][wave][lane];
-    E* y = static_cast<E*>(a.y) + (size_t)t * a.d + blockIdx.x * RB + 4 * q4;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = from_f32<E>(v[i]);
+    for (int j = 0; j < 4; ++j) y[j] = from_f32<E>(v[j]);
   }
 }
 
@@ -550,20 +752,20 @@ FewLayout few_layout(const moe_few* f) {
   auto take = [&](size_t n) { const size_t o = at; at += up256(n); return o; };
   l.local = take(T * f->k * 4);
   l.logits = take(f->logits ? 0 : T * f->E * 4);
-  l.h = take(T * f->k * f->H * e);
-  l.hs = take(T * f->Hs * e);
+  l.h = take((T * f->k + 1) * f->H * e);
+  l.hs = take((T + 1) * f->Hs * e);
   l.bytes = at;
   return l;
 }
 
 template <class E, bool MX, int ACT, int NT>
 void few_launch(const FewArgs& a, hipStream_t s) {
-  const int64_t items = std::min<int64_t>(a.E_r, (int64_t)a.T * a.k) * (a.H / 16) + a.Hs / 16;
-  const int most = (NT == 1 ? 4 : 2) * num_cus();  // as many as are resident at once
-  MOE_TIMED("few_gu", s, few_gu_kernel<E, MX, ACT, NT>
-            <<<(int)std::max<int64_t>(1, std::min<int64_t>(items, most)), 64 * gu_waves(NT), 0, s>>>(a));
+  const int64_t items =
+      (std::min<int64_t>(a.E_r, (int64_t)a.T * a.k) * (a.H / 16) + a.Hs / 16) / gu_groups(MX) * passes(MX, NT);
+  const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(items, num_cus()));
+  MOE_TIMED("few_gu", s, few_gu_kernel<E, MX, ACT, NT><<<blocks, FT, 0, s>>>(a));
 #define FEW_DOWN(RB) \
-  MOE_TIMED("few_down", s, few_down_kernel<E, MX, NT, RB><<<a.d / RB, 64 * DW, 0, s>>>(a))
+  MOE_TIMED("few_down", s, few_down_kernel<E, MX, NT, RB><<<a.d / RB, FT, 0, s>>>(a))
   if (a.d / 16 >= num_cus()) FEW_DOWN(16);
   else if (a.d / 8 >= num_cus()) FEW_DOWN(8);
   else FEW_DOWN(4);
