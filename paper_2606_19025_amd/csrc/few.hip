@@ -38,24 +38,13 @@ struct FewArgs {
   void* y;
   // workspace
   int32_t* w_local;  // [T k]
-  void* h;         // [T k + 1, H]: rows of resident routes; zeros
-  void* hs;        // [T + 1, Hs]; zeros
+  void* h;         // [T k, H]: rows of resident routes
+  void* hs;        // [T, Hs]
   int T, d, E, k, E_r, H, Hs, gate;
   float inv_tau;
 };
 
 // ------------------------------------------------------------------ logits
-// The rows of zeros behind h and hs, which few_down_kernel reads for tokens that are not
-// routed to an expert.
-template <class E>
-DEVI void few_zero_rows(const FewArgs& a) {
-  if (blockIdx.x || blockIdx.y) return;
-  E* h = static_cast<E*>(a.h) + (size_t)a.T * a.k * a.H;
-  E* hs = static_cast<E*>(a.hs) + (size_t)a.T * a.Hs;
-  for (int i = threadIdx.x; i < a.H; i += blockDim.x) h[i] = from_f32<E>(0.f);
-  for (int i = threadIdx.x; i < a.Hs; i += blockDim.x) hs[i] = from_f32<E>(0.f);
-}
-
 // bf16: 32 tokens by LE experts per block.  The sums are the router's, to the bit: wave w
 // takes the 64-wide slices w, w + 8, ... of d on v_mfma_f32_32x32x16_bf16 with the same
 // sixteen k in each, and the waves' sums are added in order.  Few experts per block, so
@@ -68,7 +57,6 @@ __global__ __launch_bounds__(64 * LW) void few_logits_bf16_kernel(FewArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane & 31, half = lane >> 5;
   const int e0 = blockIdx.x * LE, t0 = blockIdx.y * 32;
-  few_zero_rows<bf16_t>(a);
   const int n = (a.d + 63) / 64;
   const bool has_t = t0 + row < a.T, has_e = row < LE && e0 + row < a.E;
   const bf16_t* xr = x + (size_t)(has_t ? t0 + row : 0) * a.d;
@@ -120,7 +108,6 @@ __global__ __launch_bounds__(256) void few_logits_f32_kernel(FewArgs a) {
   const float* x = static_cast<const float*>(a.x);
   const float* w = static_cast<const float*>(a.w_router);
   const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
-  few_zero_rows<float>(a);
   const int lr = threadIdx.x >> 4, lc = (threadIdx.x & 15) * 4;  // the thread's 16 bytes of a chunk
   const float* xp = x + (size_t)min(t0 + lr, a.T - 1) * a.d;
   const float* wp = w + (size_t)min(e0 + lr, a.E - 1) * a.d;
@@ -160,7 +147,7 @@ struct FewTables {
   int16_t expert[256];        // active expert -> local id
   int slot[256];              // tokens of a local expert
   int lmap[256];
-  int n_active, n_small;      // active experts, and those with up to 16 tokens
+  int n_class[3];             // experts with up to Q tokens, up to 16, more
 };
 
 // Top-k, gates and local ids of token t, by 16 lanes (the router's selection on logits in
@@ -225,8 +212,10 @@ DEVI void few_select(const FewArgs& a, FewTables& tb, int t, bool publish) {
   }
 }
 
-// The active experts, those with up to 16 tokens first, each class in ascending order.  All
-// threads call it, with slot[] zero and the routes in local[]; it ends with a barrier.
+// The active experts by their number of tokens (up to Q, up to 16, more), each class in
+// ascending order.  All threads call it, with slot[] zero and the routes in local[]; it
+// ends with a barrier.
+template <int Q>
 DEVI void few_active(const FewArgs& a, FewTables& tb) {
   for (int i = threadIdx.x; i < a.T * a.k; i += blockDim.x)
     if (tb.local[i] >= 0) atomicAdd(&tb.slot[tb.local[i]], 1);
@@ -234,18 +223,18 @@ DEVI void few_active(const FewArgs& a, FewTables& tb) {
   if (threadIdx.x < 64) {
     const int lane = threadIdx.x;
     int n = 0;
-    for (int big = 0; big < 2; ++big) {
+    for (int cl = 0; cl < 3; ++cl) {
+      const int n0 = n;
       for (int r0 = 0; r0 < a.E_r; r0 += 64) {
         const int r = r0 + lane;
         const int c = r < a.E_r ? tb.slot[r] : 0;
-        const bool on = c > 0 && (c > 16) == (big == 1);
+        const bool on = c > 0 && (c <= Q ? 0 : c <= 16 ? 1 : 2) == cl;
         const uint64_t m = __ballot(on);
         if (on) tb.expert[n + __popcll(m & ((1ull << lane) - 1ull))] = (int16_t)r;
         n += __popcll(m);
       }
-      if (big == 0 && lane == 0) tb.n_small = n;
+      if (lane == 0) tb.n_class[cl] = n - n0;
     }
-    if (lane == 0) tb.n_active = n;
   }
   __syncthreads();
 }
@@ -320,30 +309,30 @@ constexpr int FT = 64 * FW;
 constexpr int GU_RING = 28 * 1024;
 constexpr int down_ring(int NT) { return NT <= 2 ? 36 * 1024 : 32 * 1024; }
 
-// A wave's stream of steps: RT tiles of weights and N of activations each.  WP: DMA parts of
-// a weight tile (fewer than all where only its first rows count).
-template <class E, bool MX, int RT, int N, int WP, int RING>
+// A wave's stream of steps: RT tiles of weights and N of activations each.  WP, XP: DMA parts
+// of a tile of either (fewer than all where only its first rows count).
+template <class E, bool MX, int RT, int N, int WP, int XP, int RING>
 struct Stream {
   using F = Fmt<E, MX>;
   using PW = Piece<F::WROW>;
   using PX = Piece<F::XROW>;
-  static constexpr int W_TILE = WP * 1024, X_TILE = 16 * F::XROW;
+  static constexpr int W_TILE = WP * 1024, X_TILE = XP * 1024;
   static constexpr int STAGE = RT * W_TILE + N * X_TILE + (MX ? 256 : 0);
-  static constexpr int PER = RT * WP + N * PX::PARTS + (MX ? 1 : 0);  // DMA instructions of a step
+  static constexpr int PER = RT * WP + N * XP + (MX ? 1 : 0);  // DMA instructions of a step
   static constexpr int D0 = RING / STAGE, D = D0 > 12 ? 12 : D0;        // steps in flight
   static_assert(D >= 2 && D * PER <= 63, "a ring of two steps, counted by vmcnt");
 
   // lane offsets, and what a lane past the end of a cut MXFP4 step (K % 128 == 64, its last
   // two of four chunks) goes back to stay in the row
-  unsigned woff[WP], xoff[N][PX::PARTS], soff;
-  unsigned wback, xback;
+  unsigned woff[WP], xoff[N][XP], soff;
+  unsigned wback;
   char* ring;
   unsigned ring_lds;
   int K;
 
   DEVI Stream(char* wave_ring, int k) : ring(wave_ring), K(k) {
     ring_lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void_t*)wave_ring);
-    wback = xback = soff = 0;
+    wback = soff = 0;
   }
   // line: bytes of a weight row; rows: those of the matrix tile that exist (16, or fewer)
   DEVI void weights(unsigned line, int rows) {
@@ -355,7 +344,7 @@ struct Stream {
   // the row of activations of each column of tile n, by column
   DEVI void column(int n, int row_of_lane16) {
 #pragma unroll
-    for (int p = 0; p < PX::PARTS; ++p) {
+    for (int p = 0; p < XP; ++p) {
       const int row = __shfl(row_of_lane16, PX::row(p), 64);
       xoff[n][p] = (unsigned)row * (unsigned)(K * sizeof(E)) + PX::chunk(p) * 16;
     }
@@ -374,7 +363,7 @@ struct Stream {
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int p = 0; p < PX::PARTS; ++p) {
+      for (int p = 0; p < XP; ++p) {
         unsigned o = xoff[n][p];
         if (MX && c && PX::chunk(p) >= 8) o -= 128;
         few_dma16(x + (uint64_t)st * F::XROW, o, at + RT * W_TILE + n * X_TILE + p * 1024);
@@ -469,6 +458,14 @@ struct Cols {
 constexpr int pass_tiles(bool MX, int NT) { return MX && NT > 2 ? 2 : NT; }
 constexpr int passes(bool MX, int NT) { return MX && NT > 2 ? 2 : 1; }
 
+// How a class of experts is taken: N tiles of XP DMA parts at a time, PASS times; COMPACT: the
+// expert's tokens moved to the front of one tile.
+template <int N_, int XP_, int PASS_, bool COMPACT_>
+struct Class {
+  static constexpr int N = N_, XP = XP_, PASS = PASS_;
+  static constexpr bool COMPACT = COMPACT_;
+};
+
 // ------------------------------------------------------------------ first projections
 // An item is 16 HG hidden units of one expert (for SwiGLU as many rows of W_g and of W_u);
 // its k is cut into a consecutive part for each wave, and the waves' sums are added in order
@@ -477,15 +474,16 @@ constexpr int passes(bool MX, int NT) { return MX && NT > 2 ? 2 : 1; }
 //
 // The shared experts' items come first: their loads are issued before the routes' tables are
 // made, which every block does for itself (a launch of its own for them would take longer
-// than their two microseconds).  Then the experts with up to 16 tokens, in one tile, and
-// those with more.
+// than their two microseconds).  Then the experts with so few tokens that one DMA
+// instruction brings their activations, those with up to 16, and those with more.
 constexpr int gu_groups(bool MX) { return MX ? 2 : 1; }
 
 template <class E, bool MX, int ACT, int NT>
 __global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
   using F = Fmt<E, MX>;
   constexpr int HG = gu_groups(MX), R = ACT == MOE_ACT_SWIGLU ? 2 : 1, RT = R * HG;
-  constexpr int HB = 16 * HG, NP = pass_tiles(MX, NT), PASS = passes(MX, NT);
+  constexpr int HB = 16 * HG, NP = pass_tiles(MX, NT);
+  constexpr int PARTS = Piece<F::XROW>::PARTS, Q = Piece<F::XROW>::RPI;
   __shared__ __attribute__((aligned(1024))) char rings[FW][GU_RING];
   __shared__ f32x4_t red[FW][RT][NP][64];
   __shared__ FewTables tb;
@@ -504,18 +502,18 @@ __global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
       else few_select<16>(a, tb, t, blockIdx.x == 0);
     }
     __syncthreads();
-    few_active(a, tb);
+    few_active<Q>(a, tb);
   };
 
   // The block's items lo + i gridDim < hi, each (expert of the class, pass, hidden units).
-  auto stream = [&](auto tiles, bool shared, int first, int lo, int hi, auto&& between) {
-    constexpr int N = decltype(tiles)::value;
-    const bool compact = !shared && N < NT && PASS * N < NT;
-    const int H = shared ? a.Hs : a.H, per = H / HB * (compact ? 1 : PASS);
+  auto stream = [&](auto cl, bool shared, int first, int lo, int hi, auto&& between) {
+    using C = decltype(cl);
+    constexpr int N = C::N;
+    const int H = shared ? a.Hs : a.H, per = H / HB * C::PASS;
     const unsigned line = MX ? (unsigned)a.d / 2 : (unsigned)a.d * sizeof(E), sline = mx_stride(a.d);
     const char* W = static_cast<const char*>(shared ? a.sgu : a.wgu);
     const uint8_t* S = shared ? a.sgu_s : a.wgu_s;
-    Stream<E, MX, RT, N, Piece<F::WROW>::PARTS, GU_RING> st(rings[wave], a.d);
+    Stream<E, MX, RT, N, Piece<F::WROW>::PARTS, C::XP, GU_RING> st(rings[wave], a.d);
     using ST = decltype(st);
     st.weights(line, 16);
     if constexpr (MX) {
@@ -529,7 +527,7 @@ __global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
     };
     auto cols = [&](int it, int r) {
       const int my = lane >= a.T ? -1 : shared ? lane : route_to(a, tb, lane, r);
-      return Cols<N>(my, compact, compact ? 0 : it % per / (H / HB) * 16 * N);
+      return Cols<N>(my, C::COMPACT, C::PASS == 1 ? 0 : it % per / (H / HB) * 16 * N);
     };
     int issued = 0, l_it = lo, l_s = 0;
     uint64_t w[RT], sc = 0;
@@ -605,41 +603,47 @@ __global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
     }
   };
 
-  typedef std::integral_constant<int, 1> One;
-  typedef std::integral_constant<int, NP> All;
-  const int n_s = a.Hs / HB * PASS, n_r = a.H / HB;
-  stream(All{}, true, 0, blockIdx.x, n_s, tables);
+  typedef Class<1, 1, 1, true> Few;
+  typedef Class<1, PARTS, 1, true> One;
+  typedef Class<NP, PARTS, passes(MX, NT), false> All;
+  const int n_s = a.Hs / HB * All::PASS, n_r = a.H / HB;
   // the first of this block's numbers from `from` on
   auto next = [&](int from) {
     const int m = (from - (int)blockIdx.x) % (int)gridDim.x;
     return from + (m > 0 ? (int)gridDim.x - m : -m);
   };
   auto nothing = [] {};
-  const int e1 = tb.n_small * n_r, e2 = e1 + (tb.n_active - tb.n_small) * n_r * PASS;
+  if (NT == 1 && a.T <= Q) stream(Few{}, true, 0, blockIdx.x, n_s, tables);
+  else stream(All{}, true, 0, blockIdx.x, n_s, tables);
+  int from = n_s, first = 0;
+  auto routed = [&](auto cl, int experts) {
+    const int n_i = experts * n_r * decltype(cl)::PASS;
+    stream(cl, false, first, next(from) - from, n_i, nothing);
+    from += n_i;
+    first += experts;
+  };
+  routed(Few{}, tb.n_class[0]);
   if constexpr (NT == 1) {
-    stream(One{}, false, 0, next(n_s) - n_s, e1, nothing);
+    routed(All{}, tb.n_class[1]);
   } else {
-    stream(One{}, false, 0, next(n_s) - n_s, e1, nothing);
-    stream(All{}, false, tb.n_small, next(n_s + e1) - n_s - e1, e2 - e1, nothing);
+    routed(One{}, tb.n_class[1]);
+    routed(All{}, tb.n_class[2]);
   }
 }
 
 // ------------------------------------------------------------------ second projections
-// A block is RB columns of y (rows of W_d; the matrix instruction's other rows repeat the
-// last one) and the whole reduction: the shared experts' hidden units, then all active
-// experts', in steps of which each wave takes consecutive ones, its stream running on from
-// expert to expert.  RB is 16, or less where that would leave CUs without a block: cutting the
-// reduction into parts instead, added by the last block to finish, took three times as long
-// (the fences write back each XCD's whole L2).
-//
-// Up to 16 tokens (NT 1) the accumulators run on too, every token in its own column (rows of
-// zeros for those not routed to the expert).  With more, an expert's tokens are moved
-// together into one tile if they fit, and its sums are added to the wave's own rows of y
-// in LDS.
+// A block is RB columns of y (rows of W_d; the matrix instruction's other rows are not used)
+// and the whole reduction: the shared experts' hidden units, then all active experts', in
+// steps of which each wave takes consecutive ones, its stream running on from expert to
+// expert.  An expert's sums are added to the wave's own rows of y in LDS, and the waves' rows
+// in order at the end.  RB is 16, or less where that would leave CUs without a block: cutting
+// the reduction into parts instead, added by the last block to finish, took three times as
+// long (the fences write back each XCD's whole L2).
 template <class E, bool MX, int NT, int RB>
 __global__ __launch_bounds__(FT) void few_down_kernel(FewArgs a) {
   using F = Fmt<E, MX>;
-  constexpr int NP = pass_tiles(MX, NT), PASS = passes(MX, NT);
+  constexpr int NP = pass_tiles(MX, NT);
+  constexpr int PARTS = Piece<F::XROW>::PARTS, Q = Piece<F::XROW>::RPI;
   constexpr int WP = RB < 16 && Piece<F::WROW>::PARTS == 2 ? 1 : Piece<F::WROW>::PARTS;
   __shared__ __attribute__((aligned(1024))) char rings[FW][down_ring(NT)];
   __shared__ f32x4_t red[FW][16 * NT][RB / 4];
@@ -652,81 +656,111 @@ __global__ __launch_bounds__(FT) void few_down_kernel(FewArgs a) {
     for (int i = threadIdx.x; i < a.T * a.k; i += FT) tb.local[i] = (int16_t)a.w_local[i];
     for (int i = threadIdx.x; i < 256; i += FT) tb.slot[i] = 0;
     __syncthreads();
-    few_active(a, tb);
+    few_active<Q>(a, tb);
   };
 
-  // The wave's share of the steps of `experts` experts (PASS passes over each if not compact).
-  auto stream = [&](auto tiles, bool shared, int first, int experts, auto&& between) {
-    constexpr int N = decltype(tiles)::value;
-    const bool compact = !shared && N < NT && PASS * N < NT;
-    const int H = shared ? a.Hs : a.H, n_h = ceil_div(H, F::KS), n_p = compact ? 1 : PASS;
-    const int64_t all = (int64_t)experts * n_p * n_h;
+  // The wave's share of the steps of `experts` experts (C::PASS passes over each).
+  auto stream = [&](auto cl, bool shared, int first, int experts, auto&& between) {
+    using C = decltype(cl);
+    constexpr int N = C::N;
+    const int H = shared ? a.Hs : a.H, n_h = ceil_div(H, F::KS);
+    const int64_t all = (int64_t)experts * C::PASS * n_h;
     const int s_lo = (int)(all * wave / FW), s_hi = (int)(all * (wave + 1) / FW);
     const unsigned line = MX ? (unsigned)H / 2 : (unsigned)H * sizeof(E), sline = mx_stride(H);
     const char* W = static_cast<const char*>(shared ? a.sd : a.wd) + (size_t)blockIdx.x * RB * line;
     const uint8_t* S = (shared ? a.sd_s : a.wd_s) + (size_t)blockIdx.x * RB * sline;
-    Stream<E, MX, 1, N, WP, down_ring(NT)> st(rings[wave], H);
+    Stream<E, MX, 1, N, WP, C::XP, down_ring(NT)> st(rings[wave], H);
     using ST = decltype(st);
     st.weights(line, RB);
     st.soff = (unsigned)min(l16, RB - 1) * sline;
-    const int zero_row = shared ? a.T : a.T * a.k;
-    auto expert = [&](int s) {
-      return shared ? 0 : __builtin_amdgcn_readfirstlane((int)tb.expert[first + s / (n_h * n_p)]);
+    // pass v = expert * PASS + pass: its columns
+    auto expert = [&](int v) {
+      return shared ? 0 : __builtin_amdgcn_readfirstlane((int)tb.expert[first + v / C::PASS]);
     };
-    auto cols = [&](int s, int r) {
+    auto cols = [&](int v, int r) {
       const int my = lane >= a.T ? -1 : shared ? lane : route_to(a, tb, lane, r);
-      return Cols<N>(my, compact, compact ? 0 : s / n_h % n_p * 16 * N);
+      return Cols<N>(my, C::COMPACT, v % C::PASS * 16 * N);
     };
-    int issued = s_lo;
+    // the step to load next: slot of the ring, pass, step in it
+    int left = s_hi - s_lo, flying = 0, l_slot = 0, l_v = n_h ? s_lo / n_h : 0, l_s = s_lo - l_v * n_h;
+    bool fresh = true;
     uint64_t w = 0, sc = 0;
     const uint64_t x = uniform64(shared ? a.hs : a.h);
     auto issue = [&]() {
-      const int s = issued % n_h;
-      if (issued == s_lo || s == 0) {
-        const int r = expert(issued);
-        const Cols<N> c = cols(issued, r);
+      if (left == 0) return;
+      if (fresh) {
+        fresh = false;
+        const int r = expert(l_v);
+        const Cols<N> c = cols(l_v, r);
 #pragma unroll
-        for (int i = 0; i < N; ++i) st.column(i, c.row[i] >= 0 ? c.row[i] : zero_row);
+        for (int i = 0; i < N; ++i) st.column(i, max(c.row[i], 0));
         w = uniform64(W + (size_t)r * a.d * line);
         if constexpr (MX) sc = uniform64(S + (size_t)r * a.d * sline);
       }
-      st.issue((issued - s_lo) % ST::D, s, &w, sc, x);
-      ++issued;
-    };
-    for (int i = 0; i < ST::D; ++i)
-      if (issued < s_hi) issue();
-    between();
-    f32x4_t acc[1][N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) acc[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int s = s_lo; s < s_hi; ++s) {
-      wait_vm_groups<ST::PER, ST::D - 1>(issued - s - 1);
-      typename ST::Frags f;
-      st.read(f, (s - s_lo) % ST::D, s % n_h);
-      WAIT_LGKMCNT(0);  // the operands are in registers: their place may be refilled
-      if (issued < s_hi) issue();
-      ST::mma(f, acc);
-      // the end of the wave's steps, or (every token its own column: only there) of an expert
-      if (s + 1 == s_hi || ((NT > 1 || PASS > 1) && (s + 1) % n_h == 0)) {
-        const Cols<N> c = cols(s, expert(s));
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int t = NT == 1 ? l16 : c.t[i];
-          if ((NT == 1 || c.row[i] >= 0) && 4 * q4 < RB) red[wave][t][q4] += acc[0][i];
-          acc[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
+      st.issue(l_slot, l_s, &w, sc, x);
+      l_slot = l_slot + 1 == ST::D ? 0 : l_slot + 1;
+      if (++l_s == n_h) {
+        l_s = 0;
+        ++l_v;
+        fresh = true;
       }
+      --left;
+      ++flying;
+    };
+    int v = l_v, s = l_s, slot = 0, todo = left;
+    for (int i = 0; i < ST::D; ++i) issue();
+    between();
+    while (todo > 0) {
+      f32x4_t acc[1][N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) acc[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      int n = min(todo, n_h - s);
+      todo -= n;
+      // two steps at a time, so that a wave waits half as often for its operands
+      for (; n >= 2; n -= 2, s += 2) {
+        wait_vm_groups<ST::PER, ST::D - 2>(flying - 2);
+        typename ST::Frags f, g;
+        st.read(f, slot, s);
+        slot = slot + 1 == ST::D ? 0 : slot + 1;
+        st.read(g, slot, s + 1);
+        slot = slot + 1 == ST::D ? 0 : slot + 1;
+        WAIT_LGKMCNT(0);  // the operands are in registers: their places may be refilled
+        flying -= 2;
+        issue();
+        issue();
+        ST::mma(f, acc);
+        ST::mma(g, acc);
+      }
+      if (n) {
+        wait_vm_groups<ST::PER, ST::D - 1>(flying - 1);
+        typename ST::Frags f;
+        st.read(f, slot, s);
+        slot = slot + 1 == ST::D ? 0 : slot + 1;
+        WAIT_LGKMCNT(0);
+        --flying;
+        issue();
+        ST::mma(f, acc);
+      }
+      s = 0;
+      const Cols<N> c = cols(v, expert(v));
+      ++v;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (c.row[i] >= 0 && 4 * q4 < RB) red[wave][c.t[i]][q4] += acc[0][i];
     }
   };
-  typedef std::integral_constant<int, 1> One;
-  typedef std::integral_constant<int, NP> All;
-  stream(All{}, true, 0, a.Hs ? 1 : 0, tables);
+  typedef Class<1, 1, 1, true> Few;
+  typedef Class<1, PARTS, 1, true> One;
+  typedef Class<NP, PARTS, passes(MX, NT), false> All;
+  if (NT == 1 && a.T <= Q) stream(Few{}, true, 0, a.Hs ? 1 : 0, tables);
+  else stream(All{}, true, 0, a.Hs ? 1 : 0, tables);
   auto nothing = [] {};
+  stream(Few{}, false, 0, tb.n_class[0], nothing);
   if constexpr (NT == 1) {
-    stream(One{}, false, 0, tb.n_active, nothing);
+    stream(All{}, false, tb.n_class[0], tb.n_class[1], nothing);
   } else {
-    stream(One{}, false, 0, tb.n_small, nothing);
-    stream(All{}, false, tb.n_small, tb.n_active - tb.n_small, nothing);
+    stream(One{}, false, tb.n_class[0], tb.n_class[1], nothing);
+    stream(All{}, false, tb.n_class[0] + tb.n_class[1], tb.n_class[2], nothing);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < a.T * (RB / 4); i += FT) {
@@ -752,8 +786,8 @@ FewLayout few_layout(const moe_few* f) {
   auto take = [&](size_t n) { const size_t o = at; at += up256(n); return o; };
   l.local = take(T * f->k * 4);
   l.logits = take(f->logits ? 0 : T * f->E * 4);
-  l.h = take((T * f->k + 1) * f->H * e);
-  l.hs = take((T + 1) * f->Hs * e);
+  l.h = take(T * f->k * f->H * e);
+  l.hs = take(T * f->Hs * e);
   l.bytes = at;
   return l;
 }
