@@ -45,20 +45,21 @@ struct FewArgs {
 };
 
 // ------------------------------------------------------------------ logits
-// bf16: 32 tokens by LE experts per block.  The sums are the router's, to the bit: wave w
+// bf16: LT tokens by LE experts per block.  The sums are the router's, to the bit: wave w
 // takes the 64-wide slices w, w + 8, ... of d on v_mfma_f32_32x32x16_bf16 with the same
-// sixteen k in each, and the waves' sums are added in order.  Few experts per block, so
-// that a single token's logits come from many CUs.
-constexpr int LE = 8;
+// sixteen k in each, and the waves' sums are added in order.  Most of the instruction's rows
+// are empty: a block's time is that of its loads, and with 8 by 8 many CUs share them
+// (48 tokens, d = 2048, 64 experts: with 32 tokens 5 us, so 2).
+constexpr int LE = 8, LT = 8;
 __global__ __launch_bounds__(64 * LW) void few_logits_bf16_kernel(FewArgs a) {
-  __shared__ float part[LW][32 * LE];
+  __shared__ float part[LW][LT * LE];
   const bf16_t* x = static_cast<const bf16_t*>(a.x);
   const bf16_t* w = static_cast<const bf16_t*>(a.w_router);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane & 31, half = lane >> 5;
-  const int e0 = blockIdx.x * LE, t0 = blockIdx.y * 32;
+  const int e0 = blockIdx.x * LE, t0 = blockIdx.y * LT;
   const int n = (a.d + 63) / 64;
-  const bool has_t = t0 + row < a.T, has_e = row < LE && e0 + row < a.E;
+  const bool has_t = row < LT && t0 + row < a.T, has_e = row < LE && e0 + row < a.E;
   const bf16_t* xr = x + (size_t)(has_t ? t0 + row : 0) * a.d;
   const bf16_t* wr = w + (size_t)(has_e ? e0 + row : 0) * a.d;
   f32x16_t acc = {};
@@ -84,10 +85,10 @@ __global__ __launch_bounds__(64 * LW) void few_logits_bf16_kernel(FewArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int i = (r >> 2) * 8 + half * 4 + (r & 3);
-      part[wave][i * LE + row] = acc[r];
+      if (i < LT) part[wave][i * LE + row] = acc[r];
     }
   __syncthreads();
-  if (threadIdx.x < 32 * LE) {
+  if (threadIdx.x < LT * LE) {
     const int t = t0 + threadIdx.x / LE, e = e0 + threadIdx.x % LE;
     float v = part[0][threadIdx.x];
 #pragma unroll
@@ -150,19 +151,25 @@ struct FewTables {
   int n_class[3];             // experts with up to Q tokens, up to 16, more
 };
 
-// Top-k, gates and local ids of token t, by 16 lanes (the router's selection on logits in
-// global memory): lane s of a group holds the experts s, s + 16, ...
+// Top-k and gates of token t, by 16 lanes (the router's selection on logits in
+// global memory): lane s of a group holds the experts s, s + 16, ... in v[].
 template <int NE>
-DEVI void few_select(const FewArgs& a, FewTables& tb, int t, bool publish) {
+DEVI void few_logits_of(const FewArgs& a, int t, float (&v)[NE]) {
+  const int s = threadIdx.x & 15;
+#pragma unroll
+  for (int q = 0; q < NE; ++q) {
+    const int e = q * 16 + s;
+    v[q] = t < a.T && e < a.E ? sel_value(a.logits[(size_t)t * a.E + e]) : 0.f;
+  }
+}
+template <int NE>
+DEVI void few_select(const FewArgs& a, FewTables& tb, int t, const float (&v)[NE], bool publish) {
   const int lane = threadIdx.x & 63, s = lane & 15;
-  const float* z = a.logits + (size_t)t * a.E;
   const bool has = t < a.T;
-  float v[NE];
   uint64_t cand[NE];
 #pragma unroll
   for (int q = 0; q < NE; ++q) {
     const int e = q * 16 + s;
-    v[q] = has && e < a.E ? sel_value(z[e]) : 0.f;
     cand[q] = has && e < a.E ? ((uint64_t)sel_key(v[q]) << 32) | (uint32_t)~e : 0ull;
   }
   int my_id = 0;
@@ -199,15 +206,38 @@ DEVI void few_select(const FewArgs& a, FewTables& tb, int t, bool publish) {
   if (s < a.k && has) {
     const float g = a.gate == MOE_GATE_SIGMOID ? sigmoid_f(my_z) : expf(my_z - zmax) / denom;
     const int o = t * a.k + s;
-    // (a resident set larger than E_r says: its last experts are ghosts here)
-    const int l = tb.lmap[my_id] < a.E_r ? tb.lmap[my_id] : -1;
     tb.gate[o] = g;
-    tb.local[o] = (int16_t)l;
+    tb.local[o] = (int16_t)my_id;  // (few_localise makes it the local id)
     if (publish) {
-      a.w_local[o] = l;
       if (a.idx) a.idx[o] = my_id;
       if (a.tw) a.tw[o] = g;
-      if (a.local) a.local[o] = l;
+    }
+  }
+}
+
+// All tokens' selections by the WAVES waves of a block, every wave's logits loaded first.
+template <int WAVES, int NE>
+DEVI void few_select_all(const FewArgs& a, FewTables& tb, bool publish) {
+  constexpr int P = FEW_T / (4 * WAVES);
+  const int t = (threadIdx.x >> 6) * 4 + ((threadIdx.x & 63) >> 4);
+  float v[P][NE];
+#pragma unroll
+  for (int p = 0; p < P; ++p) few_logits_of<NE>(a, t + p * 4 * WAVES, v[p]);
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    if ((t & ~3) + p * 4 * WAVES < a.T) few_select<NE>(a, tb, t + p * 4 * WAVES, v[p], publish);
+}
+
+// Local ids of the routes' experts, or -1, from lmap[].
+DEVI void few_localise(const FewArgs& a, FewTables& tb, bool publish) {
+  for (int i = threadIdx.x; i < a.T * a.k; i += blockDim.x) {
+    const int m = tb.lmap[tb.local[i]];
+    // (a resident set larger than E_r says: its last experts are ghosts here)
+    const int l = m < a.E_r ? m : -1;
+    tb.local[i] = (int16_t)l;
+    if (publish) {
+      a.w_local[i] = l;
+      if (a.local) a.local[i] = l;
     }
   }
 }
@@ -303,11 +333,13 @@ DEVI bf16x8_t mx_widen8(unsigned c, float s) {
   return v;
 }
 
-constexpr int FW = 4;             // waves of few_gu_kernel and few_down_kernel, one block per CU
-constexpr int FT = 64 * FW;
+// Waves that stream weights in few_gu_kernel and few_down_kernel, whose blocks have a CU each.
+// The second's steps are a quarter as long, so that it takes two waves per SIMD to keep the
+// loads coming.
+constexpr int FW = 4, FT = 64 * FW, DW = 8, DT = 64 * DW;
 // Bytes of a wave's ring: what a CU's 160 KB leave beside the sums and tables.
-constexpr int GU_RING = 28 * 1024;
-constexpr int down_ring(int NT) { return NT <= 2 ? 36 * 1024 : 32 * 1024; }
+constexpr int gu_ring(int tiles) { return (tiles <= 2 ? 28 : 26) * 1024; }
+constexpr int down_ring(int NT) { return (NT == 1 ? 18 : NT == 2 ? 17 : NT == 3 ? 16 : 14) * 1024; }
 
 // A wave's stream of steps: RT tiles of weights and N of activations each.  WP, XP: DMA parts
 // of a tile of either (fewer than all where only its first rows count).
@@ -453,10 +485,10 @@ struct Cols {
   }
 };
 
-// Tiles that a pass over an expert's weights takes, and passes over all of a batch's NT tiles.
-// (MXFP4 activations take 4 KB of a stage per tile: more than two would leave no ring.)
-constexpr int pass_tiles(bool MX, int NT) { return MX && NT > 2 ? 2 : NT; }
-constexpr int passes(bool MX, int NT) { return MX && NT > 2 ? 2 : 1; }
+// Tiles that a pass over an expert's weights takes of a batch's NT.  (A tile of MXFP4
+// activations takes 4 KB of a stage, others 2: more would leave no ring.)
+constexpr int gu_tiles(bool MX, int NT) { return NT == 4 || (MX && NT > 2) ? 2 : NT; }
+constexpr int down_tiles(bool MX, int NT) { return MX ? 1 : NT > 3 ? 2 : NT; }
 
 // How a class of experts is taken: N tiles of XP DMA parts at a time, PASS times; COMPACT: the
 // expert's tokens moved to the front of one tile.
@@ -467,132 +499,76 @@ struct Class {
 };
 
 // ------------------------------------------------------------------ first projections
-// An item is 16 HG hidden units of one expert (for SwiGLU as many rows of W_g and of W_u);
-// its k is cut into a consecutive part for each wave, and the waves' sums are added in order
-// through LDS.  A wave's stream of steps runs on over the block's items: the next item's
-// loads are in flight while this one's sums are added.
+// An item is 16 hidden units of one expert (for SwiGLU as many rows of W_g and of W_u).  Four
+// waves of the block stream it, a consecutive part of its k each, and four more add their sums
+// in order, apply the activation and store h, while the first are at the next item: their
+// streams of steps run on over the block's items.
 //
 // The shared experts' items come first: their loads are issued before the routes' tables are
 // made, which every block does for itself (a launch of its own for them would take longer
 // than their two microseconds).  Then the experts with so few tokens that one DMA
 // instruction brings their activations, those with up to 16, and those with more.
-constexpr int gu_groups(bool MX) { return MX ? 2 : 1; }
-
 template <class E, bool MX, int ACT, int NT>
-__global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
+__global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
   using F = Fmt<E, MX>;
-  constexpr int HG = gu_groups(MX), R = ACT == MOE_ACT_SWIGLU ? 2 : 1, RT = R * HG;
-  constexpr int HB = 16 * HG, NP = pass_tiles(MX, NT);
+  constexpr int R = ACT == MOE_ACT_SWIGLU ? 2 : 1, NP = gu_tiles(MX, NT);
   constexpr int PARTS = Piece<F::XROW>::PARTS, Q = Piece<F::XROW>::RPI;
-  __shared__ __attribute__((aligned(1024))) char rings[FW][GU_RING];
-  __shared__ f32x4_t red[FW][RT][NP][64];
+  constexpr int RING = gu_ring(NP);
+  __shared__ __attribute__((aligned(1024))) char rings[FW][RING];
+  __shared__ f32x4_t red[2][FW][R][NP][64];  // (an item's sums, and the next one's)
   __shared__ FewTables tb;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int q4 = lane >> 4;
+  const bool streams = wave < FW;
+  const int me = blockIdx.x, all = gridDim.x;  // the block takes the items me, me + all, ...
   const int steps = ceil_div(a.d, F::KS);
-  const int s_lo = steps * wave / FW, n = steps * (wave + 1) / FW - s_lo;
+  const int s_lo = streams ? steps * wave / FW : 0, n = streams ? steps * (wave + 1) / FW - s_lo : 0;
 
   auto tables = [&]() {
-    if (wave == 0) build_local_map(a.resident, a.E, tb.lmap);
-    for (int i = threadIdx.x; i < 256; i += FT) tb.slot[i] = 0;
+    if (wave == 2 * FW - 1) build_local_map(a.resident, a.E, tb.lmap);
+    for (int i = threadIdx.x; i < 256; i += 2 * FT) tb.slot[i] = 0;
+    if (a.E <= 64) few_select_all<2 * FW, 4>(a, tb, blockIdx.x == 0);
+    else if (a.E <= 128) few_select_all<2 * FW, 8>(a, tb, blockIdx.x == 0);
+    else few_select_all<2 * FW, 16>(a, tb, blockIdx.x == 0);
     __syncthreads();
-    for (int t = wave * 4 + q4; t - q4 < a.T; t += FW * 4) {
-      if (a.E <= 64) few_select<4>(a, tb, t, blockIdx.x == 0);
-      else if (a.E <= 128) few_select<8>(a, tb, t, blockIdx.x == 0);
-      else few_select<16>(a, tb, t, blockIdx.x == 0);
-    }
-    __syncthreads();
+    few_localise(a, tb, blockIdx.x == 0);
     few_active<Q>(a, tb);
   };
 
-  // The block's items lo + i gridDim < hi, each (expert of the class, pass, hidden units).
+  // The block's items lo, lo + all .. below hi of a class: (expert, pass, hidden units).
+  int buf = 0;
   auto stream = [&](auto cl, bool shared, int first, int lo, int hi, auto&& between) {
     using C = decltype(cl);
     constexpr int N = C::N;
-    const int H = shared ? a.Hs : a.H, per = H / HB * C::PASS;
-    const unsigned line = MX ? (unsigned)a.d / 2 : (unsigned)a.d * sizeof(E), sline = mx_stride(a.d);
-    const char* W = static_cast<const char*>(shared ? a.sgu : a.wgu);
-    const uint8_t* S = shared ? a.sgu_s : a.wgu_s;
-    Stream<E, MX, RT, N, Piece<F::WROW>::PARTS, C::XP, GU_RING> st(rings[wave], a.d);
-    using ST = decltype(st);
-    st.weights(line, 16);
-    if constexpr (MX) {
-      const int tile = min(lane >> 4, RT - 1);  // (tiles g HG + hg)
-      st.soff = (unsigned)((tile / HG) * H + (tile % HG) * 16 + (lane & 15)) * sline;
-    }
-    const int items = hi > lo ? (hi - lo + (int)gridDim.x - 1) / (int)gridDim.x : 0, total = items * n;
-    // what item `it` is
+    const int H = shared ? a.Hs : a.H, n_h = H / 16, per = n_h * C::PASS;
+    // an item's expert, first hidden unit and columns
     auto expert = [&](int it) {
       return shared ? 0 : __builtin_amdgcn_readfirstlane((int)tb.expert[first + it / per]);
     };
     auto cols = [&](int it, int r) {
       const int my = lane >= a.T ? -1 : shared ? lane : route_to(a, tb, lane, r);
-      return Cols<N>(my, C::COMPACT, C::PASS == 1 ? 0 : it % per / (H / HB) * 16 * N);
+      return Cols<N>(my, C::COMPACT, C::PASS == 1 ? 0 : it % per / n_h * 16 * N);
     };
-    int issued = 0, l_it = lo, l_s = 0;
-    uint64_t w[RT], sc = 0;
-    const uint64_t x = uniform64(a.x);
-    auto issue = [&]() {
-      if (l_s == 0) {
-        const int r = expert(l_it), h0 = l_it % (H / HB) * HB;
-        const Cols<N> c = cols(l_it, r);
+    if (!streams) {
+      between();
+      for (int it = lo; it < hi; it += all) {
+        const int r = expert(it), h0 = it % n_h * 16;
+        const Cols<N> c = cols(it, r);
+        __syncthreads();  // the item's sums are there
 #pragma unroll
-        for (int i = 0; i < N; ++i) st.column(i, c.row[i] >= 0 ? c.t[i] : 0);
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
-          w[i] = uniform64(W + ((size_t)r * R * H + (size_t)(i / HG) * H + h0 + i % HG * 16) * line);
-        if constexpr (MX) sc = uniform64(S + ((size_t)r * R * H + h0) * sline);
-      }
-      st.issue(issued % ST::D, s_lo + l_s, w, sc, x);
-      ++issued;
-      if (++l_s == n) {
-        l_s = 0;
-        l_it += gridDim.x;
-      }
-    };
-    for (int i = 0; i < ST::D; ++i)
-      if (issued < total) issue();
-    between();
-    int done = 0;
-    for (int it = lo; it < hi; it += gridDim.x) {
-      f32x4_t acc[RT][N];
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int m = 0; m < N; ++m) acc[i][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      for (int s = 0; s < n; ++s) {
-        wait_vm_groups<ST::PER, ST::D - 1>(issued - done - 1);
-        typename ST::Frags f;
-        st.read(f, done % ST::D, s_lo + s);
-        WAIT_LGKMCNT(0);  // the operands are in registers: their place may be refilled
-        if (issued < total) issue();
-        ST::mma(f, acc);
-        ++done;
-      }
-      __syncthreads();  // the previous item's sums have been read
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int m = 0; m < N; ++m) red[wave][i][m][lane] = acc[i][m];
-      __syncthreads();
-      const int r = expert(it), h0 = it % (H / HB) * HB;
-      const Cols<N> c = cols(it, r);
-#pragma unroll
-      for (int m = 0; m < N; ++m)
-#pragma unroll
-        for (int g = 0; g < HG; ++g) {
-          // tile m of hidden group g by one wave: hidden units h0 + 16 g + 4 q4 ..
-          if (wave != (m * HG + g) % FW) continue;
+        for (int m = 0; m < N; ++m) {
+          if (wave - FW != m % FW) continue;
           f32x4_t v[R];
 #pragma unroll
           for (int i = 0; i < R; ++i) {
-            v[i] = red[0][i * HG + g][m][lane];
+            v[i] = red[buf][0][i][m][lane];
 #pragma unroll
-            for (int q = 1; q < FW; ++q) v[i] += red[q][i * HG + g][m][lane];
+            for (int q = 1; q < FW; ++q) v[i] += red[buf][q][i][m][lane];
           }
+          // hidden units h0 + 4 q4 .. of column l16's token
           if (c.row[m] >= 0) {
             const float gate = shared ? 1.0f : tb.gate[c.row[m]];
-            E* out = static_cast<E*>(shared ? a.hs : a.h) + (size_t)c.row[m] * H + h0 + 16 * g + 4 * q4;
+            E* out = static_cast<E*>(shared ? a.hs : a.h) + (size_t)c.row[m] * H + h0 + 4 * q4;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float s = gate * silu_f(v[0][i]);
@@ -600,21 +576,82 @@ __global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
             }
           }
         }
+        buf ^= 1;
+      }
+      return;
+    }
+    const unsigned line = MX ? (unsigned)a.d / 2 : (unsigned)a.d * sizeof(E), sline = mx_stride(a.d);
+    const char* W = static_cast<const char*>(shared ? a.sgu : a.wgu);
+    const uint8_t* S = shared ? a.sgu_s : a.wgu_s;
+    Stream<E, MX, R, N, Piece<F::WROW>::PARTS, C::XP, RING> st(rings[wave & (FW - 1)], a.d);
+    using ST = decltype(st);
+    st.weights(line, 16);
+    if constexpr (MX) st.soff = (unsigned)(min(lane >> 4, R - 1) * H + (lane & 15)) * sline;
+    int left = hi > lo ? (hi - lo + all - 1) / all * n : 0;
+    int flying = 0, l_slot = 0, l_it = lo, l_s = 0;
+    uint64_t w[R], sc = 0;
+    const uint64_t x = uniform64(a.x);
+    auto issue = [&]() {
+      if (left == 0) return;
+      if (l_s == 0) {
+        const int r = expert(l_it), h0 = l_it % n_h * 16;
+        const Cols<N> c = cols(l_it, r);
+#pragma unroll
+        for (int i = 0; i < N; ++i) st.column(i, c.row[i] >= 0 ? c.t[i] : 0);
+#pragma unroll
+        for (int i = 0; i < R; ++i) w[i] = uniform64(W + ((size_t)r * R * H + (size_t)i * H + h0) * line);
+        if constexpr (MX) sc = uniform64(S + ((size_t)r * R * H + h0) * sline);
+      }
+      st.issue(l_slot, s_lo + l_s, w, sc, x);
+      l_slot = l_slot + 1 == ST::D ? 0 : l_slot + 1;
+      if (++l_s == n) {
+        l_s = 0;
+        l_it += all;
+      }
+      --left;
+      ++flying;
+    };
+    for (int i = 0; i < ST::D; ++i) issue();
+    between();
+    int slot = 0;
+    for (int it = lo; it < hi; it += all) {
+      f32x4_t acc[R][N];
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int m = 0; m < N; ++m) acc[i][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int s = 0; s < n; ++s) {
+        wait_vm_groups<ST::PER, ST::D - 1>(flying - 1);
+        typename ST::Frags f;
+        st.read(f, slot, s_lo + s);
+        slot = slot + 1 == ST::D ? 0 : slot + 1;
+        WAIT_LGKMCNT(0);  // the operands are in registers: their place may be refilled
+        --flying;
+        issue();
+        ST::mma(f, acc);
+      }
+      // (this buffer's sums of two items ago were read before the last barrier)
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int m = 0; m < N; ++m) red[buf][wave][i][m][lane] = acc[i][m];
+      __syncthreads();
+      buf ^= 1;
     }
   };
 
   typedef Class<1, 1, 1, true> Few;
   typedef Class<1, PARTS, 1, true> One;
-  typedef Class<NP, PARTS, passes(MX, NT), false> All;
-  const int n_s = a.Hs / HB * All::PASS, n_r = a.H / HB;
+  typedef Class<NP, PARTS, (NT + NP - 1) / NP, false> All;
+  const int n_s = a.Hs / 16 * All::PASS, n_r = a.H / 16;
   // the first of this block's numbers from `from` on
   auto next = [&](int from) {
-    const int m = (from - (int)blockIdx.x) % (int)gridDim.x;
-    return from + (m > 0 ? (int)gridDim.x - m : -m);
+    const int m = (from - me) % all;
+    return from + (m > 0 ? all - m : -m);
   };
   auto nothing = [] {};
-  if (NT == 1 && a.T <= Q) stream(Few{}, true, 0, blockIdx.x, n_s, tables);
-  else stream(All{}, true, 0, blockIdx.x, n_s, tables);
+  if (NT == 1 && a.T <= Q) stream(Few{}, true, 0, me, n_s, tables);
+  else stream(All{}, true, 0, me, n_s, tables);
   int from = n_s, first = 0;
   auto routed = [&](auto cl, int experts) {
     const int n_i = experts * n_r * decltype(cl)::PASS;
@@ -640,21 +677,21 @@ __global__ __launch_bounds__(FT) void few_gu_kernel(FewArgs a) {
 // the reduction into parts instead, added by the last block to finish, took three times as
 // long (the fences write back each XCD's whole L2).
 template <class E, bool MX, int NT, int RB>
-__global__ __launch_bounds__(FT) void few_down_kernel(FewArgs a) {
+__global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
   using F = Fmt<E, MX>;
-  constexpr int NP = pass_tiles(MX, NT);
+  constexpr int NP = down_tiles(MX, NT);
   constexpr int PARTS = Piece<F::XROW>::PARTS, Q = Piece<F::XROW>::RPI;
   constexpr int WP = RB < 16 && Piece<F::WROW>::PARTS == 2 ? 1 : Piece<F::WROW>::PARTS;
-  __shared__ __attribute__((aligned(1024))) char rings[FW][down_ring(NT)];
-  __shared__ f32x4_t red[FW][16 * NT][RB / 4];
+  __shared__ __attribute__((aligned(1024))) char rings[DW][down_ring(NT)];
+  __shared__ f32x4_t red[DW][16 * NT][RB / 4];
   __shared__ FewTables tb;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, q4 = lane >> 4;
   for (int i = lane; i < 16 * NT * (RB / 4); i += 64) (&red[wave][0][0])[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   auto tables = [&]() {
-    for (int i = threadIdx.x; i < a.T * a.k; i += FT) tb.local[i] = (int16_t)a.w_local[i];
-    for (int i = threadIdx.x; i < 256; i += FT) tb.slot[i] = 0;
+    for (int i = threadIdx.x; i < a.T * a.k; i += DT) tb.local[i] = (int16_t)a.w_local[i];
+    for (int i = threadIdx.x; i < 256; i += DT) tb.slot[i] = 0;
     __syncthreads();
     few_active<Q>(a, tb);
   };
@@ -665,7 +702,7 @@ __global__ __launch_bounds__(FT) void few_down_kernel(FewArgs a) {
     constexpr int N = C::N;
     const int H = shared ? a.Hs : a.H, n_h = ceil_div(H, F::KS);
     const int64_t all = (int64_t)experts * C::PASS * n_h;
-    const int s_lo = (int)(all * wave / FW), s_hi = (int)(all * (wave + 1) / FW);
+    const int s_lo = (int)(all * wave / DW), s_hi = (int)(all * (wave + 1) / DW);
     const unsigned line = MX ? (unsigned)H / 2 : (unsigned)H * sizeof(E), sline = mx_stride(H);
     const char* W = static_cast<const char*>(shared ? a.sd : a.wd) + (size_t)blockIdx.x * RB * line;
     const uint8_t* S = (shared ? a.sd_s : a.wd_s) + (size_t)blockIdx.x * RB * sline;
@@ -751,7 +788,7 @@ __global__ __launch_bounds__(FT) void few_down_kernel(FewArgs a) {
   };
   typedef Class<1, 1, 1, true> Few;
   typedef Class<1, PARTS, 1, true> One;
-  typedef Class<NP, PARTS, passes(MX, NT), false> All;
+  typedef Class<NP, PARTS, (NT + NP - 1) / NP, false> All;
   if (NT == 1 && a.T <= Q) stream(Few{}, true, 0, a.Hs ? 1 : 0, tables);
   else stream(All{}, true, 0, a.Hs ? 1 : 0, tables);
   auto nothing = [] {};
@@ -763,11 +800,11 @@ __global__ __launch_bounds__(FT) void few_down_kernel(FewArgs a) {
     stream(All{}, false, tb.n_class[0] + tb.n_class[1], tb.n_class[2], nothing);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < a.T * (RB / 4); i += FT) {
+  for (int i = threadIdx.x; i < a.T * (RB / 4); i += DT) {
     const int t = i / (RB / 4), c = i % (RB / 4);
     f32x4_t v = red[0][t][c];
 #pragma unroll
-    for (int q = 1; q < FW; ++q) v += red[q][t][c];
+    for (int q = 1; q < DW; ++q) v += red[q][t][c];
     E* y = static_cast<E*>(a.y) + (size_t)t * a.d + blockIdx.x * RB + 4 * c;
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] = from_f32<E>(v[j]);
@@ -794,14 +831,13 @@ FewLayout few_layout(const moe_few* f) {
 
 template <class E, bool MX, int ACT, int NT>
 void few_launch(const FewArgs& a, hipStream_t s) {
-  const int64_t items =
-      (std::min<int64_t>(a.E_r, (int64_t)a.T * a.k) * (a.H / 16) + a.Hs / 16) / gu_groups(MX) * passes(MX, NT);
-  const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(items, num_cus()));
-  MOE_TIMED("few_gu", s, few_gu_kernel<E, MX, ACT, NT><<<blocks, FT, 0, s>>>(a));
+  const int64_t items = std::min<int64_t>(a.E_r, (int64_t)a.T * a.k) * (a.H / 16) + a.Hs / 16;
+  const int cus = num_cus(), blocks = (int)std::max<int64_t>(1, std::min<int64_t>(items, cus));
+  MOE_TIMED("few_gu", s, few_gu_kernel<E, MX, ACT, NT><<<blocks, 2 * FT, 0, s>>>(a));
 #define FEW_DOWN(RB) \
-  MOE_TIMED("few_down", s, few_down_kernel<E, MX, NT, RB><<<a.d / RB, FT, 0, s>>>(a))
-  if (a.d / 16 >= num_cus()) FEW_DOWN(16);
-  else if (a.d / 8 >= num_cus()) FEW_DOWN(8);
+  MOE_TIMED("few_down", s, few_down_kernel<E, MX, NT, RB><<<a.d / RB, DT, 0, s>>>(a))
+  if (a.d / 16 >= cus) FEW_DOWN(16);
+  else if (a.d / 8 >= cus) FEW_DOWN(8);
   else FEW_DOWN(4);
 #undef FEW_DOWN
 }
@@ -834,7 +870,7 @@ hipError_t launch_few(const moe_few* f, hipStream_t s) {
   a.T = f->T; a.d = f->d; a.E = f->E; a.k = f->k; a.E_r = f->E_r; a.H = f->H; a.Hs = f->Hs;
   a.gate = f->gate; a.inv_tau = f->inv_tau;
   if (f->dtype == MOE_BF16)
-    MOE_TIMED("few_logits", s, few_logits_bf16_kernel<<<dim3(ceil_div(f->E, LE), ceil_div(f->T, 32)),
+    MOE_TIMED("few_logits", s, few_logits_bf16_kernel<<<dim3(ceil_div(f->E, LE), ceil_div(f->T, LT)),
                                                         64 * LW, 0, s>>>(a));
   else
     MOE_TIMED("few_logits", s, few_logits_f32_kernel<<<dim3(ceil_div(f->E, 16), ceil_div(f->T, 16)),
