@@ -148,7 +148,7 @@ struct FewTables {
   int16_t expert[256];        // active expert -> local id
   int slot[256];              // tokens of a local expert
   int lmap[256];
-  int n_class[3];             // experts with up to Q tokens, up to 16, more
+  int n_class[3];             // experts with few tokens, more, many (few_active)
 };
 
 // Top-k and gates of token t, by 16 lanes (the router's selection on logits in
@@ -242,10 +242,10 @@ DEVI void few_localise(const FewArgs& a, FewTables& tb, bool publish) {
   }
 }
 
-// The active experts by their number of tokens (up to Q, up to 16, more), each class in
+// The active experts by their number of tokens (up to Q, up to M, more), each class in
 // ascending order.  All threads call it, with slot[] zero and the routes in local[]; it
 // ends with a barrier.
-template <int Q>
+template <int Q, int M>
 DEVI void few_active(const FewArgs& a, FewTables& tb) {
   for (int i = threadIdx.x; i < a.T * a.k; i += blockDim.x)
     if (tb.local[i] >= 0) atomicAdd(&tb.slot[tb.local[i]], 1);
@@ -258,7 +258,7 @@ DEVI void few_active(const FewArgs& a, FewTables& tb) {
       for (int r0 = 0; r0 < a.E_r; r0 += 64) {
         const int r = r0 + lane;
         const int c = r < a.E_r ? tb.slot[r] : 0;
-        const bool on = c > 0 && (c <= Q ? 0 : c <= 16 ? 1 : 2) == cl;
+        const bool on = c > 0 && (c <= Q ? 0 : c <= M ? 1 : 2) == cl;
         const uint64_t m = __ballot(on);
         if (on) tb.expert[n + __popcll(m & ((1ull << lane) - 1ull))] = (int16_t)r;
         n += __popcll(m);
@@ -280,18 +280,21 @@ DEVI int route_to(const FewArgs& a, const FewTables& tb, int t, int r) {
 
 // ------------------------------------------------------------------ operands
 // One step of a wave: tiles of 16 weight rows and of 16 tokens by KS of k, brought to the
-// wave's own ring in LDS by DMA, whole row pieces of WROW (weights) and XROW (activations)
+// wave's own ring in LDS by DMA, whole row pieces of 128 (weights) and XROW (activations)
 // bytes, and read from there as operands: lane (r, q) = (lane % 16, lane / 16) holds row r.
 //   bf16   KS 64, two v_mfma_f32_16x16x32_bf16 per pair of tiles
 //   fp32   KS 32, eight v_mfma_f32_16x16x4_f32
-//   MXFP4  KS 128 (and a word of four scales per row), widened to bf16 (exactly, a value
-//          has two significant bits): four v_mfma_f32_16x16x32_bf16 on bf16 activations
+//   MXFP4  KS 256 (and eight scales per row), widened to bf16 (exactly, a value has two
+//          significant bits): eight v_mfma_f32_16x16x32_bf16 on bf16 activations
 // (Loaded in operand order instead, straight to registers, a load instruction touches 16
-// rows and a CU's address unit was the bound: 2.3 to 3.1 TB/s over the GPU.)
+// rows and a CU's address unit was the bound: 2.3 to 3.1 TB/s over the GPU.  MXFP4 steps of
+// 128 fetched each 128-byte line for its halves twice.)
+// XF, XM: DMA parts of a tile of activations for experts with few tokens and with more: 8 and
+// 16 tokens, MXFP4 4 and 8 (a whole tile would take half of a ring).
 template <class E, bool MX> struct Fmt;
-template <> struct Fmt<bf16_t, false> { static constexpr int KS = 64, WROW = 128, XROW = 128; };
-template <> struct Fmt<float, false> { static constexpr int KS = 32, WROW = 128, XROW = 128; };
-template <> struct Fmt<bf16_t, true> { static constexpr int KS = 128, WROW = 64, XROW = 256; };
+template <> struct Fmt<bf16_t, false> { static constexpr int KS = 64, XROW = 128, XF = 1, XM = 2; };
+template <> struct Fmt<float, false> { static constexpr int KS = 32, XROW = 128, XF = 1, XM = 2; };
+template <> struct Fmt<bf16_t, true> { static constexpr int KS = 256, XROW = 512, XF = 2, XM = 4; };
 
 // 16 bytes per lane from base + off (base uniform) to LDS at lds + 16 lane.  The asm sets m0
 // and leaves the one wait state an LDS DMA needs after it.
@@ -317,7 +320,7 @@ DEVI uint64_t uniform64(const void* p) {
 template <int B>
 struct Piece {
   static constexpr int LPR = B / 16, RPI = 64 / LPR, PARTS = 16 / RPI;
-  DEVI static int swz(int r) { return LPR == 4 ? (r >> 2) & 3 : LPR == 8 ? (r >> 1) & 7 : r & 15; }
+  DEVI static int swz(int r) { return LPR == 8 ? (r >> 1) & 7 : r & 15; }
   DEVI static int row(int part) { return part * RPI + (int)(threadIdx.x & 63) / LPR; }
   DEVI static int chunk(int part) { return ((int)(threadIdx.x & 63) % LPR) ^ swz(row(part)); }
   DEVI static const char* at(const char* tile, int r, int c) { return tile + r * B + ((c ^ swz(r)) << 4); }
@@ -346,32 +349,28 @@ constexpr int down_ring(int NT) { return (NT == 1 ? 18 : NT == 2 ? 17 : NT == 3 
 template <class E, bool MX, int RT, int N, int WP, int XP, int RING>
 struct Stream {
   using F = Fmt<E, MX>;
-  using PW = Piece<F::WROW>;
+  using PW = Piece<128>;
   using PX = Piece<F::XROW>;
-  static constexpr int W_TILE = WP * 1024, X_TILE = XP * 1024;
-  static constexpr int STAGE = RT * W_TILE + N * X_TILE + (MX ? 256 : 0);
-  static constexpr int PER = RT * WP + N * XP + (MX ? 1 : 0);  // DMA instructions of a step
-  static constexpr int D0 = RING / STAGE, D = D0 > 12 ? 12 : D0;        // steps in flight
+  static constexpr int W_TILE = WP * 1024, X_TILE = XP * 1024, X_AT = RT * W_TILE, S_AT = X_AT + N * X_TILE;
+  static constexpr int STAGE = S_AT + (MX ? 512 : 0);
+  static constexpr int PER = RT * WP + N * XP + (MX ? 2 : 0);   // DMA instructions of a step
+  static constexpr int D0 = RING / STAGE, D = D0 > 12 ? 12 : D0;  // steps in flight
+  static constexpr int XN = F::XROW / 64;                        // a lane's 16-byte chunks of a tile of x
   static_assert(D >= 2 && D * PER <= 63, "a ring of two steps, counted by vmcnt");
+  static_assert(!MX || RT <= 4, "a DMA instruction brings a word of scales for 64 rows");
 
-  // lane offsets, and what a lane past the end of a cut MXFP4 step (K % 128 == 64, its last
-  // two of four chunks) goes back to stay in the row
-  unsigned woff[WP], xoff[N][XP], soff;
-  unsigned wback;
+  unsigned woff[WP], xoff[N][XP], soff;  // lane offsets
   char* ring;
   unsigned ring_lds;
   int K;
 
-  DEVI Stream(char* wave_ring, int k) : ring(wave_ring), K(k) {
+  DEVI Stream(char* wave_ring, int k) : soff(0), ring(wave_ring), K(k) {
     ring_lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void_t*)wave_ring);
-    wback = soff = 0;
   }
-  // line: bytes of a weight row; rows: those of the matrix tile that exist (16, or fewer)
+  // line: bytes of a weight row; rows: those of a tile that exist (16, or fewer)
   DEVI void weights(unsigned line, int rows) {
 #pragma unroll
     for (int p = 0; p < WP; ++p) woff[p] = min(PW::row(p), rows - 1) * line + PW::chunk(p) * 16;
-    // (one part: the lane's chunk is the same in every tile)
-    wback = MX && PW::chunk(0) >= 2 ? 32 : 0;
   }
   // the row of activations of each column of tile n, by column
   DEVI void column(int n, int row_of_lane16) {
@@ -381,33 +380,43 @@ struct Stream {
       xoff[n][p] = (unsigned)row * (unsigned)(K * sizeof(E)) + PX::chunk(p) * 16;
     }
   }
-  DEVI bool cut(int st) const { return MX && (st + 1) * F::KS > K; }
 
-  // w[i], scales: uniform addresses of the tiles' first row and of the scales at step 0
+  // w[i], scales, x: uniform addresses of the tiles' first row at step 0.  K is a multiple of
+  // 64, so only an MXFP4 step can be cut: its lanes past the row's end read the row's piece
+  // from its start, and read() makes their weights zeros.
   DEVI void issue(int slot, int st, const uint64_t* w, uint64_t scales, uint64_t x) const {
     const unsigned at = ring_lds + slot * STAGE;
-    const bool c = cut(st);
+    const int rest = K - st * F::KS;
+    const bool cut = MX && rest < F::KS;
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int p = 0; p < WP; ++p)
-        few_dma16(w[i] + (uint64_t)st * F::WROW, MX && c ? woff[p] - wback : woff[p], at + i * W_TILE + p * 1024);
+      for (int p = 0; p < WP; ++p) {
+        unsigned o = woff[p];
+        if (cut && PW::chunk(p) * 32 >= rest) o -= PW::chunk(p) * 16;
+        few_dma16(w[i] + (uint64_t)st * 128, o, at + i * W_TILE + p * 1024);
+      }
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int p = 0; p < XP; ++p) {
         unsigned o = xoff[n][p];
-        if (MX && c && PX::chunk(p) >= 8) o -= 128;
-        few_dma16(x + (uint64_t)st * F::XROW, o, at + RT * W_TILE + n * X_TILE + p * 1024);
+        if (cut && PX::chunk(p) * 8 >= rest) o -= PX::chunk(p) * 16;
+        few_dma16(x + (uint64_t)st * F::XROW, o, at + X_AT + n * X_TILE + p * 1024);
       }
-    if constexpr (MX) few_dma4(scales + (uint64_t)st * 4, soff, at + RT * W_TILE + N * X_TILE);
+    if constexpr (MX) {
+      // (a row of scales is whole words: the second one may not be there)
+      few_dma4(scales + (uint64_t)st * 8, soff, at + S_AT);
+      few_dma4(scales + (uint64_t)st * 8 + (rest > 128 ? 4 : 0), soff, at + S_AT + 256);
+    }
   }
 
-  // Operands of one step, in registers.
+  // Operands of one step, in registers (of tiles that are brought in part, the rows that are
+  // there again).
   struct Frags {
-    u32x4_t w[RT][MX ? 1 : 2];
-    u32x4_t x[N][MX ? 4 : 2];
-    unsigned s[RT];
+    u32x4_t w[RT][2];
+    u32x4_t x[N][XN];
+    unsigned s[RT][2];
   };
   DEVI void read(Frags& f, int slot, int st) const {
     const char* at = ring + slot * STAGE;
@@ -415,37 +424,45 @@ struct Stream {
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int p = 0; p < (MX ? 1 : 2); ++p)
-        f.w[i][p] = *reinterpret_cast<const u32x4_t*>(PW::at(at + i * W_TILE, r, 4 * p + q));
+      for (int p = 0; p < 2; ++p)
+        f.w[i][p] = *reinterpret_cast<const u32x4_t*>(PW::at(at + i * W_TILE, r & (WP * PW::RPI - 1), 4 * p + q));
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int p = 0; p < (MX ? 4 : 2); ++p)
-        f.x[n][p] = *reinterpret_cast<const u32x4_t*>(PX::at(at + RT * W_TILE + n * X_TILE, r, MX ? 4 * q + p : 4 * p + q));
+      for (int p = 0; p < XN; ++p)
+        f.x[n][p] = *reinterpret_cast<const u32x4_t*>(
+            PX::at(at + X_AT + n * X_TILE, r & (XP * PX::RPI - 1), MX ? 16 * (p >> 2) + 4 * q + (p & 3) : 4 * p + q));
     if constexpr (MX) {
 #pragma unroll
       for (int i = 0; i < RT; ++i)
-        f.s[i] = *reinterpret_cast<const unsigned*>(at + RT * W_TILE + N * X_TILE + (16 * i + r) * 4) >> (8 * q) & 255u;
-      if (cut(st) && q >= 2)
 #pragma unroll
-        for (int i = 0; i < RT; ++i) f.w[i][0] = u32x4_t{0u, 0u, 0u, 0u};
+        for (int p = 0; p < 2; ++p)
+          f.s[i][p] = *reinterpret_cast<const unsigned*>(at + S_AT + p * 256 + (16 * i + r) * 4) >> (8 * q) & 255u;
+      const int rest = K - st * F::KS;
+      if (rest < F::KS)
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+            if (128 * p + 32 * q >= rest) f.w[i][p] = u32x4_t{0u, 0u, 0u, 0u};
     }
   }
   DEVI static void mma(const Frags& f, f32x4_t (&acc)[RT][N]) {
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      if constexpr (MX) {
-        const float s = mx_scale_f32(f.s[i]);
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          const bf16x8_t w = mx_widen8(f.w[i][0][p], s);
+      for (int p = 0; p < 2; ++p) {
+        if constexpr (MX) {
+          const float s = mx_scale_f32(f.s[i][p]);
 #pragma unroll
-          for (int n = 0; n < N; ++n)
-            acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8_t, f.x[n][p]), acc[i][n], 0, 0, 0);
-        }
-      } else {
+          for (int e = 0; e < 4; ++e) {
+            const bf16x8_t w = mx_widen8(f.w[i][p][e], s);
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+            for (int n = 0; n < N; ++n)
+              acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  w, __builtin_bit_cast(bf16x8_t, f.x[n][4 * p + e]), acc[i][n], 0, 0, 0);
+          }
+        } else {
 #pragma unroll
           for (int n = 0; n < N; ++n) {
             if constexpr (sizeof(E) == 2) {
@@ -458,45 +475,54 @@ struct Stream {
                 acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], acc[i][n], 0, 0, 0);
             }
           }
+        }
       }
-    }
   }
 };
 
-// Row of activations of each column of a wave's N tiles, from my_row (lane l: token l's, or
-// -1): the column's token t and its row.  compact: the tokens that have a row are moved to
-// the front (at most 16 of them); otherwise token first + 16 n + column.
-template <int N>
+// How a class of experts is taken: N tiles of XP DMA parts at a time, PASS times; COMPACT: the
+// expert's tokens moved to the front of one tile.  CT: columns of a tile that are used.
+template <class E, bool MX, int N_, int XP_, int PASS_, bool COMPACT_>
+struct Class {
+  static constexpr int N = N_, XP = XP_, PASS = PASS_, CT = XP_ * Piece<Fmt<E, MX>::XROW>::RPI;
+  static constexpr bool COMPACT = COMPACT_;
+};
+// Few tokens, more in one compact tile, any number (in passes over the weights).
+template <class E, bool MX, int NT, int NP>
+struct Classes {
+  using F = Fmt<E, MX>;
+  typedef Class<E, MX, 1, F::XF, 1, true> Few;
+  typedef Class<E, MX, 1, F::XM, 1, true> More;
+  typedef Class<E, MX, NP, F::XM, (16 * NT + NP * More::CT - 1) / (NP * More::CT), false> All;
+};
+
+// Row of activations of each column of a wave's tiles of class C, from my_row (lane l: token
+// l's, or -1): the column's token t and its row, -1 for none.  Compact: the tokens that have
+// a row are moved to the front; otherwise pass p takes the tokens from p N CT on.
+template <class C>
 struct Cols {
-  int t[N], row[N];
-  DEVI Cols(int my_row, bool compact, int first) {
+  int t[C::N], row[C::N];
+  DEVI Cols(int my_row, int pass) {
     const int lane = threadIdx.x & 63, l16 = lane & 15;
     int who = lane;
-    if (compact) {
+    if constexpr (C::COMPACT) {
       const uint64_t on = __ballot(my_row >= 0), below = (1ull << lane) - 1ull;
       const int to = my_row >= 0 ? __popcll(on & below) : __popcll(on) + __popcll(~on & below);
       who = __builtin_amdgcn_ds_permute(to * 4, lane);
     }
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      t[n] = __shfl(who, (first + 16 * n + l16) & 63, 64);
-      row[n] = __shfl(my_row, t[n], 64);
+    for (int n = 0; n < C::N; ++n) {
+      const int at = (pass * C::N + n) * C::CT + l16;
+      t[n] = __shfl(who, at & 63, 64);
+      const int r = __shfl(my_row, t[n], 64);
+      row[n] = l16 < C::CT && at < 64 ? r : -1;
     }
   }
 };
 
-// Tiles that a pass over an expert's weights takes of a batch's NT.  (A tile of MXFP4
-// activations takes 4 KB of a stage, others 2: more would leave no ring.)
-constexpr int gu_tiles(bool MX, int NT) { return NT == 4 || (MX && NT > 2) ? 2 : NT; }
+// Tiles that a pass over an expert's weights takes of a batch's NT, where tokens are many.
+constexpr int gu_tiles(bool MX, int NT) { return MX ? 1 : NT == 4 ? 2 : NT; }
 constexpr int down_tiles(bool MX, int NT) { return MX ? 1 : NT > 3 ? 2 : NT; }
-
-// How a class of experts is taken: N tiles of XP DMA parts at a time, PASS times; COMPACT: the
-// expert's tokens moved to the front of one tile.
-template <int N_, int XP_, int PASS_, bool COMPACT_>
-struct Class {
-  static constexpr int N = N_, XP = XP_, PASS = PASS_;
-  static constexpr bool COMPACT = COMPACT_;
-};
 
 // ------------------------------------------------------------------ first projections
 // An item is 16 hidden units of one expert (for SwiGLU as many rows of W_g and of W_u).  Four
@@ -512,7 +538,7 @@ template <class E, bool MX, int ACT, int NT>
 __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
   using F = Fmt<E, MX>;
   constexpr int R = ACT == MOE_ACT_SWIGLU ? 2 : 1, NP = gu_tiles(MX, NT);
-  constexpr int PARTS = Piece<F::XROW>::PARTS, Q = Piece<F::XROW>::RPI;
+  using CS = Classes<E, MX, NT, NP>;
   constexpr int RING = gu_ring(NP);
   __shared__ __attribute__((aligned(1024))) char rings[FW][RING];
   __shared__ f32x4_t red[2][FW][R][NP][64];  // (an item's sums, and the next one's)
@@ -532,7 +558,7 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
     else few_select_all<2 * FW, 16>(a, tb, blockIdx.x == 0);
     __syncthreads();
     few_localise(a, tb, blockIdx.x == 0);
-    few_active<Q>(a, tb);
+    few_active<CS::Few::CT, CS::More::CT>(a, tb);
   };
 
   // The block's items lo, lo + all .. below hi of a class: (expert, pass, hidden units).
@@ -547,13 +573,13 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
     };
     auto cols = [&](int it, int r) {
       const int my = lane >= a.T ? -1 : shared ? lane : route_to(a, tb, lane, r);
-      return Cols<N>(my, C::COMPACT, C::PASS == 1 ? 0 : it % per / n_h * 16 * N);
+      return Cols<C>(my, C::PASS == 1 ? 0 : it % per / n_h);
     };
     if (!streams) {
       between();
       for (int it = lo; it < hi; it += all) {
         const int r = expert(it), h0 = it % n_h * 16;
-        const Cols<N> c = cols(it, r);
+        const Cols<C> c = cols(it, r);
         __syncthreads();  // the item's sums are there
 #pragma unroll
         for (int m = 0; m < N; ++m) {
@@ -583,7 +609,7 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
     const unsigned line = MX ? (unsigned)a.d / 2 : (unsigned)a.d * sizeof(E), sline = mx_stride(a.d);
     const char* W = static_cast<const char*>(shared ? a.sgu : a.wgu);
     const uint8_t* S = shared ? a.sgu_s : a.wgu_s;
-    Stream<E, MX, R, N, Piece<F::WROW>::PARTS, C::XP, RING> st(rings[wave & (FW - 1)], a.d);
+    Stream<E, MX, R, N, 2, C::XP, RING> st(rings[wave & (FW - 1)], a.d);
     using ST = decltype(st);
     st.weights(line, 16);
     if constexpr (MX) st.soff = (unsigned)(min(lane >> 4, R - 1) * H + (lane & 15)) * sline;
@@ -595,7 +621,7 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
       if (left == 0) return;
       if (l_s == 0) {
         const int r = expert(l_it), h0 = l_it % n_h * 16;
-        const Cols<N> c = cols(l_it, r);
+        const Cols<C> c = cols(l_it, r);
 #pragma unroll
         for (int i = 0; i < N; ++i) st.column(i, c.row[i] >= 0 ? c.t[i] : 0);
 #pragma unroll
@@ -640,9 +666,9 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
     }
   };
 
-  typedef Class<1, 1, 1, true> Few;
-  typedef Class<1, PARTS, 1, true> One;
-  typedef Class<NP, PARTS, (NT + NP - 1) / NP, false> All;
+  typedef typename CS::Few Few;
+  typedef typename CS::More More;
+  typedef typename CS::All All;
   const int n_s = a.Hs / 16 * All::PASS, n_r = a.H / 16;
   // the first of this block's numbers from `from` on
   auto next = [&](int from) {
@@ -650,7 +676,7 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
     return from + (m > 0 ? all - m : -m);
   };
   auto nothing = [] {};
-  if (NT == 1 && a.T <= Q) stream(Few{}, true, 0, me, n_s, tables);
+  if (a.T <= Few::CT) stream(Few{}, true, 0, me, n_s, tables);
   else stream(All{}, true, 0, me, n_s, tables);
   int from = n_s, first = 0;
   auto routed = [&](auto cl, int experts) {
@@ -660,12 +686,8 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
     first += experts;
   };
   routed(Few{}, tb.n_class[0]);
-  if constexpr (NT == 1) {
-    routed(All{}, tb.n_class[1]);
-  } else {
-    routed(One{}, tb.n_class[1]);
-    routed(All{}, tb.n_class[2]);
-  }
+  routed(More{}, tb.n_class[1]);
+  if constexpr (16 * NT > More::CT) routed(All{}, tb.n_class[2]);
 }
 
 // ------------------------------------------------------------------ second projections
@@ -680,8 +702,8 @@ template <class E, bool MX, int NT, int RB>
 __global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
   using F = Fmt<E, MX>;
   constexpr int NP = down_tiles(MX, NT);
-  constexpr int PARTS = Piece<F::XROW>::PARTS, Q = Piece<F::XROW>::RPI;
-  constexpr int WP = RB < 16 && Piece<F::WROW>::PARTS == 2 ? 1 : Piece<F::WROW>::PARTS;
+  using CS = Classes<E, MX, NT, NP>;
+  constexpr int WP = RB < 16 ? 1 : 2;
   __shared__ __attribute__((aligned(1024))) char rings[DW][down_ring(NT)];
   __shared__ f32x4_t red[DW][16 * NT][RB / 4];
   __shared__ FewTables tb;
@@ -693,7 +715,7 @@ __global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
     for (int i = threadIdx.x; i < a.T * a.k; i += DT) tb.local[i] = (int16_t)a.w_local[i];
     for (int i = threadIdx.x; i < 256; i += DT) tb.slot[i] = 0;
     __syncthreads();
-    few_active<Q>(a, tb);
+    few_active<CS::Few::CT, CS::More::CT>(a, tb);
   };
 
   // The wave's share of the steps of `experts` experts (C::PASS passes over each).
@@ -709,14 +731,14 @@ __global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
     Stream<E, MX, 1, N, WP, C::XP, down_ring(NT)> st(rings[wave], H);
     using ST = decltype(st);
     st.weights(line, RB);
-    st.soff = (unsigned)min(l16, RB - 1) * sline;
+    if constexpr (MX) st.soff = (unsigned)min(l16, RB - 1) * sline;
     // pass v = expert * PASS + pass: its columns
     auto expert = [&](int v) {
       return shared ? 0 : __builtin_amdgcn_readfirstlane((int)tb.expert[first + v / C::PASS]);
     };
     auto cols = [&](int v, int r) {
       const int my = lane >= a.T ? -1 : shared ? lane : route_to(a, tb, lane, r);
-      return Cols<N>(my, C::COMPACT, v % C::PASS * 16 * N);
+      return Cols<C>(my, v % C::PASS);
     };
     // the step to load next: slot of the ring, pass, step in it
     int left = s_hi - s_lo, flying = 0, l_slot = 0, l_v = n_h ? s_lo / n_h : 0, l_s = s_lo - l_v * n_h;
@@ -728,7 +750,7 @@ __global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
       if (fresh) {
         fresh = false;
         const int r = expert(l_v);
-        const Cols<N> c = cols(l_v, r);
+        const Cols<C> c = cols(l_v, r);
 #pragma unroll
         for (int i = 0; i < N; ++i) st.column(i, max(c.row[i], 0));
         w = uniform64(W + (size_t)r * a.d * line);
@@ -779,26 +801,23 @@ __global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
         ST::mma(f, acc);
       }
       s = 0;
-      const Cols<N> c = cols(v, expert(v));
+      const Cols<C> c = cols(v, expert(v));
       ++v;
 #pragma unroll
       for (int i = 0; i < N; ++i)
         if (c.row[i] >= 0 && 4 * q4 < RB) red[wave][c.t[i]][q4] += acc[0][i];
     }
   };
-  typedef Class<1, 1, 1, true> Few;
-  typedef Class<1, PARTS, 1, true> One;
-  typedef Class<NP, PARTS, (NT + NP - 1) / NP, false> All;
-  if (NT == 1 && a.T <= Q) stream(Few{}, true, 0, a.Hs ? 1 : 0, tables);
+  typedef typename CS::Few Few;
+  typedef typename CS::More More;
+  typedef typename CS::All All;
+  if (a.T <= Few::CT) stream(Few{}, true, 0, a.Hs ? 1 : 0, tables);
   else stream(All{}, true, 0, a.Hs ? 1 : 0, tables);
   auto nothing = [] {};
   stream(Few{}, false, 0, tb.n_class[0], nothing);
-  if constexpr (NT == 1) {
-    stream(All{}, false, tb.n_class[0], tb.n_class[1], nothing);
-  } else {
-    stream(One{}, false, tb.n_class[0], tb.n_class[1], nothing);
+  stream(More{}, false, tb.n_class[0], tb.n_class[1], nothing);
+  if constexpr (16 * NT > More::CT)
     stream(All{}, false, tb.n_class[0] + tb.n_class[1], tb.n_class[2], nothing);
-  }
   __syncthreads();
   for (int i = threadIdx.x; i < a.T * (RB / 4); i += DT) {
     const int t = i / (RB / 4), c = i % (RB / 4);
