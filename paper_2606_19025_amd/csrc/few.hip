@@ -637,7 +637,8 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
       --left;
       ++flying;
     };
-    for (int i = 0; i < ST::D; ++i) issue();
+#pragma unroll 1
+    for (int i = 0; i < ST::D; ++i) issue();  // (unrolled, its code took longer to fetch than to run)
     between();
     int slot = 0;
     for (int it = lo; it < hi; it += all) {
@@ -767,7 +768,8 @@ __global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
       ++flying;
     };
     int v = l_v, s = l_s, slot = 0, todo = left;
-    for (int i = 0; i < ST::D; ++i) issue();
+#pragma unroll 1
+    for (int i = 0; i < ST::D; ++i) issue();  // (unrolled, its code took longer to fetch than to run)
     between();
     while (todo > 0) {
       f32x4_t acc[1][N];
