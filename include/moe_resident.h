@@ -410,6 +410,39 @@ int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype,
                          int cols, const int32_t* n_rows, void* x, hipStream_t stream);
 
 /*
+ * Grouped expert FFN, forward, in MXFP4 (evaluation from experts held in 4 bits):
+ * moe_grouped_ffn_fwd with rows and weights as codes and scales of moe_mxfp4_quantize,
+ * multiplied as such with fp32 accumulation.  Group g is rows [offsets[g], offsets[g+1]):
+ *   h = act(X Wgu^T)  (SwiGLU or SiLU, of fp32 sums), quantised to MXFP4 row by row
+ *   y = h Wd^T        rounded to bf16
+ * x [cap, d / 2] and x_scales [cap, moe_mxfp4_scale_stride(d)]: the dispatched rows (see
+ * n_rows of moe_mxfp4_quantize); w_gate_up [n_groups, 2H (SiLU: H), d / 2] and w_down
+ * [n_groups, d, H / 2] with their scales; y [cap, d] bf16, rows of each group only.
+ * offsets: device, n_groups + 1 non-decreasing int32 values, each group clamped to [0, cap].
+ * ws: device workspace (256-byte aligned) of at least moe_mxfp4_ffn_fwd_workspace_size(cap,
+ * H) bytes (h); its contents on entry are ignored.
+ * A NaN block (scale 255) makes the rows it enters NaN, and no others.
+ * Limits: n_groups <= 256, d % 64 == 0, H % 64 == 0, cap max(d, H) / 2 and n_groups 2H d / 2
+ * below 2^32 - 16 (operands are addressed with 32-bit byte offsets); codes and y 16-byte
+ * aligned, scales 4-byte.
+ */
+typedef struct moe_mxfp4_ffn {
+  int cap, d, H, n_groups, activation;
+  const uint8_t* x;
+  const uint8_t* x_scales;
+  const uint8_t* w_gate_up;
+  const uint8_t* w_gate_up_scales;
+  const uint8_t* w_down;
+  const uint8_t* w_down_scales;
+  const int32_t* offsets;
+  void* y;
+  void* ws;
+  size_t ws_bytes;
+} moe_mxfp4_ffn;
+size_t moe_mxfp4_ffn_fwd_workspace_size(int cap, int H);
+int moe_mxfp4_ffn_fwd(const moe_mxfp4_ffn* f, hipStream_t stream);
+
+/*
  * The whole layer's forward for a few tokens (evaluation on a handful of tokens,
  * generation), where moe_layer_fwd's time is that of its many launches and of
  * rows that it moves: three launches, each active expert's weights read once.
@@ -439,7 +472,7 @@ int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype,
  * only if they are ordered on a stream.
  * Limits: 0 <= T <= 64, 1 <= k <= 8, k <= E <= 256, d % 64 == 0, H % 64 == 0, Hs % 64 == 0,
  * 2 max(H, Hs) d below 2^31;
- * x, y, the weights and codes 16-byte aligned.
+ * x, y, the weights and codes 16-byte aligned, scales 4-byte.
  */
 enum { MOE_W_PLAIN = 0, MOE_W_MXFP4 = 1 };
 typedef struct moe_few {

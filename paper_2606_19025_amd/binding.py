@@ -28,6 +28,7 @@ EXPORTS = [
     "moe_combine_bwd", "moe_layer_fwd", "moe_layer_bwd",
     "moe_layernorm_fwd", "moe_layernorm_bwd_workspace_size", "moe_layernorm_bwd",
     "moe_mxfp4_scale_stride", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
+    "moe_mxfp4_ffn_fwd_workspace_size", "moe_mxfp4_ffn_fwd",
     "moe_few_fwd_workspace_size", "moe_few_fwd",
     "moe_expert_delta", "moe_adamw_step", "moe_outer_nesterov", "moe_replica_mean",
     "moe_gen_placement", "moe_migration_map", "moe_copy_expert_rows", "moe_warmup_lr",
@@ -76,6 +77,8 @@ _SIGS = {
     "moe_mxfp4_scale_stride": (_I, [_I]),
     "moe_mxfp4_quantize": (_I, [_P, _I, _I, _I, _P, _P, _P, _P]),
     "moe_mxfp4_dequantize": (_I, [_P, _P, _I, _I, _I, _P, _P, _P]),
+    "moe_mxfp4_ffn_fwd_workspace_size": (_Z, [_I, _I]),
+    "moe_mxfp4_ffn_fwd": (_I, [_P, _P]),
     "moe_few_fwd_workspace_size": (_Z, [_P]),
     "moe_few_fwd": (_I, [_P, _P]),
     "moe_expert_delta": (_I, [_P, _P, C.POINTER(C.c_void_p), _I, _Z, _P, _P, _P]),
@@ -117,6 +120,14 @@ class moe_layer(C.Structure):
     _fields_ += [(n, _P) for n in ("y", "dy", "d_topk_w", "dz", "dw_router", "d_bias", "dx",
                                    "ws_route")]
     _fields_ += [("ws_route_bytes", _Z), ("sets", moe_ffn_set * 2)]
+
+
+class moe_mxfp4_ffn(C.Structure):
+    """The MXFP4 expert FFN's arguments (struct moe_mxfp4_ffn of include/moe_resident.h)."""
+    _fields_ = [(n, _I) for n in ("cap", "d", "H", "n_groups", "activation")]
+    _fields_ += [(n, _P) for n in ("x", "x_scales", "w_gate_up", "w_gate_up_scales", "w_down",
+                                   "w_down_scales", "offsets", "y", "ws")]
+    _fields_ += [("ws_bytes", _Z)]
 
 
 class moe_few(C.Structure):
@@ -341,6 +352,15 @@ def moe_mxfp4_quantize(x, dtype, rows, cols, n_rows, codes, scales, stream=None)
 def moe_mxfp4_dequantize(codes, scales, dtype, rows, cols, n_rows, x, stream=None):
     return _check("moe_mxfp4_dequantize", lib().moe_mxfp4_dequantize(
         _ptr(codes), _ptr(scales), dtype, rows, cols, _ptr(n_rows), _ptr(x), _stream(stream)))
+
+
+def moe_mxfp4_ffn_fwd_workspace_size(cap, H) -> int:
+    return lib().moe_mxfp4_ffn_fwd_workspace_size(cap, H)
+
+
+def moe_mxfp4_ffn_fwd(ffn, stream=None):
+    """ffn: a moe_mxfp4_ffn."""
+    return _check("moe_mxfp4_ffn_fwd", lib().moe_mxfp4_ffn_fwd(C.byref(ffn), _stream(stream)))
 
 
 def moe_few_fwd_workspace_size(few) -> int:

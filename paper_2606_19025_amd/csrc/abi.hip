@@ -9,6 +9,7 @@
 #include <string>
 #include <vector>
 
+#include "gemm.h"
 #include "kernels.h"
 #include "mx.h"
 #include "moe_resident.h"
@@ -554,6 +555,40 @@ int moe_mxfp4_dequantize(const uint8_t* codes, const uint8_t* scales, int dtype,
       "moe_mxfp4_dequantize");
 }
 
+size_t moe_mxfp4_ffn_fwd_workspace_size(int cap, int H) {
+  return cap < 0 || H < 1 ? 0 : moe::mx_ffn_ws_bytes(cap, H);
+}
+
+int moe_mxfp4_ffn_fwd(const moe_mxfp4_ffn* f, hipStream_t stream) {
+  REQUIRE(f != nullptr, "the arguments must not be NULL");
+  REQUIRE(f->activation == MOE_ACT_SWIGLU || f->activation == MOE_ACT_SILU,
+          "activation = %d is not an expert form", f->activation);
+  REQUIRE(f->cap >= 0 && f->d >= 1 && f->H >= 1 && f->n_groups >= 0,
+          "bad sizes cap = %d, d = %d, H = %d, n_groups = %d", f->cap, f->d, f->H, f->n_groups);
+  SUPPORT(f->n_groups <= moe::kMaxGroups, "n_groups = %d: at most %d groups", f->n_groups,
+          moe::kMaxGroups);
+  SUPPORT(f->d % 64 == 0 && f->H % 64 == 0, "d = %d and H = %d must be multiples of 64", f->d, f->H);
+  SUPPORT((int64_t)f->cap * std::max(f->d, f->H) / 2 < 0xFFFFFFF0L &&
+              (int64_t)f->n_groups * f->H * f->d < 0xFFFFFFF0L,
+          "MXFP4 operands must each stay below 4 GiB (cap = %d, H = %d, groups = %d)", f->cap, f->H,
+          f->n_groups);
+  REQUIRE(f->offsets, "offsets must not be NULL");
+  REQUIRE(f->n_groups == 0 ||
+              (f->w_gate_up && f->w_gate_up_scales && f->w_down && f->w_down_scales),
+          "the experts' codes and scales must not be NULL");
+  REQUIRE(f->cap == 0 || (f->x && f->x_scales && f->y), "x, its scales and y must not be NULL");
+  for (const void* p : {(const void*)f->x, (const void*)f->w_gate_up, (const void*)f->w_down,
+                        (const void*)f->y})
+    SUPPORT(p == nullptr || aligned16(p), "codes and y must be 16-byte aligned");
+  for (const void* p : {f->x_scales, f->w_gate_up_scales, f->w_down_scales})
+    SUPPORT((reinterpret_cast<uintptr_t>(p) & 3u) == 0, "scales must be 4-byte aligned");
+  const size_t need = moe::mx_ffn_ws_bytes(f->cap, f->H);
+  REQUIRE(need == 0 || (f->ws && f->ws_bytes >= need), "workspace of %zu bytes needed (got %zu)", need,
+          f->ws_bytes);
+  SUPPORT((reinterpret_cast<uintptr_t>(f->ws) & 255u) == 0, "the workspace must be 256-byte aligned");
+  return hip_status(moe::launch_mx_ffn(f, stream), "moe_mxfp4_ffn_fwd");
+}
+
 namespace {
 // Everything of a moe_few but its pointers.
 int check_few_sizes(const moe_few* f) {
@@ -600,6 +635,9 @@ int moe_few_fwd(const moe_few* f, hipStream_t stream) {
   for (const void* p : {f->x, f->w_router, f->w_gate_up, f->w_down, f->shared_gate_up,
                         f->shared_down, (const void*)f->y})
     SUPPORT(p == nullptr || aligned16(p), "x, y and the weights must be 16-byte aligned");
+  for (const void* p : {f->w_gate_up_scales, f->w_down_scales, f->shared_gate_up_scales,
+                        f->shared_down_scales})
+    SUPPORT((reinterpret_cast<uintptr_t>(p) & 3u) == 0, "scales must be 4-byte aligned");
   const size_t need = moe::few_ws_bytes(f);
   REQUIRE(need == 0 || (f->ws && f->ws_bytes >= need), "workspace of %zu bytes needed (got %zu)", need,
           f->ws_bytes);

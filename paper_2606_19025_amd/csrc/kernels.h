@@ -118,6 +118,10 @@ constexpr int kFewTokens = 64, kFewRoutes = 8;
 size_t few_ws_bytes(const moe_few* f);
 hipError_t launch_few(const moe_few* f, hipStream_t s);
 
+// Grouped expert FFN in MXFP4 (gemm_mx.hip).
+size_t mx_ffn_ws_bytes(int cap, int H);
+hipError_t launch_mx_ffn(const moe_mxfp4_ffn* f, hipStream_t s);
+
 // MXFP4 rows (mx.hip); n_rows: device count of the rows to convert, or NULL (all).
 hipError_t launch_mx_quantize(const void* x, int bf16, int rows, int cols, const int32_t* n_rows,
                               uint8_t* codes, uint8_t* scales, hipStream_t s);

@@ -380,6 +380,49 @@ def mxfp4_dequantize(codes, scales, dtype=torch.bfloat16, out=None, n_rows=None,
     return out
 
 
+class MxFFN:
+    """The grouped expert FFN in MXFP4 on up to ``cap`` dispatched rows: moe_mxfp4_quantize of
+    the rows, then moe_mxfp4_ffn_fwd on weights given once as (codes, scales) pairs of
+    ``mxfp4_quantize``: ``w_gate_up`` of [E_r, 2H (SiLU: H), d], ``w_down`` of [E_r, d, H]."""
+
+    def __init__(self, cap, w_gate_up, w_down, expert="swiglu"):
+        (gu, gu_s), (dn, dn_s) = w_gate_up, w_down
+        dev = self.device = gu.device
+        r1 = 2 if B.ACTIVATIONS[expert] == B.MOE_ACT_SWIGLU else 1
+        self.cap, (E_r, d), H = int(cap), dn.shape[:2], 2 * dn.shape[2]
+        self.d, self.H, self.E_r = d, H, E_r
+        stride = B.moe_mxfp4_scale_stride
+        for name, t, shape in (("w_gate_up codes", gu, (E_r, r1 * H, d // 2)),
+                               ("w_gate_up scales", gu_s, (E_r, r1 * H, stride(d))),
+                               ("w_down codes", dn, (E_r, d, H // 2)),
+                               ("w_down scales", dn_s, (E_r, d, stride(H)))):
+            _check_tensor(name, t, shape, torch.uint8, dev, "layer")
+        new = lambda *s, dt=torch.uint8: torch.empty(*s, dtype=dt, device=dev)
+        self.xq, self.xs = new(self.cap, d // 2), new(self.cap, stride(d))
+        self.y = new(self.cap, d, dt=torch.bfloat16)
+        ws_bytes = B.moe_mxfp4_ffn_fwd_workspace_size(self.cap, H)
+        self.ws = new(max(ws_bytes, 1))
+        # (held here: the library keeps addresses only)
+        self._held = (gu, gu_s, dn, dn_s)
+        p = B._ptr
+        self._ffn = B.moe_mxfp4_ffn(
+            cap=self.cap, d=d, H=H, n_groups=E_r, activation=B.ACTIVATIONS[expert], x=p(self.xq),
+            x_scales=p(self.xs), w_gate_up=p(gu), w_gate_up_scales=p(gu_s), w_down=p(dn),
+            w_down_scales=p(dn_s), y=p(self.y), ws=p(self.ws), ws_bytes=ws_bytes)
+
+    def forward(self, xp, offsets, stream=None):
+        """y [cap, d] of the dispatched rows xp [cap, d] (bf16 or fp32), whose groups are
+        [offsets[g], offsets[g + 1]); rows past offsets[E_r] are neither read nor written."""
+        _check_current(self.device, "layer")
+        _check_tensor("xp", xp, (self.cap, self.d), xp.dtype, self.device, "layer")
+        _check_tensor("offsets", offsets, (self.E_r + 1,), torch.int32, self.device, "layer")
+        B.moe_mxfp4_quantize(xp, B.dtype_code(xp), self.cap, self.d, offsets.data_ptr() + 4 * self.E_r,
+                             self.xq, self.xs, stream)
+        self._ffn.offsets = offsets.data_ptr()
+        B.moe_mxfp4_ffn_fwd(self._ffn, stream)
+        return self.y
+
+
 class InferenceMoELayer:
     """The layer's forward for few tokens on weights that stay: evaluation and generation.
 

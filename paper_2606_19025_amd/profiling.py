@@ -84,6 +84,7 @@ _SYMBOLS = [
     (r"outer_nesterov_kernel", lambda m: "outer_nesterov"),
     (r"replica_mean_kernel", lambda m: "replica_mean"),
     (r"copy_expert_rows_kernel", lambda m: "copy_expert_rows"),
+    (r"mx_gemm_kernel(?:<|ILi)(\d)", lambda m: "mx_gemm_" + ("gu", "up", "down")[int(m.group(1))]),
     (r"few_logits_(?:bf16|f32)_kernel", lambda m: "few_logits"),
     (r"(norm_fwd|norm_bwd|norm_dw|mx_quantize|mx_dequantize|few_gu|few_down)_kernel", lambda m: m.group(1)),
 ]
@@ -93,7 +94,7 @@ _SOURCES = [("gemm_", "gemm.hip"), ("splitk_", "gemm.hip"), ("zero_counters", "g
             ("combine_", "dispatch.hip"), ("unpermute", "dispatch.hip"),
             ("expert_delta", "dispatch.hip"), ("adamw", "optim.hip"), ("outer_", "optim.hip"),
             ("replica_", "optim.hip"),
-            ("copy_expert_rows", "placement.hip"), ("norm_", "norm.hip"), ("mx_", "mx.hip"),
+            ("copy_expert_rows", "placement.hip"), ("norm_", "norm.hip"), ("mx_gemm", "gemm_mx.hip"), ("mx_", "mx.hip"),
             ("few_", "few.hip")]
 
 
