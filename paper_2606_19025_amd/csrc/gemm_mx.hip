@@ -39,26 +39,30 @@ struct MxGemmArgs {
   int K, N, H;
 };
 
-constexpr unsigned kPast = 0xFFFFFFF0u;  // an offset past every operand
+// An offset past every operand; the range check holds with a step's offset added too.
+constexpr unsigned kPast = 0xFFFFFFF0u;
 
-DEVI u32x4_t mx_rsrc(const void* base) {
+DEVI u32x4_t mx_rsrc(const void* base, size_t bytes) {
   const uint64_t b = (uint64_t)(uintptr_t)base;
   u32x4_t r;
   r[0] = __builtin_amdgcn_readfirstlane((unsigned)b);
   r[1] = __builtin_amdgcn_readfirstlane((unsigned)(b >> 32) & 0xFFFFu);
-  r[2] = kPast;
+  r[2] = __builtin_amdgcn_readfirstlane((unsigned)bytes);
   r[3] = 0x00020000u;
   return r;
 }
-// 16 (4) bytes per lane at byte offset off to LDS at lds + 16 (4) lane.  The asm sets m0 and
+// 16 bytes per lane at byte offset off + soff (soff uniform) to LDS at lds + 16 lane.  The asm sets m0 and
 // leaves the one wait state an LDS DMA needs after it.
-DEVI void mx_dma16(u32x4_t rsrc, unsigned off, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "s"(lds)
+DEVI void mx_dma16(u32x4_t rsrc, unsigned off, unsigned soff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(off), "s"(rsrc),
+               "s"(soff), "s"(lds)
                : "m0", "memory");
 }
-DEVI void mx_dma4(u32x4_t rsrc, unsigned off, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(off), "s"(rsrc), "s"(lds)
-               : "m0", "memory");
+
+// silu by the hardware's exp2 and reciprocal: off by a few 2^-24 and 1.5 |g| 2^-24 of itself
+// (the rounding of g log2 e); expf and a division made the epilogue a quarter of a tile's time.
+DEVI float silu_hw(float g) {
+  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * g));
 }
 
 // A block's tile: WR x WC waves of MI x NJ MFMA tiles.
@@ -66,12 +70,13 @@ template <int MI_, int NJ_, int WR_, int WC_>
 struct MxTile {
   static constexpr int MI = MI_, NJ = NJ_, WR = WR_, WC = WC_, NW = WR * WC, NT = 64 * NW;
   static constexpr int BM = 16 * MI * WR, BN = 16 * NJ * WC;
-  static constexpr int PA = BM / (8 * NW), PB = BN / (8 * NW);       // 8-row DMA pieces per wave
-  static constexpr int SP = (BM + BN) / 32, PS = (SP + NW - 1) / NW;  // 32-row scale pieces, per wave
-  static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = NW * PS * 256;
-  static constexpr int STAGE = A_BYTES + B_BYTES + S_BYTES;
-  static constexpr int EPI = 2048;  // a wave's staging: 16 rows of 64 bf16
-  static constexpr int LDS = 2 * STAGE + NW * EPI;
+  static constexpr int PA = BM / (8 * NW), PB = BN / (8 * NW);  // 8-row DMA pieces per wave
+  static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
+  static constexpr int SP = (BM + BN) / 64, S_STAGE = NW * 1024;     // 64-row scale pieces
+  static constexpr int S_AT = 2 * STAGE, E_AT = S_AT + 2 * S_STAGE;
+  static constexpr int EPI = 1024;  // a wave's staging: 8 rows of 64 bf16
+  static constexpr int LDS = E_AT + NW * EPI;
+  static_assert(SP <= NW && BM % 64 == 0 && BN % 64 == 0, "a scale piece per wave at most");
 };
 
 template <int KIND, class T>
@@ -89,7 +94,9 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
   const int steps = (p.K + 255) / 256;
   const unsigned line = p.K / 2, sline = mx_stride(p.K);
   const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void_t*)lds);
-  const u32x4_t ra = mx_rsrc(p.a), rb = mx_rsrc(p.b), rsa = mx_rsrc(p.as), rsb = mx_rsrc(p.bs);
+  const size_t b_rows = (size_t)ng * p.N;
+  const u32x4_t ra = mx_rsrc(p.a, (size_t)p.g.cap * line), rb = mx_rsrc(p.b, b_rows * line);
+  const u32x4_t rs = wave * 64 < T::BM ? mx_rsrc(p.as, (size_t)p.g.cap * sline) : mx_rsrc(p.bs, b_rows * sline);
 
   // Tiles are dealt to the XCDs (blocks are placed on them round-robin) in equal consecutive
   // shares; within a group they run in bands of 4 m-tiles, so that the tiles an XCD runs at
@@ -128,52 +135,53 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
     }
   };
 
-  unsigned oa[T::PA], ob[T::PB], os[T::PS];  // lane offsets of the tile at hand
-  auto chunk_of = [&](int row) { return (lane & 7) ^ ((row >> 1) & 7); };
+  // Lane offsets of the tile at hand.  A wave's pieces are 8 NW rows apart, a multiple of 16:
+  // the lane's chunk of its row is the same in all of them.
+  static_assert(NW % 2 == 0, "pieces 16 rows apart");
+  unsigned oa[T::PA], ob[T::PB], os;
+  const int chunk = (lane & 7) ^ (((wave * 8 + (lane >> 3)) >> 1) & 7);
   auto aim = [&](const Where& w) {
 #pragma unroll
     for (int i = 0; i < T::PA; ++i) {
       const int r = (i * NW + wave) * 8 + (lane >> 3);
-      oa[i] = (unsigned)min(w.row0 + r, w.row1 - 1) * line + chunk_of(r) * 16;
+      oa[i] = (unsigned)min(w.row0 + r, w.row1 - 1) * line + chunk * 16;
     }
     const unsigned bg = (unsigned)w.g * (unsigned)p.N;
 #pragma unroll
     for (int i = 0; i < T::PB; ++i) {
       const int r = (i * NW + wave) * 8 + (lane >> 3);
-      ob[i] = (bg + (unsigned)b_row(w.n0, r)) * line + chunk_of(r) * 16;
+      ob[i] = (bg + (unsigned)b_row(w.n0, r)) * line + chunk * 16;
     }
-#pragma unroll
-    for (int i = 0; i < T::PS; ++i) {
-      // piece: 32 rows of A, then of B (pieces past the last repeat it, into space of their own)
-      const int piece = min(i * NW + wave, T::SP - 1), r = piece * 32 + (lane >> 1);
-      const unsigned row = r < T::BM ? (unsigned)min(w.row0 + r, w.row1 - 1)
-                                     : bg + (unsigned)b_row(w.n0, r - T::BM);
-      os[i] = row * sline + (lane & 1) * 4;
-    }
+    // scales: 64 rows of A, then of B, by wave
+    const int r = wave * 64 + lane;
+    os = wave >= T::SP ? kPast : (r < T::BM ? (unsigned)min(w.row0 + r, w.row1 - 1) : bg + (unsigned)b_row(w.n0, r - T::BM)) * sline;
   };
-  auto issue = [&](int kt) {
+  // Part q of 4 of a k-step's loads; even k-steps bring the scales of two, 16 bytes of a row
+  // (8 at a time, their requests to the L2 were as many as the codes').
+  auto issue_part = [&](int kt, auto even, int q) {
     const unsigned at = lds0 + (kt & 1) * T::STAGE;
-    const int rest = p.K - kt * 256;  // (below 256: the last k-step, cut)
+    // the chunks past a cut last k-step read zeros
+    const bool in = chunk * 32 < p.K - kt * 256;
 #pragma unroll
-    for (int i = 0; i < T::PA; ++i) {
-      const bool in = rest >= 256 || chunk_of((i * NW + wave) * 8 + (lane >> 3)) * 32 < rest;
-      mx_dma16(ra, in ? oa[i] + kt * 128 : kPast, at + (i * NW + wave) * 1024);
-    }
+    for (int i = 0; i < T::PA; ++i)
+      if (i % 4 == q) mx_dma16(ra, in ? oa[i] : kPast, kt * 128, at + (i * NW + wave) * 1024);
 #pragma unroll
-    for (int i = 0; i < T::PB; ++i) {
-      const bool in = rest >= 256 || chunk_of((i * NW + wave) * 8 + (lane >> 3)) * 32 < rest;
-      mx_dma16(rb, in ? ob[i] + kt * 128 : kPast, at + T::A_BYTES + (i * NW + wave) * 1024);
-    }
+    for (int i = 0; i < T::PB; ++i)
+      if (i % 4 == q) mx_dma16(rb, in ? ob[i] : kPast, kt * 128, at + T::A_BYTES + (i * NW + wave) * 1024);
+    if (decltype(even)::value && q == 3)
+      mx_dma16(rs, os, kt * 8, lds0 + T::S_AT + (kt >> 1 & 1) * T::S_STAGE + wave * 1024);
+  };
+  auto issue_first = [&]() {
 #pragma unroll
-    for (int i = 0; i < T::PS; ++i) {
-      const bool in = rest > 128 || (lane & 1) == 0;
-      const bool of_a = (i * NW + wave) * 32 < T::BM;  // (wave-uniform)
-      mx_dma4(of_a ? rsa : rsb, in ? os[i] + kt * 8 : kPast,
-              at + T::A_BYTES + T::B_BYTES + (i * NW + wave) * 256);
-    }
+    for (int q = 0; q < 4; ++q) issue_part(0, std::true_type{}, q);
+    if (steps > 1)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) issue_part(1, std::false_type{}, q);
   };
 
-  // Operands: the wave's rows of one k128 half, and the columns of one chunk (a half's j).
+  // Operands: the wave's rows of one k128 half, and the columns of one chunk (a half's j), with
+  // their words of four scales (shifted to the lane's own where they are used: sooner
+  // would wait for the read).
   struct Rows {
     u32x4_t v[MI];
     unsigned s[MI];
@@ -183,25 +191,27 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
     unsigned s;
   };
   // a tile's rows are 16 apart: its place in a stage is the first one's plus 2048 bytes each
-  // (the other half's chunk is 64 bytes further or back), 128 bytes of scales
+  // (the other half's chunk is 64 bytes further or back), 256 bytes of scales
   const unsigned place = l16 * 128 + ((q4 ^ ((l16 >> 1) & 7)) << 4), sh = 8 * q4;
   const unsigned rows_at = wr * MI * 2048, cols_at = T::A_BYTES + wc * NJ * 2048;
-  const unsigned rs_at = T::A_BYTES + T::B_BYTES + wr * MI * 128 + l16 * 8;
-  const unsigned cs_at = T::A_BYTES + T::B_BYTES + T::BM * 8 + wc * NJ * 128 + l16 * 8;
-  auto read_rows = [&](Rows& f, int kt, int half) {
+  const unsigned rs_at = T::S_AT + wr * MI * 256 + l16 * 16, cs_at = T::S_AT + T::BM * 16 + wc * NJ * 256 + l16 * 16;
+  // word of a row's scales at a half of k-step kt
+  auto scales = [&](int kt, int half) { return lds + (kt >> 1 & 1) * T::S_STAGE + (kt & 1) * 8 + half * 4; };
+  // mask: zero for a word past the end of its row (the second one of a cut last k-step)
+  auto read_rows = [&](Rows& f, int kt, int half, unsigned mask = ~0u) {
     const char* at = lds + (kt & 1) * T::STAGE;
     const char* v = at + rows_at + (place ^ (half * 64));
-    const char* sc = at + rs_at + half * 4;
+    const char* sc = scales(kt, half) + rs_at;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       f.v[i] = *reinterpret_cast<const u32x4_t*>(v + i * 2048);
-      f.s[i] = *reinterpret_cast<const unsigned*>(sc + i * 128) >> sh;
+      f.s[i] = *reinterpret_cast<const unsigned*>(sc + i * 256) & mask;
     }
   };
-  auto read_col = [&](Col& f, int kt, int half, int j) {
+  auto read_col = [&](Col& f, int kt, int half, int j, unsigned mask = ~0u) {
     const char* at = lds + (kt & 1) * T::STAGE;
     f.v = *reinterpret_cast<const u32x4_t*>(at + cols_at + (place ^ (half * 64)) + j * 2048);
-    f.s = *reinterpret_cast<const unsigned*>(at + cs_at + half * 4 + j * 128) >> sh;
+    f.s = *reinterpret_cast<const unsigned*>(scales(kt, half) + cs_at + j * 256) & mask;
   };
   f32x4_t acc[MI][NJ];
   auto wide = [](u32x4_t v) {
@@ -213,14 +223,14 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
       acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(b.v), wide(a.v[i]), acc[i][j], 4, 4, 0,
-                                                                   (int)b.s, 0, (int)a.s[i]);
+                                                                   (int)(b.s >> sh), 0, (int)(a.s[i] >> sh));
   };
 
   if (tile >= t_end) return;
   Where w = decode(tile);
   aim(w);
-  issue(0);
-  if (steps > 1) issue(1);
+  issue_first();
+  const unsigned past = p.K - (steps - 1) * 256 > 128 ? ~0u : 0u;
   for (;;) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -236,27 +246,38 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) read_col(b[c], 0, 0, c);
     // (no branch inside a k-step: the compiler would move its products past it)
-    auto step = [&](auto refill, auto next, int kt) {
+    auto step = [&](auto refill, auto next, auto even, int kt) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         if (c == C - 4) {
           WAIT_LGKMCNT(0);
           WAIT_VMCNT(0);
           __syncthreads();  // this stage has been read, the next one is whole
-          if constexpr (decltype(refill)::value) issue(kt + 2);
           if constexpr (decltype(next)::value) read_rows(a0, kt + 1, 0);
         }
-        if (c == 1) read_rows(a1, kt, 1);
+        if (c == 1) {
+          if constexpr (decltype(next)::value) read_rows(a1, kt, 1);
+          else read_rows(a1, kt, 1, past);
+        }
         mma(c < NJ ? a0 : a1, b[c % 4], c % NJ);
-        if (c + 4 < C) read_col(b[c % 4], kt, (c + 4) / NJ, (c + 4) % NJ);
-        else if constexpr (decltype(next)::value) read_col(b[c % 4], kt + 1, 0, c + 4 - C);
+        if (c + 4 < C) {
+          if (decltype(next)::value || c + 4 < NJ) read_col(b[c % 4], kt, (c + 4) / NJ, (c + 4) % NJ);
+          else read_col(b[c % 4], kt, 1, (c + 4) % NJ, past);
+        } else if constexpr (decltype(next)::value) read_col(b[c % 4], kt + 1, 0, c + 4 - C);
+        if constexpr (decltype(refill)::value)
+          if (c >= C - 4) issue_part(kt + 2, even, c - (C - 4));
         __builtin_amdgcn_sched_barrier(0);  // (reads moved further ahead cost registers)
       }
     };
+    typedef std::true_type Yes;
+    typedef std::false_type No;
     int kt = 0;
-    for (; kt + 2 < steps; ++kt) step(std::true_type{}, std::true_type{}, kt);
-    if (kt + 1 < steps) step(std::false_type{}, std::true_type{}, kt++);
-    step(std::false_type{}, std::false_type{}, kt);
+    while (kt + 2 < steps) {
+      step(Yes{}, Yes{}, Yes{}, kt++);
+      if (kt + 2 < steps) step(Yes{}, Yes{}, No{}, kt++);
+    }
+    if (kt + 1 < steps) step(No{}, Yes{}, No{}, kt++);
+    step(No{}, No{}, No{}, kt);
     // the next tile's first stages, while this one's results are stored
     const Where done = w;
     const bool more = tile + per_xcd < t_end;
@@ -264,8 +285,7 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
       tile += per_xcd;
       w = decode(tile);
       aim(w);
-      issue(0);
-      if (steps > 1) issue(1);
+      issue_first();
     }
     const int m0 = done.row0 + wr * MI * 16;  // this wave's first row
     // (the epilogue's lane index passes through an asm, so that its addresses are computed
@@ -274,28 +294,32 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
     asm volatile("" : "+v"(el));
     const int l16 = el & 15, q4 = el >> 4;
     if constexpr (KIND == MX_DOWN) {
-      // 16 rows of 64 columns at a time through the wave's staging, so that a store
-      // covers 128 bytes of a row; 16-byte chunk c of row r at chunk c ^ (r & 7)
-      char* stage = lds + 2 * T::STAGE + wave * T::EPI;
+      // 8 rows of 64 columns at a time through the wave's staging, so that a store covers
+      // 128 bytes of a row; 16-byte chunk c of row r at chunk c ^ r
+      char* stage = lds + T::E_AT + wave * T::EPI;
       const int c0 = done.n0 * T::BN + wc * NJ * 16;
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int jh = 0; jh < NJ; jh += 4) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f32x4_t v = acc[i][jh + j];
-            const bf16x4_t o = {(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
-            *reinterpret_cast<bf16x4_t*>(stage + l16 * 128 + (((2 * j + (q4 >> 1)) ^ (l16 & 7)) << 4) + (q4 & 1) * 8) = o;
-          }
+        for (int jh = 0; jh < NJ; jh += 4)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const int r = u * 8 + (el >> 3), c = el & 7;
-            const u32x4_t v = *reinterpret_cast<const u32x4_t*>(stage + r * 128 + ((c ^ (r & 7)) << 4));
-            const int row = m0 + i * 16 + r, col = c0 + jh * 16 + c * 8;
-            if (row < done.row1 && col < p.N) *reinterpret_cast<u32x4_t*>(p.y + (size_t)row * p.N + col) = v;
+            if (l16 >> 3 == u) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const f32x4_t v = acc[i][jh + j];
+                const bf16x4_t o = {(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
+                const int r = l16 & 7;
+                *reinterpret_cast<bf16x4_t*>(stage + r * 128 + (((2 * j + (q4 >> 1)) ^ r) << 4) + (q4 & 1) * 8) = o;
+              }
+            }
+            const int r = el >> 3, c = el & 7;
+            const u32x4_t v = *reinterpret_cast<const u32x4_t*>(stage + r * 128 + ((c ^ r) << 4));
+            const int row = m0 + i * 16 + u * 8 + r, col = c0 + jh * 16 + c * 8;
+            // (past the caches: y is not read again here)
+            if (row < done.row1 && col < p.N)
+              __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(p.y + (size_t)row * p.N + col));
           }
-        }
     } else {
       // h of 32 hidden units (a block) of row l16: 8 values in each of the lanes l16 + 16 q
       constexpr int HB = KIND == MX_GU ? NJ / 4 : NJ / 2;
@@ -311,7 +335,7 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
           for (int e = 0; e < 8; ++e) {
             const int j = (e >> 2) + (KIND == MX_GU ? 4 * b : 2 * b);
             const float g = acc[i][j][e & 3];
-            v[e] = silu_f(g);
+            v[e] = silu_hw(g);
             if constexpr (KIND == MX_GU) v[e] *= acc[i][j + 2][e & 3];
             top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
           }

@@ -2,7 +2,8 @@
 
 Tolerance, u = 2^-24: a first projection's sum of d products is off by at most d u times the
 sum of magnitudes (any order of summation), which moves h by dh = 1.1 |U| dG + |silu(G)| dU
-and a few u of itself (|silu'| <= 1.1).  h becomes codes: where its border or its block's
+(|silu'| <= 1.1); silu itself is off by a few u (exp2 and the reciprocal are good to 2 u, and
+three roundings) and, from the rounding of G log2 e, by 1.45 |G| u of itself.  h becomes codes: where its border or its block's
 scale lies within dh the neighbouring code is as right, so each quantised h lies between the
 least and the greatest of its four candidates (h -+ dh under the scales of the block's
 largest value -+ its dh).  y sums |W_d| of that range, H u of its own sum of magnitudes and
@@ -72,7 +73,7 @@ def reference(x, sizes, gu, dn, expert):
             h, dh = act * a[:, H:], 1.1 * dG * (a[:, H:].abs() + da[:, H:]) + act.abs() * da[:, H:]
         else:
             h, dh = act, 1.1 * dG
-        mid, lo, hi = quantised(h, dh + 16 * U * (h.abs() + dh))
+        mid, lo, hi = quantised(h, dh + (16 + 1.5 * G.abs()) * U * (h.abs() + dh))
         y[rows] = mid @ d2.T
         tol[rows] = (torch.maximum(hi - mid, mid - lo) + H * U * mid.abs()) @ d2.abs().T
     return y, (tol * (1 + HALF) + HALF * y.abs())
