@@ -369,9 +369,6 @@ typedef MxTile<2, 4, 2, 2> MxSmall;  // 64 x 128
 template <int KIND, class T>
 hipError_t mx_run(const MxGemmArgs& a, const char* name, hipStream_t s) {
   static_assert(T::LDS + sizeof(GroupTable) <= 160 * 1024, "LDS");
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_gemm_kernel<KIND, T>),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
-  if (e != hipSuccess) return e;
   const int blocks = num_cus() / 8 * 8 * (T::LDS * 2 <= 150 * 1024 ? 2 : 1);
   MOE_TIMED(name, s, mx_gemm_kernel<KIND, T><<<blocks, T::NT, T::LDS, s>>>(a));
   return hipGetLastError();

@@ -95,7 +95,7 @@ _SOURCES = [("gemm_", "gemm.hip"), ("splitk_", "gemm.hip"), ("zero_counters", "g
             ("expert_delta", "dispatch.hip"), ("adamw", "optim.hip"), ("outer_", "optim.hip"),
             ("replica_", "optim.hip"),
             ("copy_expert_rows", "placement.hip"), ("norm_", "norm.hip"), ("mx_gemm", "gemm_mx.hip"), ("mx_", "mx.hip"),
-            ("few_", "few.hip")]
+            ("few_logits", "few.hip"), ("few_", "few.h")]
 
 
 def timing_name(symbol: str) -> str | None:
