@@ -22,7 +22,7 @@ namespace {
 
 // Waves of a block whose rows take W waves each.
 constexpr int block_waves(int W) { return W == 1 ? 4 : W; }
-constexpr int kDwThreads = 256;
+constexpr int kDwThreads = 1024;
 
 struct NormArgs {
   const void* x;
@@ -257,20 +257,27 @@ __global__ __launch_bounds__(64 * block_waves(W)) void norm_bwd_kernel(NormArgs 
   }
 }
 
-// dw and db from the n partial rows [n][2][d]: a block takes 64 of the 2 d
-// columns, sixteen threads (16 bytes each) by sixteen shares of the partials.
+// dw and db from the n partial rows [n][2][d]: a block takes 64 of the 2 d columns, sixteen
+// threads (16 bytes each) by 64 shares of the partials, whose sums are added eight at a time.
+// (Sixteen shares: 512 partials took 7 us, a thread's 32 loads one after another; now 4.)
 __global__ __launch_bounds__(kDwThreads) void norm_dw_kernel(const float* part, int n, int d, float* dw,
-                                                     float* db, int accumulate) {
-  __shared__ f32x4_t sum[16][16];
+                                                             float* db, int accumulate) {
+  constexpr int P = kDwThreads / 16, G = 8;
+  __shared__ f32x4_t sum[P][16];
   const int q = threadIdx.x & 15, p = threadIdx.x >> 4;
   const int c = (blockIdx.x * 16 + q) * 4;
   f32x4_t s = {0.f, 0.f, 0.f, 0.f};
   if (c < 2 * d)
-    for (int i = p; i < n; i += 16) s += *reinterpret_cast<const f32x4_t*>(part + (size_t)i * 2 * d + c);
+    for (int i = p; i < n; i += P) s += *reinterpret_cast<const f32x4_t*>(part + (size_t)i * 2 * d + c);
   sum[p][q] = s;
   __syncthreads();
+  if (p < G) {
+    for (int i = p + G; i < P; i += G) s += sum[i][q];
+    sum[p][q] = s;  // (read by this thread alone so far)
+  }
+  __syncthreads();
   if (p == 0 && c < 2 * d) {
-    for (int i = 1; i < 16; ++i) s += sum[i][q];
+    for (int i = 1; i < G; ++i) s += sum[i][q];
     float* out = c < d ? dw + c : db ? db + (c - d) : nullptr;
     if (out) {
       f32x4_t* o = reinterpret_cast<f32x4_t*>(out);
