@@ -374,11 +374,25 @@ hipError_t mx_run(const MxGemmArgs& a, const char* name, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The large tiles where they fill half of the CUs, if every row that may be there is.
+// Large tiles read each operand fewer times, small ones fill the CUs sooner (two blocks on
+// each) and run one block's epilogue beside the other's products.  Large where the rows, all
+// there and spread evenly, give a CU a tile each; where the epilogue also multiplies,
+// quantises and scales (GU, UP): two tiles each and a reduction that is long beside it.
+// Measured (us, large / small; rows, groups, d, H):
+//                            first projection   second
+//   2048, 16, 2048, 1408       31 /  20          23 /  13
+//   4096,  8, 1024, 2816       43 /  32          27 /  16
+//   8192, 16, 2048, 1408       57 /  50          28 /  32
+//   16384, 8, 1024, 2816      122 / 106          36 /  44
+//   16384, 16, 2048, 1408      89 /  93          48 /  57
+//   16384, 32, 4096, 2048     204 / 282         117 / 162
+//   65536, 32, 4096, 2048     713 / 974         422 / 525
 template <int KIND>
 hipError_t mx_launch(const MxGemmArgs& a, const char* name, hipStream_t s) {
-  const int64_t large = (int64_t)(ceil_div(a.g.cap, MxLarge::BM) + a.g.n_groups / 2) * ceil_div(a.N, MxLarge::BN);
-  return large * 2 >= num_cus() ? mx_run<KIND, MxLarge>(a, name, s) : mx_run<KIND, MxSmall>(a, name, s);
+  const int64_t tiles =
+      (int64_t)(a.g.cap / MxLarge::BM + (a.g.n_groups + 1) / 2) * ceil_div(a.N, MxLarge::BN);
+  const bool large = KIND == MX_DOWN ? tiles >= num_cus() : tiles >= 2 * num_cus() && a.K >= 2048;
+  return large ? mx_run<KIND, MxLarge>(a, name, s) : mx_run<KIND, MxSmall>(a, name, s);
 }
 
 }  // namespace
