@@ -294,18 +294,27 @@ int vectors(int d, int ve, int waves) {
 }
 
 // Waves per row: one where the rows are many and a lane then holds at most `one`
-// vectors, else the fewest of 4 and 16 that leave a lane at most `more`.
+// vectors, else the fewest of 4 and 16 that leave a lane at most `more`.  Measured (bf16, us,
+// one wave / four; launch included):
+//   rows      forward, d = 1024  2048       4096         backward, d = 1024
+//   1024      6.7 / 6.7          6.7 / 6.6  9.7 / 7.9    10.4 / 8.1
+//   2048      6.6 / 6.8          8.4 / 7.4  12.1 / 10.7  12.3 / 10.0
+//   4096      7.5 / 9.0          10.9 / 11.1  16.1 / 16.5  13.9 / 13.3
+//   8192      10.4 / 13.6        15.5 / 17.1  27.3 / 24.4  16.6 / 21.1
 int row_waves(int T, int d, int ve, int one, int more) {
-  if (T >= 1024 && vectors(d, ve, 1) <= one) return 1;
+  if (T >= 4096 && vectors(d, ve, 1) <= one) return 1;
   return vectors(d, ve, 4) <= more ? 4 : 16;
 }
-int row_waves_fwd(int T, int d, int ve) { return row_waves(T, d, ve, 8, 4); }
+int row_waves_fwd(int T, int d, int ve) { return row_waves(T, d, ve, 4, 4); }
 // (a lane of the backward holds six fp32 values per element: 16 elements at most)
 int row_waves_bwd(int T, int d, int ve) { return row_waves(T, d, ve, 16 / ve, 16 / ve); }
 
+// Blocks of the backward: each writes a partial row of 2 d, so that past one per CU a block
+// takes at least four rows (1024 rows, d = 4096: 256 blocks 12.7 us, 512 14.5), up to two per
+// CU (8192 rows: 256 blocks 43 us, 512 38, 1024 43).
 int bwd_blocks(int T, int d, int ve) {
-  const int W = row_waves_bwd(T, d, ve);
-  return std::min(ceil_div(T, block_waves(W) / W), 2 * num_cus());
+  const int W = row_waves_bwd(T, d, ve), units = ceil_div(T, block_waves(W) / W);
+  return std::min(std::max(std::min(units, num_cus()), ceil_div(T, 4)), std::min(units, 2 * num_cus()));
 }
 
 template <class E>
@@ -318,8 +327,7 @@ hipError_t fwd(const NormArgs& a, hipStream_t s) {
   if (W == 1) {
     if (nv == 1) NORM_FWD(1, 1);
     else if (nv == 2) NORM_FWD(1, 2);
-    else if (nv == 4) NORM_FWD(1, 4);
-    else NORM_FWD(1, 8);
+    else NORM_FWD(1, 4);
   } else if (W == 4) {
     if (nv == 1) NORM_FWD(4, 1);
     else if (nv == 2) NORM_FWD(4, 2);
