@@ -602,9 +602,11 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
 // and the whole reduction: the shared experts' hidden units, then all active experts', in
 // steps of which each wave takes consecutive ones, its stream running on from expert to
 // expert.  An expert's sums are added to the wave's own rows of y in LDS, and the waves' rows
-// in order at the end.  RB is 16, or less where that would leave CUs without a block: cutting
-// the reduction into parts instead, added by the last block to finish, took three times as
-// long (the fences write back each XCD's whole L2).
+// in order at the end.  RB is 16, or 8 where that would leave CUs without a block (bf16, H =
+// 1408, us with 16 / 8 / 4 columns: d = 4096, 32 tokens 38 / 48 / 77; 2048, 32 tokens 52 / 42 /
+// 66; 2048, one token 15.1 / 14.3 / 23; 1024, 32 tokens 21.0 / 19.6 / 20.5).  Cutting the
+// reduction into parts instead, added by the last block to finish, took three times as long
+// (the fences write back each XCD's whole L2).
 template <class E, bool MX, int NT, int RB>
 __global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
   using F = Fmt<E, MX>;
@@ -746,8 +748,7 @@ void few_launch(const FewArgs& a, hipStream_t s) {
 #define FEW_DOWN(RB) \
   MOE_TIMED("few_down", s, few_down_kernel<E, MX, NT, RB><<<a.d / RB, DT, 0, s>>>(a))
   if (a.d / 16 >= cus) FEW_DOWN(16);
-  else if (a.d / 8 >= cus) FEW_DOWN(8);
-  else FEW_DOWN(4);
+  else FEW_DOWN(8);
 #undef FEW_DOWN
 }
 }  // namespace
