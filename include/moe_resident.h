@@ -471,7 +471,7 @@ int moe_mxfp4_ffn_fwd(const moe_mxfp4_ffn* f, hipStream_t stream);
  * compute-unit count); its contents on entry are ignored, and two calls may share it
  * only if they are ordered on a stream.
  * Limits: 0 <= T <= 64, 1 <= k <= 8, k <= E <= 256, d % 64 == 0, H % 64 == 0, Hs % 64 == 0,
- * 2 max(H, Hs) d below 2^31;
+ * 2 max(H, Hs) d below 2^31, T k max(H, Hs) below 2^29;
  * x, y, the weights and codes 16-byte aligned, scales 4-byte.
  */
 enum { MOE_W_PLAIN = 0, MOE_W_MXFP4 = 1 };

@@ -612,6 +612,9 @@ int check_few_sizes(const moe_few* f) {
   SUPPORT(f->d % 64 == 0 && f->H % 64 == 0 && f->Hs % 64 == 0,
           "d = %d, H = %d and Hs = %d must be multiples of 64", f->d, f->H, f->Hs);
   SUPPORT(2L * std::max(f->H, f->Hs) * f->d < 1L << 31, "an expert's matrix must stay below 2^31 elements");
+  // (the kernels address a row of h by a 32-bit byte offset)
+  SUPPORT((int64_t)f->T * f->k * std::max(f->H, f->Hs) < int64_t(1) << 29,
+          "T = %d: T k max(H, Hs) must stay below 2^29", f->T);
   return MOE_OK;
 }
 }  // namespace

@@ -275,7 +275,8 @@ def test_few_refusals():
     fwd = lambda **kw: B.lib().moe_few_fwd(C.byref(_few(**kw)), None)
     assert B.lib().moe_few_fwd(None, None) == -1 and B.lib().moe_few_fwd_workspace_size(None) == 0
     for kw in (dict(dtype=4), dict(T=65), dict(k=9, E=16), dict(d=96), dict(H=32), dict(Hs=96),
-               dict(weights=1, dtype=B.MOE_F32), dict(d=1 << 16, H=1 << 16), dict(x=260), dict(w_down=264), dict(ws=128)):
+               dict(weights=1, dtype=B.MOE_F32), dict(d=1 << 16, H=1 << 16),
+               dict(d=64, H=1 << 21, T=64, k=8, E=16), dict(x=260), dict(w_down=264), dict(ws=128)):
         assert fwd(**kw) == -2, kw
     for kw in (dict(T=-1), dict(E=0), dict(E=257), dict(k=0), dict(k=9), dict(E_r=9), dict(gate=3),
                dict(activation=2), dict(weights=2), dict(inv_tau=0.0), dict(inv_tau=float("inf")),
