@@ -359,8 +359,8 @@ int moe_layer_bwd(const moe_layer* layer, const char** where, hipStream_t stream
  * x, y [T,d] dtype (y may be x); weight [d] fp32, bias [d] fp32 or NULL (none);
  * mean, rstd [T] fp32 (the backward reads them).  eps must be finite and >= 0;
  * a row of equal values needs eps > 0.
- * Limits: d % 8 == 0, d <= 16384, T >= 0, every array 16-byte aligned except mean
- * and rstd (4).
+ * Limits: d % 8 == 0, d <= 16384, 0 <= T < 2^30, every array 16-byte aligned except
+ * mean and rstd (4).
  */
 int moe_layernorm_fwd(const void* x, const float* weight, const float* bias, int dtype, int T,
                       int d, float eps, void* y, float* mean, float* rstd, hipStream_t stream);
@@ -467,9 +467,8 @@ int moe_mxfp4_ffn_fwd(const moe_mxfp4_ffn* f, hipStream_t stream);
  * logits [T,E] fp32, topk_idx, topk_local [T,k] int32, topk_w [T,k] fp32: outputs, each
  * may be NULL.
  * ws: device workspace (256-byte aligned) of at least moe_few_fwd_workspace_size(f) bytes
- * (which depends on the sizes, on whether logits is NULL, and on the current device's
- * compute-unit count); its contents on entry are ignored, and two calls may share it
- * only if they are ordered on a stream.
+ * (which depends on the sizes and on whether logits is NULL, and grows with T); its contents
+ * on entry are ignored, and two calls may share it only if they are ordered on a stream.
  * Limits: 0 <= T <= 64, 1 <= k <= 8, k <= E <= 256, d % 64 == 0, H % 64 == 0, Hs % 64 == 0,
  * 2 max(H, Hs) d below 2^31, T k max(H, Hs) below 2^29;
  * x, y, the weights and codes 16-byte aligned, scales 4-byte.

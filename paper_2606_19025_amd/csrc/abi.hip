@@ -478,6 +478,7 @@ int check_norm(int dtype, int T, int d) {
   REQUIRE(T >= 0 && d >= 1, "bad sizes T = %d, d = %d", T, d);
   SUPPORT(d % 8 == 0, "d = %d must be a multiple of 8", d);
   SUPPORT(d <= moe::kMaxNormWidth, "d = %d: at most %d", d, moe::kMaxNormWidth);
+  SUPPORT(T < 1 << 30, "T = %d must be below 2^30", T);
   return MOE_OK;
 }
 }  // namespace
@@ -497,7 +498,7 @@ int moe_layernorm_fwd(const void* x, const float* weight, const float* bias, int
 }
 
 size_t moe_layernorm_bwd_workspace_size(int T, int d, int dtype) {
-  if (T < 0 || d < 1) return 0;
+  if (check_norm(dtype, T, d) != MOE_OK) return 0;
   return moe::norm_bwd_ws_bytes(T, d, dtype == MOE_BF16);
 }
 
@@ -569,7 +570,7 @@ int moe_mxfp4_ffn_fwd(const moe_mxfp4_ffn* f, hipStream_t stream) {
           moe::kMaxGroups);
   SUPPORT(f->d % 64 == 0 && f->H % 64 == 0, "d = %d and H = %d must be multiples of 64", f->d, f->H);
   SUPPORT((int64_t)f->cap * std::max(f->d, f->H) / 2 < 0xFFFFFFF0L &&
-              (int64_t)f->n_groups * f->H * f->d < 0xFFFFFFF0L,
+              (int64_t)f->H * f->d < 0xFFFFFFF0L / std::max(f->n_groups, 1),
           "MXFP4 operands must each stay below 4 GiB (cap = %d, H = %d, groups = %d)", f->cap, f->H,
           f->n_groups);
   REQUIRE(f->offsets, "offsets must not be NULL");

@@ -351,6 +351,13 @@ struct Stream {
 #pragma unroll
           for (int p = 0; p < 2; ++p)
             if (128 * p + 32 * q >= rest) f.w[i][p] = u32x4_t{0u, 0u, 0u, 0u};
+      // (and the activations: 0 times an infinity that is read again is not 0)
+      if (rest < F::KS)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int p = 0; p < XN; ++p)
+            if (128 * (p >> 2) + 32 * q >= rest) f.x[n][p] = u32x4_t{0u, 0u, 0u, 0u};
     }
   }
   DEVI static void mma(const Frags& f, f32x4_t (&acc)[RT][N]) {

@@ -194,10 +194,11 @@ __global__ __launch_bounds__(64 * block_waves(W)) void norm_bwd_kernel(NormArgs 
     if (AHEAD && t + step < a.T) fetch(t + step);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      // past the row's end x, dy and w are zeros, and the mean is taken as zero: every sum is
+      const float m = R::col(i) < a.d ? mu : 0.f;
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
-        // (past the row's end dy and w are zero, so that every sum is)
-        xh[i][j] = (xh[i][j] - mu) * r;
+        xh[i][j] = (xh[i][j] - m) * r;
         dw[i][j] += g[i][j] * xh[i][j];
         db[i][j] += g[i][j];
         g[i][j] *= w[i][j];

@@ -257,7 +257,8 @@ class ResidentMoELayer:
 
 class LayerNorm:
     """The layer's pre-norm over [T, d] activations: moe_layernorm_fwd / _bwd on buffers of its
-    own (y, mean, rstd; dx, dw, db from the first backward on)."""
+    own (y, mean, rstd, dw, db; dx from the first backward on), which the next call reuses:
+    calls on different streams need a norm each."""
 
     def __init__(self, T, d, dtype=torch.bfloat16, bias=True, eps=1e-5, device="cuda"):
         self.T, self.d, self.eps, self.bias = int(T), int(d), float(eps), bool(bias)
@@ -269,7 +270,10 @@ class LayerNorm:
         self.mean, self.rstd = (torch.empty(self.T, dtype=torch.float32, device=device)
                                 for _ in range(2))
         self.device = self.y.device
-        self.dx = self.dw = self.db = self.ws = None
+        # zeros, and here: the first backward may add to them, in a captured graph too
+        self.dw = torch.zeros(self.d, dtype=torch.float32, device=device)
+        self.db = torch.zeros_like(self.dw) if self.bias else None
+        self.dx = self.ws = None
         self.ws_bytes = 0
 
     def _check(self, name, t, shape, dtype):
@@ -301,9 +305,6 @@ class LayerNorm:
         self._check("rstd", rstd, (self.T,), torch.float32)
         if self.ws is None:
             self.dx = torch.empty_like(self.y)
-            # zeros: the first backward may add to them
-            self.dw = torch.zeros(self.d, dtype=torch.float32, device=self.device)
-            self.db = torch.zeros_like(self.dw) if self.bias else None
             self.ws_bytes = B.moe_layernorm_bwd_workspace_size(self.T, self.d, self.dt)
             self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
         B.moe_layernorm_bwd(dy, x, weight, mean, rstd, self.dt, self.T, self.d, dres, self.dx,
@@ -338,7 +339,14 @@ class PreNormMoELayer:
 def _mx_cols(x):
     if not isinstance(x, torch.Tensor) or x.dim() < 2:
         raise ValueError("MXFP4 takes tensors of rows: [..., rows, cols]")
+    if x.shape[-1] and x.numel() // x.shape[-1] >= 1 << 31:
+        raise ValueError("MXFP4 takes fewer than 2^31 rows")
     return x.shape[-1]
+
+
+def _one(n_rows):
+    """The shape that a tensor of one value has: (1,), or () as it is."""
+    return () if isinstance(n_rows, torch.Tensor) and n_rows.dim() == 0 else (1,)
 
 
 def mxfp4_quantize(x, out=None, n_rows=None, stream=None):
@@ -358,7 +366,7 @@ def mxfp4_quantize(x, out=None, n_rows=None, stream=None):
     _check_tensor("scales", scales, (*x.shape[:-1], B.moe_mxfp4_scale_stride(cols)), torch.uint8,
                   x.device, "tensor")
     if n_rows is not None:
-        _check_tensor("n_rows", n_rows, n_rows.shape, torch.int32, x.device, "tensor")
+        _check_tensor("n_rows", n_rows, _one(n_rows), torch.int32, x.device, "tensor")
     B.moe_mxfp4_quantize(x, B.dtype_code(x), rows, cols, n_rows, codes, scales, stream)
     return out
 
@@ -375,7 +383,7 @@ def mxfp4_dequantize(codes, scales, dtype=torch.bfloat16, out=None, n_rows=None,
                   codes.device, "tensor")
     _check_tensor("out", out, (*codes.shape[:-1], cols), dtype, codes.device, "tensor")
     if n_rows is not None:
-        _check_tensor("n_rows", n_rows, n_rows.shape, torch.int32, codes.device, "tensor")
+        _check_tensor("n_rows", n_rows, _one(n_rows), torch.int32, codes.device, "tensor")
     B.moe_mxfp4_dequantize(codes, scales, B.dtype_code(out), rows, cols, n_rows, out, stream)
     return out
 
@@ -383,7 +391,8 @@ def mxfp4_dequantize(codes, scales, dtype=torch.bfloat16, out=None, n_rows=None,
 class MxFFN:
     """The grouped expert FFN in MXFP4 on up to ``cap`` dispatched rows: moe_mxfp4_quantize of
     the rows, then moe_mxfp4_ffn_fwd on weights given once as (codes, scales) pairs of
-    ``mxfp4_quantize``: ``w_gate_up`` of [E_r, 2H (SiLU: H), d], ``w_down`` of [E_r, d, H]."""
+    ``mxfp4_quantize``: ``w_gate_up`` of [E_r, 2H (SiLU: H), d], ``w_down`` of [E_r, d, H].
+    Its buffers are reused by the next call: calls on different streams need one each."""
 
     def __init__(self, cap, w_gate_up, w_down, expert="swiglu"):
         (gu, gu_s), (dn, dn_s) = w_gate_up, w_down
@@ -430,8 +439,8 @@ class InferenceMoELayer:
     seen): ``w_gate_up`` [E_r, 2H, d] and ``w_down`` [E_r, d, H] (SiLU experts: [E_r, H, d]) of
     the router's dtype, or each a (codes, scales) pair of ``mxfp4_quantize``; the shared
     experts' likewise, [1, ...].  ``few`` takes up to 64 tokens; the outputs of its last call
-    are y, logits, topk_idx, topk_w and topk_local, in buffers that the next call reuses (two
-    calls on different streams need a layer each)."""
+    are y, logits, topk_idx, topk_w and topk_local, in buffers that the next call reuses, whatever
+    its number of tokens (two calls on different streams need a layer each)."""
 
     MAX_TOKENS = 64
 
@@ -494,23 +503,29 @@ class InferenceMoELayer:
             w_down_scales=p(dn_s), shared_gate_up_scales=p(sgu_s), shared_down_scales=p(sd_s))
         self.y = self.logits = self.topk_idx = self.topk_w = self.topk_local = self._ws = None
 
+    def _buffers(self):
+        """Outputs and workspace for the most tokens (the workspace grows with them)."""
+        f, N = self._few, self.MAX_TOKENS
+        new = lambda n, dt: torch.empty(N, n, dtype=dt, device=self.device)
+        self._out = dict(y=new(self.d, self.dtype), logits=new(self.E, torch.float32),
+                         topk_w=new(self.k, torch.float32), topk_idx=new(self.k, torch.int32),
+                         topk_local=new(self.k, torch.int32))
+        f.T = N
+        for name, t in self._out.items():
+            setattr(f, name, t.data_ptr())
+        f.ws_bytes = B.moe_few_fwd_workspace_size(f)
+        self._ws = torch.empty(max(f.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+        f.ws = self._ws.data_ptr()
+
     def _size(self, T):
-        """Buffers and arguments for T tokens (kept until T changes)."""
+        """Outputs of T tokens."""
         if not 0 <= T <= self.MAX_TOKENS:
             raise ValueError(f"few takes up to {self.MAX_TOKENS} tokens, got {T}")
-        f, dev = self._few, self.device
-        self.y = torch.empty(T, self.d, dtype=self.dtype, device=dev)
-        self.logits = torch.empty(T, self.E, dtype=torch.float32, device=dev)
-        self.topk_w = torch.empty(T, self.k, dtype=torch.float32, device=dev)
-        self.topk_idx, self.topk_local = (torch.empty(T, self.k, dtype=torch.int32, device=dev)
-                                          for _ in range(2))
-        f.T = T
-        for name in ("y", "logits", "topk_w", "topk_idx", "topk_local"):
-            setattr(f, name, getattr(self, name).data_ptr())
-        f.ws_bytes = B.moe_few_fwd_workspace_size(f)
-        self._ws = torch.empty(max(f.ws_bytes, 1), dtype=torch.uint8, device=dev)
-        f.ws = self._ws.data_ptr()
-        self.T = T
+        if self._ws is None:
+            self._buffers()
+        for name, t in self._out.items():
+            setattr(self, name, t[:T])
+        self.T = self._few.T = T
 
     def few(self, x, stream=None):
         """y [T, d] of up to 64 tokens x [T, d], by moe_few_fwd."""

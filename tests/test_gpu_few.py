@@ -236,6 +236,50 @@ def test_few_graph_streams_and_two_at_once(gpu_lib, mx):
 
 
 @pytest.mark.gpu
+def test_few_graph_outlives_other_sizes(gpu_lib):
+    """A captured call of 5 tokens, replayed after eager calls of more and fewer and after other
+    tensors were made and dropped."""
+    c = case(5, 192, 16, 8, 2, 128, 64)
+    L = build(c, make(c, 4))
+    x = torch.randn(5, 192, device="cuda").to(torch.bfloat16)
+    ref = L.few(x).clone()
+    L.few(x)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = L.few(x)
+    for T in (64, 1, 33, 5):
+        more = torch.randn(T, 192, device="cuda").to(torch.bfloat16)
+        more[:min(T, 5)] = x[:T]
+        got = L.few(more)
+        junk = [torch.full((1 << 18,), 3.0, device="cuda") for _ in range(8)]
+        assert torch.isfinite(got).all() and L.topk_idx.shape == (T, 2)
+        assert T != 5 or torch.equal(got, ref)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref) and all((j == 3.0).all() for j in junk)
+
+
+@pytest.mark.gpu
+def test_few_infinities_in_a_cut_step(gpu_lib):
+    """MXFP4 widths that are no multiple of a step: an infinity is multiplied by its own weights
+    alone.  Weights of ones (and gates of 1): the sums are infinite, no NaN; the other token
+    stays as it is."""
+    for d, H in ((64, 64), (320, 192), (448, 64)):
+        q = lambda *s: mxfp4_quantize(torch.ones(*s, dtype=torch.bfloat16, device="cuda"))
+        L = InferenceMoELayer(1, np.array([1]), torch.ones(1, d, dtype=torch.bfloat16, device="cuda"),
+                              q(1, 2 * H, d), q(1, d, H), gate="sigmoid")
+        x = torch.ones(2, d, dtype=torch.bfloat16, device="cuda")
+        clean = L.few(x).clone()
+        for at in range(0, d, 8):
+            x[0] = 1.0
+            x[0, at + at // 8 % 8] = float("inf")
+            y = L.few(x)
+            assert torch.equal(y[1], clean[1])
+            assert L.topk_w[0].item() == 1 and (y[0] == float("inf")).all(), (d, H, at)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_few_agrees_with_the_training_layer(gpu_lib, dtype):
     """Behind the pre-norm, on the same weights: the training layer's forward, whose routes it

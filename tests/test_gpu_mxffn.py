@@ -105,6 +105,29 @@ def test_mxffn_matches_64_bits(gpu_lib, sizes, d, H, expert):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,H,expert", [(2112, 576, "swiglu"), (2048, 1088, "silu"), (512, 64, "swiglu"),
+                                        (4160, 512, "silu"), (2304, 1216, "swiglu")])
+def test_mxffn_large_tiles(gpu_lib, d, H, expert):
+    """Room for so many rows that the large tiles are taken, and few of them there (the others
+    NaN): ragged groups, cut and whole last steps of the reduction, one step and many."""
+    sizes = [300, 0, 401, 1, 257]
+    print("[mxffn]", sizes, d, H, expert, flush=True)
+    x, off, gu, dn = make(sizes, d, H, expert)
+    n, cap = sum(sizes), 33000
+    L = MxFFN(cap, gu, dn, expert=expert)
+    L.y.fill_(7.0)
+    L.ws.fill_(0xFF)
+    room = torch.full((cap, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    room[:n] = x
+    y = L.forward(room, off)
+    ref, tol = reference(x, sizes, gu, dn, expert)
+    assert torch.isfinite(y[:n]).all()
+    over = ((y[:n].double() - ref).abs() - tol).max().item()
+    assert over <= 0, f"{over:.3e} past its bound"
+    assert (y[n:] == 7).all()
+
+
+@pytest.mark.gpu
 def test_mxffn_offsets_out_of_range_and_empty(gpu_lib):
     """Groups are clamped to [0, cap]; no groups or no rows write nothing."""
     x, off, gu, dn = make([20, 30, 14], 128, 64)
@@ -204,7 +227,7 @@ def test_mxffn_refusals():
     assert B.lib().moe_mxfp4_ffn_fwd(None, None) == -1
     for kw in (dict(d=96), dict(H=32), dict(n_groups=257), dict(cap=1 << 22, d=4096), dict(x=p + 8),
                dict(y=p + 4), dict(x_scales=p + 2), dict(w_down_scales=p + 1), dict(ws=p + 16),
-               dict(n_groups=256, H=8192, d=4096)):
+               dict(n_groups=256, H=8192, d=4096), dict(cap=1, n_groups=16, H=1 << 30, d=1 << 30)):
         kw = dict(kw, ws_bytes=1 << 40)
         assert f(**kw) == -2, kw
     for kw in (dict(cap=-1), dict(n_groups=-1), dict(d=0), dict(H=0), dict(activation=2), dict(offsets=None),

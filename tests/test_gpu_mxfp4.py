@@ -119,6 +119,20 @@ def test_rows_past_the_device_count(gpu_lib, n):
 
 
 @pytest.mark.gpu
+def test_count_of_rows_is_one_value(gpu_lib):
+    x = torch.randn(4, 64, device="cuda")
+    one = torch.tensor(2, dtype=torch.int32, device="cuda")
+    pair = mxfp4_quantize(x, n_rows=one)
+    mxfp4_dequantize(*pair, n_rows=one)
+    for bad in (torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"),
+                torch.zeros(1, dtype=torch.int32), 3):
+        with pytest.raises(ValueError):
+            mxfp4_quantize(x, n_rows=bad)
+        with pytest.raises(ValueError):
+            mxfp4_dequantize(*pair, n_rows=bad)
+
+
+@pytest.mark.gpu
 def test_round_trip_keeps_its_values_and_replays(gpu_lib):
     """Values of the format come back as they are; a captured pass follows its input."""
     x = torch.randn(64, 256, device="cuda")

@@ -96,6 +96,56 @@ def test_norm_matches_64_bits(gpu_lib, T, d, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,d,dtype", [(4096, 8, "bf16"), (4097, 520, "bf16"), (4099, 1024, "bf16"),
+                                       (4100, 2040, "bf16"), (4096, 256, "f32"), (5003, 264, "f32"),
+                                       (4098, 520, "f32"), (4101, 1024, "f32")])
+def test_norm_a_row_per_wave(gpu_lib, T, d, dtype):
+    """Many rows: one wave each (at most 4 rows of a wave, 4 waves, 512 partials by 64 shares)."""
+    test_norm_matches_64_bits(gpu_lib, T, d, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_equal_and_huge(gpu_lib, dtype):
+    """Rows of one value whose multiple by rstd overflows: x - mean is zero, and the lanes past
+    the row's end (x zero there, the mean not) must not make it NaN.  The sums of 8 terms
+    are exact for x (a power of two); for g they take at most 9 additions and two products."""
+    x = torch.full((6, 8), 2.0 ** 120, dtype=DT[dtype], device="cuda")
+    t = inputs(6, 8, dtype, seed=3)
+    N = LayerNorm(6, 8, dtype=DT[dtype])
+    N.forward(x, t["w"], t["b"])
+    assert (N.mean == 2.0 ** 120).all()
+    N.backward(t["dy"], x, t["w"])
+    g = t["dy"].double() * t["w"].double()
+    ref = N.rstd.double()[:, None] * (g - g.mean(1, keepdim=True))
+    tol = 16 * U * N.rstd.double()[:, None] * (g.abs() + g.abs().mean(1, keepdim=True))
+    check("dx", N.dx, ref, (tol + half(dtype) * ref.abs()) * (1 + half(dtype)))
+    assert (N.dw == 0).all() and torch.isfinite(N.db).all()
+
+
+@pytest.mark.gpu
+def test_norm_first_backward_in_a_graph(gpu_lib):
+    """Its first backward captured, adding to dw: every replay adds."""
+    t = inputs(40, 256, "f32", seed=8)
+    M = LayerNorm(40, 256, dtype=torch.float32)
+    M.forward(t["x"], t["w"], t["b"])
+    M.backward(t["dy"], t["x"], t["w"])
+    N = LayerNorm(40, 256, dtype=torch.float32)
+    N.forward(t["x"], t["w"], t["b"])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        N.backward(t["dy"], t["x"], t["w"], accumulate_dw=1)
+    for i in range(1, 5):
+        g.replay()
+        torch.cuda.synchronize()
+        # (i sums of equal parts: one rounding each)
+        assert ((N.dw - i * M.dw).abs() <= i * i * U * M.dw.abs()).all()
+        assert ((N.db - i * M.db).abs() <= i * i * U * M.db.abs()).all()
+        assert torch.equal(N.dx, M.dx)
+
+
+@pytest.mark.gpu
 def test_norm_against_differences(gpu_lib):
     """The gradients of L = sum(y * dy) against central differences of the 64-bit forward: step
     e = 1e-5 leaves a relative error of order e^2, far under the 1e-4 allowed to fp32."""
@@ -259,6 +309,8 @@ def test_norm_refusals():
     assert fwd(eps=float("nan")) == -1 and fwd(eps=-1.0) == -1 and fwd(y=None) == -1 and fwd(r=None) == -1
     need = B.moe_layernorm_bwd_workspace_size(4, 64, B.MOE_BF16)
     assert need >= 2 * 64 * 4 and B.moe_layernorm_bwd_workspace_size(-1, 64, 0) == 0
+    assert B.moe_layernorm_bwd_workspace_size(4, 2 ** 31 - 1, 0) == 0  # (sizes that are refused)
+    assert B.moe_layernorm_bwd_workspace_size(4, 60, 0) == 0 and fwd(T=1 << 30) == -2
 
     def bwd(dy=p, x=p, w=p, m=p, r=p, dt=B.MOE_BF16, T=4, d=64, res=None, dx=p, dw=p, db=p, ws=p, n=need):
         return L.moe_layernorm_bwd(dy, x, w, m, r, dt, T, d, res, dx, dw, db, 0, ws, n, None)
