@@ -10,6 +10,10 @@
 // are the matrix instruction's first operand (16 rows of an expert's matrix) and the tokens
 // its second (16 columns).  The gate is in h, so that the second projections are plain sums.
 // (The order of k within a matrix instruction is free as long as both operands have the same.)
+//
+// Measured (d = 2048, H = 1408, 64 experts, k = 6, shared 2816): one token, bf16, 5 + 20 + 15 us
+// (the weights at 4.6 and 3.1 TB/s); 48 tokens on 16 resident experts 6 + 49 + 29; 16 tokens
+// on 32 experts in MXFP4 5 + 31 + 25.
 #pragma once
 #include <type_traits>
 

@@ -17,7 +17,12 @@
 //
 // A k-step is 2 NJ chunks of MI products; a chunk's columns are read four chunks ahead.  Four
 // chunks before its end all of the stage has been read: the wave waits for the next
-// stage's DMA, takes the barrier (this stage is free, the next is whole) and refills it.  A tile's first two stages are issued before the previous tile's epilogue.
+// stage's DMA, takes the barrier (this stage is free, the next is whole) and refills it.
+// A tile's first two stages are issued before the previous tile's epilogue.
+//
+// Measured (65536 rows in 32 groups, d = 4096, H = 2048): first projection 670 us, second 393:
+// 3.3 and 2.8 PFLOP/s.  The matrix units are busy 40 % of the time at the 1.8 GHz that their
+// power leaves, the LDS pipe about 70 %; a k-step takes 2.1 us, a tile's epilogue 7.
 #include "gemm.h"
 #include "kernels.h"
 #include "mx.h"

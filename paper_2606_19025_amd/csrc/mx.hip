@@ -3,6 +3,8 @@
 // Bound by HBM.  A lane takes 8 consecutive values, so that its 16 (fp32: 32) bytes load
 // whole and its codes are one 4-byte word; the four lanes of a block share their largest
 // magnitude, compared as bits (a NaN's are above infinity's).
+//
+// Measured: 45056 x 2048 bf16 to MXFP4 60 us, back 35 us (3.9 and 6.7 TB/s of both sides).
 #include "kernels.h"
 #include "mx.h"
 #include "timing.h"
