@@ -20,9 +20,10 @@
 // stage's DMA, takes the barrier (this stage is free, the next is whole) and refills it.
 // A tile's first two stages are issued before the previous tile's epilogue.
 //
-// Measured (65536 rows in 32 groups, d = 4096, H = 2048): first projection 670 us, second 393:
-// 3.3 and 2.8 PFLOP/s.  The matrix units are busy 40 % of the time at the 1.8 GHz that their
-// power leaves, the LDS pipe about 70 %; a k-step takes 2.1 us, a tile's epilogue 7.
+// Measured (65536 rows in 32 groups, d = 4096, H = 2048): first projection 635 us, second 390:
+// 3.5 and 2.8 PFLOP/s, by the clock that power leaves (1.8 GHz; a single call 595 and 380).
+// Before the last two steps the matrix units were busy 40 % of the time, the LDS pipe about
+// 70 %; a k-step took 2.1 us, a tile's epilogue 7.
 #include "gemm.h"
 #include "kernels.h"
 #include "mx.h"
@@ -145,20 +146,24 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
   static_assert(NW % 2 == 0, "pieces 16 rows apart");
   unsigned oa[T::PA], ob[T::PB], os;
   const int chunk = (lane & 7) ^ (((wave * 8 + (lane >> 3)) >> 1) & 7);
+  // (its lane index passes through an asm: kept from tile to tile, parts of the offsets went
+  // through scratch memory, and each reload waited for the loads issued before it)
   auto aim = [&](const Where& w) {
+    int al = lane;
+    asm volatile("" : "+v"(al));
 #pragma unroll
     for (int i = 0; i < T::PA; ++i) {
-      const int r = (i * NW + wave) * 8 + (lane >> 3);
-      oa[i] = (unsigned)min(w.row0 + r, w.row1 - 1) * line + chunk * 16;
+      const int r = (i * NW + wave) * 8 + (al >> 3);
+      oa[i] = (unsigned)min(w.row0 + r, w.row1 - 1) * line + ((al & 7) ^ (((wave * 8 + (al >> 3)) >> 1) & 7)) * 16;
     }
     const unsigned bg = (unsigned)w.g * (unsigned)p.N;
 #pragma unroll
     for (int i = 0; i < T::PB; ++i) {
-      const int r = (i * NW + wave) * 8 + (lane >> 3);
-      ob[i] = (bg + (unsigned)b_row(w.n0, r)) * line + chunk * 16;
+      const int r = (i * NW + wave) * 8 + (al >> 3);
+      ob[i] = (bg + (unsigned)b_row(w.n0, r)) * line + ((al & 7) ^ (((wave * 8 + (al >> 3)) >> 1) & 7)) * 16;
     }
     // scales: 64 rows of A, then of B, by wave
-    const int r = wave * 64 + lane;
+    const int r = wave * 64 + al;
     os = wave >= T::SP ? kPast : (r < T::BM ? (unsigned)min(w.row0 + r, w.row1 - 1) : bg + (unsigned)b_row(w.n0, r - T::BM)) * sline;
   };
   // Part q of 4 of a k-step's loads; even k-steps bring the scales of two, 16 bytes of a row
@@ -184,39 +189,32 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
       for (int q = 0; q < 4; ++q) issue_part(1, std::false_type{}, q);
   };
 
-  // Operands: the wave's rows of one k128 half, and the columns of one chunk (a half's j), with
-  // their words of four scales (shifted to the lane's own where they are used: sooner
-  // would wait for the read).
-  struct Rows {
-    u32x4_t v[MI];
-    unsigned s[MI];
-  };
-  struct Col {
-    u32x4_t v;
-    unsigned s;
-  };
+  // Operands: the wave's rows of one k128 half, and the columns of one chunk (a half's j).
+  // Scales: the words of both halves, read once a k-step, of which a lane's own bytes are
+  // packed where they are first used (sooner would wait for the read); the instruction
+  // picks the half's byte.
+  struct Rows { u32x4_t v[MI]; };
+  u32x2_t raw_a[MI], raw_b[4];
+  unsigned sa[MI], sb[NJ];
   // a tile's rows are 16 apart: its place in a stage is the first one's plus 2048 bytes each
   // (the other half's chunk is 64 bytes further or back), 256 bytes of scales
-  const unsigned place = l16 * 128 + ((q4 ^ ((l16 >> 1) & 7)) << 4), sh = 8 * q4;
+  const unsigned place = l16 * 128 + ((q4 ^ ((l16 >> 1) & 7)) << 4), pick = q4 | (4 + q4) << 8;
   const unsigned rows_at = wr * MI * 2048, cols_at = T::A_BYTES + wc * NJ * 2048;
   const unsigned rs_at = T::S_AT + wr * MI * 256 + l16 * 16, cs_at = T::S_AT + T::BM * 16 + wc * NJ * 256 + l16 * 16;
-  // word of a row's scales at a half of k-step kt
-  auto scales = [&](int kt, int half) { return lds + (kt >> 1 & 1) * T::S_STAGE + (kt & 1) * 8 + half * 4; };
-  // mask: zero for a word past the end of its row (the second one of a cut last k-step)
-  auto read_rows = [&](Rows& f, int kt, int half, unsigned mask = ~0u) {
-    const char* at = lds + (kt & 1) * T::STAGE;
-    const char* v = at + rows_at + (place ^ (half * 64));
-    const char* sc = scales(kt, half) + rs_at;
+  auto scales = [&](int kt) { return lds + (kt >> 1 & 1) * T::S_STAGE + (kt & 1) * 8; };
+  auto pack = [&](u32x2_t w) { return __builtin_amdgcn_perm(w[1], w[0], pick); };
+  auto read_rows = [&](Rows& f, int kt, int half) {
+    const char* v = lds + (kt & 1) * T::STAGE + rows_at + (place ^ (half * 64));
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      f.v[i] = *reinterpret_cast<const u32x4_t*>(v + i * 2048);
-      f.s[i] = *reinterpret_cast<const unsigned*>(sc + i * 256) & mask;
-    }
+    for (int i = 0; i < MI; ++i) f.v[i] = *reinterpret_cast<const u32x4_t*>(v + i * 2048);
   };
-  auto read_col = [&](Col& f, int kt, int half, int j, unsigned mask = ~0u) {
-    const char* at = lds + (kt & 1) * T::STAGE;
-    f.v = *reinterpret_cast<const u32x4_t*>(at + cols_at + (place ^ (half * 64)) + j * 2048);
-    f.s = *reinterpret_cast<const unsigned*>(scales(kt, half) + cs_at + j * 256) & mask;
+  auto read_row_scales = [&](int kt) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) raw_a[i] = *reinterpret_cast<const u32x2_t*>(scales(kt) + rs_at + i * 256);
+  };
+  auto read_col = [&](u32x4_t& f, int kt, int half, int j) {
+    f = *reinterpret_cast<const u32x4_t*>(lds + (kt & 1) * T::STAGE + cols_at + (place ^ (half * 64)) + j * 2048);
+    if (half == 0) raw_b[j % 4] = *reinterpret_cast<const u32x2_t*>(scales(kt) + cs_at + j * 256);
   };
   f32x4_t acc[MI][NJ];
   auto wide = [](u32x4_t v) {
@@ -224,18 +222,20 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
     return r;
   };
   // the weights are the first operand: a lane holds four consecutive columns of one row
-  auto mma = [&](const Rows& a, const Col& b, int j) {
+  auto mma = [&](const Rows& a, u32x4_t b, auto half, int j) {
+    constexpr int HALF = decltype(half)::value;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
-      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(b.v), wide(a.v[i]), acc[i][j], 4, 4, 0,
-                                                                   (int)(b.s >> sh), 0, (int)(a.s[i] >> sh));
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(b), wide(a.v[i]), acc[i][j], 4, 4, HALF,
+                                                                   (int)sb[j], HALF, (int)sa[i]);
   };
 
   if (tile >= t_end) return;
   Where w = decode(tile);
   aim(w);
   issue_first();
-  const unsigned past = p.K - (steps - 1) * 256 > 128 ? ~0u : 0u;
+  // the second word of a cut last k-step may be past the end of its row
+  const unsigned past = p.K - (steps - 1) * 256 > 128 ? ~0u : 0xFFu;
   for (;;) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -246,8 +246,9 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
     // 2 NJ chunks to a k-step, the columns of four of them in registers
     constexpr int C = 2 * NJ;
     Rows a0, a1;
-    Col b[4];
+    u32x4_t b[4];
     read_rows(a0, 0, 0);
+    read_row_scales(0);
 #pragma unroll
     for (int c = 0; c < 4; ++c) read_col(b[c], 0, 0, c);
     // (no branch inside a k-step: the compiler would move its products past it)
@@ -258,17 +259,25 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
           WAIT_LGKMCNT(0);
           WAIT_VMCNT(0);
           __syncthreads();  // this stage has been read, the next one is whole
-          if constexpr (decltype(next)::value) read_rows(a0, kt + 1, 0);
+          if constexpr (decltype(next)::value) {
+            read_rows(a0, kt + 1, 0);
+            read_row_scales(kt + 1);
+          }
         }
-        if (c == 1) {
-          if constexpr (decltype(next)::value) read_rows(a1, kt, 1);
-          else read_rows(a1, kt, 1, past);
+        const unsigned mask = decltype(next)::value ? ~0u : past;
+        if (c == 0) {
+#pragma unroll
+          for (int i = 0; i < MI; ++i) sa[i] = pack(raw_a[i]) & mask;
         }
-        mma(c < NJ ? a0 : a1, b[c % 4], c % NJ);
-        if (c + 4 < C) {
-          if (decltype(next)::value || c + 4 < NJ) read_col(b[c % 4], kt, (c + 4) / NJ, (c + 4) % NJ);
-          else read_col(b[c % 4], kt, 1, (c + 4) % NJ, past);
-        } else if constexpr (decltype(next)::value) read_col(b[c % 4], kt + 1, 0, c + 4 - C);
+        if (c == 1) read_rows(a1, kt, 1);
+        if (c < NJ) {
+          sb[c] = pack(raw_b[c % 4]) & mask;
+          mma(a0, b[c % 4], std::integral_constant<int, 0>{}, c);
+        } else {
+          mma(a1, b[c % 4], std::integral_constant<int, 1>{}, c - NJ);
+        }
+        if (c + 4 < C) read_col(b[c % 4], kt, (c + 4) / NJ, (c + 4) % NJ);
+        else if constexpr (decltype(next)::value) read_col(b[c % 4], kt + 1, 0, c + 4 - C);
         if constexpr (decltype(refill)::value)
           if (c >= C - 4) issue_part(kt + 2, even, c - (C - 4));
         __builtin_amdgcn_sched_barrier(0);  // (reads moved further ahead cost registers)
@@ -285,7 +294,7 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
     step(No{}, No{}, No{}, kt);
     // (the last products stay here: moved past the branch below, their operands went through
     // scratch memory and waited for the next tile's loads; 65536 rows, first projection 790
-    // us and now 680, second 465 and 398)
+    // us and then 680, second 465 and 398)
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -387,24 +396,21 @@ hipError_t mx_run(const MxGemmArgs& a, const char* name, hipStream_t s) {
 }
 
 // Large tiles read each operand fewer times, small ones fill the CUs sooner (two blocks on
-// each) and run one block's epilogue beside the other's products.  Large where the rows, all
-// there and spread evenly, give a CU a tile each; where the epilogue also multiplies,
-// quantises and scales (GU, UP): two tiles each and a reduction that is long beside it.
-// Measured (us, large / small; rows, groups, d, H):
+// each).  Large where the rows, all there and spread evenly, give every CU a tile.
+// Measured (us, large / small, and the large tiles; rows, groups, d, H):
 //                            first projection   second
-//   2048, 16, 2048, 1408       31 /  20          23 /  13
-//   4096,  8, 1024, 2816       43 /  32          27 /  16
-//   8192, 16, 2048, 1408       57 /  50          28 /  32
-//   16384, 8, 1024, 2816      122 / 106          36 /  44
-//   16384, 16, 2048, 1408      89 /  93          48 /  57
-//   16384, 32, 4096, 2048     204 / 282         117 / 162
-//   65536, 32, 4096, 2048     713 / 974         422 / 525
+//   2048, 16, 2048, 1408       24 /  20  176      18 /  13  128
+//   4096,  8, 1024, 2816       32 /  33  440      25 /  16   80
+//   8192,  4, 1024, 2816       45 /  59  748      25 /  25  136
+//   8192,  8, 4096, 1024       41 /  61  288      33 /  38  576
+//   8192, 16, 2048, 1408       44 /  50  440      23 /  32  320
+//   16384, 8, 1024, 2816       85 / 113 1496      31 /  46  272
+//   65536, 32, 4096, 2048     595 / 974 4352     380 / 529 4352
 template <int KIND>
 hipError_t mx_launch(const MxGemmArgs& a, const char* name, hipStream_t s) {
   const int64_t tiles =
       (int64_t)(a.g.cap / MxLarge::BM + (a.g.n_groups + 1) / 2) * ceil_div(a.N, MxLarge::BN);
-  const bool large = KIND == MX_DOWN ? tiles >= num_cus() : tiles >= 2 * num_cus() && a.K >= 2048;
-  return large ? mx_run<KIND, MxLarge>(a, name, s) : mx_run<KIND, MxSmall>(a, name, s);
+  return tiles >= num_cus() ? mx_run<KIND, MxLarge>(a, name, s) : mx_run<KIND, MxSmall>(a, name, s);
 }
 
 }  // namespace
