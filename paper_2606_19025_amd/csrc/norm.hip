@@ -321,10 +321,14 @@ int bwd_blocks(int T, int d, int ve) {
   return std::min(std::max(std::min(units, num_cus()), ceil_div(T, 4)), std::min(units, 2 * num_cus()));
 }
 
+// Rows of one launch: a grid dimension holds less than 2^32 threads (a larger one is not refused
+// but taken modulo 2^32), so that more rows are taken by several launches.  A power of two.
+constexpr int rows_per_launch(int W) { return (int)((int64_t(1) << 31) / (64 * W)); }
+
 template <class E>
-hipError_t fwd(const NormArgs& a, hipStream_t s) {
+void fwd_rows(const NormArgs& a, int W, hipStream_t s) {
   constexpr int VE = Vec16<E>::N;
-  const int W = row_waves_fwd(a.T, a.d, VE), nv = vectors(a.d, VE, W);
+  const int nv = vectors(a.d, VE, W);
 #define NORM_FWD(W_, NV_)                                                                 \
   MOE_TIMED("norm_fwd", s, norm_fwd_kernel<E, W_, NV_>                                    \
             <<<ceil_div(a.T, block_waves(W_) / W_), 64 * block_waves(W_), 0, s>>>(a))
@@ -342,7 +346,22 @@ hipError_t fwd(const NormArgs& a, hipStream_t s) {
     else NORM_FWD(16, 4);
   }
 #undef NORM_FWD
-  return hipGetLastError();
+}
+
+template <class E>
+hipError_t fwd(const NormArgs& a, hipStream_t s) {
+  const int W = row_waves_fwd(a.T, a.d, Vec16<E>::N), most = rows_per_launch(W);
+  for (int t = 0; t < a.T; t += most) {
+    NormArgs part = a;
+    part.x = static_cast<const E*>(a.x) + (size_t)t * a.d;
+    part.y = static_cast<E*>(a.y) + (size_t)t * a.d;
+    part.mean = a.mean + t;
+    part.rstd = a.rstd + t;
+    part.T = std::min(a.T - t, most);
+    fwd_rows<E>(part, W, s);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <class E, bool RES>

@@ -105,6 +105,33 @@ def test_norm_a_row_per_wave(gpu_lib, T, d, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,d", [((1 << 26) + 5, 8), ((1 << 24) + 3, 2056), ((1 << 22) + 1, 8200)])
+def test_norm_more_rows_than_a_grid(gpu_lib, T, d):
+    """Rows of one, four and sixteen waves, more of them than a launch's 2^32 threads hold, in
+    place: every row is written, and those around the launches' borders are right."""
+    if torch.cuda.mem_get_info()[0] < 2 * T * d + 12 * T + (4 << 30):
+        pytest.skip("not enough free memory")
+    print(f"[norm] T={T} d={d}", flush=True)
+    t = inputs(64, d, "bf16", seed=T + d)
+    x = torch.empty(T, d, dtype=torch.bfloat16, device="cuda")
+    x[: T // 64 * 64].view(-1, 64, d)[:] = t["x"]
+    x[T // 64 * 64:] = t["x"][: T % 64]
+    mean, rstd = torch.full((2, T), float("nan"), device="cuda")
+    B.moe_layernorm_fwd(x, t["w"], t["b"], B.MOE_BF16, T, d, 1e-5, x, mean, rstd)
+    check_forward(t["x"], t["w"], t["b"], 1e-5, x[:64], mean[:64], rstd[:64], half("bf16"))
+    for v in (mean, rstd):  # the same rows again and again
+        assert torch.equal(v[: T // 64 * 64].view(-1, 64), v[:64].expand(T // 64, 64))
+        assert torch.equal(v[T // 64 * 64:], v[: T % 64])
+    step = max(1, (1 << 28) // (64 * d))  # (in parts: a comparison of all needs as many bytes again)
+    for lo in range(0, T // 64, step):
+        hi = min(T // 64, lo + step)
+        assert (x[64 * lo:64 * hi].view(-1, 64, d) == x[:64]).all(), lo
+    assert torch.equal(x[T // 64 * 64:], x[: T % 64])
+    del x, mean, rstd
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_norm_equal_and_huge(gpu_lib, dtype):
     """Rows of one value whose multiple by rstd overflows: x - mean is zero, and the lanes past
