@@ -399,7 +399,7 @@ int moe_layernorm_bwd(const void* dy, const void* x, const float* weight, const 
  * x [rows, cols] dtype.  n_rows: device int32, only the first *n_rows rows are
  * converted and the others left as they are (rows that a dispatch has filled:
  * offsets + n_groups); NULL converts all.
- * Limits: cols % 32 == 0, rows >= 0, rows * cols / 8 below 2^40; x and codes 16-byte aligned.
+ * Limits: cols % 32 == 0, rows >= 0, rows * cols <= 2^37 - 2^13; x and codes 16-byte aligned.
  */
 int moe_mxfp4_scale_stride(int cols);
 int moe_mxfp4_quantize(const void* x, int dtype, int rows, int cols, const int32_t* n_rows,

@@ -528,7 +528,7 @@ int check_mx(int dtype, int rows, int cols, const void* x, const uint8_t* codes,
   if ((r = check_dtype(dtype)) != MOE_OK) return r;
   REQUIRE(rows >= 0 && cols >= 1, "bad sizes rows = %d, cols = %d", rows, cols);
   SUPPORT(cols % moe::MX_BLOCK == 0, "cols = %d must be a multiple of 32", cols);
-  SUPPORT((int64_t)rows * (cols / 8) < (int64_t)1 << 40, "rows = %d of cols = %d are too many", rows,
+  SUPPORT((int64_t)rows * (cols / 8) <= moe::kMxWords, "rows = %d of cols = %d are too many", rows,
           cols);
   REQUIRE(rows == 0 || (x && codes && scales), "x, codes and scales must not be NULL");
   SUPPORT(aligned16(x) && aligned16(codes), "x and codes must be 16-byte aligned");

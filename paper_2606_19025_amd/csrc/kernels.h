@@ -123,6 +123,9 @@ size_t mx_ffn_ws_bytes(int cap, int H);
 hipError_t launch_mx_ffn(const moe_mxfp4_ffn* f, hipStream_t s);
 
 // MXFP4 rows (mx.hip); n_rows: device count of the rows to convert, or NULL (all).
+// kMxWords: words of eight codes at most.  A block of 256 threads takes 1024, and a grid holds less
+// than 2^32 threads (a larger one is not refused but taken modulo 2^32).
+constexpr int64_t kMxWords = ((int64_t(1) << 24) - 1) * 1024;
 hipError_t launch_mx_quantize(const void* x, int bf16, int rows, int cols, const int32_t* n_rows,
                               uint8_t* codes, uint8_t* scales, hipStream_t s);
 hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int bf16, int rows,

@@ -109,6 +109,8 @@ __global__ __launch_bounds__(MX_THREADS) void mx_dequantize_kernel(const uint8_t
   }
 }
 
+static_assert((kMxWords / (MX_THREADS * MX_UNITS) + 1) * MX_THREADS <= int64_t(1) << 32, "a grid holds every word");
+
 MxArgs mx_args(int rows, int cols, const int32_t* n_rows) {
   MxArgs a;
   a.per_row = cols / 8;

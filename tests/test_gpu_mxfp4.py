@@ -168,6 +168,19 @@ def test_mx_refusals():
             mxfp4_quantize(bad)
 
 
+def test_mx_more_words_than_a_grid():
+    """A grid holds fewer than 2^32 threads of four words each: past that the call is refused (with
+    an unaligned x, whose check comes later and ends the calls that may go on here)."""
+    if torch.cuda.device_count() > 0:
+        pytest.skip("host-only rejection test: runs where no GPU is visible")
+    L, p = B.lib(), 256  # a fake, never dereferenced address
+    for rows, cols, many in ((2 ** 22 - 1, 2 ** 15, False), (2 ** 24 - 1, 2 ** 13, False), (2 ** 22, 2 ** 15, True),
+                             (2 ** 24, 2 ** 13, True), (2 ** 31 - 1, 32, False), (2 ** 31 - 1, 64, True)):
+        for r in (L.moe_mxfp4_quantize(p + 4, B.MOE_BF16, rows, cols, None, p, p, None),
+                  L.moe_mxfp4_dequantize(p, p, B.MOE_BF16, rows, cols, None, p + 4, None)):
+            assert r == -2 and ("too many" in B.moe_last_error()) == many, (rows, cols, B.moe_last_error())
+
+
 def test_the_oracle_of_these_tests():
     """By hand: 5 is a tie (4 and 6: the even code, 4), 7.9 saturates, the scale is 2^(2 - 2)."""
     x = np.zeros((1, 32))
