@@ -587,7 +587,7 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
   typedef typename CS::Few Few;
   typedef typename CS::More More;
   typedef typename CS::All All;
-  const int n_s = a.Hs / 16 * All::PASS, n_r = a.H / 16;
+  const int n_s = a.Hs / 16 * (a.T <= Few::CT ? Few::PASS : All::PASS), n_r = a.H / 16;
   // the first of this block's numbers from `from` on
   auto next = [&](int from) {
     const int m = (from - me) % all;

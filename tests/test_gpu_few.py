@@ -301,6 +301,44 @@ def test_few_agrees_with_the_training_layer(gpu_lib, dtype):
     assert ((L.y.double() - y.double()).abs() <= 2 * tol + 2 * h * scale).all()
 
 
+def kernel_us(L, x, name, n=10):
+    """The least of n times of one kernel of a call, us."""
+    L.few(x)
+    torch.cuda.synchronize()
+    best = float("inf")
+    for _ in range(n):
+        B.moe_timing_enable(8)
+        try:
+            L.few(x)
+            torch.cuda.synchronize()
+            best = min(best, B.moe_timing_collect()[name][1] * 1e3)
+        finally:
+            B.moe_timing_enable(0)
+    return best
+
+
+def shared_only(dtype="bf16", mx=False, d=1024, Hs=1 << 16):
+    """A layer of shared experts alone, so large (100 MB in 4 bits) that reading them
+    is all of its time."""
+    dt = DT[dtype]
+    q = mxfp4_quantize if mx else lambda w: w
+    w = lambda *s: q(torch.full(s, 0.5, dtype=dt, device="cuda"))
+    none = lambda *s: q(torch.empty(0, *s, dtype=dt, device="cuda"))
+    return InferenceMoELayer(1, np.array([0]), torch.ones(1, d, dtype=dt, device="cuda"), none(128, d), none(d, 64),
+                             shared_gate_up=w(1, 2 * Hs, d), shared_down=w(1, d, Hs))
+
+
+@pytest.mark.gpu
+def test_few_shared_items_once(gpu_lib):
+    """Four tokens' shared first projections from MXFP4 are made once: 16 tokens read the weights
+    twice, four of them once, in little more than half of the time (made twice, in all of it)."""
+    L = shared_only(mx=True)
+    x = torch.ones(16, 1024, dtype=torch.bfloat16, device="cuda")
+    few, more = kernel_us(L, x[:4], "few_gu"), kernel_us(L, x, "few_gu")
+    print(f"[few] 4 tokens {few:.1f} us, 16 {more:.1f}", flush=True)
+    assert few < 0.8 * more
+
+
 def _few(**kw):
     p = 256  # a fake, never dereferenced address
     a = dict(dtype=B.MOE_BF16, weights=0, activation=0, gate=0, T=4, d=128, E=8, k=2, E_r=4, H=64, Hs=64,
