@@ -445,7 +445,9 @@ int moe_mxfp4_ffn_fwd(const moe_mxfp4_ffn* f, hipStream_t stream);
 /*
  * The whole layer's forward for a few tokens (evaluation on a handful of tokens,
  * generation), where moe_layer_fwd's time is that of its many launches and of
- * rows that it moves: three launches, each active expert's weights read once.
+ * rows that it moves: three launches, each active expert's weights read once or, for the
+ * shared experts and for those that many of the tokens are routed to, a few times
+ * (MOE_W_MXFP4: once per 8 tokens; MOE_W_PLAIN: twice past 48 tokens in bf16, 32 in fp32).
  *
  *   the routing of moe_route_mask, bit for bit (logits, topk_idx, topk_w, topk_local)
  *   h[t,j,:] = s_j(x_t) act(Wgu_e x_t)         (e: the expert of the resident route j of t)

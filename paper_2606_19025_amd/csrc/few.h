@@ -4,7 +4,10 @@
 //   h_tj = s_tj act(Wgu_e x_t)                      for each resident route (t, j) to expert e
 //   y_t  = sum_j Wd_e h_tj + Wd_s act(Wgu_s x_t)    (s: the shared experts, gate 1)
 //
-// Bound by HBM: every active expert's weights are read once, for a handful of tokens each.
+// Bound by the weights' bytes: every active expert's are read once, for a handful of tokens each;
+// those of an expert with more tokens than a pass holds, and the shared experts', once per pass:
+// MXFP4 ceil(T / 8) passes past 8 tokens, bf16 two past 48 tokens, fp32 two past 32 (experts with
+// up to 16 tokens: one).  An expert's pass without tokens is not skipped.
 // Three launches: the logits (few_logits_*), the first projections (few_gu_kernel) and the
 // second ones with the sum over experts (few_down_kernel).  No rows are moved: the weights
 // are the matrix instruction's first operand (16 rows of an expert's matrix) and the tokens
@@ -397,12 +400,14 @@ struct Stream {
   }
 };
 
-// How a class of experts is taken: N tiles of XP DMA parts at a time, PASS times; COMPACT: the
-// expert's tokens moved to the front of one tile.  CT: columns of a tile that are used.
-template <class E, bool MX, int N_, int XP_, int PASS_, bool COMPACT_>
+// How a class of experts is taken: N tiles of XP DMA parts at a time; COMPACT: the expert's
+// tokens moved to the front of one tile, otherwise all T tokens in as many passes over the weights
+// as they need (most: MOST).  CT: columns of a tile that are used.
+template <class E, bool MX, int N_, int XP_, int MOST_, bool COMPACT_>
 struct Class {
-  static constexpr int N = N_, XP = XP_, PASS = PASS_, CT = XP_ * Piece<Fmt<E, MX>::XROW>::RPI;
+  static constexpr int N = N_, XP = XP_, MOST = MOST_, CT = XP_ * Piece<Fmt<E, MX>::XROW>::RPI;
   static constexpr bool COMPACT = COMPACT_;
+  DEVI static int passes(int T) { return MOST == 1 ? 1 : ceil_div(T, N * CT); }
 };
 // Few tokens, more in one compact tile, any number (in passes over the weights).
 template <class E, bool MX, int NT, int NP>
@@ -483,14 +488,14 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
   auto stream = [&](auto cl, bool shared, int first, int lo, int hi, auto&& between) {
     using C = decltype(cl);
     constexpr int N = C::N;
-    const int H = shared ? a.Hs : a.H, n_h = H / 16, per = n_h * C::PASS;
+    const int H = shared ? a.Hs : a.H, n_h = H / 16, per = n_h * C::passes(a.T);
     // an item's expert, first hidden unit and columns
     auto expert = [&](int it) {
       return shared ? 0 : __builtin_amdgcn_readfirstlane((int)tb.expert[first + it / per]);
     };
     auto cols = [&](int it, int r) {
       const int my = lane >= a.T ? -1 : shared ? lane : route_to(a, tb, lane, r);
-      return Cols<C>(my, C::PASS == 1 ? 0 : it % per / n_h);
+      return Cols<C>(my, C::MOST == 1 ? 0 : it % per / n_h);
     };
     if (!streams) {
       between();
@@ -587,7 +592,7 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
   typedef typename CS::Few Few;
   typedef typename CS::More More;
   typedef typename CS::All All;
-  const int n_s = a.Hs / 16 * (a.T <= Few::CT ? Few::PASS : All::PASS), n_r = a.H / 16;
+  const int n_s = a.Hs / 16 * (a.T <= Few::CT ? 1 : All::passes(a.T)), n_r = a.H / 16;
   // the first of this block's numbers from `from` on
   auto next = [&](int from) {
     const int m = (from - me) % all;
@@ -598,7 +603,7 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
   else stream(All{}, true, 0, me, n_s, tables);
   int from = n_s, first = 0;
   auto routed = [&](auto cl, int experts) {
-    const int n_i = experts * n_r * decltype(cl)::PASS;
+    const int n_i = experts * n_r * decltype(cl)::passes(a.T);
     stream(cl, false, first, next(from) - from, n_i, nothing);
     from += n_i;
     first += experts;
@@ -638,12 +643,12 @@ __global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
     few_active<CS::Few::CT, CS::More::CT>(a, tb);
   };
 
-  // The wave's share of the steps of `experts` experts (C::PASS passes over each).
+  // The wave's share of the steps of `experts` experts (`passes` over each).
   auto stream = [&](auto cl, bool shared, int first, int experts, auto&& between) {
     using C = decltype(cl);
     constexpr int N = C::N;
-    const int H = shared ? a.Hs : a.H, n_h = ceil_div(H, F::KS);
-    const int64_t all = (int64_t)experts * C::PASS * n_h;
+    const int H = shared ? a.Hs : a.H, n_h = ceil_div(H, F::KS), passes = C::passes(a.T);
+    const int64_t all = (int64_t)experts * passes * n_h;
     const int s_lo = (int)(all * wave / DW), s_hi = (int)(all * (wave + 1) / DW);
     const unsigned line = MX ? (unsigned)H / 2 : (unsigned)H * sizeof(E), sline = mx_stride(H);
     const char* W = static_cast<const char*>(shared ? a.sd : a.wd) + (size_t)blockIdx.x * RB * line;
@@ -652,13 +657,13 @@ __global__ __launch_bounds__(DT) void few_down_kernel(FewArgs a) {
     using ST = decltype(st);
     st.weights(line, RB);
     if constexpr (MX) st.soff = (unsigned)min(l16, RB - 1) * sline;
-    // pass v = expert * PASS + pass: its columns
+    // pass v = expert * passes + pass: its columns
     auto expert = [&](int v) {
-      return shared ? 0 : __builtin_amdgcn_readfirstlane((int)tb.expert[first + v / C::PASS]);
+      return shared ? 0 : __builtin_amdgcn_readfirstlane((int)tb.expert[first + v / passes]);
     };
     auto cols = [&](int v, int r) {
       const int my = lane >= a.T ? -1 : shared ? lane : route_to(a, tb, lane, r);
-      return Cols<C>(my, v % C::PASS);
+      return Cols<C>(my, v % passes);
     };
     // the step to load next: slot of the ring, pass, step in it
     int left = s_hi - s_lo, flying = 0, l_slot = 0, l_v = n_h ? s_lo / n_h : 0, l_s = s_lo - l_v * n_h;

@@ -339,6 +339,21 @@ def test_few_shared_items_once(gpu_lib):
     assert few < 0.8 * more
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,mx,T,more,passes,many", [("bf16", True, 8, 16, 1, 2), ("bf16", True, 24, 64, 3, 8),
+                                                         ("f32", False, 24, 64, 1, 2)])
+def test_few_passes_by_tokens(gpu_lib, dtype, mx, T, more, passes, many):
+    """Shared weights are read as often as the tokens need: T tokens' passes over them against
+    more tokens' (all readings made by both, whatever T, the times were the same).  The bound
+    lies halfway between the passes' ratio and one."""
+    L = shared_only(dtype, mx)
+    x = torch.ones(more, 1024, dtype=DT[dtype], device="cuda")
+    for name in ("few_gu", "few_down"):
+        few, all_ = kernel_us(L, x[:T], name), kernel_us(L, x, name)
+        print(f"[few] {name} {T} tokens {few:.1f} us, {more} {all_:.1f}", flush=True)
+        assert few < (1 + passes / many) / 2 * all_, name
+
+
 def _few(**kw):
     p = 256  # a fake, never dereferenced address
     a = dict(dtype=B.MOE_BF16, weights=0, activation=0, gate=0, T=4, d=128, E=8, k=2, E_r=4, H=64, Hs=64,
