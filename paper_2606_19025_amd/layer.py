@@ -18,6 +18,8 @@ points run with E := E_r and every expert resident.
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import binding as B
@@ -48,6 +50,16 @@ def _check_current(device, owner):
     if torch.cuda.current_device() != device.index:
         raise ValueError(f"the {owner} is on {device}, the current device is "
                          f"cuda:{torch.cuda.current_device()}")
+
+
+def _on(stream):
+    """Context in which torch allocates (and fills) on a call's stream: a buffer that the call makes
+    may be memory that the current stream still works on, or reuses when the buffer is dropped."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
 
 
 class ResidentMoELayer:
@@ -204,7 +216,8 @@ class ResidentMoELayer:
         sets = self._sets(x, w_gate_up, w_down, shared_gate_up, shared_down)
         if self.ws_fwd is None:
             self.ws_fwd_bytes = B.moe_grouped_ffn_fwd_workspace_size(sets, dt, d)
-            self.ws_fwd = self._alloc(max(self.ws_fwd_bytes, 1), dt=torch.uint8)
+            with _on(stream):
+                self.ws_fwd = self._alloc(max(self.ws_fwd_bytes, 1), dt=torch.uint8)
         if hook is None:
             B.moe_layer_fwd(self._step(sets, self.ws_fwd, self.ws_fwd_bytes, x, w_router,
                                        router_bias), stream)
@@ -234,7 +247,8 @@ class ResidentMoELayer:
         sets = self._sets(x, w_gate_up, w_down, shared_gate_up, shared_down, dy)
         if self.ws_ffn is None:
             self.ws_ffn_bytes = B.moe_grouped_ffn_bwd_workspace_size(sets, dt, d)
-            self.ws_ffn = self._alloc(self.ws_ffn_bytes, dt=torch.uint8)
+            with _on(stream):
+                self.ws_ffn = self._alloc(self.ws_ffn_bytes, dt=torch.uint8)
         if hook is None:
             B.moe_layer_bwd(self._step(sets, self.ws_ffn, self.ws_ffn_bytes, x, w_router, dy=dy,
                                        accumulate_dw=accumulate_dw), stream)
@@ -258,7 +272,8 @@ class ResidentMoELayer:
 class LayerNorm:
     """The layer's pre-norm over [T, d] activations: moe_layernorm_fwd / _bwd on buffers of its
     own (y, mean, rstd, dw, db; dx from the first backward on), which the next call reuses:
-    calls on different streams need a norm each."""
+    calls on different streams need a norm each.  A call on another stream than the one current
+    at construction, where dw and db are set to zero, has to be ordered behind it."""
 
     def __init__(self, T, d, dtype=torch.bfloat16, bias=True, eps=1e-5, device="cuda"):
         self.T, self.d, self.eps, self.bias = int(T), int(d), float(eps), bool(bias)
@@ -304,9 +319,10 @@ class LayerNorm:
         self._check("mean", mean, (self.T,), torch.float32)
         self._check("rstd", rstd, (self.T,), torch.float32)
         if self.ws is None:
-            self.dx = torch.empty_like(self.y)
             self.ws_bytes = B.moe_layernorm_bwd_workspace_size(self.T, self.d, self.dt)
-            self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+            with _on(stream):
+                self.dx = torch.empty_like(self.y)
+                self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
         B.moe_layernorm_bwd(dy, x, weight, mean, rstd, self.dt, self.T, self.d, dres, self.dx,
                             self.dw, self.db, accumulate_dw, self.ws, self.ws_bytes, stream)
         return self.dx
@@ -351,15 +367,16 @@ def _one(n_rows):
 
 def mxfp4_quantize(x, out=None, n_rows=None, stream=None):
     """(codes, scales) of x [..., rows, cols] in MXFP4: uint8 [..., rows, cols / 2] and
-    [..., rows, moe_mxfp4_scale_stride(cols)].  out: such a pair to write to; n_rows: device
-    int32, how many rows to convert (None: all)."""
+    [..., rows, moe_mxfp4_scale_stride(cols)].  out: such a pair to write to (None: a new one, of
+    the call's stream); n_rows: device int32, how many rows to convert (None: all)."""
     cols = _mx_cols(x)
     _check_current(x.device, "tensor")
     rows = x.numel() // cols if cols else 0
     if out is None:
-        out = (torch.empty(*x.shape[:-1], cols // 2, dtype=torch.uint8, device=x.device),
-               torch.empty(*x.shape[:-1], B.moe_mxfp4_scale_stride(cols), dtype=torch.uint8,
-                           device=x.device))
+        with _on(stream):
+            out = (torch.empty(*x.shape[:-1], cols // 2, dtype=torch.uint8, device=x.device),
+                   torch.empty(*x.shape[:-1], B.moe_mxfp4_scale_stride(cols), dtype=torch.uint8,
+                               device=x.device))
     codes, scales = out
     _check_tensor("x", x, x.shape, x.dtype, x.device, "tensor")
     _check_tensor("codes", codes, (*x.shape[:-1], cols // 2), torch.uint8, x.device, "tensor")
@@ -377,7 +394,8 @@ def mxfp4_dequantize(codes, scales, dtype=torch.bfloat16, out=None, n_rows=None,
     _check_current(codes.device, "tensor")
     rows = 2 * codes.numel() // cols if cols else 0
     if out is None:
-        out = torch.empty(*codes.shape[:-1], cols, dtype=dtype, device=codes.device)
+        with _on(stream):
+            out = torch.empty(*codes.shape[:-1], cols, dtype=dtype, device=codes.device)
     _check_tensor("codes", codes, codes.shape, torch.uint8, codes.device, "tensor")
     _check_tensor("scales", scales, (*codes.shape[:-1], B.moe_mxfp4_scale_stride(cols)), torch.uint8,
                   codes.device, "tensor")
@@ -392,7 +410,8 @@ class MxFFN:
     """The grouped expert FFN in MXFP4 on up to ``cap`` dispatched rows: moe_mxfp4_quantize of
     the rows, then moe_mxfp4_ffn_fwd on weights given once as (codes, scales) pairs of
     ``mxfp4_quantize``: ``w_gate_up`` of [E_r, 2H (SiLU: H), d], ``w_down`` of [E_r, d, H].
-    Its buffers are reused by the next call: calls on different streams need one each."""
+    Its buffers are reused by the next call: calls on different streams need one each.  They are
+    made at construction, behind whose stream a call on another one has to be ordered."""
 
     def __init__(self, cap, w_gate_up, w_down, expert="swiglu"):
         (gu, gu_s), (dn, dn_s) = w_gate_up, w_down
@@ -517,12 +536,13 @@ class InferenceMoELayer:
         self._ws = torch.empty(max(f.ws_bytes, 1), dtype=torch.uint8, device=self.device)
         f.ws = self._ws.data_ptr()
 
-    def _size(self, T):
+    def _size(self, T, stream=None):
         """Outputs of T tokens."""
         if not 0 <= T <= self.MAX_TOKENS:
             raise ValueError(f"few takes up to {self.MAX_TOKENS} tokens, got {T}")
         if self._ws is None:
-            self._buffers()
+            with _on(stream):
+                self._buffers()
         for name, t in self._out.items():
             setattr(self, name, t[:T])
         self.T = self._few.T = T
@@ -531,7 +551,7 @@ class InferenceMoELayer:
         """y [T, d] of up to 64 tokens x [T, d], by moe_few_fwd."""
         _check_current(self.device, "layer")
         if self.y is None or x.shape[0] != self.T:
-            self._size(x.shape[0])
+            self._size(x.shape[0], stream)
         _check_tensor("x", x, (self.T, self.d), self.dtype, self.device, "layer")
         self._few.x = x.data_ptr()
         B.moe_few_fwd(self._few, stream)

@@ -152,6 +152,47 @@ def test_round_trip_keeps_its_values_and_replays(gpu_lib):
         assert torch.equal(out, mxfp4_dequantize(*mxfp4_quantize(live), torch.float32))
 
 
+@pytest.mark.gpu
+def test_new_buffers_are_of_the_calls_stream(gpu_lib):
+    """Buffers that a call makes on another stream than the current one are not memory that the
+    current stream has yet to write: the latter is kept busy, then fills tensors of the same sizes,
+    which are dropped at once (their memory is the next to be given out on that stream)."""
+    from paper_2606_19025_amd.layer import InferenceMoELayer, LayerNorm, ResidentMoELayer
+    T, d, k, H = 64, 512, 2, 256
+    g = torch.Generator(device="cuda").manual_seed(5)
+    n = lambda *s: torch.randn(*s, generator=g, device="cuda").mul(0.3).bfloat16()
+    x, dy, w = n(T, d), n(T, d), torch.ones(d, device="cuda")
+    router, gu, dn = n(8, d), n(8, 2 * H, d), n(8, d, H)
+    big, res = n(2048, 2048), torch.ones(8, dtype=torch.uint8)
+    pair = mxfp4_quantize(big)
+    norms, few = [LayerNorm(T, d, bias=False) for _ in range(3)], lambda: InferenceMoELayer(k, res, router, gu, dn)
+    layers, fews = [ResidentMoELayer(T, d, 8, k, H, res) for _ in range(3)], [few() for _ in range(3)]
+    for N in norms:
+        N.forward(x, w)
+
+    def step(R, stream):
+        y = R.forward(x, router, gu, dn, stream=stream)
+        return [y, R.backward(dy, x, router, gu, dn, stream=stream), R.dw_gate_up]
+
+    calls = [lambda i, s: list(mxfp4_quantize(big, stream=s)),
+             lambda i, s: [mxfp4_dequantize(*pair, stream=s)],
+             lambda i, s: [norms[i].backward(dy, x, w, stream=s), norms[i].dw],
+             lambda i, s: [fews[i].few(x, stream=s), fews[i].logits], lambda i, s: step(layers[i], s)]
+    side, busy = torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+    for call in calls:
+        want = [v.clone() for v in call(0, None)]
+        for i, s in ((1, side), (2, side.cuda_stream)):
+            torch.cuda.synchronize()
+            for _ in range(8):
+                busy @ busy
+            sizes = [1 << b for b in range(9, 24)] + [3 << b for b in range(9, 22)]
+            junk = [torch.full((m,), 0x5A, dtype=torch.uint8, device="cuda") for m in sizes]
+            del junk
+            got = call(i, s)
+            torch.cuda.synchronize()
+            assert all(torch.equal(u, v) for u, v in zip(got, want))
+
+
 def test_mx_refusals():
     if torch.cuda.device_count() > 0:
         pytest.skip("host-only rejection test: runs where no GPU is visible")
