@@ -523,16 +523,19 @@ class InferenceMoELayer:
         self.y = self.logits = self.topk_idx = self.topk_w = self.topk_local = self._ws = None
 
     def _buffers(self):
-        """Outputs and workspace for the most tokens (the workspace grows with them)."""
+        """Outputs and workspace for the most tokens that the library takes at this width (the
+        workspace grows with them)."""
         f, N = self._few, self.MAX_TOKENS
         new = lambda n, dt: torch.empty(N, n, dtype=dt, device=self.device)
         self._out = dict(y=new(self.d, self.dtype), logits=new(self.E, torch.float32),
                          topk_w=new(self.k, torch.float32), topk_idx=new(self.k, torch.int32),
                          topk_local=new(self.k, torch.int32))
-        f.T = N
         for name, t in self._out.items():
             setattr(f, name, t.data_ptr())
-        f.ws_bytes = B.moe_few_fwd_workspace_size(f)
+        for f.T in range(N, 0, -1):
+            f.ws_bytes = B.moe_few_fwd_workspace_size(f)
+            if f.ws_bytes:  # (0: refused; the call then says what)
+                break
         self._ws = torch.empty(max(f.ws_bytes, 1), dtype=torch.uint8, device=self.device)
         f.ws = self._ws.data_ptr()
 

@@ -385,6 +385,20 @@ def test_few_refusals():
     assert B.moe_few_fwd_workspace_size(_few(logits=256)) < B.moe_few_fwd_workspace_size(_few())
 
 
+def test_inference_layer_workspace_of_wide_experts():
+    """Experts so wide that 64 tokens of 8 routes are past the library's limit: fewer are taken,
+    and the workspace is theirs."""
+    H = 1 << 20
+    L = InferenceMoELayer(8, np.zeros(8), torch.zeros(8, 64), torch.zeros(0, 2 * H, 64), torch.zeros(0, 64, H))
+    L._size(1)
+    need = [B.moe_few_fwd_workspace_size(L._few)]
+    L._size(63)
+    need.append(B.moe_few_fwd_workspace_size(L._few))
+    assert 0 < need[0] < need[1] == L._few.ws_bytes == L._ws.numel()
+    L._size(64)
+    assert B.moe_few_fwd_workspace_size(L._few) == 0 and "2^29" in B.moe_last_error()
+
+
 def test_inference_layer_checks():
     """Wrong shapes, types and mixtures are refused when the layer is built (on any device)."""
     E, d, H = 6, 128, 64
