@@ -43,7 +43,7 @@ class MoeError(RuntimeError):
 
 
 _lib = None
-_torch = None  # set with _lib
+_torch = _raw_stream = None  # set with _lib
 
 _P = C.c_void_p
 _I = C.c_int
@@ -158,7 +158,7 @@ def ffn_set(xp, w_gate_up, w_down, offsets, cap, H, n_groups, gu, h, yp=None, dy
 
 def lib(path: str | None = None):
     """Load the native library once (raises if it has not been built)."""
-    global _lib, _torch
+    global _lib, _torch, _raw_stream
     if _lib is None:
         p = path or LIB_PATH
         if not os.path.exists(p):
@@ -167,7 +167,7 @@ def lib(path: str | None = None):
         # torch first: the library must bind to the HIP runtime torch already
         # initialised (one runtime per process)
         import torch
-        _torch = torch
+        _torch, _raw_stream = torch, _raw_stream_of(torch)
         handle = C.CDLL(p)
         for name, (res, args) in _SIGS.items():
             f = getattr(handle, name)
@@ -185,11 +185,17 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _raw_stream_of(torch):
+    """The function that takes a device to its current stream's handle.  torch.cuda.current_stream()
+    makes a Stream object of it first, which took 2.9 of a small call's 7 us (torch's own short
+    way 0.3, where this torch has it)."""
+    return (getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            or (lambda device: torch.cuda.current_stream(device).cuda_stream))
+
+
 def _stream(s):
     if s is None:
-        # the current stream's handle; torch.cuda.current_stream() makes a Stream object of
-        # it first, which took 2.9 of a small call's 7 us (this way 0.3)
-        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device())
+        return _raw_stream(_torch.cuda.current_device())
     if isinstance(s, int):
         return s
     return s.cuda_stream

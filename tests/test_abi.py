@@ -206,3 +206,12 @@ def test_ffn_forward_workspace_holds_the_down_projection_parts(lib):
     # the backward's workspace holds dX's parts besides its counters
     bwd = B.ffn_set(p, p, p, p, 8192, 2816, 8, p, p, dyp=p, dgu=p, dxp=p, dw_gate_up=p, dw_down=p)
     assert B.moe_grouped_ffn_bwd_workspace_size([bwd], B.MOE_BF16, d) >= one
+
+
+def test_stream_handle_without_torchs_short_way():
+    """A torch without the private function that takes a device to its stream's handle."""
+    from types import SimpleNamespace as N
+    cuda = N(current_stream=lambda device: N(cuda_stream=100 + device))
+    short = N(_C=N(_cuda_getCurrentRawStream=lambda device: 7 + device), cuda=cuda)
+    assert B._raw_stream_of(short)(2) == 9
+    assert B._raw_stream_of(N(_C=N(), cuda=cuda))(2) == 102
