@@ -75,7 +75,7 @@ int moe_abi_version(void);
  * resident [E] uint8 (nonzero = resident on this worker);
  * logits [T,E] fp32 or NULL (not written when NULL);
  * topk_idx, topk_local [T,k] int32; topk_w [T,k] fp32.
- * Limits: 1 <= k <= E <= 256, T >= 0, d >= 1 (d % 8 == 0 for bf16).
+ * Limits: 1 <= k <= E <= 256, 0 <= T < 2^28 - 32, d >= 1 (d % 8 == 0 for bf16).
  */
 int moe_route_mask(const void* x, const void* w_router, const float* router_bias, int dtype,
                    int T, int d, int E, int k, float inv_tau, int gate,
@@ -101,6 +101,7 @@ int moe_route_mask(const void* x, const void* w_router, const float* router_bias
  * (relative error <= 2^-17 per element), otherwise as three bf16 parts that
  * hold all of it; fp32 layers multiply in fp32.
  * Every sum is taken in a fixed order, so results are run-to-run identical.
+ * Limits: T < 2^26 - 32.
  */
 size_t moe_route_bwd_workspace_size(int T, int d, int E);
 int moe_route_bwd(const void* x, const void* w_router, int dtype, int T, int d, int E, int k,
@@ -122,7 +123,8 @@ int moe_route_bwd(const void* x, const void* w_router, int dtype, int T, int d, 
  *
  * cap = T * min(k, E_r) bounds n; perm and xp have cap rows, of which rows
  * n..cap-1 are left untouched.  ws: at least moe_dispatch_workspace_size()
- * bytes; its contents on entry are ignored.  Limits: E_r <= 256.
+ * bytes; its contents on entry are ignored.  Limits: E_r <= 256, T < 2^29 - 32
+ * (2^26 - 32 for k > 8).
  */
 size_t moe_dispatch_workspace_size(int T, int k, int E_r);
 int moe_dispatch(const void* x, int dtype, int T, int d, int k, int E_r,
@@ -155,7 +157,7 @@ int moe_dispatch_noalloc(const void* x, int dtype, int T, int d, int k, int E_r,
  *   dx[t,:] (+)= sum_{j: inv_perm[t,j] >= 0} dxp[inv_perm[t,j], :]
  * A token whose routes are all ghosts gets exactly 0 (or keeps dx when
  * accumulate != 0).  dxp [cap,d], dx [T,d], both dtype.  Slots outside
- * [0, cap) are treated as ghost routes (cap = rows of dxp).
+ * [0, cap) are treated as ghost routes (cap = rows of dxp).  Limits: T < 2^26 - 32.
  */
 int moe_dispatch_bwd(const void* dxp, int dtype, int T, int d, int k, int cap,
                      const int32_t* inv_perm, void* dx, int accumulate, hipStream_t stream);
@@ -285,6 +287,7 @@ int moe_grouped_ffn_bwd_sets(const moe_ffn_set* sets, int n_sets, int dtype, int
  * Ghost routes are skipped; a token whose routes are all ghosts gets exactly
  * y_add[t,:] (exactly 0 when y_add == NULL).  yp [cap,d], y_add, y [T,d].
  * Slots outside [0, cap) are treated as ghost routes (cap = rows of yp).
+ * Limits: T < 2^26 - 32.
  */
 int moe_combine_fwd(const void* yp, int dtype, int T, int d, int k, int cap, const float* topk_w,
                     const int32_t* inv_perm, const void* y_add, void* y, hipStream_t stream);
@@ -294,6 +297,7 @@ int moe_combine_fwd(const void* yp, int dtype, int T, int d, int k, int cap, con
  *   dyp[p,:]      = topk_w[t,j] * dy[t,:]         for p = inv_perm[t,j] >= 0
  *   d_topk_w[t,j] = <dy[t,:], yp[p,:]>  (fp32), 0 for a ghost route
  * yp, dyp [cap,d]; slots outside [0, cap) are treated as ghost routes.
+ * Limits: T < 2^26 - 32.
  */
 int moe_combine_bwd(const void* dy, const void* yp, int dtype, int T, int d, int k, int cap,
                     const float* topk_w, const int32_t* inv_perm, void* dyp, float* d_topk_w,

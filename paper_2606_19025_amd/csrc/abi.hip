@@ -55,6 +55,14 @@ int check_dtype(int dtype) {
   return MOE_OK;
 }
 
+// A launch of `threads` per token, in blocks of up to 32 tokens: a grid of 2^32 threads or more is
+// not refused but taken modulo 2^32.
+int check_grid(int T, int threads) {
+  const long long most = (1LL << 32) / threads - 32;
+  SUPPORT(T < most, "T = %d: fewer than %lld tokens", T, most);
+  return MOE_OK;
+}
+
 // row vectors of 16 bytes: d % 8 == 0 and 16-byte aligned base pointers
 int check_rows16(int d, const char* name, const void* p) {
   SUPPORT(d % 8 == 0, "d = %d must be a multiple of 8", d);
@@ -174,6 +182,7 @@ int moe_route_mask(const void* x, const void* w_router, const float* router_bias
   REQUIRE(std::isfinite(inv_tau) && inv_tau > 0.f, "inv_tau must be finite and > 0");
   REQUIRE(w_router && resident, "w_router and resident must not be NULL");
   REQUIRE(T == 0 || (x && topk_idx && topk_w && topk_local), "x and the top-k outputs must not be NULL");
+  if ((r = check_grid(T, 16)) != MOE_OK) return r;
   if (dtype == MOE_BF16) {
     if ((r = check_rows16(d, "x", x)) != MOE_OK) return r;
     if ((r = check_rows16(d, "w_router", w_router)) != MOE_OK) return r;
@@ -205,6 +214,7 @@ int moe_route_bwd(const void* x, const void* w_router, int dtype, int T, int d, 
   REQUIRE(T == 0 || (x && topk_idx && topk_w && d_topk_w && dz && dx),
           "x, topk_idx, topk_w, d_topk_w, dz and dx must not be NULL");
   REQUIRE(gate != MOE_GATE_SOFTMAX || T == 0 || logits, "logits are required for MOE_GATE_SOFTMAX");
+  if ((r = check_grid(T, 64)) != MOE_OK) return r;
   const size_t need = moe::route_bwd_ws_bytes(T, d, E);
   REQUIRE(ws && ws_bytes >= need, "workspace of %zu bytes needed (got %zu)", need, ws_bytes);
   if ((r = check_rows16(d, "x", x)) != MOE_OK) return r;
@@ -232,6 +242,7 @@ int moe_dispatch(const void* x, int dtype, int T, int d, int k, int E_r,
   REQUIRE(offsets && (E_r == 0 || counts), "counts and offsets must not be NULL");
   REQUIRE(T == 0 || (x && topk_local && inv_perm && (E_r == 0 || (perm && xp))),
           "x, topk_local, perm, inv_perm and xp must not be NULL");
+  if ((r = check_grid(T, k > 8 ? 64 : 8)) != MOE_OK) return r;
   const size_t need = moe::dispatch_ws_bytes(T, k, E_r);
   REQUIRE(ws && ws_bytes >= need, "workspace of %zu bytes needed (got %zu)", need, ws_bytes);
   if ((r = check_rows16(d, "x", x)) != MOE_OK) return r;
@@ -251,6 +262,7 @@ int moe_dispatch_noalloc(const void* x, int dtype, int T, int d, int k, int E_r,
   REQUIRE(offsets && (E_r == 0 || counts), "counts and offsets must not be NULL");
   REQUIRE(T == 0 || (x && topk_local && inv_perm && (E_r == 0 || (perm && xp))),
           "x, topk_local, perm, inv_perm and xp must not be NULL");
+  if ((r = check_grid(T, k > 8 ? 64 : 8)) != MOE_OK) return r;
   const size_t need = moe::dispatch_ws_bytes(T, k, E_r);
   SUPPORT(need <= MOE_DISPATCH_NOALLOC_MAX_WS,
           "moe_dispatch_noalloc: T = %d, E_r = %d need a %zu-byte workspace, above the "
@@ -270,6 +282,7 @@ int moe_dispatch_bwd(const void* dxp, int dtype, int T, int d, int k, int cap,
   REQUIRE(T >= 0 && d >= 1 && k >= 1 && cap >= 0, "bad sizes T = %d, d = %d, k = %d, cap = %d",
           T, d, k, cap);
   REQUIRE(T == 0 || (inv_perm && dx && dxp), "dxp, inv_perm and dx must not be NULL");
+  if ((r = check_grid(T, 64)) != MOE_OK) return r;
   if ((r = check_rows16(d, "dxp", dxp)) != MOE_OK) return r;
   if ((r = check_rows16(d, "dx", dx)) != MOE_OK) return r;
   return hip_status(moe::launch_dispatch_bwd(dxp, dtype == MOE_BF16, T, d, k, cap, inv_perm, dx,
@@ -405,6 +418,7 @@ int moe_combine_fwd(const void* yp, int dtype, int T, int d, int k, int cap, con
   REQUIRE(T >= 0 && d >= 1 && k >= 1 && cap >= 0, "bad sizes T = %d, d = %d, k = %d, cap = %d",
           T, d, k, cap);
   REQUIRE(T == 0 || (topk_w && inv_perm && y), "topk_w, inv_perm and y must not be NULL");
+  if ((r = check_grid(T, 64)) != MOE_OK) return r;
   if ((r = check_rows16(d, "yp", yp)) != MOE_OK) return r;
   if ((r = check_rows16(d, "y_add", y_add)) != MOE_OK) return r;
   if ((r = check_rows16(d, "y", y)) != MOE_OK) return r;
@@ -422,6 +436,7 @@ int moe_combine_bwd(const void* dy, const void* yp, int dtype, int T, int d, int
           T, d, k, cap);
   REQUIRE(T == 0 || (dy && topk_w && inv_perm && d_topk_w), "dy, topk_w, inv_perm and d_topk_w must not be NULL");
   if ((r = check_rows16(d, "dy", dy)) != MOE_OK) return r;
+  if ((r = check_grid(T, 64)) != MOE_OK) return r;
   if ((r = check_rows16(d, "yp", yp)) != MOE_OK) return r;
   if ((r = check_rows16(d, "dyp", dyp)) != MOE_OK) return r;
   return hip_status(moe::launch_combine_bwd(dy, yp, dtype == MOE_BF16, T, d, k, cap, topk_w,

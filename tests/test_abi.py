@@ -215,3 +215,21 @@ def test_stream_handle_without_torchs_short_way():
     short = N(_C=N(_cuda_getCurrentRawStream=lambda device: 7 + device), cuda=cuda)
     assert B._raw_stream_of(short)(2) == 9
     assert B._raw_stream_of(N(_C=N(), cuda=cuda))(2) == 102
+
+
+@pytest.mark.parametrize("name,k,most", [("route_mask", 2, 1 << 28), ("route_bwd", 2, 1 << 26), ("dispatch", 8, 1 << 29),
+                                         ("dispatch", 9, 1 << 26), ("dispatch_bwd", 2, 1 << 26),
+                                         ("combine_fwd", 2, 1 << 26), ("combine_bwd", 2, 1 << 26)])
+def test_more_tokens_than_a_grid_are_refused(lib, name, k, most):
+    """A grid of 2^32 threads or more would be taken modulo 2^32: the calls that launch some per
+    token end before that.  (One below the limit gets as far as the refusal of an unaligned array.)"""
+    p, x, dt, ws = 256, 256 + 4, B.MOE_BF16, 1 << 50  # fake, never dereferenced addresses
+    call = {
+        "route_mask": lambda T: lib.moe_route_mask(x, p, None, dt, T, 8, 16, k, 1.0, 0, p, None, p, p, p, None),
+        "route_bwd": lambda T: lib.moe_route_bwd(x, p, dt, T, 8, 16, k, 1.0, 0, p, p, p, p, p, p, p, p, 0, p, ws, None),
+        "dispatch": lambda T: lib.moe_dispatch(x, dt, T, 8, k, 4, p, p, p, p, p, p, p, ws, None),
+        "dispatch_bwd": lambda T: lib.moe_dispatch_bwd(x, dt, T, 8, k, 100, p, p, 0, None),
+        "combine_fwd": lambda T: lib.moe_combine_fwd(x, dt, T, 8, k, 100, p, p, None, p, None),
+        "combine_bwd": lambda T: lib.moe_combine_bwd(p, x, dt, T, 8, k, 100, p, p, p, p, None)}[name]
+    assert call(most - 32) == ERR_UNSUPPORTED and "fewer than" in B.moe_last_error()
+    assert call(most - 33) == ERR_UNSUPPORTED and "aligned" in B.moe_last_error()
