@@ -134,6 +134,25 @@ def test_few_matches_64_bits(gpu_lib, c):
     check(c, t, build(c, t))
 
 
+WIDE = [
+    # d of 4096 and more: blocks of 16 columns of y; the router's other paths past 2048 and 4096
+    case(1, 4096, 8, 4, 2, 64, 64), case(17, 4160, 8, 5, 2, 192, 64), case(33, 4096, 100, 12, 4, 64, expert="silu"),
+    case(64, 4160, 6, 3, 3, 64, 128, bias=True), case(40, 8192, 33, 4, 2, 64), case(9, 2112, 48, 20, 4, 64, 64),
+    case(50, 2112, 130, 20, 8, 64), case(5, 4160, 6, 3, 2, 64, 64, dtype="f32"),
+    case(16, 4096, 8, 3, 2, 64, dtype="f32", expert="silu"), case(21, 4160, 8, 3, 2, 64, 64, dtype="f32"),
+    case(60, 4096, 8, 3, 2, 64, dtype="f32"), case(3, 4096, 8, 4, 2, 192, 320, mx=True),
+    case(8, 4160, 8, 4, 2, 320, mx=True), case(16, 4160, 8, 3, 2, 192, 64, mx=True, expert="silu"),
+    case(17, 4096, 8, 3, 2, 64, 192, mx=True), case(40, 4160, 6, 3, 2, 192, 320, mx=True),
+    case(64, 4096, 8, 5, 3, 64, mx=True),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("c", WIDE, ids=lambda c: "-".join(str(v) for v in c.values()))
+def test_few_wide_rows(gpu_lib, c):
+    test_few_matches_64_bits(gpu_lib, c)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("mx", [False, True])
 def test_few_all_ghosts_and_one_expert_for_all(gpu_lib, mx):

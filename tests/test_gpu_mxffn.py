@@ -127,6 +127,41 @@ def test_mxffn_large_tiles(gpu_lib, d, H, expert):
     assert (y[n:] == 7).all()
 
 
+def tiles(sizes, bm, N, bn):
+    return sum(-(-n // bm) for n in sizes) * -(-N // bn)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("expert,H", [("swiglu", 1088), ("silu", 2112)])
+@pytest.mark.parametrize("large", [True, False])
+def test_mxffn_blocks_take_several_tiles(gpu_lib, large, expert, H):
+    """More tiles than blocks (256 of large ones, 512 of small ones) in both projections: a block
+    loads its next tile while it stores one."""
+    d = 1216 if large else 1600
+    if not large:
+        H = 832 if expert == "swiglu" else 1664
+    sizes = [2300, 0, 1, 4097, 255, 5000, 513, 7000] if large else [65 + 7 * i % 60 for i in range(40)]
+    N = 2 * H if expert == "swiglu" else H
+    for cols in (N, d):
+        # the large tiles are taken from one per CU on
+        if large:
+            assert tiles(sizes, 256, cols, 256) > 256 and sum(sizes) // 256 * -(-cols // 256) > 256
+        else:
+            assert tiles(sizes, 64, cols, 128) > 512 and (sum(sizes) // 256 + 20) * -(-cols // 256) < 256
+    print("[mxffn]", len(sizes), sum(sizes), d, H, expert, flush=True)
+    x, off, gu, dn = make(sizes, d, H, expert, extra=5)
+    n = sum(sizes)
+    L = MxFFN(n + 5, gu, dn, expert=expert)
+    L.y.fill_(7.0)
+    L.ws.fill_(0xFF)
+    y = L.forward(x, off).clone()
+    ref, tol = reference(x[:n], sizes, gu, dn, expert)
+    assert torch.isfinite(y).all()
+    over = ((y[:n].double() - ref).abs() - tol).max().item()
+    assert over <= 0, f"{over:.3e} past its bound"
+    assert (y[n:] == 7).all() and torch.equal(L.forward(x, off), y)
+
+
 @pytest.mark.gpu
 def test_mxffn_offsets_out_of_range_and_empty(gpu_lib):
     """Groups are clamped to [0, cap]; no groups or no rows write nothing."""

@@ -105,6 +105,15 @@ def test_norm_a_row_per_wave(gpu_lib, T, d, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,d,dtype", [(300, 4104, "bf16"), (601, 8192, "bf16"), (1100, 16384, "bf16"),
+                                       (299, 4104, "f32"), (700, 16376, "f32")])
+def test_norm_sixteen_waves_take_several_rows(gpu_lib, T, d, dtype):
+    """More rows than blocks where a row is a block's sixteen waves' (at most 5 rows of a block, one
+    addition each, 275 partials)."""
+    test_norm_matches_64_bits(gpu_lib, T, d, dtype)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T,d", [((1 << 26) + 5, 8), ((1 << 24) + 3, 2056), ((1 << 22) + 1, 8200)])
 def test_norm_more_rows_than_a_grid(gpu_lib, T, d):
     """Rows of one, four and sixteen waves, more of them than a launch's 2^32 threads hold, in
