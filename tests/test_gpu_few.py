@@ -299,6 +299,39 @@ def test_few_infinities_in_a_cut_step(gpu_lib):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,mx", [("bf16", False), ("f32", False), ("bf16", True)])
+def test_few_what_is_not_finite_stays_where_it_is(gpu_lib, dtype, mx):
+    """NaN tokens: their rows alone, with moe_route_mask's routes; a NaN in an expert's weights:
+    the tokens that are routed to it."""
+    c = case(20, 192, 24, 10, 3, 128, 64, dtype=dtype, mx=mx)
+    t = make(c, 6)
+    L = build(c, t)
+    clean = L.few(t["x"]).clone()
+    x = t["x"]
+    t["x"] = x.clone()
+    t["x"][4], t["x"][11, 7], t["x"][19, 100] = float("nan"), float("nan"), float("-inf")
+    y = L.few(t["x"])
+    logits, idx, w, local = routing(c, t, 20)
+    assert torch.equal(L.topk_idx, idx) and torch.equal(L.topk_local, local)
+    for a, b in ((L.logits, logits), (L.topk_w, w)):
+        assert torch.equal(a.nan_to_num(7.0, 8.0, 9.0), b.nan_to_num(7.0, 8.0, 9.0))
+    bad = torch.zeros(20, dtype=torch.bool, device="cuda")
+    bad[[4, 11, 19]] = True
+    assert torch.equal(y[~bad], clean[~bad]) and not torch.isfinite(y[bad]).any()
+    for name, at in (("w_gate_up", (6, 200, 70)), ("w_down", (2, 190, 127))):
+        w = dict(t["w"])
+        v = (mxfp4_dequantize(*w[name]) if mx else w[name]).clone()
+        v[at] = float("nan")
+        w[name] = mxfp4_quantize(v) if mx else v
+        M = build(c, dict(t, w=w))
+        y = M.few(x)
+        hit = (M.topk_local == at[0]).any(1)
+        assert hit.any() and not hit.all() and torch.equal(y[~hit], clean[~hit])
+        # (a row of W_d: one column of y)
+        assert y[hit][:, at[1] if name == "w_down" else slice(None)].isnan().all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_few_agrees_with_the_training_layer(gpu_lib, dtype):
     """Behind the pre-norm, on the same weights: the training layer's forward, whose routes it

@@ -193,6 +193,27 @@ def test_mxffn_nan_stays_in_its_rows(gpu_lib):
 
 
 @pytest.mark.gpu
+def test_mxffn_silu_at_its_lower_end(gpu_lib):
+    """Gate sums of -82 to -96 under up projections of 2^107: past -87.3 the exponential or its
+    reciprocal leaves fp32's normal numbers, and silu, at most 1.03e-36 there, may be 0 or off by
+    that much, which is added to the header's bound.  Every product and sum is exact (x of ones,
+    the gate's weights -0.5 and -0.75), W_d the identity: y is h's codes, exact in bf16."""
+    d = H = 128
+    wg = torch.full((H, d), -0.5, device="cuda")
+    for j in range(H):
+        wg[j, : 72 + 56 * j // H] = -0.75
+    wu = torch.full((H, d), 2.0 ** 100, device="cuda")
+    gu, dn = mxfp4_quantize(torch.cat([wg, wu])[None]), mxfp4_quantize(torch.eye(d, device="cuda")[None])
+    y = MxFFN(3, gu, dn).forward(torch.ones(3, d, device="cuda"), torch.tensor([0, 3], dtype=torch.int32, device="cuda"))
+    g = wg.double().sum(1)[None]
+    u = 2.0 ** 107
+    h = g / (1 + torch.exp(-g)) * u
+    mid, lo, hi = quantised(h, (16 + 1.5 * g.abs()) * U * h.abs() + 1.1e-36 * u)
+    assert g.min() == -96 + 0.25 and g.max() == -82 and (mid[g < -89] != 0).any()
+    assert ((y.double() >= lo) & (y.double() <= hi)).all()
+
+
+@pytest.mark.gpu
 def test_mxffn_graph_and_stream(gpu_lib):
     x, off, gu, dn = make([70, 0, 300], 256, 192)
     L = MxFFN(370, gu, dn)
