@@ -398,9 +398,12 @@ hipError_t mx_run(const MxGemmArgs& a, const char* name, hipStream_t s) {
 }
 
 // Large tiles read each operand fewer times, small ones fill the CUs sooner (two blocks on
-// each).  Large where the rows, all there and spread evenly, give every CU a tile.
+// each) and pad small groups less.  Large where the rows, all there and spread evenly, give every
+// CU a tile that is more than half full.
 // Measured (us, large / small, and the large tiles; rows, groups, d, H):
 //                            first projection   second
+//   128, 128, 2048, 1408      140 /  74  704      70 /  47  512
+//   256, 256, 1024, 1408      169 /  78 1419      72 /  48  516
 //   2048, 16, 2048, 1408       24 /  20  176      18 /  13  128
 //   4096,  8, 1024, 2816       32 /  33  440      25 /  16   80
 //   8192,  4, 1024, 2816       45 /  59  748      25 /  25  136
@@ -408,11 +411,23 @@ hipError_t mx_run(const MxGemmArgs& a, const char* name, hipStream_t s) {
 //   8192, 16, 2048, 1408       44 /  50  440      23 /  32  320
 //   16384, 8, 1024, 2816       85 / 113 1496      31 /  46  272
 //   65536, 32, 4096, 2048     595 / 974 4352     380 / 529 4352
+// and by rows of a group (the tiles of small groups are mostly padding):
+//          64 groups, 2048, 1408     32 groups, 4096, 2048     256 groups, 1024, 704
+//   64       75 /  51   41 /  32       88 /  67   47 /  35       98 /  54   56 /  38
+//   96       77 /  69   43 /  44       91 /  92   51 /  50       99 /  76   59 /  54
+//  128       77 /  71   44 /  48       94 /  98   52 /  54      101 /  78   63 /  60
+//  160       79 /  88   47 /  59       94 / 114   54 /  65      102 /  99   68 /  72
+//  192       80 /  89   49 /  61       96 / 118   56 /  68      105 / 102   73 /  77
+//  256       82 / 118   54 /  83       99 / 163   60 /  94      108 / 138   80 / 108
+// The rows that are there are known on the device only.  With a quarter of cap's (6144 in 16
+// groups, 2048, 1408: 24 / 19, 18 / 12; 16384 in 8, 1024, 2816: 31 / 31, 25 / 15; 16384 in 16,
+// 2048, 1408: 25 / 29, 19 / 18) the choice for all of them is up to half again slower.
 template <int KIND>
 hipError_t mx_launch(const MxGemmArgs& a, const char* name, hipStream_t s) {
   const int64_t tiles =
       (int64_t)(a.g.cap / MxLarge::BM + (a.g.n_groups + 1) / 2) * ceil_div(a.N, MxLarge::BN);
-  return tiles >= num_cus() ? mx_run<KIND, MxLarge>(a, name, s) : mx_run<KIND, MxSmall>(a, name, s);
+  const bool large = tiles >= num_cus() && a.g.cap > MxLarge::BM / 2 * a.g.n_groups;
+  return large ? mx_run<KIND, MxLarge>(a, name, s) : mx_run<KIND, MxSmall>(a, name, s);
 }
 
 }  // namespace

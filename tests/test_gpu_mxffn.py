@@ -127,6 +127,15 @@ def test_mxffn_large_tiles(gpu_lib, d, H, expert):
     assert (y[n:] == 7).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes,d,H,expert", [([1] * 256, 192, 704, "swiglu"), ([0, 1] * 64, 1088, 320, "silu"),
+                                              ([127] * 48, 576, 1408, "swiglu"), ([129] * 48, 576, 1408, "swiglu")])
+def test_mxffn_few_rows_in_many_groups(gpu_lib, sizes, d, H, expert):
+    """Groups of one row and fewer, and of half a large tile and one more (the border of the tiles'
+    choice)."""
+    test_mxffn_matches_64_bits(gpu_lib, sizes, d, H, expert)
+
+
 def tiles(sizes, bm, N, bn):
     return sum(-(-n // bm) for n in sizes) * -(-N // bn)
 
