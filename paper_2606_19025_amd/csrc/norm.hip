@@ -15,7 +15,9 @@
 // block order, so the results do not depend on timing.
 //
 // Measured (bf16): 8192 x 2048 forward 14 us (4.7 TB/s), backward with dres 26 us (5.2), dw and
-// db 4.4 us; 16384 x 4096 backward 101 us (5.3 TB/s).  One row: 2.4 us.
+// db 4.4 us; 16384 x 4096 backward 101 us (5.3 TB/s).  One row: 2.4 us.  Rows of sixteen waves:
+// 8192 x 8192 backward 125 us, 8192 x 16384 238 us (4.3 and 4.5 TB/s; they have 128 registers a lane, of
+// which 3 to 17 are spilled, fetch nothing ahead and read w for every row).
 #include "common.h"
 #include "kernels.h"
 #include "timing.h"
@@ -298,20 +300,31 @@ int vectors(int d, int ve, int waves) {
 }
 
 // Waves per row: one where the rows are many and a lane then holds at most `one`
-// vectors, else the fewest of 4 and 16 that leave a lane at most `more`.  Measured (bf16, us,
-// one wave / four; launch included):
-//   rows      forward, d = 1024  2048       4096         backward, d = 1024
-//   1024      6.7 / 6.7          6.7 / 6.6  9.7 / 7.9    10.4 / 8.1
-//   2048      6.6 / 6.8          8.4 / 7.4  12.1 / 10.7  12.3 / 10.0
-//   4096      7.5 / 9.0          10.9 / 11.1  16.1 / 16.5  13.9 / 13.3
-//   8192      10.4 / 13.6        15.5 / 17.1  27.3 / 24.4  16.6 / 21.1
+// vectors, else the fewest of 4 and 16 that leave a lane at most `more`.  Measured (us, one wave /
+// four; launch included):
+//   bf16      forward, d = 512   1024         2048         backward, d = 512   1024
+//   1024      6.5 / 6.3          6.4 / 6.4    6.6 / 6.7    7.7 / 7.9    10.8 / 8.8
+//   2048      6.6 / 6.9          6.5 / 6.8    8.2 / 7.5    8.3 / 8.6    12.2 / 10.1
+//   4096      6.9 / 8.0          7.3 / 9.2    11.3 / 11.0  9.9 / 12.1   14.2 / 13.5
+//   6144      6.9 / 10.0         8.9 / 11.4   13.6 / 14.3  10.8 / 16.1  15.7 / 16.2
+//   8192      7.6 / 11.7         10.3 / 13.8  15.4 / 16.7  11.8 / 19.0  16.5 / 20.2
+//   fp32      forward, d = 512   1024         backward, d = 512   640          768          896          1024
+//   1024      6.5 / 6.4          6.7 / 6.8    7.9 / 7.4                                                  10.6 / 8.4
+//   2048      7.0 / 6.6          7.1 / 7.3    8.6 / 8.4                                                  12.7 / 9.8
+//   4096      7.4 / 8.6          10.0 / 10.3  10.0 / 11.2  12.0 / 11.9  12.7 / 12.3  14.2 / 12.7  14.5 / 13.8
+//   6144      8.1 / 10.9         11.7 / 13.2  11.2 / 14.8  14.0 / 16.2  15.9 / 15.9  17.7 / 16.2  19.1 / 16.9
+//   8192      9.3 / 12.7         13.8 / 15.9  13.2 / 17.9  16.8 / 19.0  18.7 / 19.2  21.0 / 20.6  22.5 / 21.5
+//   16384     15.2 / 20.1        24.3 / 26.5  20.9 / 28.8  25.8 / 31.0  29.1 / 30.9  33.0 / 33.1  37.0 / 37.1
 int row_waves(int T, int d, int ve, int one, int more) {
   if (T >= 4096 && vectors(d, ve, 1) <= one) return 1;
   return vectors(d, ve, 4) <= more ? 4 : 16;
 }
 int row_waves_fwd(int T, int d, int ve) { return row_waves(T, d, ve, 4, 4); }
-// (a lane of the backward holds six fp32 values per element: 16 elements at most)
-int row_waves_bwd(int T, int d, int ve) { return row_waves(T, d, ve, 16 / ve, 16 / ve); }
+// (a lane of the backward holds six fp32 values per element: 16 elements at most; fp32 rows past
+// 768 columns take four waves)
+int row_waves_bwd(int T, int d, int ve) {
+  return row_waves(T, d, ve, ve == 4 && d > 768 ? 2 : 16 / ve, 16 / ve);
+}
 
 // Blocks of the backward: each writes a partial row of 2 d, so that past one per CU a block
 // takes at least four rows (1024 rows, d = 4096: 256 blocks 12.7 us, 512 14.5), up to two per
