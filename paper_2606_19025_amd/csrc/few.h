@@ -15,8 +15,12 @@
 // (The order of k within a matrix instruction is free as long as both operands have the same.)
 //
 // Measured (d = 2048, H = 1408, 64 experts, k = 6, shared 2816): one token, bf16, 5 + 20 + 15 us
-// (the weights at 4.6 and 3.1 TB/s); 48 tokens on 16 resident experts 6 + 49 + 29; 16 tokens
-// on 32 experts in MXFP4 5 + 31 + 25.
+// (the weights at 4.6 and 3.1 TB/s); 48 tokens on 16 resident experts 6 + 48 + 28; 16 tokens
+// on 32 experts in MXFP4 5 + 31 + 25.  Some 130 MB of weights, which calls on the same ones may find
+// in the last-level cache (256 MB); six layers in turn, other tokens each time: one token 41 us a
+// call against 37, the 16 tokens 72 against 68.
+// MXFP4, all 32 experts at hand, by tokens (event times of the projections, us): 1 16 + 14, 4 26 + 21,
+// 8 30 + 25, 16 37 + 31, 24 43 + 36, 33 58 + 47, 48 110 + 89, 64 183 + 147.
 #pragma once
 #include <type_traits>
 
@@ -513,7 +517,11 @@ __global__ __launch_bounds__(2 * FT) void few_gu_kernel(FewArgs a) {
 #pragma unroll
             for (int q = 1; q < FW; ++q) v[i] += red[buf][q][i][m][lane];
           }
-          // hidden units h0 + 4 q4 .. of column l16's token
+          // hidden units h0 + 4 q4 .. of column l16's token.  h is rounded to E once, the gate in
+          // it: the matrix instruction of bf16 weights takes bf16 only, and a second one on the
+          // rest (h - bf16(h)) would double the activations, which are half of the second
+          // projections' loads already.  y is then off by 2.3e-3 of its norm, where rounding it
+          // alone leaves 1.7e-3; moe_layer_fwd rounds h and each route's output.
           if (c.row[m] >= 0) {
             const float gate = shared ? 1.0f : tb.gate[c.row[m]];
             E* out = static_cast<E*>(shared ? a.hs : a.h) + (size_t)c.row[m] * H + h0 + 4 * q4;

@@ -20,10 +20,11 @@
 // stage's DMA, takes the barrier (this stage is free, the next is whole) and refills it.
 // A tile's first two stages are issued before the previous tile's epilogue.
 //
-// Measured (65536 rows in 32 groups, d = 4096, H = 2048): first projection 635 us, second 390:
-// 3.5 and 2.8 PFLOP/s, by the clock that power leaves (1.8 GHz; a single call 595 and 380).
-// Before the last two steps the matrix units were busy 40 % of the time, the LDS pipe about
-// 70 %; a k-step took 2.1 us, a tile's epilogue 7.
+// Measured (65536 rows in 32 groups, d = 4096, H = 2048): first projection 658 us, second 400:
+// 3.3 and 2.7 PFLOP/s, by the clock that power leaves (1.76 GHz; calls apart 580 and 375).  Over
+// both the matrix units are busy 41 % of the time, the LDS pipe about as much (operands and
+// scales 27, conflicts 3, the DMA's writes some 11): what is left are the waits at each k-step's
+// barrier and the epilogues, which have no products beside them.
 #include "gemm.h"
 #include "kernels.h"
 #include "mx.h"
@@ -149,7 +150,8 @@ __global__ __launch_bounds__(T::NT) void mx_gemm_kernel(MxGemmArgs p) {
   unsigned oa[T::PA], ob[T::PB], os;
   const int chunk = (lane & 7) ^ (((wave * 8 + (lane >> 3)) >> 1) & 7);
   // (its lane index passes through an asm: kept from tile to tile, parts of the offsets went
-  // through scratch memory, and each reload waited for the loads issued before it)
+  // through scratch memory, and each reload waited for the loads issued before it.  The large
+  // tiles still spill 3 to 8 registers, 16 to 36 bytes a lane)
   auto aim = [&](const Where& w) {
     int al = lane;
     asm volatile("" : "+v"(al));

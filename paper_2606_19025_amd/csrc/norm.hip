@@ -14,8 +14,8 @@
 // stores one fp32 partial row per block; a second launch adds the partials in
 // block order, so the results do not depend on timing.
 //
-// Measured (bf16): 8192 x 2048 forward 14 us (4.7 TB/s), backward with dres 26 us (5.2), dw and
-// db 4.4 us; 16384 x 4096 backward 101 us (5.3 TB/s).  One row: 2.4 us.  Rows of sixteen waves:
+// Measured (bf16): 8192 x 2048 forward 15 us (4.5 TB/s), backward with dres 26 us (5.2), dw and
+// db 4.7 us; 16384 x 4096 backward 100 us (5.4 TB/s).  One row: 2.6 us.  Rows of sixteen waves:
 // 8192 x 8192 backward 125 us, 8192 x 16384 238 us (4.3 and 4.5 TB/s; they have 128 registers a lane, of
 // which 3 to 17 are spilled, fetch nothing ahead and read w for every row).
 #include "common.h"
