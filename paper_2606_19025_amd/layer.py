@@ -442,7 +442,8 @@ class MxFFN:
         """y [cap, d] of the dispatched rows xp [cap, d] (bf16 or fp32), whose groups are
         [offsets[g], offsets[g + 1]); rows past offsets[E_r] are neither read nor written."""
         _check_current(self.device, "layer")
-        _check_tensor("xp", xp, (self.cap, self.d), xp.dtype, self.device, "layer")
+        dtype = torch.float32 if getattr(xp, "dtype", None) is torch.float32 else torch.bfloat16
+        _check_tensor("xp", xp, (self.cap, self.d), dtype, self.device, "layer")
         _check_tensor("offsets", offsets, (self.E_r + 1,), torch.int32, self.device, "layer")
         B.moe_mxfp4_quantize(xp, B.dtype_code(xp), self.cap, self.d, offsets.data_ptr() + 4 * self.E_r,
                              self.xq, self.xs, stream)
@@ -553,6 +554,8 @@ class InferenceMoELayer:
     def few(self, x, stream=None):
         """y [T, d] of up to 64 tokens x [T, d], by moe_few_fwd."""
         _check_current(self.device, "layer")
+        if not isinstance(x, torch.Tensor) or x.dim() != 2:
+            raise ValueError("x must be a tensor of tokens: [T, d]")
         if self.y is None or x.shape[0] != self.T:
             self._size(x.shape[0], stream)
         _check_tensor("x", x, (self.T, self.d), self.dtype, self.device, "layer")

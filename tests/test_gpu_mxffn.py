@@ -190,6 +190,27 @@ def test_mxffn_offsets_out_of_range_and_empty(gpu_lib):
 
 
 @pytest.mark.gpu
+def test_mxffn_and_few_refuse_what_is_no_tensor_of_rows(gpu_lib):
+    """Before anything is launched, and without a trace in the layer's outputs."""
+    from paper_2606_19025_amd.layer import InferenceMoELayer
+    x, off, gu, dn = make([20, 30, 14], 128, 64)
+    F = MxFFN(64, gu, dn)
+    whole = F.forward(x, off)
+    for bad in (None, 3, x.half(), x.double(), x[:63], x[:, :64], x.T.contiguous().T, x.cpu()):
+        with pytest.raises(ValueError):
+            F.forward(bad, off)
+    for bad in (None, off.long(), off[:3], off.cpu()):
+        with pytest.raises(ValueError):
+            F.forward(x, bad)
+    L = InferenceMoELayer(2, np.ones(3), torch.ones(3, 128, dtype=torch.bfloat16, device="cuda"), gu, dn)
+    y = L.few(x).clone()
+    for bad in (None, 3, x[0], x[None], x.half(), x[:, :64], x.float(), torch.cat([x, x])):
+        with pytest.raises(ValueError):
+            L.few(bad)
+    assert torch.equal(L.few(x), y) and torch.equal(F.forward(x, off), whole)
+
+
+@pytest.mark.gpu
 def test_mxffn_nan_stays_in_its_rows(gpu_lib):
     x, off, gu, dn = make([100, 28], 128, 128)
     L = MxFFN(128, gu, dn)
