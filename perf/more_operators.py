@@ -280,7 +280,7 @@ def _plain_xent(s):
     counted = y >= 0
     at = y.clamp(min=0)[:, None]
     loss = lse - z.gather(1, at)[:, 0] + c["z_coef"] * lse * lse
-    loss = torch.where(counted, loss, 0.0)
+    loss, lse = torch.where(counted, loss, 0.0), torch.where(counted, lse, 0.0)
     n = counted.sum().float()
     out = dict(loss=loss, lse=lse, total=torch.stack([loss.sum(), n]))
     if c["way"] == "fwd":
@@ -420,8 +420,8 @@ def _exact_xent(s):
     c, y = s["case"], s["labels"].long()
     x, w = s["x"].double(), s["w"].double()
     z = x.matmul(w.t()).mul_(c["scale"])
-    lse = torch.logsumexp(z, dim=1)
     keep = y.ge(0)
+    lse = torch.logsumexp(z, dim=1) * keep  # tokens that do not count have none
     rows = keep.nonzero()[:, 0]
     loss = torch.zeros_like(lse)
     loss[rows] = lse[rows] - z[rows, y[rows]] + c["z_coef"] * lse[rows] ** 2
