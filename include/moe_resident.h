@@ -389,6 +389,66 @@ int moe_layernorm_bwd(const void* dy, const void* x, const float* weight, const 
                       hipStream_t stream);
 
 /*
+ * The norms and the residual sum around a block F of a Peri-LN transformer (App. B,
+ * x + LN(F(LN(x)))), in one pass between one block and the next:
+ *   n  = norm(f; post_weight, post_bias), or f where post_weight is NULL
+ *   x_out = x + scale g n, rounded to dtype;  g: 1, gate[c] or gate[t] (gate_kind)
+ *   u  = norm(x_out; pre_weight, pre_bias): what the next block takes
+ * with the norm of moe_layernorm_fwd.  Either norm may be missing (post_weight NULL: plain
+ * pre-norm blocks; u NULL: the last sum), not both.
+ * x, f, x_out, u [T,d] dtype (x_out may be x); weights, biases [d] fp32, biases NULL: none;
+ * gate [d] or [T] fp32; post_mean, post_rstd, pre_mean, pre_rstd [T] fp32: the statistics of f
+ * and x_out, written by the forward and read by the backward (of the norms that there are).
+ *
+ * moe_block_norm_bwd, from du and dres, the gradients that reach u and x_out (dres: past the
+ * next block; NULL: none, not without u):
+ *   dx = dres + the pre-norm's gradient of du: the gradient of x_out, and of x
+ *   df = the gradient of f;  d_pre_weight, d_pre_bias, d_post_weight, d_post_bias [d] fp32 and
+ *   d_gate [d] or [T] fp32 (biases' may be NULL).
+ * Arrays over [d] are added to where accumulate != 0, else overwritten (zeros when T = 0); a
+ * gradient per token is always overwritten.  dx may be du or dres; df may be f.  x_out is what
+ * the forward wrote; x and u are not read.
+ * ws: device workspace (16-byte aligned) of at least moe_block_norm_bwd_workspace_size(T, d,
+ * dtype) bytes (which depends on the current device's compute-unit count); its contents on
+ * entry are ignored.  The sums over t are taken in a fixed order.
+ * Limits: those of moe_layernorm_fwd; scale finite; the statistics and a gate per token 4-byte
+ * aligned.
+ */
+enum { MOE_BLOCK_GATE_NONE = 0, MOE_BLOCK_GATE_CHANNEL = 1, MOE_BLOCK_GATE_TOKEN = 2 };
+typedef struct moe_block_norm {
+  int dtype, T, d, gate_kind;
+  float scale, eps;
+  const void* x;
+  const void* f;
+  const float* post_weight;
+  const float* post_bias;
+  const float* gate;
+  const float* pre_weight;
+  const float* pre_bias;
+  void* x_out;
+  void* u;
+  float* post_mean;
+  float* post_rstd;
+  float* pre_mean;
+  float* pre_rstd;
+  const void* du; /* from here on: backward */
+  const void* dres;
+  void* dx;
+  void* df;
+  float* d_post_weight;
+  float* d_post_bias;
+  float* d_gate;
+  float* d_pre_weight;
+  float* d_pre_bias;
+  int accumulate;
+  void* ws;
+  size_t ws_bytes;
+} moe_block_norm;
+int moe_block_norm_fwd(const moe_block_norm* p, hipStream_t stream);
+size_t moe_block_norm_bwd_workspace_size(int T, int d, int dtype);
+int moe_block_norm_bwd(const moe_block_norm* p, hipStream_t stream);
+
+/*
  * MXFP4 (microscaled 4-bit floating point): every 32 consecutive values of a row are
  * a block with one E8M0 scale byte s, standing for 2^(s - 127), and an E2M1 code
  * each (sign in bit 3; magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6).
@@ -548,6 +608,54 @@ int moe_expert_delta(const float* theta_start, const float* theta_now,
 int moe_adamw_step(float* theta, const float* grad, float* m, float* v, size_t n, int step,
                    float lr, float beta1, float beta2, float eps, float weight_decay,
                    void* theta_bf16, hipStream_t stream);
+
+/*
+ * The norm of all gradients of a step together, and clipping by it.
+ *   norm[0] = sqrt(sum over all tensors of grad^2), summed in fp64
+ *   norm[1] = norm[0] > max_norm ? max_norm / norm[0] : 1: the scale
+ * grads is a HOST array of n_grads tensors of n values each, fp32 or bf16 (dtype), of any
+ * alignment that their type has (16-byte aligned ones are faster); norm: device, 2 fp32 values.
+ * A tensor that is listed twice counts twice.  A norm that is not finite (an infinity or a
+ * NaN among the gradients) has the scale NaN.
+ * ws: device workspace (8-byte aligned) of at least moe_grad_norm_workspace_size(grads, n_grads)
+ * bytes (which depends on the sizes alone and on the current device's compute-unit count); its
+ * contents on entry are ignored.
+ * moe_grad_clip writes norm[1] * grad, rounded once, to out (which may be grad; otherwise it
+ * overlaps no grad and no other out); with a scale of NaN it clips nothing: values in place stay
+ * as they are, others are copied.  norm is read on the device.  moe_grad_norm does not read out.
+ * Limits: max_norm > 0 (infinite: the norm alone), 0 <= n_grads, n < 2^44.
+ */
+typedef struct moe_grad {
+  const void* grad;
+  void* out;
+  size_t n;
+  int dtype;
+} moe_grad;
+size_t moe_grad_norm_workspace_size(const moe_grad* grads, int n_grads);
+int moe_grad_norm(const moe_grad* grads, int n_grads, float max_norm, float* norm, void* ws,
+                  size_t ws_bytes, hipStream_t stream);
+int moe_grad_clip(const moe_grad* grads, int n_grads, const float* norm, hipStream_t stream);
+
+/*
+ * moe_adamw_steps: moe_adamw_step over many tensors, with clipped gradients: tensor i is bit
+ * for bit moe_adamw_step of the fp32 products norm[1] * grad at the rate lr * lr_scale (one fp32
+ * product) with its own weight decay; theta_bf16 may be NULL.  tensors is a HOST array; grad is
+ * fp32 or bf16 (grad_dtype).  norm: what moe_grad_norm wrote, read on the device, or NULL (scale
+ * 1); with a scale of NaN nothing is touched: no step is taken.  The tensors must not overlap.
+ * Arrays 16-byte aligned; n < 2^43.
+ */
+typedef struct moe_adamw_tensor {
+  float* theta;
+  const void* grad;
+  float* m;
+  float* v;
+  void* theta_bf16;
+  size_t n;
+  int grad_dtype;
+  float lr_scale, weight_decay;
+} moe_adamw_tensor;
+int moe_adamw_steps(const moe_adamw_tensor* tensors, int n_tensors, int step, float lr, float beta1,
+                    float beta2, float eps, const float* norm, hipStream_t stream);
 
 /*
  * moe_outer_nesterov: the outer step of a round on the replica-group average

@@ -27,9 +27,11 @@ EXPORTS = [
     "moe_grouped_ffn_bwd_workspace_size", "moe_grouped_ffn_bwd_sets", "moe_combine_fwd",
     "moe_combine_bwd", "moe_layer_fwd", "moe_layer_bwd",
     "moe_layernorm_fwd", "moe_layernorm_bwd_workspace_size", "moe_layernorm_bwd",
+    "moe_block_norm_fwd", "moe_block_norm_bwd_workspace_size", "moe_block_norm_bwd",
     "moe_mxfp4_scale_stride", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
     "moe_mxfp4_ffn_fwd_workspace_size", "moe_mxfp4_ffn_fwd",
     "moe_few_fwd_workspace_size", "moe_few_fwd",
+    "moe_grad_norm_workspace_size", "moe_grad_norm", "moe_grad_clip", "moe_adamw_steps",
     "moe_expert_delta", "moe_adamw_step", "moe_outer_nesterov", "moe_replica_mean",
     "moe_gen_placement", "moe_migration_map", "moe_copy_expert_rows", "moe_warmup_lr",
     "moe_adamw_step_rows", "moe_timing_enable", "moe_timing_collect",
@@ -75,6 +77,13 @@ _SIGS = {
     "moe_layernorm_fwd": (_I, [_P, _P, _P, _I, _I, _I, _F, _P, _P, _P, _P]),
     "moe_layernorm_bwd_workspace_size": (_Z, [_I, _I, _I]),
     "moe_layernorm_bwd": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _Z, _P]),
+    "moe_block_norm_fwd": (_I, [_P, _P]),
+    "moe_block_norm_bwd_workspace_size": (_Z, [_I, _I, _I]),
+    "moe_block_norm_bwd": (_I, [_P, _P]),
+    "moe_grad_norm_workspace_size": (_Z, [_P, _I]),
+    "moe_grad_norm": (_I, [_P, _I, _F, _P, _P, _Z, _P]),
+    "moe_grad_clip": (_I, [_P, _I, _P, _P]),
+    "moe_adamw_steps": (_I, [_P, _I, _I, _F, _F, _F, _F, _P, _P]),
     "moe_mxfp4_scale_stride": (_I, [_I]),
     "moe_mxfp4_quantize": (_I, [_P, _I, _I, _I, _P, _P, _P, _P]),
     "moe_mxfp4_dequantize": (_I, [_P, _P, _I, _I, _I, _P, _P, _P]),
@@ -143,6 +152,29 @@ class moe_few(C.Structure):
     _fields_ += [("ws_bytes", _Z)]
 
 
+class moe_block_norm(C.Structure):
+    """The arguments of the norms around a block (struct moe_block_norm of include/moe_resident.h)."""
+    _fields_ = [(n, _I) for n in ("dtype", "T", "d", "gate_kind")]
+    _fields_ += [("scale", _F), ("eps", _F)]
+    _fields_ += [(n, _P) for n in ("x", "f", "post_weight", "post_bias", "gate", "pre_weight",
+                                   "pre_bias", "x_out", "u", "post_mean", "post_rstd", "pre_mean",
+                                   "pre_rstd", "du", "dres", "dx", "df", "d_post_weight",
+                                   "d_post_bias", "d_gate", "d_pre_weight", "d_pre_bias")]
+    _fields_ += [("accumulate", _I), ("ws", _P), ("ws_bytes", _Z)]
+
+
+class moe_grad(C.Structure):
+    """A gradient of a list (struct moe_grad of include/moe_resident.h)."""
+    _fields_ = [("grad", _P), ("out", _P), ("n", _Z), ("dtype", _I)]
+
+
+class moe_adamw_tensor(C.Structure):
+    """A tensor of AdamW's list (struct moe_adamw_tensor of include/moe_resident.h)."""
+    _fields_ = [("theta", _P), ("grad", _P), ("m", _P), ("v", _P), ("theta_bf16", _P), ("n", _Z),
+                ("grad_dtype", _I), ("lr_scale", _F), ("weight_decay", _F)]
+
+
+BLOCK_GATES = {None: 0, "channel": 1, "token": 2}
 MOE_W_PLAIN, MOE_W_MXFP4 = 0, 1
 MOE_ACT_SWIGLU, MOE_ACT_SILU = 0, 1
 ACTIVATIONS = {"swiglu": MOE_ACT_SWIGLU, "silu": MOE_ACT_SILU}
@@ -347,6 +379,40 @@ def moe_layernorm_bwd(dy, x, weight, mean, rstd, dtype, T, d, dres, dx, dw, db, 
     return _check("moe_layernorm_bwd", lib().moe_layernorm_bwd(
         _ptr(dy), _ptr(x), _ptr(weight), _ptr(mean), _ptr(rstd), dtype, T, d, _ptr(dres), _ptr(dx),
         _ptr(dw), _ptr(db), accumulate_dw, _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_block_norm_fwd(block, stream=None):
+    """block: a moe_block_norm."""
+    return _check("moe_block_norm_fwd", lib().moe_block_norm_fwd(C.byref(block), _stream(stream)))
+
+
+def moe_block_norm_bwd_workspace_size(T, d, dtype) -> int:
+    return lib().moe_block_norm_bwd_workspace_size(T, d, dtype)
+
+
+def moe_block_norm_bwd(block, stream=None):
+    return _check("moe_block_norm_bwd", lib().moe_block_norm_bwd(C.byref(block), _stream(stream)))
+
+
+def moe_grad_norm_workspace_size(grads, n_grads) -> int:
+    """grads: an array of moe_grad."""
+    return lib().moe_grad_norm_workspace_size(grads, n_grads)
+
+
+def moe_grad_norm(grads, n_grads, max_norm, norm, ws, ws_bytes, stream=None):
+    return _check("moe_grad_norm", lib().moe_grad_norm(grads, n_grads, max_norm, _ptr(norm), _ptr(ws),
+                                                       ws_bytes, _stream(stream)))
+
+
+def moe_grad_clip(grads, n_grads, norm, stream=None):
+    return _check("moe_grad_clip", lib().moe_grad_clip(grads, n_grads, _ptr(norm), _stream(stream)))
+
+
+def moe_adamw_steps(tensors, n_tensors, step, lr, beta1=0.9, beta2=0.95, eps=1e-8, norm=None,
+                    stream=None):
+    """tensors: an array of moe_adamw_tensor."""
+    return _check("moe_adamw_steps", lib().moe_adamw_steps(tensors, n_tensors, step, lr, beta1, beta2,
+                                                           eps, _ptr(norm), _stream(stream)))
 
 
 def moe_mxfp4_scale_stride(cols) -> int:

@@ -537,6 +537,70 @@ int moe_layernorm_bwd(const void* dy, const void* x, const float* weight, const 
 }
 
 namespace {
+int check_block(const moe_block_norm* p, bool fwd) {
+  REQUIRE(p != nullptr, "the arguments must not be NULL");
+  int r;
+  if ((r = check_norm(p->dtype, p->T, p->d)) != MOE_OK) return r;
+  REQUIRE(p->gate_kind >= MOE_BLOCK_GATE_NONE && p->gate_kind <= MOE_BLOCK_GATE_TOKEN,
+          "gate_kind = %d is none", p->gate_kind);
+  const bool channel = p->gate_kind == MOE_BLOCK_GATE_CHANNEL, token = p->gate_kind == MOE_BLOCK_GATE_TOKEN;
+  const bool post = p->post_weight != nullptr, pre = p->pre_weight != nullptr, any = p->T > 0;
+  REQUIRE(std::isfinite(p->scale), "scale must be finite");
+  REQUIRE(post || pre, "post_weight and pre_weight must not both be NULL");
+  REQUIRE(post || !p->post_bias, "post_bias without post_weight");
+  REQUIRE(pre || !p->pre_bias, "pre_bias without pre_weight");
+  REQUIRE(p->gate_kind == MOE_BLOCK_GATE_NONE ? !p->gate : p->gate || (token && !any),
+          "gate must be given with its gate_kind, and only then");
+  REQUIRE(!any || !post || (p->post_mean && p->post_rstd), "post_mean and post_rstd must not be NULL");
+  REQUIRE(!any || !pre || (p->pre_mean && p->pre_rstd), "pre_mean and pre_rstd must not be NULL");
+  const float* gate16 = channel ? p->gate : nullptr;
+  for (const void* q : {(const void*)p->f, (const void*)p->x_out, (const void*)p->post_weight,
+                        (const void*)p->post_bias, (const void*)gate16, (const void*)p->pre_weight,
+                        (const void*)p->pre_bias})
+    SUPPORT(q == nullptr || aligned16(q), "arrays must be 16-byte aligned");
+  if (fwd) {
+    REQUIRE(std::isfinite(p->eps) && p->eps >= 0.f, "eps must be finite and >= 0");
+    REQUIRE(!any || (p->x && p->f && p->x_out), "x, f and x_out must not be NULL");
+    REQUIRE(!any || pre == (p->u != nullptr), "u must be given with pre_weight, and only then");
+    SUPPORT(aligned16(p->x) && aligned16(p->u), "arrays must be 16-byte aligned");
+    return MOE_OK;
+  }
+  REQUIRE(!any || (p->f && p->dx && p->df), "f, dx and df must not be NULL");
+  REQUIRE(!any || !pre || (p->du && p->x_out), "du and x_out must not be NULL");
+  REQUIRE(!any || pre || p->dres, "dres must not be NULL without a pre-norm");
+  REQUIRE(!pre || p->d_pre_weight, "d_pre_weight must not be NULL");
+  REQUIRE(!post || p->d_post_weight, "d_post_weight must not be NULL");
+  REQUIRE(p->gate_kind == MOE_BLOCK_GATE_NONE || p->d_gate || (token && !any), "d_gate must not be NULL");
+  const float* d_gate16 = channel ? p->d_gate : nullptr;
+  for (const void* q : {p->du, p->dres, (const void*)p->dx, (const void*)p->df,
+                        (const void*)p->d_post_weight, (const void*)p->d_post_bias, (const void*)d_gate16,
+                        (const void*)p->d_pre_weight, (const void*)p->d_pre_bias, (const void*)p->ws})
+    SUPPORT(q == nullptr || aligned16(q), "arrays must be 16-byte aligned");
+  const size_t need = moe::block_norm_ws_bytes(p->T, p->d, p->dtype == MOE_BF16);
+  REQUIRE(need == 0 || (p->ws && p->ws_bytes >= need), "workspace of %zu bytes needed (got %zu)", need,
+          p->ws_bytes);
+  return MOE_OK;
+}
+}  // namespace
+
+int moe_block_norm_fwd(const moe_block_norm* p, hipStream_t stream) {
+  const int r = check_block(p, true);
+  if (r != MOE_OK) return r;
+  return hip_status(moe::launch_block_norm_fwd(p, stream), "moe_block_norm_fwd");
+}
+
+size_t moe_block_norm_bwd_workspace_size(int T, int d, int dtype) {
+  if (check_norm(dtype, T, d) != MOE_OK) return 0;
+  return moe::block_norm_ws_bytes(T, d, dtype == MOE_BF16);
+}
+
+int moe_block_norm_bwd(const moe_block_norm* p, hipStream_t stream) {
+  const int r = check_block(p, false);
+  if (r != MOE_OK) return r;
+  return hip_status(moe::launch_block_norm_bwd(p, stream), "moe_block_norm_bwd");
+}
+
+namespace {
 int check_mx(int dtype, int rows, int cols, const void* x, const uint8_t* codes,
              const uint8_t* scales) {
   int r;
@@ -700,6 +764,78 @@ int moe_adamw_step(float* theta, const float* grad, float* m, float* v, size_t n
   return hip_status(moe::launch_adamw(theta, grad, m, v, n, lr, beta1, beta2, eps, weight_decay,
                                       c1, c2, theta_bf16, stream),
                     "moe_adamw_step");
+}
+
+namespace {
+int check_grads(const moe_grad* g, int n, bool out) {
+  REQUIRE(n >= 0, "n_grads = %d must be >= 0", n);
+  REQUIRE(n == 0 || g, "grads must not be NULL");
+  for (int i = 0; i < n; ++i) {
+    int r;
+    if ((r = check_dtype(g[i].dtype)) != MOE_OK) return r;
+    REQUIRE(g[i].n == 0 || (g[i].grad && (!out || g[i].out)), "tensor %d: grad%s must not be NULL", i,
+            out ? " and out" : "");
+    SUPPORT(g[i].n < (size_t)1 << 44, "tensor %d: %zu values are too many", i, g[i].n);
+    const uintptr_t size = g[i].dtype == MOE_BF16 ? 2 : 4;
+    SUPPORT(((uintptr_t)g[i].grad | (out ? (uintptr_t)g[i].out : 0)) % size == 0,
+            "tensor %d must be aligned to its type", i);
+  }
+  return MOE_OK;
+}
+}  // namespace
+
+size_t moe_grad_norm_workspace_size(const moe_grad* grads, int n_grads) {
+  if (check_grads(grads, n_grads, false) != MOE_OK) return 0;
+  return moe::grad_norm_ws_bytes(grads, n_grads);
+}
+
+int moe_grad_norm(const moe_grad* grads, int n_grads, float max_norm, float* norm, void* ws,
+                  size_t ws_bytes, hipStream_t stream) {
+  const int r = check_grads(grads, n_grads, false);
+  if (r != MOE_OK) return r;
+  REQUIRE(max_norm > 0.f, "max_norm must be > 0");
+  REQUIRE(norm, "norm must not be NULL");
+  SUPPORT((uintptr_t)norm % 4 == 0 && (uintptr_t)ws % 8 == 0, "norm and ws must be aligned");
+  const size_t need = moe::grad_norm_ws_bytes(grads, n_grads);
+  REQUIRE(need == 0 || (ws && ws_bytes >= need), "workspace of %zu bytes needed (got %zu)", need,
+          ws_bytes);
+  return hip_status(moe::launch_grad_norm(grads, n_grads, max_norm, norm, ws, stream),
+                    "moe_grad_norm");
+}
+
+int moe_grad_clip(const moe_grad* grads, int n_grads, const float* norm, hipStream_t stream) {
+  const int r = check_grads(grads, n_grads, true);
+  if (r != MOE_OK) return r;
+  REQUIRE(norm, "norm must not be NULL");
+  SUPPORT((uintptr_t)norm % 4 == 0, "norm must be aligned");
+  return hip_status(moe::launch_grad_clip(grads, n_grads, norm, stream), "moe_grad_clip");
+}
+
+int moe_adamw_steps(const moe_adamw_tensor* tensors, int n_tensors, int step, float lr, float beta1,
+                    float beta2, float eps, const float* norm, hipStream_t stream) {
+  REQUIRE(n_tensors >= 0, "n_tensors = %d must be >= 0", n_tensors);
+  REQUIRE(n_tensors == 0 || tensors, "tensors must not be NULL");
+  REQUIRE(step >= 1, "step = %d must be >= 1", step);
+  REQUIRE(beta1 >= 0.f && beta1 < 1.f && beta2 >= 0.f && beta2 < 1.f && eps >= 0.f,
+          "betas must lie in [0, 1) and eps must be >= 0");
+  SUPPORT((uintptr_t)norm % 4 == 0, "norm must be aligned");
+  for (int i = 0; i < n_tensors; ++i) {
+    const moe_adamw_tensor& p = tensors[i];
+    int r;
+    if ((r = check_dtype(p.grad_dtype)) != MOE_OK) return r;
+    REQUIRE(p.n == 0 || (p.theta && p.grad && p.m && p.v),
+            "tensor %d: theta, grad, m and v must not be NULL", i);
+    SUPPORT(p.n < (size_t)1 << 43, "tensor %d: %zu values are too many", i, p.n);
+    for (const void* q : {(const void*)p.theta, p.grad, (const void*)p.m, (const void*)p.v,
+                          (const void*)p.theta_bf16})
+      SUPPORT(q == nullptr || aligned16(q), "tensor %d: arrays must be 16-byte aligned", i);
+  }
+  const float c1 = (float)(1.0 - std::pow((double)beta1, (double)step));
+  const float c2 = (float)(1.0 - std::pow((double)beta2, (double)step));
+  REQUIRE(c1 > 0.f && c2 > 0.f, "bias corrections must be positive (betas > 0 at step %d)", step);
+  return hip_status(moe::launch_adamw_steps(tensors, n_tensors, lr, beta1, beta2, eps, c1, c2, norm,
+                                            stream),
+                    "moe_adamw_steps");
 }
 
 int moe_outer_nesterov(float* theta_start, float* theta_now, const float* delta_avg,

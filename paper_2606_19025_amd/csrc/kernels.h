@@ -103,6 +103,16 @@ hipError_t launch_outer_nesterov(float* start, float* now, const float* delta, f
 hipError_t launch_replica_mean(const float* local, const float* const* peers, int n_peers,
                                size_t n, float* out, hipStream_t s);
 
+// AdamW over many tensors (optim.hip); norm: NULL, or what launch_grad_norm wrote.
+hipError_t launch_adamw_steps(const moe_adamw_tensor* p, int n, float lr, float beta1, float beta2,
+                              float eps, float c1, float c2, const float* norm, hipStream_t s);
+
+// The gradients' norm and clipping (grad.hip).
+size_t grad_norm_ws_bytes(const moe_grad* g, int n);
+hipError_t launch_grad_norm(const moe_grad* g, int n, float max_norm, float* norm, void* ws,
+                            hipStream_t s);
+hipError_t launch_grad_clip(const moe_grad* g, int n, const float* norm, hipStream_t s);
+
 // Layer norm (norm.hip), the MoE layer's pre-norm.  The backward's ws holds one partial
 // row of dw and db per block (norm_bwd_ws_bytes()); its contents on entry are ignored.
 constexpr int kMaxNormWidth = 16384;
@@ -112,6 +122,11 @@ size_t norm_bwd_ws_bytes(int T, int d, int bf16);
 hipError_t launch_norm_bwd(const void* dy, const void* x, const float* w, const float* mean,
                            const float* rstd, int bf16, int T, int d, const void* dres, void* dx,
                            float* dw, float* db, int accumulate, void* ws, hipStream_t s);
+
+// The norms and the residual sum around a block (block_norm.hip).
+hipError_t launch_block_norm_fwd(const moe_block_norm* p, hipStream_t s);
+size_t block_norm_ws_bytes(int T, int d, int bf16);
+hipError_t launch_block_norm_bwd(const moe_block_norm* p, hipStream_t s);
 
 // The whole layer for a few tokens (few.hip).
 constexpr int kFewTokens = 64, kFewRoutes = 8;

@@ -84,6 +84,75 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   }
 }
 
+// AdamW over many tensors, gradients multiplied by the clip's scale first: a launch covers up to
+// kAdamTensors tensors, whose table is a kernel argument; tensors are cut into chunks of kAdamChunk
+// values, which the blocks take in turn.
+constexpr int kAdamTensors = 44, kAdamChunk = 8192;
+struct AdamTable {
+  float* theta[kAdamTensors];
+  const void* grad[kAdamTensors];
+  float* m[kAdamTensors];
+  float* v[kAdamTensors];
+  bf16_t* low[kAdamTensors];  // or NULL
+  size_t n[kAdamTensors];
+  float lr[kAdamTensors], wd[kAdamTensors];
+  int first[kAdamTensors + 1];  // chunks before each tensor
+  uint8_t bf16[kAdamTensors];   // the gradient's type
+  int count;
+  float b1, b2, eps, c1, c2;
+};
+static_assert(sizeof(AdamTable) <= 3900, "kernel arguments hold 4 KiB");
+
+__global__ __launch_bounds__(256) void adamw_steps_kernel(AdamTable t, const float* norm) {
+  const float scale = norm ? norm[1] : 1.0f;
+  if (scale != scale) return;  // the gradients' norm is not finite: no step
+  const int chunks = t.first[t.count];
+  for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+    int q = 0;
+    for (int hi = t.count - 1; q < hi;) {
+      const int mid = (q + hi + 1) >> 1;
+      if (t.first[mid] <= c) q = mid;
+      else hi = mid - 1;
+    }
+    const size_t at = (size_t)(c - t.first[q]) * kAdamChunk;
+    const int n = (int)min(t.n[q] - at, (size_t)kAdamChunk), n4 = n / 4;
+    float* const th = t.theta[q] + at;
+    float* const m = t.m[q] + at;
+    float* const v = t.v[q] + at;
+    bf16_t* const low = t.low[q] ? t.low[q] + at : nullptr;
+    const bool bf16 = t.bf16[q];
+    const float* const g = static_cast<const float*>(t.grad[q]) + (bf16 ? 0 : at);
+    const bf16_t* const gb = static_cast<const bf16_t*>(t.grad[q]) + (bf16 ? at : 0);
+    AdamArgs a{};
+    a.lr = t.lr[q]; a.wd = t.wd[q];
+    a.b1 = t.b1; a.b2 = t.b2; a.eps = t.eps; a.c1 = t.c1; a.c2 = t.c2;
+    for (int i = threadIdx.x; i < n4; i += 256) {
+      f32x4_t tt = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(th) + i);
+      f32x4_t mm = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(m) + i);
+      f32x4_t vv = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(v) + i);
+      f32x4_t gg;
+      if (bf16) gg = __builtin_convertvector(reinterpret_cast<const bf16x4_t*>(gb)[i], f32x4_t);
+      else gg = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(g) + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float x = tt[e], y = mm[e], z = vv[e];
+        adam_elem(a, x, gg[e] * scale, y, z);
+        tt[e] = x; mm[e] = y; vv[e] = z;
+      }
+      __builtin_nontemporal_store(tt, reinterpret_cast<f32x4_t*>(th) + i);
+      __builtin_nontemporal_store(mm, reinterpret_cast<f32x4_t*>(m) + i);
+      __builtin_nontemporal_store(vv, reinterpret_cast<f32x4_t*>(v) + i);
+      if (low) reinterpret_cast<bf16x4_t*>(low)[i] = __builtin_convertvector(tt, bf16x4_t);
+    }
+    for (int i = n4 * 4 + threadIdx.x; i < n; i += 256) {
+      float x = th[i], y = m[i], z = v[i];
+      adam_elem(a, x, (bf16 ? (float)gb[i] : g[i]) * scale, y, z);
+      th[i] = x; m[i] = y; v[i] = z;
+      if (low) low[i] = (bf16_t)x;
+    }
+  }
+}
+
 struct OuterArgs {
   float* start;
   float* now;
@@ -169,6 +238,35 @@ hipError_t launch_adamw(float* theta, const float* grad, float* m, float* v, siz
              c1, c2};
   MOE_TIMED("adamw_step", s, adamw_kernel<<<stream_blocks(n, kFewBlocks, n >= (64u << 20) ? 1 : 2), 256, 0, s>>>(a));
   return hipGetLastError();
+}
+
+hipError_t launch_adamw_steps(const moe_adamw_tensor* p, int n, float lr, float beta1, float beta2,
+                              float eps, float c1, float c2, const float* norm, hipStream_t s) {
+  AdamTable t;
+  t.b1 = beta1; t.b2 = beta2; t.eps = eps; t.c1 = c1; t.c2 = c2;
+  t.count = 0;
+  t.first[0] = 0;
+  for (int i = 0; i <= n; ++i) {
+    const bool end = i == n;
+    // (a launch's chunks are counted in 31 bits: a tensor that does not fit opens the next)
+    const int64_t chunks = end ? 0 : (int64_t)((p[i].n + kAdamChunk - 1) / kAdamChunk);
+    if (t.count > 0 && (end || t.count == kAdamTensors || t.first[t.count] + chunks > INT32_MAX)) {
+      const int blocks = std::min(t.first[t.count], 2 * num_cus());
+      MOE_TIMED("adamw_steps", s, adamw_steps_kernel<<<blocks, 256, 0, s>>>(t, norm));
+      if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      t.count = 0;
+    }
+    if (end || chunks == 0) continue;
+    const int k = t.count++;
+    t.theta[k] = p[i].theta; t.grad[k] = p[i].grad; t.m[k] = p[i].m; t.v[k] = p[i].v;
+    t.low[k] = static_cast<bf16_t*>(p[i].theta_bf16);
+    t.n[k] = p[i].n;
+    t.lr[k] = lr * p[i].lr_scale;
+    t.wd[k] = p[i].weight_decay;
+    t.bf16[k] = p[i].grad_dtype == MOE_BF16;
+    t.first[k + 1] = t.first[k] + (int)chunks;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_outer_nesterov(float* start, float* now, const float* delta, float* mom,

@@ -352,6 +352,151 @@ class PreNormMoELayer:
                                   stream=stream)
 
 
+class BlockNorm:
+    """The norms and the residual sum between one block and the next, moe_block_norm_fwd / _bwd:
+    x' = x + scale g n with n = norm(f) (``post``; else f), then u = norm(x') (``pre``).  gate: None,
+    "channel" (g [d]) or "token" (g [T]); bias: whether the norms have biases.
+
+    Buffers of its own, which the next call reuses: x, u and the norms' statistics (post_mean,
+    post_rstd, pre_mean, pre_rstd) of the forward; dx, df (from the first backward on) and the
+    gradients d_post_weight, d_post_bias, d_gate, d_pre_weight, d_pre_bias of the backward.  As with
+    ``LayerNorm``, calls on different streams need one each, and a call on another stream than the
+    one current at construction, where the gradients are set to zero, has to be ordered behind it."""
+
+    def __init__(self, T, d, dtype=torch.bfloat16, post=True, pre=True, gate=None, bias=True,
+                 scale=1.0, eps=1e-5, device="cuda"):
+        self.T, self.d, self.post, self.pre, self.bias = int(T), int(d), bool(post), bool(pre), bool(bias)
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"unsupported dtype {dtype}")
+        if gate not in B.BLOCK_GATES:
+            raise ValueError(f"gate must be None, 'channel' or 'token', got {gate!r}")
+        if not (self.post or self.pre):
+            raise ValueError("a block needs a norm before or behind it")
+        self.dtype, self.gate, f32 = dtype, gate, torch.float32
+        new = lambda *s, dt=f32: torch.empty(*s, dtype=dt, device=device)
+        zeros = lambda there, *s: torch.zeros(*s, dtype=f32, device=device) if there else None
+        self.x = new(self.T, self.d, dt=dtype)
+        self.device = self.x.device
+        self.u = new(self.T, self.d, dt=dtype) if self.pre else None
+        self.post_mean, self.post_rstd = (new(self.T) if self.post else None for _ in range(2))
+        self.pre_mean, self.pre_rstd = (new(self.T) if self.pre else None for _ in range(2))
+        # zeros, and here: the first backward may add to them, in a captured graph too
+        self.d_post_weight = zeros(self.post, self.d)
+        self.d_post_bias = zeros(self.post and self.bias, self.d)
+        self.d_pre_weight = zeros(self.pre, self.d)
+        self.d_pre_bias = zeros(self.pre and self.bias, self.d)
+        self.gate_shape = (self.T,) if gate == "token" else (self.d,)
+        self.d_gate = zeros(gate is not None, *self.gate_shape)
+        self.dx = self.df = self.ws = None
+        p = B._ptr
+        self._args = B.moe_block_norm(
+            dtype=B.MOE_BF16 if dtype == torch.bfloat16 else B.MOE_F32, T=self.T, d=self.d,
+            gate_kind=B.BLOCK_GATES[gate], scale=float(scale), eps=float(eps),
+            d_post_weight=p(self.d_post_weight), d_post_bias=p(self.d_post_bias),
+            d_gate=p(self.d_gate), d_pre_weight=p(self.d_pre_weight), d_pre_bias=p(self.d_pre_bias))
+
+    def _check(self, name, t, shape, dtype):
+        _check_tensor(name, t, shape, dtype, self.device, "norm")
+
+    def _vector(self, name, t, there, shape):
+        """The address of a vector of floats that is there, or not, by the norm's form."""
+        if there:
+            self._check(name, t, shape, torch.float32)
+            return t.data_ptr()
+        if t is not None:
+            raise ValueError(f"{name} given to a norm built without one")
+        return None
+
+    def _weights(self, post_weight, post_bias, gate, pre_weight, pre_bias=None, forward=False):
+        a, d = self._args, (self.d,)
+        a.post_weight = self._vector("post_weight", post_weight, self.post, d)
+        a.post_bias = self._vector("post_bias", post_bias, self.post and self.bias, d)
+        a.gate = self._vector("gate", gate, self.gate is not None, self.gate_shape)
+        a.pre_weight = self._vector("pre_weight", pre_weight, self.pre, d)
+        # (the backward reads no bias of the pre-norm)
+        a.pre_bias = self._vector("pre_bias", pre_bias, forward and self.pre and self.bias, d)
+
+    def _rows(self, **stats):
+        for name, t in stats.items():
+            own = getattr(self, name)
+            if t is not None and own is None:
+                raise ValueError(f"{name} given to a norm built without one")
+            if t is not None:
+                self._check(name, t, (self.T,), torch.float32)
+            setattr(self._args, name, B._ptr(own if t is None else t))
+
+    def forward(self, x, f, post_weight=None, post_bias=None, gate=None, pre_weight=None,
+                pre_bias=None, stream=None):
+        """(x', u) of the residual stream x and the block's output f (u: None without a pre-norm)."""
+        _check_current(self.device, "norm")
+        self._check("x", x, (self.T, self.d), self.dtype)
+        self._check("f", f, (self.T, self.d), self.dtype)
+        self._weights(post_weight, post_bias, gate, pre_weight, pre_bias, forward=True)
+        self._rows(post_mean=None, post_rstd=None, pre_mean=None, pre_rstd=None)
+        a = self._args
+        a.x, a.f, a.x_out, a.u = x.data_ptr(), f.data_ptr(), self.x.data_ptr(), B._ptr(self.u)
+        B.moe_block_norm_fwd(a, stream)
+        return self.x, self.u
+
+    def backward(self, du, f, post_weight=None, post_bias=None, gate=None, pre_weight=None, dres=None,
+                 x=None, post_mean=None, post_rstd=None, pre_mean=None, pre_rstd=None, accumulate=0,
+                 stream=None):
+        """(dx, df), with the weights' gradients beside them.  du, dres: the gradients of u (None
+        without a pre-norm) and of x' past the next block.  x and the statistics: x' and those of
+        the forward, where they are not the last one's.  accumulate adds to the gradients over [d]."""
+        _check_current(self.device, "norm")
+        x = self.x if x is None else x
+        if (du is None) == self.pre:
+            raise ValueError("du is the gradient of u: given with a pre-norm, and only then")
+        if dres is None and not self.pre:
+            raise ValueError("dres is needed without a pre-norm")
+        for name, t in (("du", du), ("dres", dres), ("f", f), ("x", x)):
+            if t is not None:
+                self._check(name, t, (self.T, self.d), self.dtype)
+        a = self._args
+        self._weights(post_weight, post_bias, gate, pre_weight)
+        self._rows(post_mean=post_mean, post_rstd=post_rstd, pre_mean=pre_mean, pre_rstd=pre_rstd)
+        if self.ws is None:
+            a.ws_bytes = B.moe_block_norm_bwd_workspace_size(self.T, self.d, a.dtype)
+            with _on(stream):
+                self.dx, self.df = torch.empty_like(self.x), torch.empty_like(self.x)
+                self.ws = torch.empty(max(a.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+            a.dx, a.df, a.ws = self.dx.data_ptr(), self.df.data_ptr(), self.ws.data_ptr()
+        a.du, a.dres, a.f, a.x_out = B._ptr(du), B._ptr(dres), f.data_ptr(), x.data_ptr()
+        a.accumulate = int(accumulate)
+        B.moe_block_norm_bwd(a, stream)
+        return self.dx, self.df
+
+
+class PeriNormMoELayer:
+    """ResidentMoELayer as a Peri-LN block: x' = x + scale g norm(moe(u)), u' = norm(x'), where u is
+    the normed stream that the block before it left (the first: a ``LayerNorm`` of x).
+
+    forward returns (x', u'), which the next block takes (u': None with ``pre=False``, behind the
+    last block); backward takes their gradients (du', dres) and returns those of u and x, which the
+    block before takes as its own.  ``layer`` and ``norm`` hold the outputs and gradients."""
+
+    def __init__(self, T, d, E, k, H, resident, dtype=torch.bfloat16, pre=True, gate=None,
+                 norm_bias=True, scale=1.0, eps=1e-5, device="cuda", **kw):
+        self.layer = ResidentMoELayer(T, d, E, k, H, resident, dtype=dtype, device=device, **kw)
+        self.norm = BlockNorm(T, d, dtype=dtype, pre=pre, gate=gate, bias=norm_bias, scale=scale,
+                              eps=eps, device=device)
+
+    def forward(self, x, u, norms, w_router, w_gate_up, w_down, stream=None, **kw):
+        """norms: the weights of ``BlockNorm.forward``, as a dict."""
+        f = self.layer.forward(u, w_router, w_gate_up, w_down, stream=stream, **kw)
+        return self.norm.forward(x, f, **norms, stream=stream)
+
+    def backward(self, du, dres, u, norms, w_router, w_gate_up, w_down, accumulate_dw=0, stream=None,
+                 **kw):
+        """(gradient of u, gradient of x), with the layer's and the norms' weight gradients."""
+        norms = {k: v for k, v in norms.items() if k != "pre_bias"}
+        dx, df = self.norm.backward(du, self.layer.y, **norms, dres=dres, accumulate=accumulate_dw,
+                                    stream=stream)
+        return self.layer.backward(df, u, w_router, w_gate_up, w_down, accumulate_dw=accumulate_dw,
+                                   stream=stream, **kw), dx
+
+
 def _mx_cols(x):
     if not isinstance(x, torch.Tensor) or x.dim() < 2:
         raise ValueError("MXFP4 takes tensors of rows: [..., rows, cols]")

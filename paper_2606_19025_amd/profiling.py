@@ -86,6 +86,8 @@ _SYMBOLS = [
     (r"copy_expert_rows_kernel", lambda m: "copy_expert_rows"),
     (r"mx_gemm_kernel(?:<|ILi)(\d)", lambda m: "mx_gemm_" + ("gu", "up", "down")[int(m.group(1))]),
     (r"few_logits_(?:bf16|f32)_kernel", lambda m: "few_logits"),
+    (r"(block_norm_fwd|block_norm_bwd|block_norm_dw|grad_norm_sum|grad_norm|grad_clip|adamw_steps)_kernel",
+     lambda m: m.group(1)),
     (r"(norm_fwd|norm_bwd|norm_dw|mx_quantize|mx_dequantize|few_gu|few_down)_kernel", lambda m: m.group(1)),
 ]
 
@@ -94,7 +96,8 @@ _SOURCES = [("gemm_", "gemm.hip"), ("splitk_", "gemm.hip"), ("zero_counters", "g
             ("combine_", "dispatch.hip"), ("unpermute", "dispatch.hip"),
             ("expert_delta", "dispatch.hip"), ("adamw", "optim.hip"), ("outer_", "optim.hip"),
             ("replica_", "optim.hip"),
-            ("copy_expert_rows", "placement.hip"), ("norm_", "norm.hip"), ("mx_gemm", "gemm_mx.hip"), ("mx_", "mx.hip"),
+            ("copy_expert_rows", "placement.hip"), ("norm_", "norm.hip"),
+            ("block_norm_", "block_norm.hip"), ("grad_", "grad.hip"), ("mx_gemm", "gemm_mx.hip"), ("mx_", "mx.hip"),
             ("few_logits", "few.hip"), ("few_", "few.h")]
 
 
@@ -126,7 +129,8 @@ def source_digest(name: str) -> str | None:
             h = hashlib.sha256()
             if name.endswith("_tile"):
                 fname = "gemm_tile.hip"
-            for f in (fname, "common.h") + (("gemm.h",) if fname.startswith("gemm") else ()):
+            more = ("gemm.h",) if fname.startswith("gemm") else ("norm_rows.h",) if "norm" in fname else ()
+            for f in (fname, "common.h") + more:
                 with open(os.path.join(CSRC, f)) as fh:
                     h.update(_code_only(fh.read()).encode())
             return h.hexdigest()[:16]

@@ -1,0 +1,130 @@
+"""What a worker's training step needs behind its layers: the gradients' norm, clipping and AdamW
+over all parameters.
+
+As in ``layer``, the classes own buffers and issue the C entry points; they compute nothing
+themselves.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+from .layer import _check_current, _check_tensor, _on
+
+
+def _device(tensors, owner):
+    """The device of a list of tensors, all contiguous and on it."""
+    for i, t in enumerate(tensors):
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{owner} {i} must be a tensor, got {type(t).__name__}")
+    if not tensors:
+        raise ValueError(f"no {owner} given")
+    return tensors[0].device
+
+
+def _disjoint(name, tensors):
+    """Raise ValueError if two of the tensors share memory."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), i)
+                   for i, t in enumerate(tensors) if t is not None and t.numel())
+    for (_, end, i), (begin, _, j) in zip(spans, spans[1:]):
+        if begin < end:
+            raise ValueError(f"{name} {i} and {j} overlap")
+
+
+class GradClipper:
+    """The norm of the given gradients together, and clipping by it: moe_grad_norm, moe_grad_clip.
+
+    grads: contiguous fp32 or bf16 tensors, read where they lie at every call (a layer's gradient
+    buffers).  max_norm: infinite measures alone.  out: where the clipped gradients go, tensors like
+    grads (None: in place).  ``norm`` holds the norm and the scale min(1, max_norm / norm) of the last
+    call, on the GPU; a norm that is not finite has the scale NaN and clips nothing."""
+
+    def __init__(self, grads, max_norm, out=None):
+        grads = list(grads)
+        self.device = _device(grads, "gradient")
+        self.max_norm = float(max_norm)
+        if not self.max_norm > 0:
+            raise ValueError(f"max_norm must be positive, got {max_norm}")
+        out = grads if out is None else list(out)
+        if len(out) != len(grads):
+            raise ValueError(f"{len(out)} outputs for {len(grads)} gradients")
+        for i, (g, o) in enumerate(zip(grads, out)):
+            if g.dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError(f"gradient {i} has dtype {g.dtype}: float32 or bfloat16")
+            _check_tensor(f"gradient {i}", g, g.shape, g.dtype, self.device, "clipper")
+            _check_tensor(f"output {i}", o, g.shape, g.dtype, self.device, "clipper")
+        _disjoint("outputs", out)
+        self._held = grads, out  # (the library keeps addresses only)
+        self.n = len(grads)
+        self._grads = (B.moe_grad * self.n)(*[
+            B.moe_grad(g.data_ptr(), o.data_ptr(), g.numel(), B.dtype_code(g))
+            for g, o in zip(grads, out)])
+        self.ws_bytes = B.moe_grad_norm_workspace_size(self._grads, self.n)
+        self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+        self.norm = torch.empty(2, dtype=torch.float32, device=self.device)
+
+    def measure(self, stream=None):
+        """[norm, scale] of the gradients as they are."""
+        _check_current(self.device, "clipper")
+        B.moe_grad_norm(self._grads, self.n, self.max_norm, self.norm, self.ws, self.ws_bytes, stream)
+        return self.norm
+
+    def clip(self, stream=None):
+        """[norm, scale], and the gradients clipped."""
+        self.measure(stream)
+        B.moe_grad_clip(self._grads, self.n, self.norm, stream)
+        return self.norm
+
+
+class AdamW:
+    """AdamW on many fp32 tensors at once, moe_adamw_steps, with the gradients clipped on the way
+    (max_norm; None: as they are).
+
+    theta, m, v: lists of fp32 tensors, updated in place; grads: fp32 or bf16, read where they lie
+    at every step; theta_bf16: a list of bf16 tensors (or of None among them) that receive the
+    updated parameters.  weight_decay and lr_scale: a number, or one for each tensor.  ``norm`` holds
+    the last step's [norm, scale]; a step whose norm is not finite changes nothing."""
+
+    def __init__(self, theta, grads, m=None, v=None, theta_bf16=None, max_norm=None,
+                 betas=(0.9, 0.95), eps=1e-8, weight_decay=0.0, lr_scale=1.0):
+        theta, grads = list(theta), list(grads)
+        dev = self.device = _device(theta, "parameter")
+        n = self.n = len(theta)
+        self.m = [torch.zeros_like(t) for t in theta] if m is None else list(m)
+        self.v = [torch.zeros_like(t) for t in theta] if v is None else list(v)
+        low = [None] * n if theta_bf16 is None else list(theta_bf16)
+        each = lambda x: [float(x)] * n if isinstance(x, (int, float)) else [float(y) for y in x]
+        decay, rate = each(weight_decay), each(lr_scale)
+        for name, lst in (("grads", grads), ("m", self.m), ("v", self.v), ("theta_bf16", low),
+                          ("weight_decay", decay), ("lr_scale", rate)):
+            if len(lst) != n:
+                raise ValueError(f"{len(lst)} {name} for {n} parameters")
+        for i, t in enumerate(theta):
+            for name, u in (("parameter", t), ("m", self.m[i]), ("v", self.v[i])):
+                _check_tensor(f"{name} {i}", u, t.shape, torch.float32, dev, "optimiser")
+            g = grads[i]
+            if getattr(g, "dtype", None) is not torch.bfloat16:
+                _check_tensor(f"gradient {i}", g, t.shape, torch.float32, dev, "optimiser")
+            else:
+                _check_tensor(f"gradient {i}", g, t.shape, torch.bfloat16, dev, "optimiser")
+            if low[i] is not None:
+                _check_tensor(f"theta_bf16 {i}", low[i], t.shape, torch.bfloat16, dev, "optimiser")
+        _disjoint("tensors", theta + self.m + self.v + low)
+        self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
+        self._clipper = None if max_norm is None else GradClipper(grads, max_norm)
+        self.norm = None if max_norm is None else self._clipper.norm
+        self._held = theta, grads, low  # (the library keeps addresses only)
+        p = B._ptr
+        self._tensors = (B.moe_adamw_tensor * n)(*[
+            B.moe_adamw_tensor(p(theta[i]), p(grads[i]), p(self.m[i]), p(self.v[i]), p(low[i]),
+                               theta[i].numel(), B.dtype_code(grads[i]), rate[i], decay[i])
+            for i in range(n)])
+
+    def step(self, t, lr, stream=None):
+        """Step t (1 for the first) at rate lr; returns [norm, scale] (None without max_norm)."""
+        _check_current(self.device, "optimiser")
+        if self._clipper is not None:
+            self._clipper.measure(stream)
+        B.moe_adamw_steps(self._tensors, self.n, int(t), float(lr), *self.betas, self.eps, self.norm,
+                          stream)
+        return self.norm
