@@ -449,6 +449,54 @@ size_t moe_block_norm_bwd_workspace_size(int T, int d, int dtype);
 int moe_block_norm_bwd(const moe_block_norm* p, hipStream_t stream);
 
 /*
+ * Softmax cross entropy of a linear head over a vocabulary, the loss at the end of a training
+ * step, without the logits being kept (a tile of them at a time, a piece of the vocabulary's
+ * gradients in the backward):
+ *   z[t,v]  = scale x[t,:] . w[v,:];   lse[t] = log sum_v exp z[t,v]
+ *   loss[t] = lse[t] - z[t,labels[t]] + z_coef lse[t]^2
+ *   total   = {sum_t loss[t], the number of tokens that count}
+ * A token whose label is negative does not count: loss and lse are 0, its dx is 0, nothing of its
+ * row of x is used, and its products are left out.  A label of V or more makes the loss NaN, and in
+ * the backward its dx and dw.
+ * x [N,d], w [V,d] dtype; labels [N] int32; loss, lse [N], total [2] fp32.
+ *
+ * moe_xent_bwd, from the forward's lse and the gradients dloss [N] of the losses (NULL: those of
+ * the mean over the tokens that count):
+ *   dz[t,v] = dloss[t] scale ((1 + 2 z_coef lse[t]) exp(z[t,v] - lse[t]) - (v == labels[t]))
+ *   dx[t,:] = sum_v dz[t,v] w[v,:]                (dtype)
+ *   dw[v,:] (+)= sum_t dz[t,v] x[t,:]             (dw_dtype: MOE_F32, or dtype)
+ * dz is rounded once to dtype; sums are fp32, dx is rounded once, dw is added to where accumulate_dw
+ * != 0 and rounded after the sum.  loss and total are not read.
+ * ws: device workspace (256-byte aligned) of at least moe_xent_fwd_workspace_size(p) or
+ * moe_xent_bwd_workspace_size(p) bytes (which depend on the sizes and types alone and on the
+ * current device's compute-unit count; the backward's holds up to 512 MiB of dz and 256 MiB of
+ * partial sums besides a copy of x and one of dx in fp32); its contents on entry are ignored.
+ * Two calls may share it only if they are ordered on a stream.
+ * Limits: 0 <= N < 2^27, V >= 1; bf16: d % 64 == 0, N d below 2^31 - 16; fp32: d % 8 == 0; d <= 2^16;
+ * scale and z_coef finite; x, w, dx and dw 16-byte aligned.
+ */
+typedef struct moe_xent {
+  int dtype, N, d, V;
+  float scale, z_coef;
+  const void* x;
+  const void* w;
+  const int32_t* labels;
+  float* loss;
+  float* lse;
+  float* total;
+  const float* dloss; /* from here on: backward */
+  void* dx;
+  void* dw;
+  int dw_dtype, accumulate_dw;
+  void* ws;
+  size_t ws_bytes;
+} moe_xent;
+size_t moe_xent_fwd_workspace_size(const moe_xent* p);
+int moe_xent_fwd(const moe_xent* p, hipStream_t stream);
+size_t moe_xent_bwd_workspace_size(const moe_xent* p);
+int moe_xent_bwd(const moe_xent* p, hipStream_t stream);
+
+/*
  * MXFP4 (microscaled 4-bit floating point): every 32 consecutive values of a row are
  * a block with one E8M0 scale byte s, standing for 2^(s - 127), and an E2M1 code
  * each (sign in bit 3; magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6).

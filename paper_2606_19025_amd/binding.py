@@ -28,6 +28,7 @@ EXPORTS = [
     "moe_combine_bwd", "moe_layer_fwd", "moe_layer_bwd",
     "moe_layernorm_fwd", "moe_layernorm_bwd_workspace_size", "moe_layernorm_bwd",
     "moe_block_norm_fwd", "moe_block_norm_bwd_workspace_size", "moe_block_norm_bwd",
+    "moe_xent_fwd_workspace_size", "moe_xent_fwd", "moe_xent_bwd_workspace_size", "moe_xent_bwd",
     "moe_mxfp4_scale_stride", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
     "moe_mxfp4_ffn_fwd_workspace_size", "moe_mxfp4_ffn_fwd",
     "moe_few_fwd_workspace_size", "moe_few_fwd",
@@ -84,6 +85,10 @@ _SIGS = {
     "moe_grad_norm": (_I, [_P, _I, _F, _P, _P, _Z, _P]),
     "moe_grad_clip": (_I, [_P, _I, _P, _P]),
     "moe_adamw_steps": (_I, [_P, _I, _I, _F, _F, _F, _F, _P, _P]),
+    "moe_xent_fwd_workspace_size": (_Z, [_P]),
+    "moe_xent_fwd": (_I, [_P, _P]),
+    "moe_xent_bwd_workspace_size": (_Z, [_P]),
+    "moe_xent_bwd": (_I, [_P, _P]),
     "moe_mxfp4_scale_stride": (_I, [_I]),
     "moe_mxfp4_quantize": (_I, [_P, _I, _I, _I, _P, _P, _P, _P]),
     "moe_mxfp4_dequantize": (_I, [_P, _P, _I, _I, _I, _P, _P, _P]),
@@ -161,6 +166,14 @@ class moe_block_norm(C.Structure):
                                    "pre_rstd", "du", "dres", "dx", "df", "d_post_weight",
                                    "d_post_bias", "d_gate", "d_pre_weight", "d_pre_bias")]
     _fields_ += [("accumulate", _I), ("ws", _P), ("ws_bytes", _Z)]
+
+
+class moe_xent(C.Structure):
+    """The linear head's cross entropy's arguments (struct moe_xent of include/moe_resident.h)."""
+    _fields_ = [(n, _I) for n in ("dtype", "N", "d", "V")]
+    _fields_ += [("scale", _F), ("z_coef", _F)]
+    _fields_ += [(n, _P) for n in ("x", "w", "labels", "loss", "lse", "total", "dloss", "dx", "dw")]
+    _fields_ += [("dw_dtype", _I), ("accumulate_dw", _I), ("ws", _P), ("ws_bytes", _Z)]
 
 
 class moe_grad(C.Structure):
@@ -413,6 +426,23 @@ def moe_adamw_steps(tensors, n_tensors, step, lr, beta1=0.9, beta2=0.95, eps=1e-
     """tensors: an array of moe_adamw_tensor."""
     return _check("moe_adamw_steps", lib().moe_adamw_steps(tensors, n_tensors, step, lr, beta1, beta2,
                                                            eps, _ptr(norm), _stream(stream)))
+
+
+def moe_xent_fwd_workspace_size(xent) -> int:
+    """xent: a moe_xent."""
+    return lib().moe_xent_fwd_workspace_size(C.byref(xent))
+
+
+def moe_xent_fwd(xent, stream=None):
+    return _check("moe_xent_fwd", lib().moe_xent_fwd(C.byref(xent), _stream(stream)))
+
+
+def moe_xent_bwd_workspace_size(xent) -> int:
+    return lib().moe_xent_bwd_workspace_size(C.byref(xent))
+
+
+def moe_xent_bwd(xent, stream=None):
+    return _check("moe_xent_bwd", lib().moe_xent_bwd(C.byref(xent), _stream(stream)))
 
 
 def moe_mxfp4_scale_stride(cols) -> int:

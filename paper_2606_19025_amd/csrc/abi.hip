@@ -601,6 +601,67 @@ int moe_block_norm_bwd(const moe_block_norm* p, hipStream_t stream) {
 }
 
 namespace {
+int check_xent_sizes(const moe_xent* p) {
+  REQUIRE(p != nullptr, "the arguments must not be NULL");
+  int r;
+  if ((r = check_dtype(p->dtype)) != MOE_OK) return r;
+  REQUIRE(p->N >= 0 && p->d >= 1 && p->V >= 1, "bad sizes N = %d, d = %d, V = %d", p->N, p->d, p->V);
+  SUPPORT(p->N < 1 << 27, "N = %d must be below 2^27", p->N);
+  SUPPORT(p->d <= 1 << 16, "d = %d: at most 2^16", p->d);
+  SUPPORT(p->V <= INT32_MAX - 512, "V = %d is too large", p->V);
+  if (p->dtype == MOE_BF16) {
+    SUPPORT(p->d % 64 == 0, "d = %d must be a multiple of 64 for bf16", p->d);
+    SUPPORT((int64_t)p->N * p->d < (int64_t(1) << 31) - 16, "N d = %lld must be below 2^31 - 16",
+            (long long)p->N * p->d);
+  } else {
+    SUPPORT(p->d % 8 == 0, "d = %d must be a multiple of 8", p->d);
+  }
+  return MOE_OK;
+}
+
+int check_xent(const moe_xent* p, bool fwd) {
+  int r;
+  if ((r = check_xent_sizes(p)) != MOE_OK) return r;
+  const bool any = p->N > 0;
+  REQUIRE(std::isfinite(p->scale) && std::isfinite(p->z_coef), "scale and z_coef must be finite");
+  REQUIRE(!any || (p->x && p->w && p->labels && p->lse), "x, w, labels and lse must not be NULL");
+  SUPPORT(aligned16(p->x) && aligned16(p->w), "x and w must be 16-byte aligned");
+  if (fwd) {
+    REQUIRE(p->total && (!any || p->loss), "loss and total must not be NULL");
+  } else {
+    SUPPORT(p->dw_dtype == MOE_F32 || p->dw_dtype == p->dtype, "dw_dtype = %d is neither fp32 nor dtype",
+            p->dw_dtype);
+    REQUIRE(p->dw && (!any || p->dx), "dx and dw must not be NULL");
+    SUPPORT(aligned16(p->dx) && aligned16(p->dw), "dx and dw must be 16-byte aligned");
+  }
+  const size_t need = fwd ? moe::xent_fwd_ws_bytes(p) : moe::xent_bwd_ws_bytes(p);
+  REQUIRE(p->ws && p->ws_bytes >= need, "workspace of %zu bytes needed (got %zu)", need, p->ws_bytes);
+  SUPPORT((uintptr_t)p->ws % 256 == 0, "ws must be 256-byte aligned");
+  return MOE_OK;
+}
+}  // namespace
+
+size_t moe_xent_fwd_workspace_size(const moe_xent* p) {
+  return check_xent_sizes(p) == MOE_OK ? moe::xent_fwd_ws_bytes(p) : 0;
+}
+
+int moe_xent_fwd(const moe_xent* p, hipStream_t stream) {
+  const int r = check_xent(p, true);
+  if (r != MOE_OK) return r;
+  return hip_status(moe::launch_xent_fwd(p, stream), "moe_xent_fwd");
+}
+
+size_t moe_xent_bwd_workspace_size(const moe_xent* p) {
+  return check_xent_sizes(p) == MOE_OK ? moe::xent_bwd_ws_bytes(p) : 0;
+}
+
+int moe_xent_bwd(const moe_xent* p, hipStream_t stream) {
+  const int r = check_xent(p, false);
+  if (r != MOE_OK) return r;
+  return hip_status(moe::launch_xent_bwd(p, stream), "moe_xent_bwd");
+}
+
+namespace {
 int check_mx(int dtype, int rows, int cols, const void* x, const uint8_t* codes,
              const uint8_t* scales) {
   int r;

@@ -10,15 +10,36 @@ namespace moe {
 
 // UP_FWD and DH_BWD are GU_FWD and DHH_BWD for the SiLU expert (one first
 // projection W1 [H, d] instead of [Wg; Wu]).
+// XE_*: the products of a linear head's cross entropy (xent.hip), one group of the tokens
+// that count: logits to partial sums of exponentials, logits to their gradient dz, dz W and
+// dz^T x.
 enum GemmKind {
-  GU_FWD = 0, DOWN_FWD = 1, DHH_BWD = 2, DX_BWD = 3, DWD = 4, DWGU = 5, UP_FWD = 6, DH_BWD = 7
+  GU_FWD = 0, DOWN_FWD = 1, DHH_BWD = 2, DX_BWD = 3, DWD = 4, DWGU = 5, UP_FWD = 6, DH_BWD = 7,
+  XE_LSE = 8, XE_DZ = 9, XE_DX = 10, XE_DW = 11
 };
 
 template <int KIND>
 struct Kind {
-  static constexpr bool MRAG = KIND <= DX_BWD || KIND >= UP_FWD;  // ragged in M (else in K)
-  static constexpr bool A_KC = MRAG;                                // A contiguous along k
-  static constexpr bool B_KC = KIND <= DOWN_FWD || KIND == UP_FWD;  // B contiguous along k
+  // ragged in M (else in K)
+  static constexpr bool MRAG = KIND <= DX_BWD || (KIND >= UP_FWD && KIND != XE_DW);
+  static constexpr bool A_KC = MRAG;  // A contiguous along k
+  // B contiguous along k
+  static constexpr bool B_KC = KIND <= DOWN_FWD || KIND == UP_FWD || KIND == XE_LSE || KIND == XE_DZ;
+  static constexpr bool XE = KIND >= XE_LSE;
+};
+
+// What the XE_* kinds take besides: rows are the tokens that count, columns a piece [v0, v0 + V)
+// of the vocabulary.
+struct XentArgs {
+  const void* x_all;      // x itself, taken instead of the counted tokens' copy when all count
+  const int32_t* label;   // per row
+  const float* lse;       // per row (XE_DZ)
+  const float* coef;      // per row: upstream gradient times the logits' scale (XE_DZ)
+  float2* part;           // XE_LSE: [128-column (small tiles: half a tile's) piece][cap] (max, sum), base 2
+  float* z_label;         // XE_LSE: per row, the label's logit
+  int V, v0;
+  float scale, z2;        // of the logits; 2 z_coef
+  int out_bf16;           // XE_DW: C is bf16
 };
 
 struct GemmArgs {
@@ -40,6 +61,7 @@ struct GemmArgs {
   int ksplit_max;
   float* part;
   int* ksplit_used;
+  XentArgs xe;  // XE_*; XE_DX: its fp32 partials go to part, ksplit (>= 1) parts of K
 };
 
 DEVI int clamp_row(int v, int cap) { return v < 0 ? 0 : (v > cap ? cap : v); }
@@ -128,11 +150,11 @@ struct GemmLaunch {
 #define MOE_GEMM_NAMES(S)                                                                     \
   {"gemm_gu_fwd" S, "gemm_down_fwd" S, "gemm_dhh_bwd" S, "gemm_dx_bwd" S, "gemm_dwd" S,       \
    "gemm_dwgu" S, "gemm_up_fwd" S, "gemm_dh_bwd" S, "gemm_dhh_dwd" S, "gemm_dh_dwd" S,        \
-   "gemm_dx_dwgu" S}
+   "gemm_dx_dwgu" S, "gemm_xe_lse" S, "gemm_xe_dz" S, "gemm_xe_dx_dw" S}
 constexpr const char* kGemmNames[] = MOE_GEMM_NAMES("");
 constexpr const char* kTileNames[] = MOE_GEMM_NAMES("_tile");
 constexpr int gemm_name_index(int ka, int kb) {
-  return ka == kb ? ka : ka == DHH_BWD ? 8 : ka == DH_BWD ? 9 : 10;
+  return ka >= XE_LSE ? ka + 3 : ka == kb ? ka : ka == DHH_BWD ? 8 : ka == DH_BWD ? 9 : 10;
 }
 
 // Output tiles of the bf16 launches (fp32 ones choose by themselves).  TILE_32x64:
@@ -142,5 +164,46 @@ enum TileSize { TILE_256x256, TILE_64x128, TILE_64x64, TILE_32x64 };
 // sets_b[0..nb) of kind kb (kb == ka with nb = 0: one kind).
 hipError_t run_gemm_tile(int bf16, int ka, int kb, const GemmArgs* sets_a, int na,
                          const GemmArgs* sets_b, int nb, TileSize size, hipStream_t s);
+
+// The large tiles (gemm.hip) of the XE_* kinds, bf16: kind ka over one set, or XE_DX with XE_DW
+// (b).  counters: zeroed, or NULL.
+constexpr int kXcdCounters = 8;
+hipError_t run_gemm_xent(int ka, const GemmArgs& a, const GemmArgs* b, int* counters, hipStream_t s);
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+// The gradient of logits z = scale * acc of a row with log-sum-exp lse (base 2: lse2), label column
+// yc and coefficient cf (with zf = 1 + 2 z_coef lse) at column c, where c < V; 0 past it.
+DEVI float xent_dz(float acc, float scale2, float lse2, float cf, float zf, int c, int yc, int V) {
+  const float p = __builtin_amdgcn_exp2f(acc * scale2 - lse2);
+  const float g = cf * (zf * p - (c == yc ? 1.0f : 0.0f));
+  return c < V ? g : 0.0f;
+}
+
+// Partial (max, sum of 2^(z - max)) of NJ x 4 logits acc * scale2 that a lane holds of a row at columns
+// c + 16 j + t, with those of the three lanes 16 apart that hold the row's others; columns from V on
+// are left out.
+template <int NJ>
+DEVI float2 xent_partial(const f32x4_t (&acc)[NJ], float scale2, int c, int V) {
+  float m = -INFINITY;
+  const bool whole = c + 16 * NJ <= V;  // (c is at most 12 columns past the tile's first)
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (whole || c + 16 * j + t < V) m = fmaxf(m, acc[j][t] * scale2);
+  m = fmaxf(m, __shfl_xor(m, 16, 64));
+  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  const float at = m == -INFINITY ? 0.0f : m;
+  float s = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (whole || c + 16 * j + t < V) s += __builtin_amdgcn_exp2f(acc[j][t] * scale2 - at);
+  s += __shfl_xor(s, 16, 64);
+  s += __shfl_xor(s, 32, 64);
+  return float2{m, s};
+}
 
 }  // namespace moe

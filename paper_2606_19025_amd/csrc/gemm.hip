@@ -152,8 +152,9 @@ struct Cfg {
   // The other kinds' bands run across the groups: by group their merged
   // launches were 1 % slower (the longer decode spills there).
   static constexpr bool BY_GROUP = Kind<KIND>::B_KC;
-  static constexpr int BAND = KIND == GU_FWD || KIND == UP_FWD ? 6 : KIND == DOWN_FWD ? 4
-                              : KIND == DX_BWD ? 8 : 2;
+  static constexpr int BAND = KIND == GU_FWD || KIND == UP_FWD ? 6
+                              : KIND == DOWN_FWD || KIND == XE_LSE || KIND == XE_DZ ? 4
+                              : KIND == DX_BWD || KIND == XE_DX ? 8 : 2;
   static_assert(NW * EPI_WAVE <= LDS, "epilogue staging exceeds the ring");
 };
 
@@ -201,12 +202,12 @@ constexpr unsigned kOOB = 0xFFFFFFF0u;
 DEVI __amdgpu_buffer_rsrc_t store_rsrc(void* base) {
   return __builtin_amdgcn_make_buffer_rsrc(base, (short)0, (int)kOOB, 0x00020000);
 }
-DEVI u32x4_t make_rsrc(const void* base) {
+DEVI u32x4_t make_rsrc(const void* base, unsigned bytes = kOOB) {
   const uint64_t b = (uint64_t)(uintptr_t)base;
   u32x4_t r;
   r[0] = __builtin_amdgcn_readfirstlane((unsigned)b);
   r[1] = __builtin_amdgcn_readfirstlane((unsigned)(b >> 32) & 0xFFFFu);
-  r[2] = kOOB;
+  r[2] = bytes;
   r[3] = 0x00020000u;
   return r;
 }
@@ -555,6 +556,10 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
       });
     }
   }
+  if constexpr (KA == XE_DX) {
+    prt[0] = L.s[0].ksplit;  // (chosen on the host)
+    kpt[0] = L.s[0].K / prt[0];
+  }
 #pragma unroll
   for (int q = 0; q < kMaxSets; ++q) {
     const int tot = q < L.n_sets ? mt[q] * prt[q] * ntl[q] : 0;
@@ -642,6 +647,11 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
       const int tile_n = c.tile_n;
       const bf16_t* A = static_cast<const bf16_t*>(a.A);
       const bf16_t* B = static_cast<const bf16_t*>(a.B) + (K_::MRAG ? (size_t)tl.g * a.b_gs : 0);
+      if constexpr (K_::XE) {
+        const bool all = __builtin_amdgcn_readfirstlane(gtab[q].b[1]) == a.cap;
+        if (KIND == XE_DW && all) B = static_cast<const bf16_t*>(a.xe.x_all);
+        if (K_::B_KC && all) A = static_cast<const bf16_t*>(a.xe.x_all);
+      }
       const int Kd = K_::MRAG ? a.K : tl.rows;
       c.nk = (Kd + GK - 1) / GK;
       c.n_full = Kd / GK;  // k-steps without a ragged tail
@@ -666,7 +676,7 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
           if (!ok) br = 0;
           return B + (size_t)br * a.ldb;
         } else {
-          return B + (size_t)min(tl.n0 + r, a.N - 1) * a.ldb;
+          return B + (size_t)min(tl.n0 + r, (K_::XE ? a.xe.V : a.N) - 1) * a.ldb;
         }
       };
       auto b_elem = [&](int k, int col) -> const bf16_t* {  // NN / TN B(k, n = n0 + col)
@@ -701,7 +711,8 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
         for (int x = 0; x < DB; ++x) c.tb.p[x] = tb.p[x];
       }
       c.rs_a = make_rsrc(A);
-      c.rs_b = make_rsrc(B);
+      // (XE_DX: rows of W past the piece read zeros, whatever lies there)
+      c.rs_b = KIND == XE_DX ? make_rsrc(B, 2u * (unsigned)a.xe.V * (unsigned)a.ldb) : make_rsrc(B);
       c.a_step = 2u * (K_::A_KC ? GK : (unsigned)GK * a.lda);
       c.b_step = 2u * (K_::B_KC ? GK : (unsigned)GK * a.ldb);
       if constexpr (K_::MRAG) {
@@ -898,6 +909,72 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
             }
           }
         }
+      } else if constexpr (KIND == XE_LSE) {
+        const float scale2 = a.xe.scale * kLog2e;
+        const int c0 = tl.n0 + wn * 128;
+#pragma unroll
+        for (int ii = 0; ii < MI; ++ii) {
+          const int row = wm * WM + ii * 16 + (ln & 15);
+          const float2 ms = xent_partial<NJ>(acc[ii], scale2, c0 + 4 * (ln >> 4), a.xe.V);
+          const bool ok = row < tl.rows;
+          const size_t m = (size_t)(tl.row0 + row);
+          if (ok && ln < 16) a.xe.part[(size_t)(c0 >> 7) * a.cap + m] = ms;
+          // the label's logit, where it lies among these columns
+          int y = ok ? a.xe.label[m] - a.xe.v0 - c0 : -1;
+          if (y >= min(128, a.xe.V - c0)) y = -1;
+          if (__ballot(y >= 0)) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+                if (y == 16 * j + 4 * (ln >> 4) + t) a.xe.z_label[m] = acc[ii][j][t] * a.xe.scale;
+          }
+        }
+      } else if constexpr (KIND == XE_DX) {
+        // fp32 partial sums ([cap, N]) of a part of K, added to those of earlier pieces
+        float* const part = a.part + (size_t)tl.split * a.c_split;
+        const int c_in = 4 * (ln >> 4);
+#pragma unroll
+        for (int ii = 0; ii < MI; ++ii) {
+          const int row = wm * WM + ii * 16 + (ln & 15);
+          if (row >= tl.rows) continue;
+          float* const c = part + (size_t)(tl.row0 + row) * a.N + tl.n0 + wn * 128 + c_in;
+          const int left = a.N - (tl.n0 + wn * 128 + c_in);
+          if (a.accumulate) {
+            f32x4_t old[NJ];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+              if (16 * j < left) old[j] = *reinterpret_cast<const f32x4_t*>(c + 16 * j);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+              if (16 * j < left) *reinterpret_cast<f32x4_t*>(c + 16 * j) = old[j] + acc[ii][j];
+          } else {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+              if (16 * j < left) *reinterpret_cast<f32x4_t*>(c + 16 * j) = acc[ii][j];
+          }
+        }
+      } else if (KIND == XE_DW && (!a.xe.out_bf16 || a.accumulate)) {
+        // straight from the accumulators: fp32, or added in fp32 to bf16 values
+        const int c_in = 4 * (ln >> 4);
+#pragma unroll
+        for (int ii = 0; ii < MI; ++ii) {
+          const int row = tl.m0 + wm * WM + ii * 16 + (ln & 15);
+          if (row >= a.xe.V) continue;
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            const int col = tl.n0 + wn * 128 + j * 16 + c_in;
+            if (col >= a.N) continue;
+            const size_t at = (size_t)row * a.ldc + col;
+            if (a.xe.out_bf16) {
+              bf16x4_t* c = reinterpret_cast<bf16x4_t*>(static_cast<bf16_t*>(a.C) + at);
+              *c = __builtin_convertvector(__builtin_convertvector(*c, f32x4_t) + acc[ii][j], bf16x4_t);
+            } else {
+              f32x4_t* c = reinterpret_cast<f32x4_t*>(static_cast<float*>(a.C) + at);
+              *c = a.accumulate ? *c + acc[ii][j] : acc[ii][j];
+            }
+          }
+        }
       } else if ((KIND == DOWN_FWD || KIND == DX_BWD) && cur.parts > 1) {
         // a K part: its fp32 partial ([cap, N], rows as the output's),
         // straight from the accumulators (here, so that the accumulators
@@ -929,6 +1006,21 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
         // (nontemporal: measured 2-4 % faster for DHH_BWD, DX_BWD and
         // DOWN_FWD; the fp32 weight gradients are not, they were 1.4-1.7x
         // slower that way).
+        if constexpr (KIND == XE_DZ) {
+          const float scale2 = a.xe.scale * kLog2e;
+#pragma unroll
+          for (int ii = 0; ii < MI; ++ii) {
+            const size_t m = (size_t)(tl.row0 + min(wm * WM + ii * 16 + (ln & 15), tl.rows - 1));
+            const float lse = a.xe.lse[m], cf = a.xe.coef[m], zf = 1.0f + a.xe.z2 * lse;
+            const int y = a.xe.label[m] - a.xe.v0;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+                acc[ii][j][t] = xent_dz(acc[ii][j][t], scale2, lse * kLog2e, cf, zf,
+                                        tl.n0 + wn * 128 + 16 * j + 4 * (ln >> 4) + t, y, a.xe.V);
+          }
+        }
 #pragma unroll
         for (int ii = 0; ii < MI; ++ii)
 #pragma unroll
@@ -949,7 +1041,8 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
             out[8 + it] = epi_get(reg, row, cg + 4);
           }
           late = true;
-        } else if constexpr (KIND == DOWN_FWD || KIND == DX_BWD || KIND == UP_FWD) {
+        } else if constexpr (KIND == DOWN_FWD || KIND == DX_BWD || KIND == UP_FWD || KIND == XE_DZ ||
+                             KIND == XE_DW) {
           const int c = ln & 15;
 #pragma unroll
           for (int it = 0; it < WM / 4; ++it) out[it] = epi_get(reg, it * 4 + (ln >> 4), c);
@@ -1066,6 +1159,18 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
           store16<true>(rg, ok ? 2u * (m * 2u * H + H + h) : kOOB, __builtin_bit_cast(u32x4_t, U));
           store16<true>(rh, ok ? 2u * (m * H + h) : kOOB, __builtin_bit_cast(u32x4_t, Hv));
         }
+      } else if constexpr (KIND == XE_DZ || KIND == XE_DW) {
+        // (dz is read again by the next launch, so it stays in the caches)
+        const int col = tl.n0 + wn * 128 + 8 * (ln & 15);
+        const __amdgpu_buffer_rsrc_t rc = store_rsrc(a.C);
+        const int rows = KIND == XE_DW ? a.xe.V : tl.rows;
+#pragma unroll
+        for (int it = 0; it < WM / 4; ++it) {
+          const int row = (KIND == XE_DW ? tl.m0 : 0) + wm * WM + it * 4 + (ln >> 4);
+          const unsigned m = (unsigned)((KIND == XE_DW ? 0 : tl.row0) + row);
+          store16<KIND == XE_DW>(rc, row < rows && col < a.N ? 2u * (m * (unsigned)a.ldc + col) : kOOB,
+                                 __builtin_bit_cast(u32x4_t, out[it]));
+        }
       } else if constexpr (KIND == DOWN_FWD || KIND == DX_BWD || KIND == UP_FWD) {
         const int c = ln & 15;
         const int col = tl.n0 + wn * 128 + 8 * c;
@@ -1116,7 +1221,8 @@ long max_tiles(const GemmArgs& a) {
   constexpr int BM = Cfg<KIND>::BM;
   const long n_tiles = ceil_div((KIND == GU_FWD) ? 2 * a.H : a.N, GT);
   return Kind<KIND>::MRAG
-             ? (ceil_div(a.cap, BM) + (long)a.n_groups) * n_tiles * std::max(1, a.ksplit_max)
+             ? (ceil_div(a.cap, BM) + (long)a.n_groups) * n_tiles *
+                   std::max(1, KIND == XE_DX ? a.ksplit : a.ksplit_max)
              : (long)a.n_groups * std::max(1, a.ksplit) * ceil_div(a.M, BM) * n_tiles;
 }
 
@@ -1149,6 +1255,16 @@ hipError_t run_gemm_bf16(const GemmArgs* sets_a, int na, const GemmArgs* sets_b,
   MOE_TIMED((kGemmNames[gemm_name_index(KA, KB)]), s, gemm_bf16_kernel<KA, KB><<<(int)blocks, 512, 0, s>>>(L));
   return hipGetLastError();
 }
+
+}  // namespace
+
+hipError_t run_gemm_xent(int ka, const GemmArgs& a, const GemmArgs* b, int* counters, hipStream_t s) {
+  if (ka == XE_LSE) return run_gemm_bf16<XE_LSE, XE_LSE>(&a, 1, nullptr, 0, s, counters);
+  if (ka == XE_DZ) return run_gemm_bf16<XE_DZ, XE_DZ>(&a, 1, nullptr, 0, s, counters);
+  return run_gemm_bf16<XE_DX, XE_DW>(&a, 1, b, 1, s, counters);
+}
+
+namespace {
 
 // counters[0..n) = 0 (the per-XCD tile counters of the next launches)
 __global__ __launch_bounds__(64) void zero_counters_kernel(int* counters, int n) {

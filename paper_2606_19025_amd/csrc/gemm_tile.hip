@@ -95,6 +95,7 @@ DEVI float dsilu_t(float g) {
 
 struct TileAt {
   int g, row0, rows, m0, tile_n;
+  bool all;  // XE_*: every token counts
 };
 
 // Four consecutive fp32 output columns n .. n + 3 of tile row i (both in range):
@@ -119,6 +120,10 @@ DEVI void store_cols(const GemmArgs& a, const TileAt& t, int i, int n, f32x4_t v
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] *= dsilu_t<float>(A[e]);
       put4(a.C, m * a.ldc + n, v);
+    } else if constexpr (KIND == XE_DX) {
+      // partial sums of part tile_n % ksplit of K, added to those of earlier pieces
+      float* const part = a.part + (size_t)(t.tile_n % a.ksplit) * a.c_split;
+      put4(part, m * a.N + n, a.accumulate ? get4(part, m * a.N + n) + v : v);
     } else {
       put4(a.C, m * a.ldc + n, v);
       if constexpr (KIND == UP_FWD) {
@@ -127,6 +132,10 @@ DEVI void store_cols(const GemmArgs& a, const TileAt& t, int i, int n, f32x4_t v
         put4(a.out2, m * a.H + n, v);
       }
     }
+  } else if (KIND == XE_DW && a.xe.out_bf16) {
+    bf16x4_t* c = reinterpret_cast<bf16x4_t*>(static_cast<bf16_t*>(a.C) + (size_t)(t.m0 + i) * a.ldc + n);
+    if (a.accumulate) v += __builtin_convertvector(*c, f32x4_t);
+    *c = __builtin_convertvector(v, bf16x4_t);
   } else {
     f32x4_t* c = reinterpret_cast<f32x4_t*>(static_cast<float*>(a.C) + (size_t)t.g * a.c_gs +
                                             (size_t)(t.m0 + i) * a.ldc + n);
@@ -161,12 +170,27 @@ DEVI void gemm_tile(const GemmArgs& a, const TileAt& tl, char* lds) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   const int l16 = lane & 15, g4 = lane >> 4;
-  const T* A = static_cast<const T*>(a.A) + (size_t)tl.row0 * a.lda;
-  const T* B = static_cast<const T*>(a.B) +
+  const void* Ab = a.A;
+  const void* Bb = a.B;
+  if constexpr (K_::XE) {
+    if (KIND == XE_DW && tl.all) Bb = a.xe.x_all;
+    if (K_::B_KC && tl.all) Ab = a.xe.x_all;
+  }
+  const T* A = static_cast<const T*>(Ab) + (size_t)tl.row0 * a.lda;
+  const T* B = static_cast<const T*>(Bb) +
                    (K_::MRAG ? (size_t)tl.g * a.b_gs : (size_t)tl.row0 * a.ldb);
-  const int Kd = K_::MRAG ? a.K : tl.rows;
+  int Kd = K_::MRAG ? a.K : tl.rows, n_tile = tl.tile_n;
+  if constexpr (KIND == XE_DX) {
+    // part tile_n % ksplit of K, in whole k-steps
+    const int part = n_tile % a.ksplit, steps = (Kd + BK - 1) / BK;
+    n_tile /= a.ksplit;
+    const int k0 = (int)((long)steps * part / a.ksplit) * BK;
+    Kd = min(Kd, (int)((long)steps * (part + 1) / a.ksplit) * BK) - k0;
+    A += k0;
+    B += (size_t)k0 * a.ldb;
+  }
   const int nk = (Kd + BK - 1) / BK;
-  const int n0 = tl.tile_n * BN;
+  const int n0 = n_tile * BN;
 
   // row of w_gate_up[g] (or of the second operand) behind tile column c; the
   // gate and up units of GU_FWD alternate in blocks of 8 NJ columns, half of a
@@ -179,7 +203,7 @@ DEVI void gemm_tile(const GemmArgs& a, const TileAt& tl, char* lds) {
       const int h = (n0 >> 1) + (c / (2 * HW)) * HW + c % HW;
       return ((c / HW) & 1) * a.H + (h < a.H ? h : 0);
     } else {
-      return min(n0 + c, a.N - 1);
+      return min(n0 + c, (K_::XE ? a.xe.V : a.N) - 1);
     }
   };
   // piece q of a k-contiguous operand: rows 8 q .. 8 q + 7
@@ -353,12 +377,45 @@ DEVI void gemm_tile(const GemmArgs& a, const TileAt& tl, char* lds) {
     st = next;
   }
 
+  // a lane's rows of the logits' kinds: row (wm MI + i) 16 + l16, columns 16 j + 4 g4 + t of the wave's
+  if constexpr (KIND == XE_LSE || KIND == XE_DZ) {
+    const float scale2 = a.xe.scale * kLog2e;
+    const int c0 = n0 + wn * 16 * NJ;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int r = (wm * MI + i) * 16 + l16;
+      const bool ok = r < tl.rows;
+      const size_t m = (size_t)(tl.row0 + (ok ? r : 0));
+      const int y = a.xe.label[m] - a.xe.v0;
+      if constexpr (KIND == XE_LSE) {
+        const float2 ms = xent_partial<NJ>(acc[i], scale2, c0 + 4 * g4, a.xe.V);
+        if (ok && g4 == 0) a.xe.part[(size_t)(c0 / (16 * NJ)) * a.cap + m] = ms;
+        if (ok && y >= c0 && y < min(c0 + 16 * NJ, a.xe.V)) {
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+              if (y - c0 == 16 * j + 4 * g4 + t) a.xe.z_label[m] = acc[i][j][t] * a.xe.scale;
+        }
+      } else {
+        const float lse = a.xe.lse[m], cf = a.xe.coef[m], zf = 1.0f + a.xe.z2 * lse;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            acc[i][j][t] = xent_dz(acc[i][j][t], scale2, lse * kLog2e, cf, zf, c0 + 16 * j + 4 * g4 + t,
+                                   y, a.xe.V);
+      }
+    }
+    if constexpr (KIND == XE_LSE) return;
+  }
+
   // epilogue, bf16 rows: through a wave-private region of the ring, so that every
   // global access is 16 bytes of a row and 2 NJ (GU_FWD: NJ) lanes in a row
   // take consecutive ones.  (With the accumulators' own 8-byte pieces, GU of
   // 8192 rows, H = 1408 and a single k-step took 34 us against 24 in the large
   // tiles.)  Chunk c (16 bytes) of row r sits at chunk c ^ key(r).
-  if constexpr (!F32 && K_::MRAG) {
+  if constexpr (!F32 && K_::MRAG && KIND != XE_DX) {
     constexpr int CPR = 2 * NJ;  // chunks per row
     char* reg = lds + wave * (16 * MI * CPR * 16);
     auto at = [&](int r, int c) { return reg + (r * CPR + (c ^ ((r >> 1) & (CPR - 1)))) * 16; };
@@ -440,7 +497,7 @@ DEVI void gemm_tile(const GemmArgs& a, const TileAt& tl, char* lds) {
     }
   } else {
     // epilogue, straight from the accumulators
-    const int m_end = K_::MRAG ? tl.rows : a.M - tl.m0;
+    const int m_end = K_::MRAG ? tl.rows : (KIND == XE_DW ? a.xe.V : a.M) - tl.m0;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       // (fp32 m/n-contiguous operands: a lane's MI indices are consecutive)
@@ -483,8 +540,11 @@ DEVI void gemm_tile(const GemmArgs& a, const TileAt& tl, char* lds) {
 constexpr int kXcds = 8;
 constexpr int kBand = 8;  // m-tiles per band of the tile order
 
-template <int KIND>
-DEVI constexpr int cols_of(const GemmArgs& a) { return KIND == GU_FWD ? 2 * a.H : a.N; }
+// Tiles of a kind's columns (XE_DX: K parts are tiles of their own).
+template <int KIND, int BN>
+__host__ __device__ inline int tiles_of(const GemmArgs& a) {
+  return ((KIND == GU_FWD ? 2 * a.H : a.N) + BN - 1) / BN * (KIND == XE_DX ? a.ksplit : 1);
+}
 
 // Weight gradients (ragged in K): a group's tiles all take its own number of
 // k-steps, so of uneven groups every XCD takes an eighth of each one's per_group
@@ -520,9 +580,8 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(GemmLaunch L) {
     const GemmArgs& a = L.s[q];
     const bool kb = KA != KB && L.kind_b[q] != 0;
     const bool mrag = kb ? Kind<KB>::MRAG : Kind<KA>::MRAG;
-    const int cols = kb ? cols_of<KB>(a) : cols_of<KA>(a);
     const int mt_g = mrag ? 0 : (a.M + BM - 1) / BM;
-    const int n_tiles = (cols + BN - 1) / BN;
+    const int n_tiles = kb ? tiles_of<KB, BN>(a) : tiles_of<KA, BN>(a);
     if (!mrag && __builtin_amdgcn_readfirstlane(gtab[q].uneven)) {
       const int per_group = mt_g * n_tiles;
       auto share = [&](int g) {
@@ -586,6 +645,7 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(GemmLaunch L) {
     }
     break;
   }
+  if constexpr (Kind<KA>::XE) tl.all = __builtin_amdgcn_readfirstlane(gtab[0].b[1]) == L.s[0].cap;
   tl.row0 = __builtin_amdgcn_readfirstlane(tl.row0);
   tl.rows = __builtin_amdgcn_readfirstlane(tl.rows);
   __syncthreads();  // the tables have been read: the ring takes their place
@@ -601,7 +661,7 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(GemmLaunch L) {
 
 template <int KIND, int MI, int NJ>
 long max_tiles(const GemmArgs& a) {
-  const long n = ceil_div(KIND == GU_FWD ? 2 * a.H : a.N, 32 * NJ);
+  const long n = tiles_of<KIND, 32 * NJ>(a);
   return n * (Kind<KIND>::MRAG ? (long)ceil_div(a.cap, 32 * MI) + std::min(a.n_groups, a.cap)
                                : (long)a.n_groups * ceil_div(a.M, 32 * MI));
 }
@@ -664,6 +724,9 @@ hipError_t run_kinds(const GemmArgs* sa, int na, const GemmArgs* sb, int nb, Til
     }
     if (size == TILE_64x64) return launch<T, KA, KB, 2, 2, 3>(sa, na, sb, nb, s);
     return launch<T, KA, KB, 2, 4, 2>(sa, na, sb, nb, s);
+  } else if constexpr (Kind<KA>::XE) {
+    if (size == TILE_64x128) return launch<T, KA, KB, 2, 4, 2>(sa, na, sb, nb, s);
+    return launch<T, KA, KB, 1, 2, 3>(sa, na, sb, nb, s);
   } else {
     // Six tiles of 64 x 128 per CU (by the bound on the group sizes) keep every
     // SIMD busy and halve the L2 traffic; with fewer, 32 x 64 tiles fill the CUs
@@ -692,6 +755,9 @@ hipError_t run_gemm_tile(int bf16, int ka, int kb, const GemmArgs* sa, int na, c
   MOE_KINDS(DHH_BWD, DWD);
   MOE_KINDS(DH_BWD, DWD);
   MOE_KINDS(DX_BWD, DWGU);
+  MOE_KINDS(XE_LSE, XE_LSE);
+  MOE_KINDS(XE_DZ, XE_DZ);
+  MOE_KINDS(XE_DX, XE_DW);
 #undef MOE_KINDS
   return hipErrorInvalidValue;
 }

@@ -128,6 +128,12 @@ hipError_t launch_block_norm_fwd(const moe_block_norm* p, hipStream_t s);
 size_t block_norm_ws_bytes(int T, int d, int bf16);
 hipError_t launch_block_norm_bwd(const moe_block_norm* p, hipStream_t s);
 
+// Cross entropy of a linear head (xent.hip).
+size_t xent_fwd_ws_bytes(const moe_xent* x);
+size_t xent_bwd_ws_bytes(const moe_xent* x);
+hipError_t launch_xent_fwd(const moe_xent* x, hipStream_t s);
+hipError_t launch_xent_bwd(const moe_xent* x, hipStream_t s);
+
 // The whole layer for a few tokens (few.hip).
 constexpr int kFewTokens = 64, kFewRoutes = 8;
 size_t few_ws_bytes(const moe_few* f);

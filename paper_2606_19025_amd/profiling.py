@@ -86,7 +86,8 @@ _SYMBOLS = [
     (r"copy_expert_rows_kernel", lambda m: "copy_expert_rows"),
     (r"mx_gemm_kernel(?:<|ILi)(\d)", lambda m: "mx_gemm_" + ("gu", "up", "down")[int(m.group(1))]),
     (r"few_logits_(?:bf16|f32)_kernel", lambda m: "few_logits"),
-    (r"(block_norm_fwd|block_norm_bwd|block_norm_dw|grad_norm_sum|grad_norm|grad_clip|adamw_steps)_kernel",
+    (r"(block_norm_fwd|block_norm_bwd|block_norm_dw|grad_norm_sum|grad_norm|grad_clip|adamw_steps|"
+     r"xent_count|xent_rows|xent_loss|xent_total|xent_zero|xent_clear|xent_dx)_kernel",
      lambda m: m.group(1)),
     (r"(norm_fwd|norm_bwd|norm_dw|mx_quantize|mx_dequantize|few_gu|few_down)_kernel", lambda m: m.group(1)),
 ]
@@ -97,7 +98,7 @@ _SOURCES = [("gemm_", "gemm.hip"), ("splitk_", "gemm.hip"), ("zero_counters", "g
             ("expert_delta", "dispatch.hip"), ("adamw", "optim.hip"), ("outer_", "optim.hip"),
             ("replica_", "optim.hip"),
             ("copy_expert_rows", "placement.hip"), ("norm_", "norm.hip"),
-            ("block_norm_", "block_norm.hip"), ("grad_", "grad.hip"), ("mx_gemm", "gemm_mx.hip"), ("mx_", "mx.hip"),
+            ("block_norm_", "block_norm.hip"), ("grad_", "grad.hip"), ("xent_", "xent.hip"), ("mx_gemm", "gemm_mx.hip"), ("mx_", "mx.hip"),
             ("few_logits", "few.hip"), ("few_", "few.h")]
 
 

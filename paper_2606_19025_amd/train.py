@@ -1,5 +1,5 @@
-"""What a worker's training step needs behind its layers: the gradients' norm, clipping and AdamW
-over all parameters.
+"""What a worker's training step needs behind its layers: the loss, the gradients' norm, clipping and
+AdamW over all parameters.
 
 As in ``layer``, the classes own buffers and issue the C entry points; they compute nothing
 themselves.
@@ -29,6 +29,75 @@ def _disjoint(name, tensors):
     for (_, end, i), (begin, _, j) in zip(spans, spans[1:]):
         if begin < end:
             raise ValueError(f"{name} {i} and {j} overlap")
+
+
+class LinearCrossEntropy:
+    """Softmax cross entropy of N tokens x [N, d] against a vocabulary w [V, d], without the logits
+    being kept: moe_xent_fwd, moe_xent_bwd.
+
+    Logits are scale x w^T; z_coef adds z_coef lse^2 to a token's loss.  Labels are int32; a negative
+    one leaves its token out.  forward returns ``loss`` [N]; ``lse`` [N] and ``total`` (the sum of the
+    losses and the number of tokens that count) stand beside it.  backward, from the last forward's
+    lse, returns ``dx`` with ``dw`` beside it, fp32 or of the weights' type (dw_dtype).  The buffers
+    are the object's own and are reused by the next call: calls on different streams need one each,
+    and a call on another stream than the one current at construction has to be ordered behind it.
+    dw and the workspaces are made by the first call that needs them, dw as zeros."""
+
+    def __init__(self, N, d, V, dtype=torch.bfloat16, scale=1.0, z_coef=0.0, dw_dtype=torch.float32,
+                 device="cuda"):
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"unsupported dtype {dtype}")
+        if dw_dtype not in (torch.float32, dtype):
+            raise ValueError(f"dw_dtype {dw_dtype} is neither float32 nor {dtype}")
+        self.N, self.d, self.V, self.dtype, self.dw_dtype = int(N), int(d), int(V), dtype, dw_dtype
+        code = lambda t: B.MOE_BF16 if t == torch.bfloat16 else B.MOE_F32
+        self.loss, self.lse = (torch.empty(self.N, dtype=torch.float32, device=device) for _ in range(2))
+        self.total = torch.empty(2, dtype=torch.float32, device=device)
+        self.device = self.total.device
+        self.dx = self.dw = self.ws_fwd = self.ws_bwd = None
+        self._args = B.moe_xent(
+            dtype=code(dtype), N=self.N, d=self.d, V=self.V, scale=float(scale), z_coef=float(z_coef),
+            loss=self.loss.data_ptr(), lse=self.lse.data_ptr(), total=self.total.data_ptr(),
+            dw_dtype=code(dw_dtype))
+
+    def _inputs(self, x, w, labels):
+        _check_current(self.device, "loss")
+        for name, t, shape, dtype in (("x", x, (self.N, self.d), self.dtype),
+                                      ("w", w, (self.V, self.d), self.dtype),
+                                      ("labels", labels, (self.N,), torch.int32)):
+            _check_tensor(name, t, shape, dtype, self.device, "loss")
+        a = self._args
+        a.x, a.w, a.labels = x.data_ptr(), w.data_ptr(), labels.data_ptr()
+        return a
+
+    def _workspace(self, size, a):
+        n = size(a)
+        return torch.empty(max(n, 1), dtype=torch.uint8, device=self.device), n
+
+    def forward(self, x, w, labels, stream=None):
+        a = self._inputs(x, w, labels)
+        if self.ws_fwd is None:
+            with _on(stream):
+                self.ws_fwd, self.ws_fwd_bytes = self._workspace(B.moe_xent_fwd_workspace_size, a)
+        a.ws, a.ws_bytes = self.ws_fwd.data_ptr(), self.ws_fwd_bytes
+        B.moe_xent_fwd(a, stream)
+        return self.loss
+
+    def backward(self, x, w, labels, dloss=None, accumulate_dw=0, stream=None):
+        """dloss: the losses' gradients [N] fp32, None: of the mean over the tokens that count."""
+        a = self._inputs(x, w, labels)
+        if dloss is not None:
+            _check_tensor("dloss", dloss, (self.N,), torch.float32, self.device, "loss")
+        if self.ws_bwd is None:
+            with _on(stream):
+                self.ws_bwd, self.ws_bwd_bytes = self._workspace(B.moe_xent_bwd_workspace_size, a)
+                self.dx = torch.empty(self.N, self.d, dtype=self.dtype, device=self.device)
+                self.dw = torch.zeros(self.V, self.d, dtype=self.dw_dtype, device=self.device)
+            a.dx, a.dw = self.dx.data_ptr(), self.dw.data_ptr()
+        a.dloss, a.accumulate_dw = B._ptr(dloss), int(accumulate_dw)
+        a.ws, a.ws_bytes = self.ws_bwd.data_ptr(), self.ws_bwd_bytes
+        B.moe_xent_bwd(a, stream)
+        return self.dx
 
 
 class GradClipper:
