@@ -9,7 +9,7 @@
 // time.
 //
 // A launch covers up to kTensors tensors, whose table is a kernel argument: no list is copied to
-// the device, and a captured launch keeps its own.  Tensors are cut into chunks of kChunk values,
+// the device, and a captured launch keeps its own.  Tensors are cut into chunks (chunk_of),
 // which the blocks take in turn; every block stores one partial sum, and a last block adds the
 // partials of all launches in order, so the result does not depend on timing.
 #include <cmath>
@@ -22,7 +22,6 @@ namespace moe {
 namespace {
 
 constexpr int kTensors = 112;
-constexpr int kChunk = 16384;
 constexpr int kThreads = 256;
 
 struct GradTable {
@@ -31,7 +30,7 @@ struct GradTable {
   size_t n[kTensors];
   int first[kTensors + 1];  // chunks before each tensor
   uint8_t bf16[kTensors];
-  int count;
+  int count, chunk;
 };
 static_assert(sizeof(GradTable) <= 3900, "kernel arguments hold 4 KiB");
 
@@ -85,8 +84,8 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(GradTable t, double
   double s = 0.0;
   for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
     const int q = tensor_of(t, c);
-    const size_t at = (size_t)(c - t.first[q]) * kChunk;
-    const size_t n = min(t.n[q] - at, (size_t)kChunk);
+    const size_t at = (size_t)(c - t.first[q]) * t.chunk;
+    const size_t n = min(t.n[q] - at, (size_t)t.chunk);
     s += t.bf16[q] ? square_sum(static_cast<const bf16_t*>(t.p[q]) + at, n)
                    : square_sum(static_cast<const float*>(t.p[q]) + at, n);
   }
@@ -145,13 +144,20 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradTable t, const 
   for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
     const int q = tensor_of(t, c);
     if (scale == 1.0f && t.p[q] == t.out[q]) continue;
-    const size_t at = (size_t)(c - t.first[q]) * kChunk;
-    const size_t n = min(t.n[q] - at, (size_t)kChunk);
+    const size_t at = (size_t)(c - t.first[q]) * t.chunk;
+    const size_t n = min(t.n[q] - at, (size_t)t.chunk);
     if (t.bf16[q])
       scale_to(static_cast<const bf16_t*>(t.p[q]) + at, static_cast<bf16_t*>(t.out[q]) + at, n, scale);
     else
       scale_to(static_cast<const float*>(t.p[q]) + at, static_cast<float*>(t.out[q]) + at, n, scale);
   }
+}
+
+// Values of a chunk, multiples of what 256 threads load at once.
+int chunk_of(const moe_grad* g, int n) {
+  size_t total = 0;
+  for (int i = 0; i < n; ++i) total += g[i].n;
+  return total < ((size_t)32 << 20) ? 4096 : 16384;
 }
 
 // Blocks of a launch of `chunks` chunks.
@@ -161,12 +167,13 @@ int chunk_blocks(int chunks) { return std::min(chunks, 8 * num_cus()); }
 template <class F>
 hipError_t for_tables(const moe_grad* g, int n, F&& f) {
   GradTable t;
+  t.chunk = chunk_of(g, n);
   t.count = 0;
   t.first[0] = 0;
   for (int i = 0; i <= n; ++i) {
     const bool end = i == n;
     // (a launch's chunks are counted in 31 bits: a tensor that does not fit opens the next)
-    const int64_t chunks = end ? 0 : (int64_t)((g[i].n + kChunk - 1) / kChunk);
+    const int64_t chunks = end ? 0 : (int64_t)((g[i].n + t.chunk - 1) / t.chunk);
     if (t.count > 0 && (end || t.count == kTensors || t.first[t.count] + chunks > INT32_MAX)) {
       if (const hipError_t e = f(t, chunk_blocks(t.first[t.count])); e != hipSuccess) return e;
       t.count = 0;

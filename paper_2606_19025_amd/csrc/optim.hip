@@ -19,6 +19,7 @@
 // results are reproducible bit for bit by any fp32 evaluation of the same
 // formulas.  The bf16 working copy that the grouped GEMMs read is written in
 // the same pass (round to nearest even).
+
 #include "common.h"
 #include "kernels.h"
 #include "timing.h"
@@ -85,9 +86,9 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
 }
 
 // AdamW over many tensors, gradients multiplied by the clip's scale first: a launch covers up to
-// kAdamTensors tensors, whose table is a kernel argument; tensors are cut into chunks of kAdamChunk
-// values, which the blocks take in turn.
-constexpr int kAdamTensors = 44, kAdamChunk = 8192;
+// kAdamTensors tensors, whose table is a kernel argument; tensors are cut into chunks, which
+// the blocks take in turn.
+constexpr int kAdamTensors = 44;
 struct AdamTable {
   float* theta[kAdamTensors];
   const void* grad[kAdamTensors];
@@ -98,7 +99,7 @@ struct AdamTable {
   float lr[kAdamTensors], wd[kAdamTensors];
   int first[kAdamTensors + 1];  // chunks before each tensor
   uint8_t bf16[kAdamTensors];   // the gradient's type
-  int count;
+  int count, chunk;
   float b1, b2, eps, c1, c2;
 };
 static_assert(sizeof(AdamTable) <= 3900, "kernel arguments hold 4 KiB");
@@ -114,8 +115,8 @@ __global__ __launch_bounds__(256) void adamw_steps_kernel(AdamTable t, const flo
       if (t.first[mid] <= c) q = mid;
       else hi = mid - 1;
     }
-    const size_t at = (size_t)(c - t.first[q]) * kAdamChunk;
-    const int n = (int)min(t.n[q] - at, (size_t)kAdamChunk), n4 = n / 4;
+    const size_t at = (size_t)(c - t.first[q]) * t.chunk;
+    const int n = (int)min(t.n[q] - at, (size_t)t.chunk), n4 = n / 4;
     float* const th = t.theta[q] + at;
     float* const m = t.m[q] + at;
     float* const v = t.v[q] + at;
@@ -244,14 +245,18 @@ hipError_t launch_adamw_steps(const moe_adamw_tensor* p, int n, float lr, float 
                               float eps, float c1, float c2, const float* norm, hipStream_t s) {
   AdamTable t;
   t.b1 = beta1; t.b2 = beta2; t.eps = eps; t.c1 = c1; t.c2 = c2;
+  size_t total = 0;
+  for (int i = 0; i < n; ++i) total += p[i].n;
+  const bool few = total >= kFewBlocks;
+  t.chunk = few ? 8192 : 1024;
   t.count = 0;
   t.first[0] = 0;
   for (int i = 0; i <= n; ++i) {
     const bool end = i == n;
     // (a launch's chunks are counted in 31 bits: a tensor that does not fit opens the next)
-    const int64_t chunks = end ? 0 : (int64_t)((p[i].n + kAdamChunk - 1) / kAdamChunk);
+    const int64_t chunks = end ? 0 : (int64_t)((p[i].n + t.chunk - 1) / t.chunk);
     if (t.count > 0 && (end || t.count == kAdamTensors || t.first[t.count] + chunks > INT32_MAX)) {
-      const int blocks = std::min(t.first[t.count], 2 * num_cus());
+      const int blocks = std::min(t.first[t.count], few ? 2 * num_cus() : 8192);
       MOE_TIMED("adamw_steps", s, adamw_steps_kernel<<<blocks, 256, 0, s>>>(t, norm));
       if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
       t.count = 0;

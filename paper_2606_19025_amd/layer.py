@@ -393,48 +393,53 @@ class BlockNorm:
             dtype=B.MOE_BF16 if dtype == torch.bfloat16 else B.MOE_F32, T=self.T, d=self.d,
             gate_kind=B.BLOCK_GATES[gate], scale=float(scale), eps=float(eps),
             d_post_weight=p(self.d_post_weight), d_post_bias=p(self.d_post_bias),
-            d_gate=p(self.d_gate), d_pre_weight=p(self.d_pre_weight), d_pre_bias=p(self.d_pre_bias))
-
-    def _check(self, name, t, shape, dtype):
-        _check_tensor(name, t, shape, dtype, self.device, "norm")
+            d_gate=p(self.d_gate), d_pre_weight=p(self.d_pre_weight), d_pre_bias=p(self.d_pre_bias),
+            u=p(self.u))
+        self._own_rows = False
+        self._rows()
 
     def _vector(self, name, t, there, shape):
         """The address of a vector of floats that is there, or not, by the norm's form."""
         if there:
-            self._check(name, t, shape, torch.float32)
+            _check_tensor(name, t, shape, torch.float32, self.device, "norm")
             return t.data_ptr()
         if t is not None:
             raise ValueError(f"{name} given to a norm built without one")
         return None
 
     def _weights(self, post_weight, post_bias, gate, pre_weight, pre_bias=None, forward=False):
-        a, d = self._args, (self.d,)
-        a.post_weight = self._vector("post_weight", post_weight, self.post, d)
-        a.post_bias = self._vector("post_bias", post_bias, self.post and self.bias, d)
-        a.gate = self._vector("gate", gate, self.gate is not None, self.gate_shape)
-        a.pre_weight = self._vector("pre_weight", pre_weight, self.pre, d)
+        a, d, vector = self._args, (self.d,), self._vector
+        a.post_weight = vector("post_weight", post_weight, self.post, d)
+        a.post_bias = vector("post_bias", post_bias, self.post and self.bias, d)
+        a.gate = vector("gate", gate, self.gate is not None, self.gate_shape)
+        a.pre_weight = vector("pre_weight", pre_weight, self.pre, d)
         # (the backward reads no bias of the pre-norm)
-        a.pre_bias = self._vector("pre_bias", pre_bias, forward and self.pre and self.bias, d)
+        a.pre_bias = vector("pre_bias", pre_bias, forward and self.pre and self.bias, d)
 
-    def _rows(self, **stats):
-        for name, t in stats.items():
-            own = getattr(self, name)
-            if t is not None and own is None:
-                raise ValueError(f"{name} given to a norm built without one")
-            if t is not None:
-                self._check(name, t, (self.T,), torch.float32)
-            setattr(self._args, name, B._ptr(own if t is None else t))
+    def _rows(self, given=None):
+        """The statistics that the call writes or reads: the norm's own, but for the given ones."""
+        if given is None and self._own_rows:
+            return
+        for name in ("post_mean", "post_rstd", "pre_mean", "pre_rstd"):
+            t = own = getattr(self, name)
+            if given is not None and given[name] is not None:
+                t = given[name]
+                if own is None:
+                    raise ValueError(f"{name} given to a norm built without one")
+                _check_tensor(name, t, (self.T,), torch.float32, self.device, "norm")
+            setattr(self._args, name, B._ptr(t))
+        self._own_rows = given is None
 
     def forward(self, x, f, post_weight=None, post_bias=None, gate=None, pre_weight=None,
                 pre_bias=None, stream=None):
         """(x', u) of the residual stream x and the block's output f (u: None without a pre-norm)."""
         _check_current(self.device, "norm")
-        self._check("x", x, (self.T, self.d), self.dtype)
-        self._check("f", f, (self.T, self.d), self.dtype)
+        for name, t in (("x", x), ("f", f)):
+            _check_tensor(name, t, (self.T, self.d), self.dtype, self.device, "norm")
         self._weights(post_weight, post_bias, gate, pre_weight, pre_bias, forward=True)
-        self._rows(post_mean=None, post_rstd=None, pre_mean=None, pre_rstd=None)
+        self._rows()
         a = self._args
-        a.x, a.f, a.x_out, a.u = x.data_ptr(), f.data_ptr(), self.x.data_ptr(), B._ptr(self.u)
+        a.x, a.f, a.x_out = x.data_ptr(), f.data_ptr(), self.x.data_ptr()
         B.moe_block_norm_fwd(a, stream)
         return self.x, self.u
 
@@ -452,10 +457,11 @@ class BlockNorm:
             raise ValueError("dres is needed without a pre-norm")
         for name, t in (("du", du), ("dres", dres), ("f", f), ("x", x)):
             if t is not None:
-                self._check(name, t, (self.T, self.d), self.dtype)
+                _check_tensor(name, t, (self.T, self.d), self.dtype, self.device, "norm")
         a = self._args
         self._weights(post_weight, post_bias, gate, pre_weight)
-        self._rows(post_mean=post_mean, post_rstd=post_rstd, pre_mean=pre_mean, pre_rstd=pre_rstd)
+        stats = dict(post_mean=post_mean, post_rstd=post_rstd, pre_mean=pre_mean, pre_rstd=pre_rstd)
+        self._rows(stats if any(t is not None for t in stats.values()) else None)
         if self.ws is None:
             a.ws_bytes = B.moe_block_norm_bwd_workspace_size(self.T, self.d, a.dtype)
             with _on(stream):
