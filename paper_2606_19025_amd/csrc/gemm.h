@@ -170,28 +170,34 @@ hipError_t run_gemm_tile(int bf16, int ka, int kb, const GemmArgs* sets_a, int n
 constexpr int kXcdCounters = 8;
 hipError_t run_gemm_xent(int ka, const GemmArgs& a, const GemmArgs* b, int* counters, hipStream_t s);
 
+// Which tiles a bf16 launch of XE_LSE or XE_DZ (b NULL), or of XE_DX with XE_DW, takes: what
+// choose_tiles estimates for an up projection, or for dX with dW, of the same sizes.
+TileSize xent_tiles(const GemmArgs& a, const GemmArgs* b);
+
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
-// The gradient of logits z = scale * acc of a row with log-sum-exp lse (base 2: lse2), label column
-// yc and coefficient cf (with zf = 1 + 2 z_coef lse) at column c, where c < V; 0 past it.
-DEVI float xent_dz(float acc, float scale2, float lse2, float cf, float zf, int c, int yc, int V) {
-  const float p = __builtin_amdgcn_exp2f(acc * scale2 - lse2);
-  const float g = cf * (zf * p - (c == yc ? 1.0f : 0.0f));
-  return c < V ? g : 0.0f;
-}
-
-// Partial (max, sum of 2^(z - max)) of NJ x 4 logits acc * scale2 that a lane holds of a row at columns
-// c + 16 j + t, with those of the three lanes 16 apart that hold the row's others; columns from V on
-// are left out.
+// Partial (max, sum of 2^(z - max)) of the 4 NJ logits z = acc * scale2 (base 2) that a lane holds of a
+// row at columns c + 16 j + t, with those of the three lanes 16 apart that hold the row's others;
+// whole: no column of the tile lies past the last, V - 1 (wave-uniform), else those are left out.
 template <int NJ>
-DEVI float2 xent_partial(const f32x4_t (&acc)[NJ], float scale2, int c, int V) {
-  float m = -INFINITY;
-  const bool whole = c + 16 * NJ <= V;  // (c is at most 12 columns past the tile's first)
+DEVI float2 xent_partial(f32x4_t (&acc)[NJ], float scale2, int c, int V, bool whole) {
+  if (!whole) {
+    const float none = scale2 < 0.0f ? INFINITY : -INFINITY;
 #pragma unroll
-  for (int j = 0; j < NJ; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-      if (whole || c + 16 * j + t < V) m = fmaxf(m, acc[j][t] * scale2);
+      for (int t = 0; t < 4; ++t)
+        if (c + 16 * j + t >= V) acc[j][t] = none;
+  }
+  float m = acc[0][0];
+  if (scale2 >= 0.0f) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) m = fmaxf(fmaxf(fmaxf(fmaxf(m, acc[j][0]), acc[j][1]), acc[j][2]), acc[j][3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) m = fminf(fminf(fminf(fminf(m, acc[j][0]), acc[j][1]), acc[j][2]), acc[j][3]);
+  }
+  m *= scale2;
   m = fmaxf(m, __shfl_xor(m, 16, 64));
   m = fmaxf(m, __shfl_xor(m, 32, 64));
   const float at = m == -INFINITY ? 0.0f : m;
@@ -199,11 +205,37 @@ DEVI float2 xent_partial(const f32x4_t (&acc)[NJ], float scale2, int c, int V) {
 #pragma unroll
   for (int j = 0; j < NJ; ++j)
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-      if (whole || c + 16 * j + t < V) s += __builtin_amdgcn_exp2f(acc[j][t] * scale2 - at);
+    for (int t = 0; t < 4; ++t) s += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[j][t], scale2, -at));
   s += __shfl_xor(s, 16, 64);
   s += __shfl_xor(s, 32, 64);
   return float2{m, s};
+}
+
+// The same lane's logits become their gradients cf (zf exp(z - lse) - [column = y]), rounded by the
+// caller; zeros from column V on.  lse2: of base 2; y: the label's column, or any other number.
+template <int NJ>
+DEVI void xent_gradient(f32x4_t (&acc)[NJ], float scale2, float lse2, float cf, float zf, int c, int y, int V,
+                        bool whole) {
+  const float k = cf * zf;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      acc[j][t] = k * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[j][t], scale2, -lse2));
+  if (__ballot((unsigned)(y - c) < 16u * NJ)) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (y == c + 16 * j + t) acc[j][t] -= cf;
+  }
+  if (!whole) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (c + 16 * j + t >= V) acc[j][t] = 0.0f;
+  }
 }
 
 }  // namespace moe

@@ -466,7 +466,14 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
   static_assert(Cfg<KA>::NW == 8 && Cfg<KB>::NW == 8, "8 waves per block");
   static_assert(Cfg<KA>::LDS == Cfg<KB>::LDS, "one LDS ring size per launch");
   constexpr int NW = 8, MI = Cfg<KA>::MI, NJ = Cfg<KA>::NJ, WM = Cfg<KA>::WM;
+  // The logits' kinds spend their epilogue on arithmetic and leave the ring alone, so that the next
+  // tile's first k-steps are loaded under it; what their rows need (label, lse, coefficient) comes with
+  // those, and dz is staged in 2 KB of a wave's own, 16 rows by 64 columns at a time.
+  constexpr bool EARLY = KA == XE_LSE || KA == XE_DZ;
+  constexpr int SETS = EARLY ? 1 : kMaxSets;
   __shared__ __attribute__((aligned(1024))) char lds[Cfg<KA>::LDS];
+  __shared__ float row_info[EARLY ? 2 : 1][EARLY ? 3 : 1][EARLY ? GT : 1];
+  __shared__ __attribute__((aligned(16))) char stage_dz[KA == XE_DZ ? NW : 1][2048];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   const int wm = wave >> 1, wn = wave & 1;
@@ -490,8 +497,8 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
   // across blocks).
   const int per_xcd = gridDim.x / N_XCD;
   const int xcd = blockIdx.x % N_XCD;
-  __shared__ GroupTable gtab[kMaxSets];
-  __shared__ int shares[kMaxSets][2];  // of uneven sets: this XCD's first tile and the next's
+  __shared__ GroupTable gtab[SETS];
+  __shared__ int shares[SETS][2];  // of uneven sets: this XCD's first tile and the next's
   if (wave < L.n_sets) {
     const GemmArgs& a = L.s[wave];
     build_group_table<GT>(a, gtab[wave], kTileRows);
@@ -759,9 +766,28 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
     });
   };
 
-  TileCtx cur;
+  // (EARLY) thread r's values of row r of the next tile
+  float info[3] = {0.f, 0.f, 0.f};
+  int info_at = 0;
+  bool stored = false;  // a tile's stores follow its loads
+  auto load_info = [&](const TileCtx& c) {
+    if constexpr (EARLY) {
+      const XentArgs& x = L.s[0].xe;
+      const int m = c.tl.row0 + min((int)threadIdx.x, c.tl.rows - 1);
+      if (threadIdx.x < GT) {
+        info[0] = __builtin_bit_cast(float, x.label[m] - x.v0);
+        if constexpr (KA == XE_DZ) {
+          info[1] = x.lse[m];
+          info[2] = x.coef[m];
+        }
+      }
+    }
+  };
+
+  TileCtx cur, early;
   if (i < total) {
     make_ctx(i, cur);
+    load_info(cur);
     prologue(cur);
   }
   while (i < total) {
@@ -832,7 +858,15 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
       bf16x8_t af0[MI], af1[MI], bq[4];
       if (nk > 0) {
         // own DMA of k-step 0 done (k-steps 1 .. min(NS, nk) - 1 may stay in flight)
-        wait_vm_groups<C_::DMA_N, NS - 1>(nk - 1);
+        // (EARLY: the epilogue's stores are newer than these loads and need not be waited for)
+        if (EARLY && stored && nk > 1) WAIT_VMCNT(C_::DMA_N + (KA == XE_DZ ? 4 * MI : MI));
+        else wait_vm_groups<C_::DMA_N, NS - 1>(nk - 1);
+        if constexpr (EARLY) {
+          stored = true;
+          if (threadIdx.x < GT)
+#pragma unroll
+            for (int q = 0; q < (KA == XE_DZ ? 3 : 1); ++q) row_info[info_at][q][threadIdx.x] = info[q];
+        }
         __syncthreads();
 #pragma unroll
         for (int f = 0; f < MI; ++f) af0[f] = frag_a(lds, 0, f);
@@ -874,6 +908,15 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
       // in 200 instead of 148 us in about half of the calls.)
       if (dyn && threadIdx.x == 0) nxt = atomicAdd(L.counters + xcd, 1);
 
+      // (every wave passed the last k-step's barrier, after which none reads the ring)
+      if constexpr (EARLY) {
+        if (i + per_xcd < total) {
+          make_ctx(i + per_xcd, early);
+          load_info(early);
+          prologue(early);
+        }
+      }
+
       // ---- epilogue, part 1: results into registers (or, for the kinds
       // that read memory and the accumulating weight gradients, the whole
       // epilogue).  Accumulator (i, j) register t
@@ -911,25 +954,64 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
         }
       } else if constexpr (KIND == XE_LSE) {
         const float scale2 = a.xe.scale * kLog2e;
-        const int c0 = tl.n0 + wn * 128;
+        const int c0 = tl.n0 + wn * 128, c = c0 + 4 * (ln >> 4);
+        const bool whole = c0 + 128 <= a.xe.V;
+        const __amdgpu_buffer_rsrc_t rp = store_rsrc(a.xe.part + (size_t)(c0 >> 7) * a.cap);
 #pragma unroll
         for (int ii = 0; ii < MI; ++ii) {
           const int row = wm * WM + ii * 16 + (ln & 15);
-          const float2 ms = xent_partial<NJ>(acc[ii], scale2, c0 + 4 * (ln >> 4), a.xe.V);
           const bool ok = row < tl.rows;
           const size_t m = (size_t)(tl.row0 + row);
-          if (ok && ln < 16) a.xe.part[(size_t)(c0 >> 7) * a.cap + m] = ms;
           // the label's logit, where it lies among these columns
-          int y = ok ? a.xe.label[m] - a.xe.v0 - c0 : -1;
-          if (y >= min(128, a.xe.V - c0)) y = -1;
+          int y = __builtin_bit_cast(int, row_info[info_at][0][row]);
+          if (!ok || y < c0 || y >= min(c0 + 128, a.xe.V)) y = -1;
           if (__ballot(y >= 0)) {
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
               for (int t = 0; t < 4; ++t)
-                if (y == 16 * j + 4 * (ln >> 4) + t) a.xe.z_label[m] = acc[ii][j][t] * a.xe.scale;
+                if (y == c + 16 * j + t) a.xe.z_label[m] = acc[ii][j][t] * a.xe.scale;
+          }
+          const float2 ms = xent_partial<NJ>(acc[ii], scale2, c, a.xe.V, whole);
+          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, ms), rp,
+                                                ok && ln < 16 ? 8u * (unsigned)m : kOOB, 0, 0);
+        }
+        info_at ^= 1;
+      } else if constexpr (KIND == XE_DZ) {
+        const float scale2 = a.xe.scale * kLog2e;
+        const int c0 = tl.n0 + wn * 128, c = c0 + 4 * (ln >> 4);
+        const bool whole = c0 + 128 <= a.xe.V;
+        const __amdgpu_buffer_rsrc_t rc = store_rsrc(a.C);
+        char* const st = stage_dz[wave];
+#pragma unroll
+        for (int ii = 0; ii < MI; ++ii) {
+          const int row = wm * WM + ii * 16 + (ln & 15);
+          const float lse = row_info[info_at][1][row];
+          xent_gradient<NJ>(acc[ii], scale2, lse * kLog2e, row_info[info_at][2][row], 1.0f + a.xe.z2 * lse, c,
+                            __builtin_bit_cast(int, row_info[info_at][0][row]), a.xe.V, whole);
+          // 16 rows of 128 bytes, 16-byte chunk q of row r at chunk q ^ (r & 7); a store covers the
+          // whole 128 bytes of 8 rows.  (dz is read again by the next launch: it stays in the caches)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < NJ / 2; ++j)
+              *reinterpret_cast<bf16x4_t*>(st + (ln & 15) * 128 + (((2 * j + (ln >> 5)) ^ (ln & 7)) << 4) +
+                                           ((ln >> 4) & 1) * 8) =
+                  __builtin_convertvector(acc[ii][h * (NJ / 2) + j], bf16x4_t);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's own)
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+              const int r = it * 8 + (ln >> 3), q = ln & 7;
+              const u32x4_t v = *reinterpret_cast<const u32x4_t*>(st + r * 128 + ((q ^ (r & 7)) << 4));
+              const int at = wm * WM + ii * 16 + r, col = c0 + h * 64 + 8 * q;
+              store16<false>(rc, at < tl.rows && col < a.N
+                                     ? 2u * ((unsigned)(tl.row0 + at) * (unsigned)a.ldc + (unsigned)col)
+                                     : kOOB, v);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           }
         }
+        info_at ^= 1;
       } else if constexpr (KIND == XE_DX) {
         // fp32 partial sums ([cap, N]) of a part of K, added to those of earlier pieces
         float* const part = a.part + (size_t)tl.split * a.c_split;
@@ -1006,21 +1088,6 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
         // (nontemporal: measured 2-4 % faster for DHH_BWD, DX_BWD and
         // DOWN_FWD; the fp32 weight gradients are not, they were 1.4-1.7x
         // slower that way).
-        if constexpr (KIND == XE_DZ) {
-          const float scale2 = a.xe.scale * kLog2e;
-#pragma unroll
-          for (int ii = 0; ii < MI; ++ii) {
-            const size_t m = (size_t)(tl.row0 + min(wm * WM + ii * 16 + (ln & 15), tl.rows - 1));
-            const float lse = a.xe.lse[m], cf = a.xe.coef[m], zf = 1.0f + a.xe.z2 * lse;
-            const int y = a.xe.label[m] - a.xe.v0;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-              for (int t = 0; t < 4; ++t)
-                acc[ii][j][t] = xent_dz(acc[ii][j][t], scale2, lse * kLog2e, cf, zf,
-                                        tl.n0 + wn * 128 + 16 * j + 4 * (ln >> 4) + t, y, a.xe.V);
-          }
-        }
 #pragma unroll
         for (int ii = 0; ii < MI; ++ii)
 #pragma unroll
@@ -1041,8 +1108,7 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
             out[8 + it] = epi_get(reg, row, cg + 4);
           }
           late = true;
-        } else if constexpr (KIND == DOWN_FWD || KIND == DX_BWD || KIND == UP_FWD || KIND == XE_DZ ||
-                             KIND == XE_DW) {
+        } else if constexpr (KIND == DOWN_FWD || KIND == DX_BWD || KIND == UP_FWD || KIND == XE_DW) {
           const int c = ln & 15;
 #pragma unroll
           for (int it = 0; it < WM / 4; ++it) out[it] = epi_get(reg, it * 4 + (ln >> 4), c);
@@ -1159,17 +1225,14 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
           store16<true>(rg, ok ? 2u * (m * 2u * H + H + h) : kOOB, __builtin_bit_cast(u32x4_t, U));
           store16<true>(rh, ok ? 2u * (m * H + h) : kOOB, __builtin_bit_cast(u32x4_t, Hv));
         }
-      } else if constexpr (KIND == XE_DZ || KIND == XE_DW) {
-        // (dz is read again by the next launch, so it stays in the caches)
+      } else if constexpr (KIND == XE_DW) {
         const int col = tl.n0 + wn * 128 + 8 * (ln & 15);
         const __amdgpu_buffer_rsrc_t rc = store_rsrc(a.C);
-        const int rows = KIND == XE_DW ? a.xe.V : tl.rows;
 #pragma unroll
         for (int it = 0; it < WM / 4; ++it) {
-          const int row = (KIND == XE_DW ? tl.m0 : 0) + wm * WM + it * 4 + (ln >> 4);
-          const unsigned m = (unsigned)((KIND == XE_DW ? 0 : tl.row0) + row);
-          store16<KIND == XE_DW>(rc, row < rows && col < a.N ? 2u * (m * (unsigned)a.ldc + col) : kOOB,
-                                 __builtin_bit_cast(u32x4_t, out[it]));
+          const int row = tl.m0 + wm * WM + it * 4 + (ln >> 4);
+          store16<true>(rc, row < a.xe.V && col < a.N ? 2u * ((unsigned)row * (unsigned)a.ldc + col) : kOOB,
+                        __builtin_bit_cast(u32x4_t, out[it]));
         }
       } else if constexpr (KIND == DOWN_FWD || KIND == DX_BWD || KIND == UP_FWD) {
         const int c = ln & 15;
@@ -1195,6 +1258,11 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
       }
     });
 
+    if constexpr (EARLY) {
+      cur = early;
+      i += per_xcd;
+      continue;
+    }
     // ---- next tile: the dealt tile is broadcast through LDS; the barrier
     // also frees the ring (every wave has read back its staged results)
     if (dyn) {
@@ -1579,6 +1647,12 @@ TileSize choose_tiles(int ka, const GemmArgs* sa, int na, const GemmArgs* sb, in
 }
 
 }  // namespace
+
+TileSize xent_tiles(const GemmArgs& a, const GemmArgs* b) {
+  bool parts = b != nullptr;
+  const int split = 1;
+  return choose_tiles(b ? DX_BWD : UP_FWD, &a, 1, b, b ? 1 : 0, &split, &parts);
+}
 
 // Rows of an expert's first weight per hidden unit: 2 (gate and up) for
 // SwiGLU, 1 for the SiLU expert.

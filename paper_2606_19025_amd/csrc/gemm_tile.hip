@@ -380,7 +380,8 @@ DEVI void gemm_tile(const GemmArgs& a, const TileAt& tl, char* lds) {
   // a lane's rows of the logits' kinds: row (wm MI + i) 16 + l16, columns 16 j + 4 g4 + t of the wave's
   if constexpr (KIND == XE_LSE || KIND == XE_DZ) {
     const float scale2 = a.xe.scale * kLog2e;
-    const int c0 = n0 + wn * 16 * NJ;
+    const int c0 = n0 + wn * 16 * NJ, c = c0 + 4 * g4;
+    const bool whole = c0 + 16 * NJ <= a.xe.V;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const int r = (wm * MI + i) * 16 + l16;
@@ -388,23 +389,19 @@ DEVI void gemm_tile(const GemmArgs& a, const TileAt& tl, char* lds) {
       const size_t m = (size_t)(tl.row0 + (ok ? r : 0));
       const int y = a.xe.label[m] - a.xe.v0;
       if constexpr (KIND == XE_LSE) {
-        const float2 ms = xent_partial<NJ>(acc[i], scale2, c0 + 4 * g4, a.xe.V);
-        if (ok && g4 == 0) a.xe.part[(size_t)(c0 / (16 * NJ)) * a.cap + m] = ms;
         if (ok && y >= c0 && y < min(c0 + 16 * NJ, a.xe.V)) {
 #pragma unroll
           for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-              if (y - c0 == 16 * j + 4 * g4 + t) a.xe.z_label[m] = acc[i][j][t] * a.xe.scale;
+              if (y == c + 16 * j + t) a.xe.z_label[m] = acc[i][j][t] * a.xe.scale;
         }
+        const float2 ms = xent_partial<NJ>(acc[i], scale2, c, a.xe.V, whole);
+        if (ok && g4 == 0) a.xe.part[(size_t)(c0 / (16 * NJ)) * a.cap + m] = ms;
       } else {
-        const float lse = a.xe.lse[m], cf = a.xe.coef[m], zf = 1.0f + a.xe.z2 * lse;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-            acc[i][j][t] = xent_dz(acc[i][j][t], scale2, lse * kLog2e, cf, zf, c0 + 16 * j + 4 * g4 + t,
-                                   y, a.xe.V);
+        const float lse = a.xe.lse[m];
+        xent_gradient<NJ>(acc[i], scale2, lse * kLog2e, a.xe.coef[m], 1.0f + a.xe.z2 * lse, c, y, a.xe.V,
+                          whole);
       }
     }
     if constexpr (KIND == XE_LSE) return;

@@ -24,10 +24,10 @@
 namespace moe {
 namespace {
 
-constexpr int kRows = 64;        // tokens of a block of the row kernels
-constexpr int kCountRows = 1024; // tokens of a counting block
-constexpr int kDirect = 8192;    // up to here every block counts all labels itself
-constexpr int kSegments = 16;    // threads of a row of partials
+constexpr int kRows = 16;         // tokens of a block of xent_rows
+constexpr int kCountRows = 1024;  // tokens of a counting block
+constexpr int kDirect = 8192;     // up to here every block counts all labels itself
+constexpr int kLossThreads = 1024;
 
 struct RowArgs {
   const void* x;
@@ -44,6 +44,8 @@ struct RowArgs {
   float* row_lse;      // backward
   float* coef;
   void* xc;
+  int* counters;       // cleared for the launches that follow
+  int n_counters;
 };
 
 DEVI int block_sum_256(int v, int* buf) {
@@ -75,6 +77,7 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
   // tokens that count before this block's, and all of them
   int before = 0, total = 0;
   if (a.N <= kDirect) {
+#pragma unroll 8
     for (int t = threadIdx.x; t < a.N; t += 256) {
       const int v = a.label[t] >= 0;
       total += v;
@@ -92,11 +95,13 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
   total = block_sum_256(total, buf);
   if (threadIdx.x < 64) {
     const int t = t0 + threadIdx.x;
-    const int y = t < a.N ? a.label[t] : -1;
+    const int y = (int)threadIdx.x < kRows && t < a.N ? a.label[t] : -1;
     const unsigned long long counts = __ballot(y >= 0);
     const int p = y < 0 ? -1 : before + __builtin_popcountll(counts & ((1ull << threadIdx.x) - 1));
-    row[threadIdx.x] = p;
-    if (t < a.N) a.pos[t] = p;
+    if ((int)threadIdx.x < kRows) {
+      row[threadIdx.x] = p;
+      if (t < a.N) a.pos[t] = p;
+    }
     if (p >= 0) {
       const bool in = y < a.V;
       a.row_label[p] = y;
@@ -110,17 +115,18 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
     }
     if (blockIdx.x == 0 && threadIdx.x < 2) a.off[threadIdx.x] = threadIdx.x ? total : 0;
   }
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < a.n_counters; i += 256) a.counters[i] = 0;
   if (total == a.N) return;  // x itself is read
   __syncthreads();
+  // sixteen threads to a row, so that all rows' loads are in flight
   const int chunks = a.d * a.size / 16;
-  const u32x4_t* src = static_cast<const u32x4_t*>(a.x);
-  u32x4_t* dst = static_cast<u32x4_t*>(a.xc);
-  for (int r = threadIdx.x >> 6; r < kRows; r += 4) {
-    const int p = row[r];
-    if (p < 0) continue;
-    for (int c = threadIdx.x & 63; c < chunks; c += 64)
-      dst[(size_t)p * chunks + c] = src[(size_t)(t0 + r) * chunks + c];
-  }
+  const int r = threadIdx.x / (256 / kRows), p = row[r];
+  if (p < 0) return;
+  const u32x4_t* src = static_cast<const u32x4_t*>(a.x) + (size_t)(t0 + r) * chunks;
+  u32x4_t* dst = static_cast<u32x4_t*>(a.xc) + (size_t)p * chunks;
+#pragma unroll 4
+  for (int c = threadIdx.x % (256 / kRows); c < chunks; c += 256 / kRows) dst[c] = src[c];
 }
 
 // (max, sum) pairs of base 2 joined.
@@ -130,61 +136,73 @@ DEVI float2 join(float2 a, float2 b) {
   return float2{m, a.y * __builtin_amdgcn_exp2f(a.x - m) + b.y * __builtin_amdgcn_exp2f(b.x - m)};
 }
 
-// lse and loss of kRows tokens a block from their P partials; the block's sum of losses.
-__global__ __launch_bounds__(kRows * kSegments) void xent_loss_kernel(
+// lse and loss of R tokens a block from their P partials, 1024 / R threads a token.  Few tokens a block
+// where there are few: 24 tokens of 1536 partials took 42 us with 64 a block.  The block that ends last
+// adds the blocks' sums of losses, in order.
+template <int R>
+__global__ __launch_bounds__(kLossThreads) void xent_loss_kernel(
     int N, int P, float z_coef, const int* pos, const int* off, const float2* part, const float* z_label,
-    float* loss, float* lse, double* sums, float* total) {
-  __shared__ float2 seg[kSegments][kRows];
-  const int r = threadIdx.x & (kRows - 1), q = threadIdx.x / kRows;
-  const int t = blockIdx.x * kRows + r;
+    float* loss, float* lse, double* sums, int* done, float* total) {
+  constexpr int S = kLossThreads / R, WAVES = kLossThreads / 64;
+  __shared__ float2 seg[WAVES][R];
+  __shared__ bool last;
+  const int r = threadIdx.x % R, q = threadIdx.x / R;
+  const int t = blockIdx.x * R + r;
   const int p = t < N ? pos[t] : -1;
   float2 v = {-INFINITY, 0.f};
-  if (p >= 0)
-    for (int i = q; i < P; i += kSegments) v = join(v, part[(size_t)i * N + p]);
-  seg[q][r] = v;
-  __syncthreads();
-  if (q != 0) return;
-  float l = 0.f, out = 0.f;
   if (p >= 0) {
-#pragma unroll
-    for (int i = 1; i < kSegments; ++i) v = join(v, seg[i][r]);
-    l = v.x * kLn2 + logf(v.y);
-    out = l - z_label[p] + z_coef * l * l;
+#pragma unroll 4
+    for (int i = q; i < P; i += S) v = join(v, part[(size_t)i * N + p]);
   }
-  if (t < N) {
-    lse[t] = l;
-    loss[t] = out;
-  }
-  double s = (double)out;
+  // the threads of a token in a wave are R lanes apart; then the waves'
+  auto across = [&]() {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if (r == 0) {
-    if (gridDim.x > 1) {
-      sums[blockIdx.x] = s;
-    } else {
-      total[0] = (float)s;
-      total[1] = N > 0 ? (float)off[1] : 0.f;
+    for (int o = R; o < 64; o *= 2) v = join(v, float2{__shfl_xor(v.x, o, 64), __shfl_xor(v.y, o, 64)});
+  };
+  across();
+  if ((threadIdx.x & 63) < R) seg[threadIdx.x >> 6][r] = v;
+  __syncthreads();
+  float out = 0.f;
+  if (threadIdx.x < 64) {
+    v = float2{-INFINITY, 0.f};
+#pragma unroll
+    for (int w = threadIdx.x / R; w < WAVES; w += 64 / R) v = join(v, seg[w][r]);
+    across();
+    if ((int)threadIdx.x < R && t < N) {
+      float l = 0.f;
+      if (p >= 0) {
+        l = v.x * kLn2 + logf(v.y);
+        out = l - z_label[p] + z_coef * l * l;
+      }
+      lse[t] = l;
+      loss[t] = out;
     }
   }
-}
-
-__global__ __launch_bounds__(256) void xent_total_kernel(const double* sums, int n, const int* off,
-                                                         float* total) {
-  __shared__ double buf[4];
+  if (threadIdx.x < 64) {
+    double s = (double)out;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (threadIdx.x == 0) {
+      __hip_atomic_store(sums + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last = __hip_atomic_fetch_add(done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    }
+  }
+  __syncthreads();
+  if (!last || threadIdx.x >= 64) return;
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += 256) s += sums[i];
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += 64)
+    s += __hip_atomic_load(sums + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = s;
-  __syncthreads();
   if (threadIdx.x == 0) {
-    total[0] = (float)(buf[0] + buf[1] + buf[2] + buf[3]);
+    total[0] = (float)s;
     total[1] = (float)off[1];
   }
 }
 
-__global__ __launch_bounds__(64) void xent_zero_kernel(int* counters, int n) {
-  if ((int)threadIdx.x < n) counters[threadIdx.x] = 0;
+// total of no tokens.
+__global__ __launch_bounds__(64) void xent_none_kernel(float* total) {
+  if (threadIdx.x < 2) total[threadIdx.x] = 0.f;
 }
 
 // n 16-byte pieces of zeros (the gradient of no tokens).
@@ -222,24 +240,30 @@ size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
 // Sizes of a call's tiles, pieces and workspace.
 struct Plan {
-  bool large;          // 256 x 256 tiles
-  TileSize tile;       // else
+  TileSize logits;     // of the logits' launches
+  TileSize pair;       // of dx with dW
   int piece;           // columns of a piece of the backward, a multiple of 256
   int fwd_piece;       // and of the forward
   int split;           // parts of K of dx
-  int parts;           // partials of a row (upper bound over the tile sizes)
+  int parts;           // partials of a row, at most
 };
 
-constexpr size_t kDzBytes = (size_t)512 << 20;
+// dz of a piece.  Smaller pieces read and write dx's partial sums more often, larger ones leave the
+// last-level cache (8192 tokens, d = 2048, 49152 words, loss and gradients, ms by MiB: 64 5.44, 128 5.20,
+// 256 5.27, 512 5.27, 1024 5.27; 1531 tokens, d = 768, 50003 words 0.52, 0.45, 0.42, 0.42, 0.42).
+constexpr size_t kDzBytes = (size_t)256 << 20;
 constexpr int kPad = 256;
+
+int tile_rows(TileSize t) { return t == TILE_256x256 ? 256 : t == TILE_32x64 ? 32 : 64; }
+int tile_cols(TileSize t) { return t == TILE_256x256 ? 256 : t == TILE_64x128 ? 128 : 64; }
+
+// fp32: six tiles of 64 x 128 per CU, or 32 x 64 ones (as the grouped GEMMs).
+TileSize f32_tiles(double tiles) { return tiles >= 6.0 * num_cus() ? TILE_64x128 : TILE_32x64; }
 
 Plan plan_of(const moe_xent& x) {
   const bool bf16 = x.dtype == MOE_BF16;
   const size_t s = bf16 ? 2 : 4;
   Plan p{};
-  p.large = bf16 && x.N > 128;
-  if (bf16) p.tile = x.N <= 32 ? TILE_32x64 : TILE_64x128;
-  else p.tile = (long)ceil_div(x.N, 64) * ceil_div(x.V, 128) >= 6L * num_cus() ? TILE_64x128 : TILE_32x64;
   const int width = up((size_t)x.V);
   // a piece's operands (rows of W and dW) below 2 GiB, dz within its budget
   const size_t most_w = std::max<size_t>(kPad, ((size_t)2 << 30) / ((size_t)x.d * 4) / kPad * kPad);
@@ -248,14 +272,27 @@ Plan plan_of(const moe_xent& x) {
   p.piece = (int)up((size_t)ceil_div(width, pieces));
   p.fwd_piece = (int)std::min<size_t>(most_w, (size_t)width);
   p.parts = ceil_div(x.V, 64) * 2 + 2;
-  // parts of K of dx, so that its few long tiles take no longer than all tiles by CUs
-  const int bm = p.large ? 256 : p.tile == TILE_32x64 && !bf16 ? 32 : 64, bn = p.large ? 256 : bm * 2;
-  const double dx_tiles = (double)ceil_div(x.N, bm) * ceil_div(x.d, bn);
-  const double dw_tiles = (double)ceil_div(p.piece, bm) * ceil_div(x.d, bn);
-  const int slots = num_cus() * (p.large ? 1 : 4);
-  const double share = std::max((dx_tiles * p.piece + dw_tiles * x.N) / slots, 512.0);
+  GemmArgs z{}, dx{}, dw{};
+  z.n_groups = dx.n_groups = dw.n_groups = 1;
+  z.cap = dx.cap = dw.cap = x.N;
+  z.N = std::min(x.V, p.fwd_piece); z.K = x.d;
+  dx.N = x.d; dx.K = std::min(x.V, p.piece);
+  dw.M = dx.K; dw.N = x.d;
+  if (bf16) {
+    p.logits = xent_tiles(z, nullptr);
+    p.pair = xent_tiles(dx, &dw);
+  } else {
+    const double cols = ceil_div(x.d, 128);
+    p.logits = f32_tiles((double)ceil_div(x.N, 64) * ceil_div(z.N, 128));
+    p.pair = f32_tiles(cols * (ceil_div(x.N, 64) + ceil_div(dw.M, 64)));
+  }
+  // Parts of K of dx: its few tiles reduce over the whole piece, so they are cut until they are three
+  // quarters of the CUs; 512 columns a part at least.  Measured (us of the backward by parts): 512 tokens,
+  // d = 2048, 32768 words 1 698, 2 394, 4 253, 8 212, 14 212, 28 242; 1531 tokens, d = 768, 50003 words
+  // 1055, 590, 365, 283, 284, 309; 4096 tokens, d = 1024, 32000 words 987, 731, 724, 748, 821, 907.
+  const double tiles = (double)ceil_div(x.N, tile_rows(p.pair)) * ceil_div(x.d, tile_cols(p.pair));
   const size_t most = ((size_t)256 << 20) / ((size_t)std::max(1, x.N) * x.d * 4);
-  p.split = (int)std::max<double>(1, std::min<double>({p.piece / share, 32.0, (double)most}));
+  p.split = (int)std::max(1.0, std::min({0.75 * num_cus() / std::max(tiles, 1.0), p.piece / 512.0, (double)most}));
   return p;
 }
 
@@ -276,9 +313,11 @@ struct Buffers {
   double* sums;
   void* dz;
   float* dx_part;
-  int* counters;
   size_t bytes;
 };
+
+// Tokens of a block of xent_loss.
+int loss_rows(int N) { return N >= 8192 ? 32 : N >= 1024 ? 16 : 4; }
 
 Buffers buffers(const moe_xent& x, const Plan& p, bool bwd, void* ws) {
   const size_t s = x.dtype == MOE_BF16 ? 2 : 4, N = x.N;
@@ -295,13 +334,16 @@ Buffers buffers(const moe_xent& x, const Plan& p, bool bwd, void* ws) {
   if (!bwd) {
     r.z_label = w.take<float>(N);
     b.part = w.take<float2>((size_t)p.parts * N);
-    b.sums = w.take<double>((N + kRows - 1) / kRows);
+    b.sums = w.take<double>((N + loss_rows(x.N) - 1) / loss_rows(x.N));
+    r.n_counters = 1;
+    r.counters = w.take<int>(1);
   } else {
     r.row_lse = w.take<float>(N);
     r.coef = w.take<float>(N);
     b.dz = w.take<char>(N * p.piece * s);
     b.dx_part = w.take<float>((size_t)p.split * N * x.d);
-    b.counters = w.take<int>(64);
+    r.n_counters = ceil_div(x.V, p.piece) * kXcdCounters;
+    r.counters = w.take<int>(r.n_counters);
   }
   b.bytes = w.used;
   return b;
@@ -336,10 +378,9 @@ GemmArgs logits(const moe_xent& x, const Buffers& b, int v0, int V) {
   return a;
 }
 
-hipError_t run(const Plan& p, int bf16, int ka, const GemmArgs& a, const GemmArgs* b, int* counters,
+hipError_t run(TileSize size, int bf16, int ka, const GemmArgs& a, const GemmArgs* b, int* counters,
                hipStream_t s) {
-  if (p.large) return run_gemm_xent(ka, a, b, counters, s);
-  const TileSize size = b && p.tile == TILE_32x64 ? TILE_64x128 : p.tile;
+  if (size == TILE_256x256) return run_gemm_xent(ka, a, b, counters, s);
   return run_gemm_tile(bf16, ka, b ? XE_DW : ka, &a, 1, b, b ? 1 : 0, size, s);
 }
 
@@ -353,24 +394,31 @@ hipError_t launch_xent_fwd(const moe_xent* x, hipStream_t s) {
   const int bf16 = x->dtype == MOE_BF16;
   const Buffers b = buffers(*x, p, false, x->ws);
   hipError_t e;
-  if (x->N > 0 && (e = rows<false>(b, s)) != hipSuccess) return e;
-  const int width = p.large ? 128 : p.tile == TILE_32x64 ? 32 : 64;  // of a partial: half a tile's columns
+  if (x->N == 0) {
+    MOE_TIMED("xent_none", s, xent_none_kernel<<<1, 64, 0, s>>>(x->total));
+    return hipGetLastError();
+  }
+  if ((e = rows<false>(b, s)) != hipSuccess) return e;
+  const int width = tile_cols(p.logits) / 2;  // of a partial: half a tile's columns
   int parts = 0;
-  for (int v0 = 0; x->N > 0 && v0 < x->V; v0 += p.fwd_piece) {
+  for (int v0 = 0; v0 < x->V; v0 += p.fwd_piece) {
     const int V = std::min(x->V - v0, p.fwd_piece);
     GemmArgs a = logits(*x, b, v0, V);
     a.xe.part = b.part + (size_t)parts * x->N;
     a.xe.z_label = b.row.z_label;
-    if ((e = run(p, bf16, XE_LSE, a, nullptr, nullptr, s)) != hipSuccess) return e;
+    if ((e = run(p.logits, bf16, XE_LSE, a, nullptr, nullptr, s)) != hipSuccess) return e;
     parts += ceil_div(V, 2 * width) * 2;
   }
-  const int blocks = std::max(1, ceil_div(x->N, kRows));
-  MOE_TIMED("xent_loss", s,
-            xent_loss_kernel<<<blocks, kRows * kSegments, 0, s>>>(
-                x->N, parts, x->z_coef, b.row.pos, b.row.off, b.part, b.row.z_label, x->loss, x->lse,
-                b.sums, x->total));
-  if ((e = hipGetLastError()) != hipSuccess || blocks == 1) return e;
-  MOE_TIMED("xent_total", s, xent_total_kernel<<<1, 256, 0, s>>>(b.sums, blocks, b.row.off, x->total));
+  const int R = loss_rows(x->N), blocks = ceil_div(x->N, R);
+#define XENT_LOSS(R_)                                                                                    \
+  MOE_TIMED("xent_loss", s,                                                                              \
+            xent_loss_kernel<R_><<<blocks, kLossThreads, 0, s>>>(                                        \
+                x->N, parts, x->z_coef, b.row.pos, b.row.off, b.part, b.row.z_label, x->loss, x->lse,    \
+                b.sums, b.row.counters, x->total))
+  if (R == 32) XENT_LOSS(32);
+  else if (R == 16) XENT_LOSS(16);
+  else XENT_LOSS(4);
+#undef XENT_LOSS
   return hipGetLastError();
 }
 
@@ -386,10 +434,10 @@ hipError_t launch_xent_bwd(const moe_xent* x, hipStream_t s) {
     GemmArgs a = logits(*x, b, v0, V);
     a.C = b.dz; a.ldc = ld;
     a.N = ld;  // (the columns past V are written too: zeros)
-    if ((e = run(p, bf16, XE_DZ, a, nullptr, nullptr, s)) != hipSuccess) return e;
+    if ((e = run(p.logits, bf16, XE_DZ, a, nullptr, nullptr, s)) != hipSuccess) return e;
     GemmArgs dx = a, dw = a;
     dx.A = b.dz; dx.lda = ld;
-    dx.N = x->d; dx.K = p.large ? ld : V;
+    dx.N = x->d; dx.K = p.pair == TILE_256x256 ? ld : V;
     dx.part = b.dx_part; dx.c_split = (long)x->N * x->d; dx.ksplit = p.split;
     dx.accumulate = v0 > 0;
     dw.A = b.dz; dw.lda = ld;
@@ -398,11 +446,8 @@ hipError_t launch_xent_bwd(const moe_xent* x, hipStream_t s) {
     dw.M = ld; dw.N = x->d;
     dw.accumulate = x->accumulate_dw;
     dw.xe.out_bf16 = x->dw_dtype == MOE_BF16;
-    if (p.large) {
-      MOE_TIMED("xent_zero", s, xent_zero_kernel<<<1, 64, 0, s>>>(b.counters, kXcdCounters));
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if ((e = run(p, bf16, XE_DX, dx, &dw, b.counters, s)) != hipSuccess) return e;
+    if ((e = run(p.pair, bf16, XE_DX, dx, &dw, b.row.counters + v0 / p.piece * kXcdCounters, s)) != hipSuccess)
+      return e;
   }
   if (x->N == 0) {
     const size_t n = (size_t)x->V * x->d * ws / 16;
