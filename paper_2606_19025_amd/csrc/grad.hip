@@ -8,7 +8,7 @@
 // overflow nor vanish there, and the conversions and multiply-adds take a fraction of the loads'
 // time.
 //
-// A launch covers up to kTensors tensors, whose table is a kernel argument: no list is copied to
+// A launch covers many tensors (GradTable), whose table is a kernel argument: no list is copied to
 // the device, and a captured launch keeps its own.  Tensors are cut into chunks (chunk_of),
 // which the blocks take in turn; every block stores one partial sum, and a last block adds the
 // partials of all launches in order, so the result does not depend on timing.
@@ -21,21 +21,29 @@
 namespace moe {
 namespace {
 
-constexpr int kTensors = 112;
 constexpr int kThreads = 256;
+constexpr int kMaxChunk = 16384;
 
+// Tensors of a launch: their pointers, the chunks before each, and the values of each one's last
+// chunk less one, with the type in the top bit (14 or 22 bytes a tensor, so that a launch takes as
+// many as it can).
+template <int N, bool OUT>
 struct GradTable {
-  const void* p[kTensors];
-  void* out[kTensors];
-  size_t n[kTensors];
-  int first[kTensors + 1];  // chunks before each tensor
-  uint8_t bf16[kTensors];
+  static constexpr int kTensors = N;
+  const void* p[N];
+  void* out[OUT ? N : 1];
+  int first[N + 1];
+  uint16_t tail[N];
   int count, chunk;
 };
-static_assert(sizeof(GradTable) <= 3900, "kernel arguments hold 4 KiB");
+typedef GradTable<272, false> NormTable;
+typedef GradTable<174, true> ClipTable;
+static_assert(sizeof(NormTable) <= 3968 && sizeof(ClipTable) <= 3968, "kernel arguments hold 4 KiB");
+static_assert(kMaxChunk <= 32768, "a tail has 15 bits");
 
 // The tensor of chunk c (wave-uniform).
-DEVI int tensor_of(const GradTable& t, int c) {
+template <class T>
+DEVI int tensor_of(const T& t, int c) {
   int lo = 0, hi = t.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -45,7 +53,24 @@ DEVI int tensor_of(const GradTable& t, int c) {
   return lo;
 }
 
-// f(i, v, N) for the values of [begin, end) in vectors of 16 bytes (VEC) or one by one.
+// Chunk c of a table: its tensor, where it starts there, its values and their type.
+struct Chunk {
+  int q;
+  size_t at, n;
+  bool bf16;
+};
+template <class T>
+DEVI Chunk chunk_at(const T& t, int c) {
+  Chunk k;
+  k.q = tensor_of(t, c);
+  k.at = (size_t)(c - t.first[k.q]) * t.chunk;
+  const unsigned tail = t.tail[k.q];
+  k.n = c + 1 < t.first[k.q + 1] ? (size_t)t.chunk : (tail & 0x7fff) + 1;
+  k.bf16 = tail >> 15;
+  return k;
+}
+
+// The sum of the squares of n values at p, in the block's threads.
 template <class E>
 DEVI double square_sum(const E* p, size_t n) {
   constexpr int V = Vec16<E>::N;
@@ -78,16 +103,14 @@ DEVI double wave_sum_f64(double v) {
   return v;
 }
 
-__global__ __launch_bounds__(kThreads) void grad_norm_kernel(GradTable t, double* part) {
+__global__ __launch_bounds__(kThreads) void grad_norm_kernel(NormTable t, double* part) {
   __shared__ double sum[kThreads / 64];
   const int chunks = t.first[t.count];
   double s = 0.0;
   for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const int q = tensor_of(t, c);
-    const size_t at = (size_t)(c - t.first[q]) * t.chunk;
-    const size_t n = min(t.n[q] - at, (size_t)t.chunk);
-    s += t.bf16[q] ? square_sum(static_cast<const bf16_t*>(t.p[q]) + at, n)
-                   : square_sum(static_cast<const float*>(t.p[q]) + at, n);
+    const Chunk k = chunk_at(t, c);
+    s += k.bf16 ? square_sum(static_cast<const bf16_t*>(t.p[k.q]) + k.at, k.n)
+                : square_sum(static_cast<const float*>(t.p[k.q]) + k.at, k.n);
   }
   s = wave_sum_f64(s);
   if ((threadIdx.x & 63) == 0) sum[threadIdx.x >> 6] = s;
@@ -137,19 +160,19 @@ DEVI void scale_to(const E* p, E* out, size_t n, float scale) {
   for (size_t i = done + threadIdx.x; i < n; i += kThreads) out[i] = from_f32<E>(to_f32(p[i]) * scale);
 }
 
-__global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradTable t, const float* norm) {
+__global__ __launch_bounds__(kThreads) void grad_clip_kernel(ClipTable t, const float* norm) {
   // (scale 1, or NaN: nothing to clip, so that values in place stay as they are)
   const float s = norm[1], scale = s < 1.0f ? s : 1.0f;
   const int chunks = t.first[t.count];
   for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const int q = tensor_of(t, c);
-    if (scale == 1.0f && t.p[q] == t.out[q]) continue;
-    const size_t at = (size_t)(c - t.first[q]) * t.chunk;
-    const size_t n = min(t.n[q] - at, (size_t)t.chunk);
-    if (t.bf16[q])
-      scale_to(static_cast<const bf16_t*>(t.p[q]) + at, static_cast<bf16_t*>(t.out[q]) + at, n, scale);
+    const Chunk k = chunk_at(t, c);
+    const void* const p = t.p[k.q];
+    void* const out = t.out[k.q];
+    if (scale == 1.0f && p == out) continue;
+    if (k.bf16)
+      scale_to(static_cast<const bf16_t*>(p) + k.at, static_cast<bf16_t*>(out) + k.at, k.n, scale);
     else
-      scale_to(static_cast<const float*>(t.p[q]) + at, static_cast<float*>(t.out[q]) + at, n, scale);
+      scale_to(static_cast<const float*>(p) + k.at, static_cast<float*>(out) + k.at, k.n, scale);
   }
 }
 
@@ -157,16 +180,16 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradTable t, const 
 int chunk_of(const moe_grad* g, int n) {
   size_t total = 0;
   for (int i = 0; i < n; ++i) total += g[i].n;
-  return total < ((size_t)32 << 20) ? 4096 : 16384;
+  return total < ((size_t)32 << 20) ? 4096 : kMaxChunk;
 }
 
 // Blocks of a launch of `chunks` chunks.
 int chunk_blocks(int chunks) { return std::min(chunks, 8 * num_cus()); }
 
-// f(table, blocks) for launches of up to kTensors tensors with values.
-template <class F>
+// f(table, blocks) for launches of up to T::kTensors tensors with values.
+template <class T, class F>
 hipError_t for_tables(const moe_grad* g, int n, F&& f) {
-  GradTable t;
+  T t;
   t.chunk = chunk_of(g, n);
   t.count = 0;
   t.first[0] = 0;
@@ -174,15 +197,14 @@ hipError_t for_tables(const moe_grad* g, int n, F&& f) {
     const bool end = i == n;
     // (a launch's chunks are counted in 31 bits: a tensor that does not fit opens the next)
     const int64_t chunks = end ? 0 : (int64_t)((g[i].n + t.chunk - 1) / t.chunk);
-    if (t.count > 0 && (end || t.count == kTensors || t.first[t.count] + chunks > INT32_MAX)) {
+    if (t.count > 0 && (end || t.count == T::kTensors || t.first[t.count] + chunks > INT32_MAX)) {
       if (const hipError_t e = f(t, chunk_blocks(t.first[t.count])); e != hipSuccess) return e;
       t.count = 0;
     }
     if (end || chunks == 0) continue;
     t.p[t.count] = g[i].grad;
-    t.out[t.count] = g[i].out;
-    t.n[t.count] = g[i].n;
-    t.bf16[t.count] = g[i].dtype == MOE_BF16;
+    if constexpr (sizeof(t.out) > sizeof(void*)) t.out[t.count] = g[i].out;
+    t.tail[t.count] = (uint16_t)((g[i].n - 1) % t.chunk | (g[i].dtype == MOE_BF16 ? 0x8000 : 0));
     t.first[t.count + 1] = t.first[t.count] + (int)chunks;
     ++t.count;
   }
@@ -193,7 +215,7 @@ hipError_t for_tables(const moe_grad* g, int n, F&& f) {
 
 size_t grad_norm_ws_bytes(const moe_grad* g, int n) {
   size_t parts = 0;
-  (void)for_tables(g, n, [&](const GradTable&, int blocks) {
+  (void)for_tables<NormTable>(g, n, [&](const NormTable&, int blocks) {
     parts += blocks;
     return hipSuccess;
   });
@@ -204,7 +226,7 @@ hipError_t launch_grad_norm(const moe_grad* g, int n, float max_norm, float* nor
                             hipStream_t s) {
   double* const part = static_cast<double*>(ws);
   int parts = 0;
-  const hipError_t e = for_tables(g, n, [&](const GradTable& t, int blocks) {
+  const hipError_t e = for_tables<NormTable>(g, n, [&](const NormTable& t, int blocks) {
     MOE_TIMED("grad_norm", s, grad_norm_kernel<<<blocks, kThreads, 0, s>>>(t, part + parts));
     parts += blocks;
     return hipGetLastError();
@@ -215,7 +237,7 @@ hipError_t launch_grad_norm(const moe_grad* g, int n, float max_norm, float* nor
 }
 
 hipError_t launch_grad_clip(const moe_grad* g, int n, const float* norm, hipStream_t s) {
-  return for_tables(g, n, [&](const GradTable& t, int blocks) {
+  return for_tables<ClipTable>(g, n, [&](const ClipTable& t, int blocks) {
     MOE_TIMED("grad_clip", s, grad_clip_kernel<<<blocks, kThreads, 0, s>>>(t, norm));
     return hipGetLastError();
   });

@@ -88,21 +88,20 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
 // AdamW over many tensors, gradients multiplied by the clip's scale first: a launch covers up to
 // kAdamTensors tensors, whose table is a kernel argument; tensors are cut into chunks, which
 // the blocks take in turn.
-constexpr int kAdamTensors = 44;
+constexpr int kAdamTensors = 72;
 struct AdamTable {
   float* theta[kAdamTensors];
   const void* grad[kAdamTensors];
   float* m[kAdamTensors];
   float* v[kAdamTensors];
   bf16_t* low[kAdamTensors];  // or NULL
-  size_t n[kAdamTensors];
   float lr[kAdamTensors], wd[kAdamTensors];
-  int first[kAdamTensors + 1];  // chunks before each tensor
-  uint8_t bf16[kAdamTensors];   // the gradient's type
+  int first[kAdamTensors + 1];   // chunks before each tensor
+  uint16_t tail[kAdamTensors];   // values of its last chunk, less one; top bit: a bf16 gradient
   int count, chunk;
   float b1, b2, eps, c1, c2;
 };
-static_assert(sizeof(AdamTable) <= 3900, "kernel arguments hold 4 KiB");
+static_assert(sizeof(AdamTable) <= 3968, "kernel arguments hold 4 KiB");
 
 __global__ __launch_bounds__(256) void adamw_steps_kernel(AdamTable t, const float* norm) {
   const float scale = norm ? norm[1] : 1.0f;
@@ -116,12 +115,13 @@ __global__ __launch_bounds__(256) void adamw_steps_kernel(AdamTable t, const flo
       else hi = mid - 1;
     }
     const size_t at = (size_t)(c - t.first[q]) * t.chunk;
-    const int n = (int)min(t.n[q] - at, (size_t)t.chunk), n4 = n / 4;
+    const unsigned tail = t.tail[q];
+    const int n = c + 1 < t.first[q + 1] ? t.chunk : (int)(tail & 0x7fff) + 1, n4 = n / 4;
     float* const th = t.theta[q] + at;
     float* const m = t.m[q] + at;
     float* const v = t.v[q] + at;
     bf16_t* const low = t.low[q] ? t.low[q] + at : nullptr;
-    const bool bf16 = t.bf16[q];
+    const bool bf16 = tail >> 15;
     const float* const g = static_cast<const float*>(t.grad[q]) + (bf16 ? 0 : at);
     const bf16_t* const gb = static_cast<const bf16_t*>(t.grad[q]) + (bf16 ? at : 0);
     AdamArgs a{};
@@ -265,10 +265,9 @@ hipError_t launch_adamw_steps(const moe_adamw_tensor* p, int n, float lr, float 
     const int k = t.count++;
     t.theta[k] = p[i].theta; t.grad[k] = p[i].grad; t.m[k] = p[i].m; t.v[k] = p[i].v;
     t.low[k] = static_cast<bf16_t*>(p[i].theta_bf16);
-    t.n[k] = p[i].n;
     t.lr[k] = lr * p[i].lr_scale;
     t.wd[k] = p[i].weight_decay;
-    t.bf16[k] = p[i].grad_dtype == MOE_BF16;
+    t.tail[k] = (uint16_t)((p[i].n - 1) % t.chunk | (p[i].grad_dtype == MOE_BF16 ? 0x8000 : 0));
     t.first[k + 1] = t.first[k] + (int)chunks;
   }
   return hipSuccess;

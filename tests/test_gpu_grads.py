@@ -17,7 +17,7 @@ BF, F32 = torch.bfloat16, torch.float32
 SIZES = {
     "one": [1], "odd": [1, 3, 7, 8, 9, 16383, 16384, 16385, 32771, 5], "empty": [0, 5, 0],
     "large": [3_000_001, 40, 1 << 20], "many": [1 + (i * 37) % 611 for i in range(300)],
-    "table": [9] * 112, "past": [9] * 113,
+    "tables": [9] * 173 + [4097] + [7] * 98 + [8191] + [3] * 200,
 }
 
 
@@ -103,7 +103,7 @@ def state(sizes, seed, types):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("kind", ["odd", "empty", "large", "many"])
+@pytest.mark.parametrize("kind", ["odd", "empty", "large", "many", "tables"])
 @pytest.mark.parametrize("clipped", [True, False])
 def test_adamw_steps_is_adamw_step_of_clipped_gradients(gpu_lib, kind, clipped):
     sizes = SIZES[kind]
