@@ -608,9 +608,10 @@ int check_xent_sizes(const moe_xent* p) {
   REQUIRE(p->N >= 0 && p->d >= 1 && p->V >= 1, "bad sizes N = %d, d = %d, V = %d", p->N, p->d, p->V);
   SUPPORT(p->N < 1 << 27, "N = %d must be below 2^27", p->N);
   SUPPORT(p->d <= 1 << 16, "d = %d: at most 2^16", p->d);
-  SUPPORT(p->V <= INT32_MAX - 512, "V = %d is too large", p->V);
+  SUPPORT(p->V < 1 << 30, "V = %d must be below 2^30", p->V);
   if (p->dtype == MOE_BF16) {
     SUPPORT(p->d % 64 == 0, "d = %d must be a multiple of 64 for bf16", p->d);
+    SUPPORT(p->N < 1 << 23, "N = %d must be below 2^23 for bf16", p->N);
     SUPPORT((int64_t)p->N * p->d < (int64_t(1) << 31) - 16, "N d = %lld must be below 2^31 - 16",
             (long long)p->N * p->d);
   } else {
@@ -623,7 +624,8 @@ int check_xent(const moe_xent* p, bool fwd) {
   int r;
   if ((r = check_xent_sizes(p)) != MOE_OK) return r;
   const bool any = p->N > 0;
-  REQUIRE(std::isfinite(p->scale) && std::isfinite(p->z_coef), "scale and z_coef must be finite");
+  REQUIRE(std::isfinite(p->scale) && p->scale != 0.f && std::isfinite(p->z_coef),
+          "scale must be finite and not 0, z_coef finite");
   REQUIRE(!any || (p->x && p->w && p->labels && p->lse), "x, w, labels and lse must not be NULL");
   SUPPORT(aligned16(p->x) && aligned16(p->w), "x and w must be 16-byte aligned");
   if (fwd) {

@@ -287,12 +287,12 @@ Plan plan_of(const moe_xent& x) {
     p.pair = f32_tiles(cols * (ceil_div(x.N, 64) + ceil_div(dw.M, 64)));
   }
   // Parts of K of dx: its few tiles reduce over the whole piece, so they are cut until they are three
-  // quarters of the CUs; 512 columns a part at least.  Measured (us of the backward by parts): 512 tokens,
+  // quarters of the CUs; 256 columns a part at least.  Measured (us of the backward by parts): 512 tokens,
   // d = 2048, 32768 words 1 698, 2 394, 4 253, 8 212, 14 212, 28 242; 1531 tokens, d = 768, 50003 words
   // 1055, 590, 365, 283, 284, 309; 4096 tokens, d = 1024, 32000 words 987, 731, 724, 748, 821, 907.
   const double tiles = (double)ceil_div(x.N, tile_rows(p.pair)) * ceil_div(x.d, tile_cols(p.pair));
   const size_t most = ((size_t)256 << 20) / ((size_t)std::max(1, x.N) * x.d * 4);
-  p.split = (int)std::max(1.0, std::min({0.75 * num_cus() / std::max(tiles, 1.0), p.piece / 512.0, (double)most}));
+  p.split = (int)std::max(1.0, std::min({0.75 * num_cus() / std::max(tiles, 1.0), p.piece / 256.0, (double)most}));
   return p;
 }
 

@@ -159,16 +159,17 @@ def test_block_norm_adds_where_asked(gpu_lib):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_block_norm_in_place(gpu_lib, dtype):
-    """x_out in x, dx in dres or du, df in f."""
-    t = inputs(33, 520, dtype, 9, "channel")
+@pytest.mark.parametrize("T,d", [(33, 520), (1100, 2048), (600, 8192), (300, 12288)])
+def test_block_norm_in_place(gpu_lib, T, d, dtype):
+    """x_out in x, dx in dres or du, df in f; also where a row's arrays are fetched rounds ahead."""
+    t = inputs(T, d, dtype, 9, "channel")
     w, pre_bias = weights(t, True, True, True)
-    K = BlockNorm(33, 520, dtype=DT[dtype], gate="channel")
+    K = BlockNorm(T, d, dtype=DT[dtype], gate="channel")
     K.forward(t["x"], t["f"], **w, pre_bias=pre_bias)
     K.backward(t["du"], t["f"], **w, dres=t["dres"])
     ref = [v.clone() for v in (K.x, K.u, K.dx, K.df, K.d_gate)]
     for target in ("dres", "du"):
-        L = BlockNorm(33, 520, dtype=DT[dtype], gate="channel")
+        L = BlockNorm(T, d, dtype=DT[dtype], gate="channel")
         s = {k: v.clone() for k, v in t.items()}
         L.x = s["x"]
         L.forward(s["x"], s["f"], **w, pre_bias=pre_bias)

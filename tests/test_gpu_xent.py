@@ -115,7 +115,7 @@ CASES = [(1, 64, 1, "bf16 f32", 0), (1, 128, 5003, "bf16 f32", 0), (7, 64, 63, "
 @pytest.mark.parametrize("N,d,V,types,ignored", CASES)
 def test_xent_matches_64_bits(gpu_lib, N, d, V, types, ignored):
     for dtype in types.split():
-        for scale, z_coef, mean, low in ((1.0, 0.0, True, False), (0.5, 1e-2, False, True)):
+        for scale, z_coef, mean, low in ((1.0, 0.0, True, False), (-0.5, 1e-2, False, True)):
             print(f"[xent] N={N} d={d} V={V} {dtype} ignored={ignored} scale={scale}", flush=True)
             t = inputs(N, d, V, dtype, N + V, ignored)
             L = LinearCrossEntropy(N, d, V, dtype=DT[dtype], scale=scale, z_coef=z_coef,
@@ -309,8 +309,9 @@ def test_c_entry_points_refuse():
     arg, unsupported = -1, -2
     both = [(dict(dtype=4), unsupported), (dict(N=-1), arg), (dict(V=0), arg), (dict(d=0), arg),
             (dict(N=1 << 27), unsupported), (dict(d=72), unsupported), (dict(d=1 << 17), unsupported),
-            (dict(N=1 << 25, d=128), unsupported), (dict(dtype=B.MOE_F32, d=12), unsupported),
-            (dict(scale=math.inf), arg), (dict(z_coef=math.nan), arg), (dict(x=None), arg),
+            (dict(N=1 << 22, d=512), unsupported), (dict(N=1 << 23), unsupported),
+            (dict(V=1 << 30), unsupported), (dict(dtype=B.MOE_F32, d=12), unsupported),
+            (dict(scale=math.inf), arg), (dict(scale=0.0), arg), (dict(z_coef=math.nan), arg), (dict(x=None), arg),
             (dict(w=None), arg), (dict(labels=None), arg), (dict(lse=None), arg),
             (dict(x=p + 8), unsupported), (dict(w=p + 2), unsupported), (dict(ws=None), arg),
             (dict(ws_bytes=100), arg), (dict(ws=p + 16), unsupported)]
