@@ -76,6 +76,9 @@ def parse():
                     help="time whole training steps: fwd + bwd + AdamW on the resident and shared "
                          "experts every step, and at the round cadence the delta average and the "
                          "outer Nesterov step")
+    ap.add_argument("--clip", type=float, default=None, metavar="NORM",
+                    help="with --optimizer: clip the step's gradients to this norm together (the "
+                         "resident and the shared experts'), and update all of them by one call")
     ap.add_argument("--placement", choices=["fixed", "random"], default="fixed",
                     help="with --optimizer: random placement (Alg. 1) redraws the worker's "
                          "resident set every --reshuffle-every rounds and migrates weights and "
@@ -217,8 +220,12 @@ def optimizer_work(n_step_params, n_round_params, n_peers):
     """Per-step bytes of the optimiser kernels: AdamW reads theta, g, m, v and
     writes theta, m, v and the bf16 copy (30 B per parameter); the outer step
     reads start, delta, momentum and writes momentum, start, now and the bf16
-    copy (26 B); the replica mean reads 1 + peers copies and writes one."""
+    copy (26 B); the replica mean reads 1 + peers copies and writes one.  With
+    --clip the gradients' norm reads every gradient, clipping in place also writes it."""
     return {"adamw_step": ("byte", 30.0 * n_step_params),
+            "adamw_steps": ("byte", 30.0 * n_step_params),
+            "grad_norm": ("byte", 4.0 * n_step_params),
+            "grad_clip": ("byte", 8.0 * n_step_params),
             "outer_nesterov": ("byte", 26.0 * n_round_params),
             "replica_mean": ("byte", 4.0 * (n_peers + 2) * n_round_params)}
 
@@ -305,6 +312,7 @@ def main():
     from paper_2606_19025_amd import binding as B
     from paper_2606_19025_amd import inputs as I
     from paper_2606_19025_amd.layer import ResidentMoELayer, expert_delta
+    from paper_2606_19025_amd.train import AdamW, GradClipper
 
     B.lib()
     wl = args.workload
@@ -314,6 +322,8 @@ def main():
     T, d, E, k, H, Er = cfg["T"], cfg["d"], cfg["E"], cfg["k"], cfg["H"], cfg["E_r"]
     Hs = cfg["n_shared"] * cfg["Hs"]
     dt = torch.bfloat16 if cfg["dtype"] == "bf16" else torch.float32
+    if args.clip is not None and not (args.optimizer and dt == torch.bfloat16):
+        sys.exit("--clip needs --optimizer and a bf16 workload")
     s_bytes = 2 if dt == torch.bfloat16 else 4
     dev = lambda a, t=dt: None if a is None else torch.from_numpy(
         np.ascontiguousarray(a, np.float32)).cuda().to(t)
@@ -420,6 +430,44 @@ def main():
         o = opt
         o["t"] += 1
         lr = 3e-4
+        if args.clip is not None:
+            clipped_update(lr)
+        else:
+            update(lr)
+        if (i + 1) % args.round_every == 0:
+            # round boundary: replica-group average of the pseudo-gradient,
+            # outer Nesterov step, every replica restarts from its result
+            expert_delta(th0, th1, peers, delta_avg=avg)
+            B.moe_outer_nesterov(th0, th1, avg, o["mom"], n_params, 0.7, 0.9, theta_bf16=o["lp"])
+            if args.placement == "random" and ((i + 1) // args.round_every) % args.reshuffle_every == 0:
+                reshuffle()
+
+    def clipped_update(lr):
+        """AdamW with the norm of all the step's gradients limited to --clip."""
+        o = opt
+        if args.placement == "random":  # (steps and rates by expert: the gradients are clipped in place)
+            if "clipper" not in o:
+                o["clipper"] = GradClipper([L.dw_gate_up, L.dw_down]
+                                           + ([L.s_dw_gate_up, L.s_dw_down] if Hs else []), args.clip)
+            o["clipper"].clip()
+            update(lr)
+            return
+        if "adamw" not in o:
+            n_gu, n_sg = o["gu"].numel(), r1 * Hs * d
+            cut = lambda t, n: [t[:n], t[n:]]
+            shared = lambda k: cut(o[k], n_sg) if Hs else []
+            flat = lambda g: g.view(-1)
+            o["adamw"] = AdamW(
+                [o["gu"], o["down"]] + shared("s_master"),
+                [flat(L.dw_gate_up), flat(L.dw_down)]
+                + ([flat(L.s_dw_gate_up), flat(L.s_dw_down)] if Hs else []),
+                cut(o["m"], n_gu) + shared("s_m"), cut(o["v"], n_gu) + shared("s_v"),
+                theta_bf16=cut(o["lp"], n_gu) + shared("s_lp"),
+                max_norm=args.clip)
+        o["adamw"].step(o["t"], lr)
+
+    def update(lr):
+        o = opt
         # local AdamW on the resident experts (gradients of the layer's last
         # backward), writing the bf16 weights in the same pass
         n_gu = o["gu"].numel()
@@ -444,13 +492,6 @@ def main():
                              o["s_v"][:n_sg], n_sg, o["t"], lr, theta_bf16=o["s_lp"][:n_sg])
             B.moe_adamw_step(o["s_master"][n_sg:], L.s_dw_down, o["s_m"][n_sg:], o["s_v"][n_sg:],
                              Hs * d, o["t"], lr, theta_bf16=o["s_lp"][n_sg:])
-        if (i + 1) % args.round_every == 0:
-            # round boundary: replica-group average of the pseudo-gradient,
-            # outer Nesterov step, every replica restarts from its result
-            expert_delta(th0, th1, peers, delta_avg=avg)
-            B.moe_outer_nesterov(th0, th1, avg, o["mom"], n_params, 0.7, 0.9, theta_bf16=o["lp"])
-            if args.placement == "random" and ((i + 1) // args.round_every) % args.reshuffle_every == 0:
-                reshuffle()
 
     def step(i):
         L.forward(x, wr, wgu, wd, bias, sgu, sd)
@@ -711,6 +752,7 @@ def main():
                    "executed_routes": n, "skip_fraction": round(1 - n / (T * k), 4),
                    "optimizer": "adamw+outer-nesterov" if opt is not None else None,
                    "placement": args.placement if opt is not None else None,
+                   **({"clip": args.clip} if opt is not None and args.clip is not None else {}),
                    "expert": args.expert},
         "roofline": roofline,
         "cpu_baseline": cpu,
