@@ -170,9 +170,11 @@ hipError_t run_gemm_tile(int bf16, int ka, int kb, const GemmArgs* sets_a, int n
 constexpr int kXcdCounters = 8;
 hipError_t run_gemm_xent(int ka, const GemmArgs& a, const GemmArgs* b, int* counters, hipStream_t s);
 
-// Which tiles a bf16 launch of XE_LSE or XE_DZ (b NULL), or of XE_DX with XE_DW, takes: what
-// choose_tiles estimates for an up projection, or for dX with dW, of the same sizes.
-TileSize xent_tiles(const GemmArgs& a, const GemmArgs* b);
+// Which tiles a bf16 launch of XE_LSE or XE_DZ takes: what choose_tiles estimates for an up
+// projection of its sizes; and which one of XE_DX with XE_DW, whose dx is cut into split[i] parts at
+// 256 x 256, 64 x 128 and 64 x 64.
+TileSize xent_logit_tiles(const GemmArgs& a);
+TileSize xent_pair_tiles(const GemmArgs& dx, const GemmArgs& dw, const int* split);
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 

@@ -278,21 +278,25 @@ Plan plan_of(const moe_xent& x) {
   z.N = std::min(x.V, p.fwd_piece); z.K = x.d;
   dx.N = x.d; dx.K = std::min(x.V, p.piece);
   dw.M = dx.K; dw.N = x.d;
+  // Parts of K of dx: its few tiles reduce over the whole piece, so they are cut until they are three
+  // quarters of the CUs; 256 columns a part at least.  Measured (us of the backward by parts): 512 tokens,
+  // d = 2048, 32768 words 1 698, 2 394, 4 253, 8 212, 14 212, 28 242; 1531 tokens, d = 768, 50003 words
+  // 1055, 590, 365, 283, 284, 309; 4096 tokens, d = 1024, 32000 words 987, 731, 724, 748, 821, 907.
+  const double most = (double)(((size_t)256 << 20) / ((size_t)std::max(1, x.N) * x.d * 4));
+  auto split_of = [&](TileSize t) {
+    const double tiles = (double)ceil_div(x.N, tile_rows(t)) * ceil_div(x.d, tile_cols(t));
+    return (int)std::max(1.0, std::min({0.75 * num_cus() / std::max(tiles, 1.0), p.piece / 256.0, most}));
+  };
   if (bf16) {
-    p.logits = xent_tiles(z, nullptr);
-    p.pair = xent_tiles(dx, &dw);
+    p.logits = xent_logit_tiles(z);
+    const int split[3] = {split_of(TILE_256x256), split_of(TILE_64x128), split_of(TILE_64x64)};
+    p.pair = xent_pair_tiles(dx, dw, split);
   } else {
     const double cols = ceil_div(x.d, 128);
     p.logits = f32_tiles((double)ceil_div(x.N, 64) * ceil_div(z.N, 128));
     p.pair = f32_tiles(cols * (ceil_div(x.N, 64) + ceil_div(dw.M, 64)));
   }
-  // Parts of K of dx: its few tiles reduce over the whole piece, so they are cut until they are three
-  // quarters of the CUs; 256 columns a part at least.  Measured (us of the backward by parts): 512 tokens,
-  // d = 2048, 32768 words 1 698, 2 394, 4 253, 8 212, 14 212, 28 242; 1531 tokens, d = 768, 50003 words
-  // 1055, 590, 365, 283, 284, 309; 4096 tokens, d = 1024, 32000 words 987, 731, 724, 748, 821, 907.
-  const double tiles = (double)ceil_div(x.N, tile_rows(p.pair)) * ceil_div(x.d, tile_cols(p.pair));
-  const size_t most = ((size_t)256 << 20) / ((size_t)std::max(1, x.N) * x.d * 4);
-  p.split = (int)std::max(1.0, std::min({0.75 * num_cus() / std::max(tiles, 1.0), p.piece / 256.0, (double)most}));
+  p.split = split_of(p.pair);
   return p;
 }
 
