@@ -40,6 +40,7 @@ struct XentArgs {
   int V, v0;
   float scale, z2;        // of the logits; 2 z_coef
   int out_bf16;           // XE_DW: C is bf16
+  int* done;              // XE_LSE: a counter to clear for the launch that follows
 };
 
 struct GemmArgs {
@@ -48,7 +49,7 @@ struct GemmArgs {
   void* C;
   const void* aux;  // gu, read by the DHH_BWD epilogue
   void* out2;       // h, written by the GU_FWD epilogue
-  const int32_t* offsets;
+  const int32_t* offsets;  // NULL: one group of all cap rows
   long lda, ldb, ldc;
   long b_gs, c_gs;  // per-group strides (elements) of B and C
   long c_split;     // stride (elements) between the split-K partial outputs
@@ -105,7 +106,7 @@ DEVI void build_group_table(const GemmArgs& a, GroupTable& t, int tile_rows) {
   int run = 0;
   for (int g0 = 0; g0 <= ng; g0 += 64) {
     const int g = g0 + lane;
-    const int c = g <= ng ? clamp_row(a.offsets[g], a.cap) : 0;
+    const int c = g > ng ? 0 : a.offsets ? clamp_row(a.offsets[g], a.cap) : g ? a.cap : 0;
     int m = wave_incl_max(g <= ng ? c : 0);
     if (g0 > 0) m = max(m, run);
     if (g <= ng) {

@@ -499,6 +499,7 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
   const int xcd = blockIdx.x % N_XCD;
   __shared__ GroupTable gtab[SETS];
   __shared__ int shares[SETS][2];  // of uneven sets: this XCD's first tile and the next's
+  if (KA == XE_LSE && blockIdx.x == 0 && threadIdx.x == 0) *L.s[0].xe.done = 0;
   if (wave < L.n_sets) {
     const GemmArgs& a = L.s[wave];
     build_group_table<GT>(a, gtab[wave], kTileRows);

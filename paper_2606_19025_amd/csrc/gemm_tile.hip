@@ -567,6 +567,7 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(GemmLaunch L) {
   GroupTable* gtab = reinterpret_cast<GroupTable*>(lds);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
+  if (KA == XE_LSE && blockIdx.x == 0 && threadIdx.x == 0) *L.s[0].xe.done = 0;
   if (wave < L.n_sets) build_group_table<BM>(L.s[wave], gtab[wave], kTileRows);
   __syncthreads();
   const int xcd = blockIdx.x % kXcds;

@@ -28,6 +28,7 @@ constexpr int kRows = 16;         // tokens of a block of xent_rows
 constexpr int kCountRows = 1024;  // tokens of a counting block
 constexpr int kDirect = 8192;     // up to here every block counts all labels itself
 constexpr int kLossThreads = 1024;
+constexpr int kAsIs = 128;        // up to here the forward leaves out no row (24 tokens 55 -> 51 us)
 
 struct RowArgs {
   const void* x;
@@ -40,11 +41,10 @@ struct RowArgs {
   int* pos;            // [N] row of a token among those that count, or -1
   int* off;            // {0, tokens that count}
   int* row_label;      // the rest by row
-  float* z_label;      // forward
   float* row_lse;      // backward
   float* coef;
   void* xc;
-  int* counters;       // cleared for the launches that follow
+  int* counters;       // backward: cleared for the launches that follow
   int n_counters;
 };
 
@@ -103,19 +103,16 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
       if (t < a.N) a.pos[t] = p;
     }
     if (p >= 0) {
-      const bool in = y < a.V;
       a.row_label[p] = y;
       if constexpr (BWD) {
         a.row_lse[p] = a.lse[t];
         // (a label that is no word of the vocabulary makes what it enters NaN)
-        a.coef[p] = in ? a.scale * (a.dloss ? a.dloss[t] : 1.0f / (float)total) : NAN;
-      } else if (!in) {
-        a.z_label[p] = NAN;
+        a.coef[p] = y < a.V ? a.scale * (a.dloss ? a.dloss[t] : 1.0f / (float)total) : NAN;
       }
     }
     if (blockIdx.x == 0 && threadIdx.x < 2) a.off[threadIdx.x] = threadIdx.x ? total : 0;
   }
-  if (blockIdx.x == 0)
+  if (BWD && blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.n_counters; i += 256) a.counters[i] = 0;
   if (total == a.N) return;  // x itself is read
   __syncthreads();
@@ -137,18 +134,19 @@ DEVI float2 join(float2 a, float2 b) {
 }
 
 // lse and loss of R tokens a block from their P partials, 1024 / R threads a token.  Few tokens a block
-// where there are few: 24 tokens of 1536 partials took 42 us with 64 a block.  The block that ends last
-// adds the blocks' sums of losses, in order.
+// where there are few: 24 tokens of 1536 partials took 42 us with 64 a block.  pos: the tokens' rows, or
+// NULL: their own numbers.  The block that ends last adds the blocks' sums of losses and tokens, in order.
 template <int R>
 __global__ __launch_bounds__(kLossThreads) void xent_loss_kernel(
-    int N, int P, float z_coef, const int* pos, const int* off, const float2* part, const float* z_label,
-    float* loss, float* lse, double* sums, int* done, float* total) {
+    int N, int V, int P, float z_coef, const int* label, const int* pos, const float2* part,
+    const float* z_label, float* loss, float* lse, double* sums, int* done, float* total) {
   constexpr int S = kLossThreads / R, WAVES = kLossThreads / 64;
   __shared__ float2 seg[WAVES][R];
   __shared__ bool last;
   const int r = threadIdx.x % R, q = threadIdx.x / R;
   const int t = blockIdx.x * R + r;
-  const int p = t < N ? pos[t] : -1;
+  const int y = t < N ? label[t] : -1;
+  const int p = y < 0 ? -1 : pos ? pos[t] : t;
   float2 v = {-INFINITY, 0.f};
   if (p >= 0) {
 #pragma unroll 4
@@ -172,32 +170,30 @@ __global__ __launch_bounds__(kLossThreads) void xent_loss_kernel(
       float l = 0.f;
       if (p >= 0) {
         l = v.x * kLn2 + logf(v.y);
-        out = l - z_label[p] + z_coef * l * l;
+        out = y < V ? l - z_label[p] + z_coef * l * l : NAN;
       }
       lse[t] = l;
       loss[t] = out;
     }
-  }
-  if (threadIdx.x < 64) {
+    const int counted = __builtin_popcountll(__ballot((int)threadIdx.x < R && y >= 0));
     double s = (double)out;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     if (threadIdx.x == 0) {
-      __hip_atomic_store(sums + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(sums + 2 * blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(sums + 2 * blockIdx.x + 1, (double)counted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       last = __hip_atomic_fetch_add(done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
     }
   }
   __syncthreads();
   if (!last || threadIdx.x >= 64) return;
+  // (even lanes the losses, odd ones the tokens)
   double s = 0.0;
-  for (int i = threadIdx.x; i < (int)gridDim.x; i += 64)
+  for (int i = threadIdx.x; i < 2 * (int)gridDim.x; i += 64)
     s += __hip_atomic_load(sums + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if (threadIdx.x == 0) {
-    total[0] = (float)s;
-    total[1] = (float)off[1];
-  }
+  for (int o = 32; o > 1; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (threadIdx.x < 2) total[threadIdx.x] = (float)s;
 }
 
 // total of no tokens.
@@ -314,7 +310,9 @@ struct Space {
 struct Buffers {
   RowArgs row;
   float2* part;
+  float* z_label;
   double* sums;
+  int* done;
   void* dz;
   float* dx_part;
   size_t bytes;
@@ -336,11 +334,10 @@ Buffers buffers(const moe_xent& x, const Plan& p, bool bwd, void* ws) {
   r.row_label = w.take<int>(N);
   r.xc = w.take<char>(N * x.d * s);
   if (!bwd) {
-    r.z_label = w.take<float>(N);
+    b.z_label = w.take<float>(N);
     b.part = w.take<float2>((size_t)p.parts * N);
-    b.sums = w.take<double>((N + loss_rows(x.N) - 1) / loss_rows(x.N));
-    r.n_counters = 1;
-    r.counters = w.take<int>(1);
+    b.sums = w.take<double>(2 * ((N + loss_rows(x.N) - 1) / loss_rows(x.N)));
+    b.done = w.take<int>(1);
   } else {
     r.row_lse = w.take<float>(N);
     r.coef = w.take<float>(N);
@@ -402,14 +399,21 @@ hipError_t launch_xent_fwd(const moe_xent* x, hipStream_t s) {
     MOE_TIMED("xent_none", s, xent_none_kernel<<<1, 64, 0, s>>>(x->total));
     return hipGetLastError();
   }
-  if ((e = rows<false>(b, s)) != hipSuccess) return e;
+  // Few tokens: every row as it is (rows are independent here, and the weights' stream sets the time)
+  const bool as_is = x->N <= kAsIs;
+  if (!as_is && (e = rows<false>(b, s)) != hipSuccess) return e;
   const int width = tile_cols(p.logits) / 2;  // of a partial: half a tile's columns
   int parts = 0;
   for (int v0 = 0; v0 < x->V; v0 += p.fwd_piece) {
     const int V = std::min(x->V - v0, p.fwd_piece);
     GemmArgs a = logits(*x, b, v0, V);
     a.xe.part = b.part + (size_t)parts * x->N;
-    a.xe.z_label = b.row.z_label;
+    a.xe.z_label = b.z_label;
+    a.xe.done = b.done;
+    if (as_is) {
+      a.offsets = nullptr;
+      a.xe.label = x->labels;
+    }
     if ((e = run(p.logits, bf16, XE_LSE, a, nullptr, nullptr, s)) != hipSuccess) return e;
     parts += ceil_div(V, 2 * width) * 2;
   }
@@ -417,8 +421,8 @@ hipError_t launch_xent_fwd(const moe_xent* x, hipStream_t s) {
 #define XENT_LOSS(R_)                                                                                    \
   MOE_TIMED("xent_loss", s,                                                                              \
             xent_loss_kernel<R_><<<blocks, kLossThreads, 0, s>>>(                                        \
-                x->N, parts, x->z_coef, b.row.pos, b.row.off, b.part, b.row.z_label, x->loss, x->lse,    \
-                b.sums, b.row.counters, x->total))
+                x->N, x->V, parts, x->z_coef, x->labels, as_is ? nullptr : b.row.pos, b.part, b.z_label, \
+                x->loss, x->lse, b.sums, b.done, x->total))
   if (R == 32) XENT_LOSS(32);
   else if (R == 16) XENT_LOSS(16);
   else XENT_LOSS(4);
