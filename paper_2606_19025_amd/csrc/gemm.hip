@@ -1260,6 +1260,7 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
     });
 
     if constexpr (EARLY) {
+      asm volatile("" ::: "memory");  // the stores stay ahead of the next tile's wait, which counts them
       cur = early;
       i += per_xcd;
       continue;

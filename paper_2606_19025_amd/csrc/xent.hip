@@ -218,7 +218,8 @@ __global__ __launch_bounds__(256) void xent_dx_kernel(E* dx, const int* pos, con
     const int t = (int)(i / chunks), c = (int)(i % chunks) * V;
     const int p = pos[t];
     float v[V] = {};
-    if (p >= 0)
+    if (p >= 0) {
+#pragma unroll 4
       for (int s = 0; s < S; ++s) {
         const float* q = part + (size_t)s * stride + (size_t)p * d + c;
 #pragma unroll
@@ -228,6 +229,7 @@ __global__ __launch_bounds__(256) void xent_dx_kernel(E* dx, const int* pos, con
           for (int e = 0; e < 4; ++e) v[j + e] += u[e];
         }
       }
+    }
     store16_f32(dx + (size_t)t * d + c, v);
   }
 }

@@ -36,10 +36,11 @@ CSRC = os.path.join(PKG, "csrc")
 CALIBRATION_BYTES = 1 << 30  # the plain copy bench.py makes for the counter scale
 
 GEMM_KINDS = ["gemm_gu_fwd", "gemm_down_fwd", "gemm_dhh_bwd", "gemm_dx_bwd", "gemm_dwd",
-              "gemm_dwgu", "gemm_up_fwd", "gemm_dh_bwd"]
+              "gemm_dwgu", "gemm_up_fwd", "gemm_dh_bwd", "gemm_xe_lse", "gemm_xe_dz", "gemm_xe_dx",
+              "gemm_xe_dw"]
 
-# launches of two GEMM kinds (the backward's dHh with dW_d, dX with dW_gu)
-_MERGED = {(2, 4): "gemm_dhh_dwd", (7, 4): "gemm_dh_dwd", (3, 5): "gemm_dx_dwgu"}
+# launches of two GEMM kinds (the backward's dHh with dW_d, dX with dW_gu; the loss's dx with dW)
+_MERGED = {(2, 4): "gemm_dhh_dwd", (7, 4): "gemm_dh_dwd", (3, 5): "gemm_dx_dwgu", (10, 11): "gemm_xe_dx_dw"}
 
 
 def _gemm_launch_name(ka: int, kb: int) -> str:
@@ -53,9 +54,9 @@ def _launch_of_first_kind(ka: int) -> str:
 
 # kernel symbol (demangled, as rocprofv3 prints it) -> timing name
 _SYMBOLS = [
-    (r"gemm_bf16_kernel(?:<|ILi)(\d)(?:, |ELi)(\d)", lambda m: _gemm_launch_name(int(m.group(1)), int(m.group(2)))),
-    (r"gemm_bf16_kernel(?:<|ILi)(\d)", lambda m: GEMM_KINDS[int(m.group(1))]),
-    (r"gemm_tile_kernel(?:<(?:[a-z_0-9]+, )?|I(?:f|DF16b)Li)(\d)(?:, |ELi)(\d)",
+    (r"gemm_bf16_kernel(?:<|ILi)(\d+)(?:, |ELi)(\d+)", lambda m: _gemm_launch_name(int(m.group(1)), int(m.group(2)))),
+    (r"gemm_bf16_kernel(?:<|ILi)(\d+)", lambda m: GEMM_KINDS[int(m.group(1))]),
+    (r"gemm_tile_kernel(?:<(?:[a-z_0-9]+, )?|I(?:f|DF16b)Li)(\d+)(?:, |ELi)(\d+)",
      lambda m: _gemm_launch_name(int(m.group(1)), int(m.group(2))) + "_tile"),
     # <bf16, KA, KB, ...>: rocprofv3's demangler takes DF16b for a bool and the KA of Li{KA}E
     # for the length of a name: <bool _Accum, int, E, 1, ...>, <bool _Accum, int, ELi, ELi2E, ...>

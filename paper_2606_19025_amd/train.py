@@ -31,6 +31,20 @@ def _disjoint(name, tensors):
             raise ValueError(f"{name} {i} and {j} overlap")
 
 
+def _apart(name, written, read):
+    """Raise ValueError if a written tensor shares memory with one that is read, but for the pair i, i
+    where both are the same."""
+    spans = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), kind, i)
+             for kind, lst in ((0, written), (1, read)) for i, t in enumerate(lst)
+             if t is not None and t.numel()]
+    ends = [(0, -1), (0, -1)]  # the furthest end so far of each kind, and whose
+    for begin, end, kind, i in sorted(spans):
+        far, j = ends[1 - kind]
+        if begin < far and not (i == j and written[i].data_ptr() == read[i].data_ptr()):
+            raise ValueError(f"{name} {i if kind == 0 else j} overlaps an input")
+        ends[kind] = max(ends[kind], (end, i))
+
+
 class LinearCrossEntropy:
     """Softmax cross entropy of N tokens x [N, d] against a vocabulary w [V, d], without the logits
     being kept: moe_xent_fwd, moe_xent_bwd.
@@ -123,6 +137,7 @@ class GradClipper:
             _check_tensor(f"gradient {i}", g, g.shape, g.dtype, self.device, "clipper")
             _check_tensor(f"output {i}", o, g.shape, g.dtype, self.device, "clipper")
         _disjoint("outputs", out)
+        _apart("output", out, grads)
         self._held = grads, out  # (the library keeps addresses only)
         self.n = len(grads)
         self._grads = (B.moe_grad * self.n)(*[
@@ -179,6 +194,7 @@ class AdamW:
             if low[i] is not None:
                 _check_tensor(f"theta_bf16 {i}", low[i], t.shape, torch.bfloat16, dev, "optimiser")
         _disjoint("tensors", theta + self.m + self.v + low)
+        _apart("tensor", theta + self.m + self.v + low, [None] * (4 * n) + grads)
         self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
         self._clipper = None if max_norm is None else GradClipper(grads, max_norm)
         self.norm = None if max_norm is None else self._clipper.norm

@@ -172,12 +172,16 @@ def test_refusals_without_a_gpu():
     for args, kw in ((([], 1.0), {}), (([f], 0.0), {}), (([f], -1.0), {}), (([f], math.nan), {}),
                      (([f.double()], 1.0), {}), (([f, 3], 1.0), {}), (([f.view(4, 2).t()], 1.0), {}),
                      (([f], 1.0), dict(out=[b])), (([f], 1.0), dict(out=[f, f])),
-                     (([f, f], 1.0), {}), (([f, f[4:]], 1.0), {})):
+                     (([f, f], 1.0), {}), (([f, f[4:]], 1.0), {}),
+                     (([f[:4], f[4:]], 1.0), dict(out=[f[4:], torch.zeros(4)])),
+                     (([f[:4], f[4:]], 1.0), dict(out=[torch.zeros(4), f[2:6]]))):
         with pytest.raises(ValueError):
             GradClipper(*args, **kw)
     for theta, grads, kw in (([b], [b], {}), ([f], [f[:4]], {}), ([f], [f, f], {}), ([f], [f.double()], {}),
                              ([f], [f], dict(m=[f])), ([f], [f], dict(theta_bf16=[f])),
-                             ([f], [f], dict(weight_decay=[0.1, 0.1])), ([f, f], [f, f], {})):
+                             ([f], [torch.ones(8)], dict(weight_decay=[0.1, 0.1])),
+                             ([f, f], [torch.ones(8), torch.ones(8)], {}), ([f], [f], {}),
+                             ([f], [torch.ones(8)], dict(m=[f], v=[torch.ones(8)]))):
         with pytest.raises(ValueError):
             AdamW(theta, grads, **kw)
 
