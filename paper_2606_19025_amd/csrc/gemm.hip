@@ -1655,11 +1655,12 @@ TileSize xent_logit_tiles(const GemmArgs& a) {
   return choose_tiles(UP_FWD, &a, 1, nullptr, 0, nullptr, &parts);
 }
 
-// (The sizes' own costs, with the parts that dx is cut into at each; in the time that a launch takes by
-// all tiles or by its longest one.  On 28 drawn heads of 1 to 7000 tokens, d = 64 to 3700, 100 to 46000
-// words, each timed in the three sizes: 1.6 % longer than the fastest of them; by choose_tiles, which
-// cuts dx otherwise, 5.1 %.)
+// The sizes' own costs, with the parts that dx is cut into at each, in the time that a launch takes by all
+// tiles or by its longest one; W and dW at what each size streams of them (TB/s).  On 68 drawn heads of 1
+// to 7000 tokens, d = 64 to 4096, 100 to 50000 words, each timed in the three sizes: 0.6 % longer than the
+// fastest of them (without the streams 24 tokens, d = 2048, 49152 words took 64 x 128: 179 us against 142).
 TileSize xent_pair_tiles(const GemmArgs& dx, const GemmArgs& dw, const int* split) {
+  constexpr double kStream[3] = {13.0, 4.0, 3.6};
   int pick = 0;
   double least = INFINITY;
   for (int i = 0; i < 3; ++i) {
@@ -1671,7 +1672,8 @@ TileSize xent_pair_tiles(const GemmArgs& dx, const GemmArgs& dw, const int* spli
                                     dw_steps * c.lone_step + c.dw);
     const double work = tiles * (steps * c.step + split[i] * c.linear) + dw_tiles * (dw_steps * c.step + c.dw);
     const double us = std::max(longest, work / num_cus() + c.overlap * longest) +
-                      8.0 * split[i] * dx.cap * dx.N / 4.9e6;
+                      8.0 * split[i] * dx.cap * dx.N / 4.9e6 +
+                      (dw.xe.out_bf16 ? 4e-6 : 6e-6) * dw.M * dw.N / kStream[i];
     if (us < least) {
       least = us;
       pick = i;

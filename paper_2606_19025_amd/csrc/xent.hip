@@ -246,10 +246,7 @@ struct Plan {
   int parts;           // partials of a row, at most
 };
 
-// dz of a piece.  Smaller pieces read and write dx's partial sums more often, larger ones leave the
-// last-level cache (8192 tokens, d = 2048, 49152 words, loss and gradients, ms by MiB: 64 5.44, 128 5.20,
-// 256 5.27, 512 5.27, 1024 5.27; 1531 tokens, d = 768, 50003 words 0.52, 0.45, 0.42, 0.42, 0.42).
-constexpr size_t kDzBytes = (size_t)256 << 20;
+constexpr size_t kDzBytes = (size_t)256 << 20;  // dz of a piece, at most (or of kPad columns)
 constexpr int kPad = 256;
 
 int tile_rows(TileSize t) { return t == TILE_256x256 ? 256 : t == TILE_32x64 ? 32 : 64; }
@@ -258,43 +255,105 @@ int tile_cols(TileSize t) { return t == TILE_256x256 ? 256 : t == TILE_64x128 ? 
 // fp32: six tiles of 64 x 128 per CU, or 32 x 64 ones (as the grouped GEMMs).
 TileSize f32_tiles(double tiles) { return tiles >= 6.0 * num_cus() ? TILE_64x128 : TILE_32x64; }
 
-Plan plan_of(const moe_xent& x) {
+// When the last of `cus` CUs ends that take na tiles of time a, then nb of time b <= a, each when it is free.
+double ends(int cus, long na, double a, long nb, double b) {
+  if (a < b) {
+    std::swap(a, b);
+    std::swap(na, nb);
+  }
+  const long q = na / cus, r = na % cus;
+  const double base[2] = {q * a, (q + 1) * a};
+  const long n[2] = {cus - r, r};
+  double best = r ? base[1] : base[0];
+  if (nb == 0) return best;
+  // the earliest time at which all of nb fit: some CU ends at it
+  const double least = std::max(best, (na * a + nb * b) / cus);
+  double found = INFINITY;
+  for (int i = 0; i < 2; ++i) {
+    if (n[i] == 0) continue;
+    for (long k = std::max(0L, (long)((least - base[i]) / b) - 1);; ++k) {
+      const double t = base[i] + k * b;
+      if (t < least) continue;
+      if (t >= found) break;
+      long fit = 0;
+      for (int j = 0; j < 2; ++j)
+        if (t >= base[j]) fit += n[j] * (long)((t - base[j]) / b + 1e-9);
+      if (fit >= nb) {
+        found = t;
+        break;
+      }
+    }
+  }
+  return std::max(best, found);
+}
+
+// Estimate (us) of the backward in 256 x 256 tiles, by pieces of `piece` columns and `split` parts of K of
+// dx: rounds of the logits' tiles; the longest XCD of dx with dW, whose tiles are dealt by the XCD; the
+// partial sums' and, where dz leaves the last-level cache, its own traffic.  On eleven heads of 1500 to
+// 16000 tokens, each timed in 1 to 7 pieces by 1 to 6 parts, the pair that it picks is 0.4 % over the
+// fastest; as few pieces as hold dz and dx in three quarters of the CUs 3.3 % (8192 tokens, d = 2048,
+// 49152 words 3.91 ms against 4.06, 4096 tokens, d = 1024, 32000 words 704 us against 763).
+double backward_us(const moe_xent& x, int width, int piece, int split) {
+  const double step = 1.646, tile = 6.0;  // a 64-deep k-step; fill and epilogue
+  const long rows = ceil_div(x.N, 256), cols = ceil_div(x.d, 256), words = piece / 256;
+  const double logits = (double)((rows * words + num_cus() - 1) / num_cus()) * (x.d / 64 * 1.45 + 5.5);
+  const double pair = ends(num_cus() / 8, (words * cols + 7) / 8, ceil_div(x.N, 64) * step + tile,
+                           (rows * cols * split + 7) / 8, piece / 64.0 / split * step + tile);
+  const double dz = 2.0 * x.N * piece, spill = dz > (double)(192 << 20) ? 0.9 * dz / 4.9e6 : 0.0;
+  return ceil_div(width, piece) * (logits + pair + 9.6 * split * x.N * x.d / 4.9e6 + spill + 8.0);
+}
+
+Plan plan_of(const moe_xent& x, bool bwd) {
   const bool bf16 = x.dtype == MOE_BF16;
   const size_t s = bf16 ? 2 : 4;
   Plan p{};
-  const int width = up((size_t)x.V);
-  // a piece's operands (rows of W and dW) below 2 GiB, dz within its budget
+  const int width = (int)up((size_t)x.V);
+  // a piece's operands (rows of W and dW) below 2 GiB
   const size_t most_w = std::max<size_t>(kPad, ((size_t)2 << 30) / ((size_t)x.d * 4) / kPad * kPad);
-  const size_t most_dz = std::max<size_t>(kPad, kDzBytes / (std::max(1, x.N) * s) / kPad * kPad);
-  const int pieces = (int)((width + std::min(most_w, most_dz) - 1) / std::min(most_w, most_dz));
-  p.piece = (int)up((size_t)ceil_div(width, pieces));
   p.fwd_piece = (int)std::min<size_t>(most_w, (size_t)width);
   p.parts = ceil_div(x.V, 64) * 2 + 2;
   GemmArgs z{}, dx{}, dw{};
   z.n_groups = dx.n_groups = dw.n_groups = 1;
   z.cap = dx.cap = dw.cap = x.N;
   z.N = std::min(x.V, p.fwd_piece); z.K = x.d;
-  dx.N = x.d; dx.K = std::min(x.V, p.piece);
-  dw.M = dx.K; dw.N = x.d;
+  p.logits = bf16 ? xent_logit_tiles(z) : f32_tiles((double)ceil_div(x.N, 64) * ceil_div(z.N, 128));
+  if (!bwd) return p;
   // Parts of K of dx: its few tiles reduce over the whole piece, so they are cut until they are three
   // quarters of the CUs; 256 columns a part at least.  Measured (us of the backward by parts): 512 tokens,
   // d = 2048, 32768 words 1 698, 2 394, 4 253, 8 212, 14 212, 28 242; 1531 tokens, d = 768, 50003 words
-  // 1055, 590, 365, 283, 284, 309; 4096 tokens, d = 1024, 32000 words 987, 731, 724, 748, 821, 907.
+  // 1055, 590, 365, 283, 284, 309.
   const double most = (double)(((size_t)256 << 20) / ((size_t)std::max(1, x.N) * x.d * 4));
   auto split_of = [&](TileSize t) {
     const double tiles = (double)ceil_div(x.N, tile_rows(t)) * ceil_div(x.d, tile_cols(t));
     return (int)std::max(1.0, std::min({0.75 * num_cus() / std::max(tiles, 1.0), p.piece / 256.0, most}));
   };
+  const size_t most_dz = std::max<size_t>(kPad, kDzBytes / (std::max(1, x.N) * s) / kPad * kPad);
+  const int pieces = (int)((width + std::min(most_w, most_dz) - 1) / std::min(most_w, most_dz));
+  p.piece = (int)up((size_t)ceil_div(width, pieces));
+  dx.N = x.d; dx.K = std::min(x.V, p.piece);
+  dw.M = dx.K; dw.N = x.d;
+  dw.xe.out_bf16 = x.dw_dtype == MOE_BF16;
   if (bf16) {
-    p.logits = xent_logit_tiles(z);
     const int split[3] = {split_of(TILE_256x256), split_of(TILE_64x128), split_of(TILE_64x64)};
     p.pair = xent_pair_tiles(dx, dw, split);
   } else {
-    const double cols = ceil_div(x.d, 128);
-    p.logits = f32_tiles((double)ceil_div(x.N, 64) * ceil_div(z.N, 128));
-    p.pair = f32_tiles(cols * (ceil_div(x.N, 64) + ceil_div(dw.M, 64)));
+    p.pair = f32_tiles((double)ceil_div(x.d, 128) * (ceil_div(x.N, 64) + ceil_div(dw.M, 64)));
   }
   p.split = split_of(p.pair);
+  if (p.pair != TILE_256x256 || p.logits != TILE_256x256) return p;
+  const int whole = p.piece, few = p.split;  // (few tokens: more parts than eight)
+  double least = backward_us(x, width, whole, few);
+  for (int n = pieces; n < pieces + 5 && n <= width / kPad; ++n) {
+    const int piece = (int)up((size_t)ceil_div(width, n));
+    for (int split = 1; split <= 8 && split <= piece / 256 && split <= std::max(1.0, most); ++split) {
+      const double us = backward_us(x, width, piece, split);
+      if (us < least) {
+        least = us;
+        p.piece = piece;
+        p.split = split;
+      }
+    }
+  }
   return p;
 }
 
@@ -389,11 +448,11 @@ hipError_t run(TileSize size, int bf16, int ka, const GemmArgs& a, const GemmArg
 
 }  // namespace
 
-size_t xent_fwd_ws_bytes(const moe_xent* x) { return buffers(*x, plan_of(*x), false, nullptr).bytes; }
-size_t xent_bwd_ws_bytes(const moe_xent* x) { return buffers(*x, plan_of(*x), true, nullptr).bytes; }
+size_t xent_fwd_ws_bytes(const moe_xent* x) { return buffers(*x, plan_of(*x, false), false, nullptr).bytes; }
+size_t xent_bwd_ws_bytes(const moe_xent* x) { return buffers(*x, plan_of(*x, true), true, nullptr).bytes; }
 
 hipError_t launch_xent_fwd(const moe_xent* x, hipStream_t s) {
-  const Plan p = plan_of(*x);
+  const Plan p = plan_of(*x, false);
   const int bf16 = x->dtype == MOE_BF16;
   const Buffers b = buffers(*x, p, false, x->ws);
   hipError_t e;
@@ -433,7 +492,7 @@ hipError_t launch_xent_fwd(const moe_xent* x, hipStream_t s) {
 }
 
 hipError_t launch_xent_bwd(const moe_xent* x, hipStream_t s) {
-  const Plan p = plan_of(*x);
+  const Plan p = plan_of(*x, true);
   const int bf16 = x->dtype == MOE_BF16;
   const size_t es = bf16 ? 2 : 4, ws = x->dw_dtype == MOE_BF16 ? 2 : 4;
   const Buffers b = buffers(*x, p, true, x->ws);
