@@ -472,9 +472,9 @@ int moe_block_norm_bwd(const moe_block_norm* p, hipStream_t stream);
  * current device's compute-unit count; the backward's holds dz of 256 MiB, or of 256 words, at most, up
  * to 256 MiB of partial sums, a copy of x and one of dx in fp32); its contents on entry are ignored.
  * Two calls may share it only if they are ordered on a stream.
- * Limits: 0 <= N < 2^27, 1 <= V < 2^30, d <= 2^16; bf16: d % 64 == 0, N < 2^23, N d below 2^31 - 16
- * (operands are addressed with 32-bit byte offsets); fp32: d % 8 == 0; scale finite and not 0, z_coef
- * finite; x, w, dx and dw 16-byte aligned.
+ * Limits: 0 <= N < 2^23, N d below 2^31 - 16 (rows are addressed with 32-bit byte offsets), 1 <= V < 2^30,
+ * d <= 2^16, bf16: d % 64 == 0, fp32: d % 8 == 0; scale finite and not 0, z_coef finite; x, w, dx and dw
+ * 16-byte aligned.
  */
 typedef struct moe_xent {
   int dtype, N, d, V;

@@ -606,17 +606,13 @@ int check_xent_sizes(const moe_xent* p) {
   int r;
   if ((r = check_dtype(p->dtype)) != MOE_OK) return r;
   REQUIRE(p->N >= 0 && p->d >= 1 && p->V >= 1, "bad sizes N = %d, d = %d, V = %d", p->N, p->d, p->V);
-  SUPPORT(p->N < 1 << 27, "N = %d must be below 2^27", p->N);
+  SUPPORT(p->N < 1 << 23, "N = %d must be below 2^23", p->N);
   SUPPORT(p->d <= 1 << 16, "d = %d: at most 2^16", p->d);
   SUPPORT(p->V < 1 << 30, "V = %d must be below 2^30", p->V);
-  if (p->dtype == MOE_BF16) {
-    SUPPORT(p->d % 64 == 0, "d = %d must be a multiple of 64 for bf16", p->d);
-    SUPPORT(p->N < 1 << 23, "N = %d must be below 2^23 for bf16", p->N);
-    SUPPORT((int64_t)p->N * p->d < (int64_t(1) << 31) - 16, "N d = %lld must be below 2^31 - 16",
-            (long long)p->N * p->d);
-  } else {
-    SUPPORT(p->d % 8 == 0, "d = %d must be a multiple of 8", p->d);
-  }
+  SUPPORT((int64_t)p->N * p->d < (int64_t(1) << 31) - 16, "N d = %lld must be below 2^31 - 16",
+          (long long)p->N * p->d);
+  if (p->dtype == MOE_BF16) SUPPORT(p->d % 64 == 0, "d = %d must be a multiple of 64 for bf16", p->d);
+  else SUPPORT(p->d % 8 == 0, "d = %d must be a multiple of 8", p->d);
   return MOE_OK;
 }
 

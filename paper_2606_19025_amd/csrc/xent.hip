@@ -308,8 +308,11 @@ Plan plan_of(const moe_xent& x, bool bwd) {
   const size_t s = bf16 ? 2 : 4;
   Plan p{};
   const int width = (int)up((size_t)x.V);
-  // a piece's operands (rows of W and dW) below 2 GiB
-  const size_t most_w = std::max<size_t>(kPad, ((size_t)2 << 30) / ((size_t)x.d * 4) / kPad * kPad);
+  // a piece's operands (rows of W and dW) below 2 GiB, its logits in 2^23 tiles of 32 x 64: a grid holds less
+  // than 2^32 threads (a larger one is not refused but taken modulo 2^32)
+  const size_t most_w =
+      std::max<size_t>(kPad, std::min(((size_t)2 << 30) / ((size_t)x.d * 4),
+                                      ((size_t)1 << 23) / (size_t)std::max(1, ceil_div(x.N, 32)) * 64) / kPad * kPad);
   p.fwd_piece = (int)std::min<size_t>(most_w, (size_t)width);
   p.parts = ceil_div(x.V, 64) * 2 + 2;
   GemmArgs z{}, dx{}, dw{};

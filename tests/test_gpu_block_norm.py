@@ -181,6 +181,31 @@ def test_block_norm_in_place(gpu_lib, T, d, dtype):
 
 
 @pytest.mark.gpu
+def test_rows_past_32_bit_offsets(gpu_lib):
+    """The last rows of arrays of over 2^31 values: bit for bit those of the rows alone (of as many
+    rows as take a wave each, so that sums run in the same order)."""
+    T, d, n = (1 << 31) // 2048 + 100, 2048, 4160
+    print("[block] large", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda *s, dt=torch.bfloat16: torch.empty(*s, dtype=dt, device="cuda").normal_(generator=g)
+    x, f, du = r(T, d), r(T, d), r(T, d)
+    w = dict(post_weight=r(d, dt=torch.float32), post_bias=r(d, dt=torch.float32),
+             gate=r(T, dt=torch.float32), pre_weight=r(d, dt=torch.float32))
+    K, S = BlockNorm(T, d, gate="token"), BlockNorm(n, d, gate="token")
+    K.forward(x, f, **w, pre_bias=w["pre_weight"])
+    K.backward(du, f, **w, dres=x)
+    last = lambda t: t[T - n:].contiguous()
+    ws = dict(w, gate=last(w["gate"]))
+    S.forward(last(x), last(f), **ws, pre_bias=w["pre_weight"])
+    S.backward(last(du), last(f), **ws, dres=last(x))
+    for a, b in ((K.x, S.x), (K.u, S.u), (K.dx, S.dx), (K.df, S.df), (K.d_gate, S.d_gate)):
+        assert torch.equal(last(a), b)
+    # sums over T rows: at most T / 512 of a group, two groups, 256 partials by 64 shares
+    ref, mag = (sum(v.double().sum(0) for v in f_(du).split(1 << 16)) for f_ in (lambda v: v, torch.abs))
+    assert ((K.d_pre_bias.double() - ref).abs() <= (T / 512 + 20) * U * mag).all()
+
+
+@pytest.mark.gpu
 def test_block_norm_of_no_rows(gpu_lib):
     w = {k: torch.ones(64, device="cuda") for k in ("post_weight", "post_bias", "gate", "pre_weight")}
     K = BlockNorm(0, 64, gate="channel")

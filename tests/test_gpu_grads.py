@@ -53,6 +53,23 @@ def test_norm_and_clip(gpu_lib, kind):
 
 
 @pytest.mark.gpu
+def test_a_tensor_past_32_bit_offsets(gpu_lib):
+    """2^31 + 7 bf16 values among small ones."""
+    n = (1 << 31) + 7
+    print("[grads] large", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    big = torch.empty(n, dtype=BF, device="cuda").normal_(generator=g)
+    small = make([5, 70], 1)
+    out = [torch.empty_like(big)] + [torch.empty_like(s) for s in small]
+    norm = GradClipper([big] + small, 3.0, out=out).clip()
+    ref = math.sqrt(sum(float((c.double() ** 2).sum()) for c in big.split(1 << 28)) + norm_of(small) ** 2)
+    assert abs(norm[0].item() - ref) <= 1.001 * U * ref
+    for a, b in zip([big[-4096:], big[:4096], big[(1 << 31) - 9: (1 << 31) + 3]] + small,
+                    [out[0][-4096:], out[0][:4096], out[0][(1 << 31) - 9: (1 << 31) + 3]] + out[1:]):
+        assert torch.equal(b, (a.float() * norm[1]).to(a.dtype))
+
+
+@pytest.mark.gpu
 def test_unaligned_gradients(gpu_lib):
     """Pieces of one buffer that start at any value."""
     flat = {F32: make([5000], 1)[0], BF: make([5000], 2, (BF,))[0]}

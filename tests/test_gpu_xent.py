@@ -153,6 +153,19 @@ def test_xent_in_several_pieces(gpu_lib, dtype):
 
 
 @pytest.mark.gpu
+def test_xent_of_weights_past_a_launchs_reach(gpu_lib):
+    """More weights than one launch addresses: the forward in pieces of the vocabulary too."""
+    N, d, V = 3, 16384, 33000
+    print("[xent large weights]", flush=True)
+    t = inputs(N, d, V, "bf16", 5, 0)
+    L = LinearCrossEntropy(N, d, V, dw_dtype=torch.bfloat16)
+    L.forward(t["x"], t["w"], t["labels"])
+    check_forward(L, t, 1.0, 0.0)
+    L.backward(t["x"], t["w"], t["labels"])
+    check_backward(L, t, 1.0, 0.0, None)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,low", [("bf16", True), ("bf16", False), ("f32", False)])
 def test_xent_adds_to_dw(gpu_lib, dtype, low):
     for N in (40, 300):
@@ -310,8 +323,9 @@ def test_c_entry_points_refuse():
                 dx=p, dw=p, ws=p, ws_bytes=1 << 40)
     arg, unsupported = -1, -2
     both = [(dict(dtype=4), unsupported), (dict(N=-1), arg), (dict(V=0), arg), (dict(d=0), arg),
-            (dict(N=1 << 27), unsupported), (dict(d=72), unsupported), (dict(d=1 << 17), unsupported),
+            (dict(dtype=B.MOE_F32, N=1 << 23), unsupported), (dict(d=72), unsupported), (dict(d=1 << 17), unsupported),
             (dict(N=1 << 22, d=512), unsupported), (dict(N=1 << 23), unsupported),
+            (dict(dtype=B.MOE_F32, N=1 << 22, d=512), unsupported),
             (dict(V=1 << 30), unsupported), (dict(dtype=B.MOE_F32, d=12), unsupported),
             (dict(scale=math.inf), arg), (dict(scale=0.0), arg), (dict(z_coef=math.nan), arg), (dict(x=None), arg),
             (dict(w=None), arg), (dict(labels=None), arg), (dict(lse=None), arg),
