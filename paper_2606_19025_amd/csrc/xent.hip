@@ -126,10 +126,10 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
   for (int c = threadIdx.x % (256 / kRows); c < chunks; c += 256 / kRows) dst[c] = src[c];
 }
 
-// (max, sum) pairs of base 2 joined.
+// (max, sum) pairs of base 2 joined.  (fmaxf leaves a NaN out: the sums carry it on)
 DEVI float2 join(float2 a, float2 b) {
   const float m = fmaxf(a.x, b.x);
-  if (m == -INFINITY) return a;
+  if (m == -INFINITY) return float2{m, a.y + b.y};
   return float2{m, a.y * __builtin_amdgcn_exp2f(a.x - m) + b.y * __builtin_amdgcn_exp2f(b.x - m)};
 }
 

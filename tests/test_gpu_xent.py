@@ -218,6 +218,26 @@ def test_a_label_that_is_no_word(gpu_lib, N):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,d,V", [(5, 64, 700), (200, 64, 700), (6000, 64, 5000)])
+def test_nan_in_the_weights(gpu_lib, dtype, N, d, V):
+    """Words whose rows are NaN, whole tiles of them and every one, make every counted token's loss NaN."""
+    t = inputs(N, d, V, dtype, 9, 0.25)
+    t["labels"][t["labels"] >= 0] = 3
+    counts = t["labels"] >= 0
+    L = LinearCrossEntropy(N, d, V, dtype=DT[dtype])
+    for lo, hi in ((64, 577), (650, 651), (0, V)):
+        w = t["w"].clone()
+        w[lo:hi] = float("nan")
+        L.forward(t["x"], w, t["labels"])
+        assert torch.isnan(L.loss[counts]).all() and torch.isnan(L.lse[counts]).all(), (lo, hi)
+        assert (L.loss[~counts] == 0).all() and torch.isnan(L.total[0])
+        L.backward(t["x"], w, t["labels"])
+        assert torch.isnan(L.dx[counts]).all() and (L.dx[~counts] == 0).all()
+        assert torch.isnan(L.dw).all()  # (every word's gradient has those tokens' lse)
+
+
+@pytest.mark.gpu
 def test_no_tokens(gpu_lib):
     L = LinearCrossEntropy(0, 64, 100)
     x, w = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(100, 64, dtype=torch.bfloat16, device="cuda")
