@@ -209,6 +209,7 @@ __global__ __launch_bounds__(64 * bwd_waves(W), 4) void block_norm_bwd_kernel(Bl
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int group = wave / W, wr = wave % W;
   const int step = gridDim.x * GROUPS;
+  const bool full = ((NV - 1) * W + wr) * 64 * VE < p.d;  // the wave's every vector holds values of the row
   float s[kSums][NV][VE], wpre[NV][VE], wpost[NV][VE], bpost[NV][VE], g[NV][VE];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -229,6 +230,7 @@ __global__ __launch_bounds__(64 * bwd_waves(W), 4) void block_norm_bwd_kernel(Bl
   float nmx = 0.f, nrx = 0.f, nmf = 0.f, nrf = 0.f, ng = 1.f;
   // (rows past the last read zeros, with means of zero: they add zeros)
   auto fetch = [&](int t, char* dst) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (what was there has been read)
     const int n = t < p.T ? bytes : 0;
     const size_t at = t < p.T ? (size_t)t * p.d : 0;
     if constexpr (PRE) {
@@ -258,8 +260,9 @@ __global__ __launch_bounds__(64 * bwd_waves(W), 4) void block_norm_bwd_kernel(Bl
   for (int t0 = first; t0 < p.T; t0 += step) {  // (the same rounds in all waves)
     const int t = t0 + group;
     const bool there = t < p.T;
-    // This round's arrays have landed: memory operations of a wave end in order, and at most the
-    // last round's stores are newer than the statistics loaded behind the arrays.
+    // This round's arrays have landed: memory operations of a wave end in order, and the last round's 2 NV
+    // stores (none of vectors past the row's end) and at least one statistic are newer.
+    if (!full) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("s_waitcnt vmcnt(%5)" : "+v"(nmx), "+v"(nrx), "+v"(nmf), "+v"(nrf), "+v"(ng) : "n"(2 * NV + 1) : "memory");
     const float mx = nmx, rx = nrx, mf = nmf, rf = nrf, ag = p.scale * ng;
     const char* src = ring[cur][wave];
