@@ -465,8 +465,9 @@ int moe_block_norm_bwd(const moe_block_norm* p, hipStream_t stream);
  *   dz[t,v] = dloss[t] scale ((1 + 2 z_coef lse[t]) exp(z[t,v] - lse[t]) - (v == labels[t]))
  *   dx[t,:] = sum_v dz[t,v] w[v,:]                (dtype)
  *   dw[v,:] (+)= sum_t dz[t,v] x[t,:]             (dw_dtype: MOE_F32, or dtype)
- * dz is rounded once to dtype; sums are fp32, dx is rounded once, dw is added to where accumulate_dw
- * != 0 and rounded after the sum.  loss and total are not read.
+ * dz without the scale and the mean's 1 / n is rounded once to dtype (bf16 and N <= 32: kept in two
+ * values, to 2^-16 of it); sums are fp32, dx is rounded once, dw is added to where accumulate_dw != 0
+ * and rounded after the sum.  loss and total are not read.
  * ws: device workspace (256-byte aligned) of at least moe_xent_fwd_workspace_size(p) or
  * moe_xent_bwd_workspace_size(p) bytes (which depend on the sizes and types alone and on the
  * current device's compute-unit count; the backward's holds dz of 256 MiB, or of 256 words, at most, up

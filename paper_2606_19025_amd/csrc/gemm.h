@@ -34,12 +34,14 @@ struct XentArgs {
   const void* x_all;      // x itself, taken instead of the counted tokens' copy when all count
   const int32_t* label;   // per row
   const float* lse;       // per row (XE_DZ)
-  const float* coef;      // per row: upstream gradient times the logits' scale (XE_DZ)
+  const float* coef;      // per row: its upstream gradient (XE_DZ)
+  const float* out;       // XE_DW: a factor of all of it
   float2* part;           // XE_LSE: [128-column (small tiles: half a tile's) piece][cap] (max, sum), base 2
   float* z_label;         // XE_LSE: per row, the label's logit
   int V, v0;
   float scale, z2;        // of the logits; 2 z_coef
   int out_bf16;           // XE_DW: C is bf16
+  int lo;                 // XE_DZ, small tiles: dz's rounding errors go this many elements behind it (0: nowhere)
   int* done;              // XE_LSE: a counter to clear for the launch that follows
 };
 

@@ -923,6 +923,13 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
       // epilogue).  Accumulator (i, j) register t
       // holds C[wm*WM + 16i + lane%16][wn*128 + 16j + 4(lane/16) + t]
       const GemmArgs& a = L.s[cur.set];
+      if constexpr (KIND == XE_DW) {
+        const float f = *a.xe.out;
+#pragma unroll
+        for (int ii = 0; ii < MI; ++ii)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[ii][j] *= f;
+      }
       const Tile tl = cur.tl;
       const int row_lim = tl.rows - wm * WM;  // rows of this wave's sub-tile to store
       char* reg = lds + wave * C_::EPI_WAVE;

@@ -102,6 +102,7 @@ struct TileAt {
 // rows of fp32 layers, weight gradients of either type.
 template <int KIND>
 DEVI void store_cols(const GemmArgs& a, const TileAt& t, int i, int n, f32x4_t v) {
+  if constexpr (KIND == XE_DW) v *= *a.xe.out;
   if constexpr (Kind<KIND>::MRAG) {
     const size_t m = (size_t)(t.row0 + i);
     if constexpr (KIND == DHH_BWD) {
@@ -489,6 +490,24 @@ DEVI void gemm_tile(const GemmArgs& a, const TileAt& tl, char* lds) {
             for (int e = 0; e < 8; ++e) v[e] = (bf16_t)silu_t<T>((float)v[e]);
             put8(a.out2, m * a.H + n, v);
           }
+        }
+      }
+      if (KIND == XE_DZ && a.xe.lo) {
+        // what the roundings left, behind (the region is this wave's own)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            const f32x4_t hi = __builtin_convertvector(__builtin_convertvector(acc[i][j], bf16x4_t), f32x4_t);
+            *reinterpret_cast<bf16x4_t*>(at(16 * i + l16, 2 * j + (g4 >> 1)) + (g4 & 1) * 8) =
+                __builtin_convertvector(acc[i][j] - hi, bf16x4_t);
+          }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const int r = p * RPP + lane / CPR;
+          const size_t m = (size_t)(tl.row0 + wm * 16 * MI + r);
+          if (!ok || r >= 16 * MI || r >= rows) continue;
+          put8(a.C, m * a.ldc + a.xe.lo + n, *reinterpret_cast<const bf16x8_t*>(at(r, c)));
         }
       }
     }

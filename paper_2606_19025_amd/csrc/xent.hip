@@ -2,7 +2,10 @@
 //
 //   z_tv = scale x_t . w_v;   lse_t = log sum_v exp z_tv;   loss_t = lse_t - z_ty + z_coef lse_t^2
 //   dz_tv = g_t ((1 + 2 z_coef lse_t) exp(z_tv - lse_t) - [v = y_t])
-//   dx = scale dz W,  dW = scale dz^T x            (the scale goes into g_t)
+//   dx = scale dz W,  dW = scale dz^T x
+// The scale, and the mean's 1 / n where that is all of g, are factors of dx and dW at their ends (out), so
+// that dz's roundings do not take them in: -1 of a label's word is exact, not off by one part in up to 2^8
+// in all tokens alike.
 //
 // Four products of 2 N V d operations (gemm.hip, gemm_tile.hip: XE_* kinds).  Forward: a tile of
 // logits ends in (max, sum of 2^(z - max)) of each of its rows, and the label's logit where it is
@@ -24,11 +27,11 @@
 namespace moe {
 namespace {
 
-constexpr int kRows = 16;         // tokens of a block of xent_rows
 constexpr int kCountRows = 1024;  // tokens of a counting block
 constexpr int kDirect = 8192;     // up to here every block counts all labels itself
 constexpr int kLossThreads = 1024;
-constexpr int kAsIs = 128;        // up to here the forward leaves out no row (24 tokens 55 -> 51 us)
+constexpr int kFew = 128;         // up to here the forward leaves out no row
+constexpr int kTwo = 32;          // up to here the backward keeps dz in two values (Plan::two)
 
 struct RowArgs {
   const void* x;
@@ -39,10 +42,12 @@ struct RowArgs {
   float scale;
   int* count;          // [blocks of kCountRows]
   int* pos;            // [N] row of a token among those that count, or -1
-  int* off;            // {0, tokens that count}
+  int* off;            // {0, tokens that count, 0, twice them}
+  int two;             // backward: a token's row is copied twice, in any case
   int* row_label;      // the rest by row
   float* row_lse;      // backward
   float* coef;
+  float* out;
   void* xc;
   int* counters;       // backward: cleared for the launches that follow
   int n_counters;
@@ -68,12 +73,12 @@ __global__ __launch_bounds__(256) void xent_count_kernel(const int32_t* label, i
   if (threadIdx.x == 0) count[blockIdx.x] = v;
 }
 
-// The rows of the tokens that count, kRows tokens a block.
-template <bool BWD>
+// The rows of the tokens that count, R tokens a block: 16, or 4 where they are few.
+template <bool BWD, int R>
 __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
   __shared__ int buf[4];
-  __shared__ int row[kRows];
-  const int t0 = blockIdx.x * kRows;
+  __shared__ int row[R];
+  const int t0 = blockIdx.x * R;
   // tokens that count before this block's, and all of them
   int before = 0, total = 0;
   if (a.N <= kDirect) {
@@ -95,10 +100,10 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
   total = block_sum_256(total, buf);
   if (threadIdx.x < 64) {
     const int t = t0 + threadIdx.x;
-    const int y = (int)threadIdx.x < kRows && t < a.N ? a.label[t] : -1;
+    const int y = (int)threadIdx.x < R && t < a.N ? a.label[t] : -1;
     const unsigned long long counts = __ballot(y >= 0);
     const int p = y < 0 ? -1 : before + __builtin_popcountll(counts & ((1ull << threadIdx.x) - 1));
-    if ((int)threadIdx.x < kRows) {
+    if ((int)threadIdx.x < R) {
       row[threadIdx.x] = p;
       if (t < a.N) a.pos[t] = p;
     }
@@ -107,23 +112,30 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
       if constexpr (BWD) {
         a.row_lse[p] = a.lse[t];
         // (a label that is no word of the vocabulary makes what it enters NaN)
-        a.coef[p] = y < a.V ? a.scale * (a.dloss ? a.dloss[t] : 1.0f / (float)total) : NAN;
+        a.coef[p] = y < a.V ? (a.dloss ? a.dloss[t] : 1.0f) : NAN;
       }
     }
-    if (blockIdx.x == 0 && threadIdx.x < 2) a.off[threadIdx.x] = threadIdx.x ? total : 0;
+    if (blockIdx.x == 0 && threadIdx.x < 4) a.off[threadIdx.x] = threadIdx.x & 1 ? total * (1 + (threadIdx.x >> 1)) : 0;
   }
+  if (BWD && blockIdx.x == 0 && threadIdx.x == 0)
+    *a.out = a.dloss ? a.scale : total ? a.scale / (float)total : 0.0f;
   if (BWD && blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.n_counters; i += 256) a.counters[i] = 0;
-  if (total == a.N) return;  // x itself is read
+  if (total == a.N && !a.two) return;  // x itself is read
   __syncthreads();
-  // sixteen threads to a row, so that all rows' loads are in flight
+  // 256 / R threads to a row, so that all rows' loads are in flight
   const int chunks = a.d * a.size / 16;
-  const int r = threadIdx.x / (256 / kRows), p = row[r];
+  const int r = threadIdx.x / (256 / R), p = row[r];
   if (p < 0) return;
   const u32x4_t* src = static_cast<const u32x4_t*>(a.x) + (size_t)(t0 + r) * chunks;
-  u32x4_t* dst = static_cast<u32x4_t*>(a.xc) + (size_t)p * chunks;
+  u32x4_t* dst = static_cast<u32x4_t*>(a.xc) + (size_t)(a.two ? 2 * p : p) * chunks;
+  u32x4_t* again = dst + (a.two ? chunks : 0);
 #pragma unroll 4
-  for (int c = threadIdx.x % (256 / kRows); c < chunks; c += 256 / kRows) dst[c] = src[c];
+  for (int c = threadIdx.x % (256 / R); c < chunks; c += 256 / R) {
+    const u32x4_t v = src[c];
+    dst[c] = v;
+    if (a.two) again[c] = v;
+  }
 }
 
 // (max, sum) pairs of base 2 joined.  (fmaxf leaves a NaN out: the sums carry it on)
@@ -207,30 +219,50 @@ __global__ __launch_bounds__(256) void xent_clear_kernel(u32x4_t* p, size_t n) {
     p[i] = u32x4_t{0u, 0u, 0u, 0u};
 }
 
-// dx[t] = the sum of its row's S partial sums in order, or zeros.
-template <class E>
+// dx[t] = the sum of its row's (TWO: both rows') S partial sums, or zeros.  SH threads share a vector's
+// partials, whose sums are added in order: where the vectors are few and the partials many (5 tokens, d =
+// 768, 192 partials 8 us, with eight 5).
+template <class E, int SH, bool TWO>
 __global__ __launch_bounds__(256) void xent_dx_kernel(E* dx, const int* pos, const float* part, size_t stride,
-                                                      int S, int N, int d) {
-  constexpr int V = Vec16<E>::N;
-  const int chunks = d / V;
+                                                      int S, int N, int d, const float* out) {
+  constexpr int V = Vec16<E>::N, AT = 256 / SH;
+  __shared__ float sum[SH > 1 ? SH : 1][SH > 1 ? AT : 1][V + 4];
+  const int chunks = d / V, sh = threadIdx.x / AT, l = threadIdx.x % AT;
   const size_t n = (size_t)N * chunks;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
+  // (every thread of a block takes the same rounds)
+  for (size_t i0 = (size_t)blockIdx.x * AT; i0 < n; i0 += (size_t)gridDim.x * AT) {
+    const size_t i = i0 + l;
     const int t = (int)(i / chunks), c = (int)(i % chunks) * V;
-    const int p = pos[t];
+    const int p = i < n ? pos[t] : -1;
     float v[V] = {};
     if (p >= 0) {
+      const float* q = part + (size_t)(TWO ? 2 * p : p) * d + c;
 #pragma unroll 4
-      for (int s = 0; s < S; ++s) {
-        const float* q = part + (size_t)s * stride + (size_t)p * d + c;
+      for (int s = sh; s < S; s += SH) {
 #pragma unroll
         for (int j = 0; j < V; j += 4) {
-          const f32x4_t u = *reinterpret_cast<const f32x4_t*>(q + j);
+          f32x4_t u = *reinterpret_cast<const f32x4_t*>(q + s * stride + j);
+          if (TWO) u += *reinterpret_cast<const f32x4_t*>(q + s * stride + d + j);
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[j + e] += u[e];
         }
       }
     }
-    store16_f32(dx + (size_t)t * d + c, v);
+    if constexpr (SH > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[sh][l][j] = v[j];
+      __syncthreads();
+      if (sh > 0) continue;
+#pragma unroll
+      for (int k = 1; k < SH; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] += sum[k][l][j];
+    }
+    const float f = *out;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] *= f;
+    if (i < n) store16_f32(dx + (size_t)t * d + c, v);
   }
 }
 
@@ -243,6 +275,12 @@ struct Plan {
   int piece;           // columns of a piece of the backward, a multiple of 256
   int fwd_piece;       // and of the forward
   int split;           // parts of K of dx
+  // bf16, up to 32 tokens: dz in two bf16 values, its rounding and what that leaves (16 bits together), as
+  // two rows of dx's and dW's products, with x twice.  A rounding is off by 2^-8 at most, alike in a token's
+  // whole row of products, and few tokens do not average it out (dW against 64 bits: 1.0 to 1.6 times a bf16
+  // output's own rounding).  A k-step of 64 rows of dW holds both: 5 tokens of d = 768 take as long, 32 of 1024 4 %
+  // and 24 of 2048 7 % longer, but 64 tokens of d = 2048 14 %, 128 30 %.
+  bool two;
   int parts;           // partials of a row, at most
 };
 
@@ -321,13 +359,16 @@ Plan plan_of(const moe_xent& x, bool bwd) {
   z.N = std::min(x.V, p.fwd_piece); z.K = x.d;
   p.logits = bf16 ? xent_logit_tiles(z) : f32_tiles((double)ceil_div(x.N, 64) * ceil_div(z.N, 128));
   if (!bwd) return p;
+  p.two = bf16 && x.N <= kTwo;
+  if (p.two && p.logits == TILE_256x256) p.logits = TILE_64x128;  // (which write both)
+  dx.cap = dw.cap = p.two ? 2 * x.N : x.N;
   // Parts of K of dx: its few tiles reduce over the whole piece, so they are cut until they are three
   // quarters of the CUs; 256 columns a part at least.  Measured (us of the backward by parts): 512 tokens,
   // d = 2048, 32768 words 1 698, 2 394, 4 253, 8 212, 14 212, 28 242; 1531 tokens, d = 768, 50003 words
   // 1055, 590, 365, 283, 284, 309.
-  const double most = (double)(((size_t)256 << 20) / ((size_t)std::max(1, x.N) * x.d * 4));
+  const double most = (double)(((size_t)256 << 20) / ((size_t)std::max(1, dx.cap) * x.d * 4));
   auto split_of = [&](TileSize t) {
-    const double tiles = (double)ceil_div(x.N, tile_rows(t)) * ceil_div(x.d, tile_cols(t));
+    const double tiles = (double)ceil_div(dx.cap, tile_rows(t)) * ceil_div(x.d, tile_cols(t));
     return (int)std::max(1.0, std::min({0.75 * num_cus() / std::max(tiles, 1.0), p.piece / 256.0, most}));
   };
   const size_t most_dz = std::max<size_t>(kPad, kDzBytes / (std::max(1, x.N) * s) / kPad * kPad);
@@ -386,7 +427,7 @@ struct Buffers {
 int loss_rows(int N) { return N >= 8192 ? 32 : N >= 1024 ? 16 : 4; }
 
 Buffers buffers(const moe_xent& x, const Plan& p, bool bwd, void* ws) {
-  const size_t s = x.dtype == MOE_BF16 ? 2 : 4, N = x.N;
+  const size_t s = x.dtype == MOE_BF16 ? 2 : 4, N = x.N, M = p.two ? 2 * N : N;
   Space w{static_cast<char*>(ws)};
   Buffers b{};
   RowArgs& r = b.row;
@@ -394,9 +435,10 @@ Buffers buffers(const moe_xent& x, const Plan& p, bool bwd, void* ws) {
   r.lse = x.lse; r.dloss = x.dloss;
   r.count = w.take<int>((N + kCountRows - 1) / kCountRows);
   r.pos = w.take<int>(N);
-  r.off = w.take<int>(2);
+  r.off = w.take<int>(4);
   r.row_label = w.take<int>(N);
-  r.xc = w.take<char>(N * x.d * s);
+  r.two = p.two;
+  r.xc = w.take<char>(M * x.d * s);
   if (!bwd) {
     b.z_label = w.take<float>(N);
     b.part = w.take<float2>((size_t)p.parts * N);
@@ -405,8 +447,9 @@ Buffers buffers(const moe_xent& x, const Plan& p, bool bwd, void* ws) {
   } else {
     r.row_lse = w.take<float>(N);
     r.coef = w.take<float>(N);
-    b.dz = w.take<char>(N * p.piece * s);
-    b.dx_part = w.take<float>((size_t)p.split * N * x.d);
+    r.out = w.take<float>(1);
+    b.dz = w.take<char>(M * p.piece * s);
+    b.dx_part = w.take<float>((size_t)p.split * M * x.d);
     r.n_counters = ceil_div(x.V, p.piece) * kXcdCounters;
     r.counters = w.take<int>(r.n_counters);
   }
@@ -422,7 +465,8 @@ hipError_t rows(const Buffers& b, hipStream_t s) {
               xent_count_kernel<<<ceil_div(r.N, kCountRows), 256, 0, s>>>(r.label, r.N, r.count));
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  MOE_TIMED("xent_rows", s, xent_rows_kernel<BWD><<<ceil_div(r.N, kRows), 256, 0, s>>>(r));
+  if (r.N <= kFew) MOE_TIMED("xent_rows", s, xent_rows_kernel<BWD, 4><<<ceil_div(r.N, 4), 256, 0, s>>>(r));
+  else MOE_TIMED("xent_rows", s, xent_rows_kernel<BWD, 16><<<ceil_div(r.N, 16), 256, 0, s>>>(r));
   return hipGetLastError();
 }
 
@@ -438,6 +482,7 @@ GemmArgs logits(const moe_xent& x, const Buffers& b, int v0, int V) {
   a.xe.label = b.row.row_label;
   a.xe.lse = b.row.row_lse;
   a.xe.coef = b.row.coef;
+  a.xe.out = b.row.out;
   a.xe.V = V; a.xe.v0 = v0;
   a.xe.scale = x.scale; a.xe.z2 = 2.0f * x.z_coef;
   return a;
@@ -463,8 +508,9 @@ hipError_t launch_xent_fwd(const moe_xent* x, hipStream_t s) {
     MOE_TIMED("xent_none", s, xent_none_kernel<<<1, 64, 0, s>>>(x->total));
     return hipGetLastError();
   }
-  // Few tokens: every row as it is (rows are independent here, and the weights' stream sets the time)
-  const bool as_is = x->N <= kAsIs;
+  // Few tokens: every row as it is (rows are independent here, and the weights' stream sets the time: 24
+  // tokens 55 -> 51 us)
+  const bool as_is = x->N <= kFew;
   if (!as_is && (e = rows<false>(b, s)) != hipSuccess) return e;
   const int width = tile_cols(p.logits) / 2;  // of a partial: half a tile's columns
   int parts = 0;
@@ -506,11 +552,19 @@ hipError_t launch_xent_bwd(const moe_xent* x, hipStream_t s) {
     GemmArgs a = logits(*x, b, v0, V);
     a.C = b.dz; a.ldc = ld;
     a.N = ld;  // (the columns past V are written too: zeros)
+    if (p.two) {
+      a.ldc = 2L * ld; a.xe.lo = ld;
+      a.lda = 2L * x->d; a.xe.x_all = b.row.xc;
+    }
     if ((e = run(p.logits, bf16, XE_DZ, a, nullptr, nullptr, s)) != hipSuccess) return e;
     GemmArgs dx = a, dw = a;
+    if (p.two) {
+      dx.offsets = dw.offsets = b.row.off + 2;
+      dx.cap = dw.cap = 2 * x->N;
+    }
     dx.A = b.dz; dx.lda = ld;
     dx.N = x->d; dx.K = p.pair == TILE_256x256 ? ld : V;
-    dx.part = b.dx_part; dx.c_split = (long)x->N * x->d; dx.ksplit = p.split;
+    dx.part = b.dx_part; dx.c_split = (long)dx.cap * x->d; dx.ksplit = p.split;
     dx.accumulate = v0 > 0;
     dw.A = b.dz; dw.lda = ld;
     dw.B = b.row.xc; dw.ldb = x->d;
@@ -529,13 +583,17 @@ hipError_t launch_xent_bwd(const moe_xent* x, hipStream_t s) {
     return hipGetLastError();
   }
   const size_t n = (size_t)x->N * x->d / (bf16 ? 8 : 4);
-  const int blocks = (int)std::min<size_t>(8192, (n + 255) / 256);
-  if (bf16)
-    MOE_TIMED("xent_dx", s, xent_dx_kernel<bf16_t><<<blocks, 256, 0, s>>>(
-        static_cast<bf16_t*>(x->dx), b.row.pos, b.dx_part, (size_t)x->N * x->d, p.split, x->N, x->d));
-  else
-    MOE_TIMED("xent_dx", s, xent_dx_kernel<float><<<blocks, 256, 0, s>>>(
-        static_cast<float*>(x->dx), b.row.pos, b.dx_part, (size_t)x->N * x->d, p.split, x->N, x->d));
+  const bool share = p.two || (p.split >= 8 && n < (size_t)num_cus() * 256);
+  const int blocks = (int)std::min<size_t>(8192, share ? (n + 31) / 32 : (n + 255) / 256);
+#define XENT_DX(E_, SH_, TWO_)                                                                          \
+  MOE_TIMED("xent_dx", s, xent_dx_kernel<E_, SH_, TWO_><<<blocks, 256, 0, s>>>(                          \
+      static_cast<E_*>(x->dx), b.row.pos, b.dx_part, (size_t)x->N * x->d * (p.two ? 2 : 1), p.split, x->N, x->d, b.row.out))
+  if (p.two) XENT_DX(bf16_t, 8, true);
+  else if (bf16 && share) XENT_DX(bf16_t, 8, false);
+  else if (bf16) XENT_DX(bf16_t, 1, false);
+  else if (share) XENT_DX(float, 8, false);
+  else XENT_DX(float, 1, false);
+#undef XENT_DX
   return hipGetLastError();
 }
 

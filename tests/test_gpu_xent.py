@@ -6,7 +6,7 @@ instructions choose: off by at most (d + 1) u sum |x w|, and by 2 u |z| of the s
 Exponentials have about one ulp (2 u) and the rounding of their argument (4 u |z - lse|); a row's sum
 passes at most 64 additions in a lane, 2 across lanes, P / 16 partials of a thread and 16 of the
 threads (each with two exponentials), P pieces of at least 32 columns.  The backward is held to the
-forward's own lse; dz is rounded by h, sums over n terms have n u of the magnitudes.
+forward's own lse; dz is rounded by h (bf16, up to 32 tokens: its two values leave h^2), sums over n terms have n u of the magnitudes.
 """
 import math
 
@@ -90,7 +90,8 @@ def check_backward(L, t, scale, z_coef, dloss, add=0.0):
     h = half(L.dtype)
     # the relative error of p, the few products' and the difference's, then dz's own rounding
     e = cf.abs() * (zf * p).abs() * (ze + 4 * U * (z - lse).abs().clamp(max=200) + 10 * U) + 6 * U * cf.abs() * one
-    e = e + (h if L.dtype == torch.bfloat16 else 2 * U) * dz.abs() + 3 * U * dz.abs() + 1e-37
+    hz = 2 * U if L.dtype != torch.bfloat16 else h * h if N <= 32 else h
+    e = e + hz * dz.abs() + 3 * U * dz.abs() + 1e-37
     x, w = t["x"].double(), t["w"].double()
     dx = dz @ w
     tol = e @ w.abs() + (V + 8) * U * (dz.abs() @ w.abs())
