@@ -17,8 +17,8 @@
 // that four sums do for five gradients; a block keeps them in registers, stores one partial
 // row of 4 d and a second launch adds the partials in a fixed order.
 //
-// Measured (bf16, all forms of gate and bias within 3 %; second launch included): 8192 x 2048 forward
-// 33 us, backward 48; 16384 x 4096 122 and 164 us (4.4 and 4.9 TB/s); 8192 x 1024 16 and 30.
+// Measured (bf16, a gate per channel; second launch included): 8192 x 2048 forward 35 us, backward 48; 16384 x
+// 4096 120 and 155 us (4.5 and 5.2 TB/s); 8192 x 1024 16 and 31; fp32 8192 x 2048 55 and 80 (4.9, 5.0 TB/s).
 #include "common.h"
 #include "kernels.h"
 #include "norm_rows.h"
@@ -191,10 +191,11 @@ constexpr int bwd_waves(int W) { return W > kBwdWaves ? W : kBwdWaves; }
 // Rows of up to 8 values a lane.  A block's groups take rows in turn, in step with each other; the
 // next rows' arrays come by DMA into LDS while this one's are worked on (16 KB of bf16 a row of 2048,
 // no registers), each wave reading what its own lanes asked for, so that no barrier is needed for
-// them (where LDS holds one round alone, fp32 rows past 4096: once it has been read).  Weights stay in registers: a load of them in the loop would wait for the DMA before it.
+// them (where LDS holds one round alone, fp32 rows past 4096: once it has been read).  Weights stay in
+// registers: a load of them in the loop would wait for the DMA before it.
 // One block a CU (a second one's partial rows cost more than it hides: 8192 x 2048 48 -> 55 us).
-// A block of four waves for each row, the next one's loads in registers: 8192 x 2048 58 us, 16384 x
-// 4096 188 (now 164).
+// Instead of this, a block of four waves for each row, the next one's loads in registers: 8192 x 2048 58
+// us, 16384 x 4096 188 (now 155).
 // PRE, POST: the norms that there are.
 template <class E, int W, int NV, bool PRE, bool POST>
 __global__ __launch_bounds__(64 * bwd_waves(W), 4) void block_norm_bwd_kernel(BlockArgs a) {
@@ -263,7 +264,10 @@ __global__ __launch_bounds__(64 * bwd_waves(W), 4) void block_norm_bwd_kernel(Bl
     // This round's arrays have landed: memory operations of a wave end in order, and the last round's 2 NV
     // stores (none of vectors past the row's end) and at least one statistic are newer.
     if (!full) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    asm volatile("s_waitcnt vmcnt(%5)" : "+v"(nmx), "+v"(nrx), "+v"(nmf), "+v"(nrf), "+v"(ng) : "n"(2 * NV + 1) : "memory");
+    asm volatile("s_waitcnt vmcnt(%5)"
+                 : "+v"(nmx), "+v"(nrx), "+v"(nmf), "+v"(nrf), "+v"(ng)
+                 : "n"(2 * NV + 1)
+                 : "memory");
     const float mx = nmx, rx = nrx, mf = nmf, rf = nrf, ag = p.scale * ng;
     const char* src = ring[cur][wave];
     if constexpr (DEPTH == 2) {
@@ -383,7 +387,7 @@ __global__ __launch_bounds__(64 * bwd_waves(W), 4) void block_norm_bwd_kernel(Bl
 }
 
 // Wide rows, 16 values a lane of a block of sixteen waves: two of the column sums are held in LDS,
-// where every lane has its own columns, and nothing is fetched ahead.
+// where every lane has its own columns (in registers they spill), and nothing is fetched ahead.
 template <class E, bool PRE, bool POST>
 __global__ __launch_bounds__(1024) void block_norm_bwd_wide_kernel(BlockArgs a) {
   constexpr int W = 16, VE = Vec16<E>::N, NV = 16 / VE;
@@ -524,7 +528,8 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_wide_kernel(BlockArgs a) 
 }
 
 // The weights' gradients from the n partial rows [n][4][d]: a block takes 16 columns of the four
-// sums, sixteen threads (16 bytes each) by 64 shares of the partials.
+// sums, sixteen threads (16 bytes each) by 64 shares of the partials (bound by their latency: 256 partials of
+// d = 4096, 16 MB, 7 us).
 constexpr int kDwShares = 64;
 __global__ __launch_bounds__(16 * kDwShares) void block_norm_dw_kernel(BlockArgs a, int n) {
   const moe_block_norm& p = a.p;
@@ -590,8 +595,8 @@ int waves_fwd(int T, int d, int ve) {
     if (vectors(d, ve, W) * ve <= 8) return W;
   return 16;
 }
-// Backward: the fewest with a vector in each lane, two of fp32 past sixteen waves' reach; 32: the
-// wide kernel.
+// Backward: the fewest with a vector in each lane (more rows in a block, and fewer barriers between waves),
+// two of fp32 past sixteen waves' reach; 32: the wide kernel.
 int waves_bwd(int d, int ve) {
   for (int W : {1, 2, 4, 8, 16})
     if (vectors(d, ve, W) <= 1) return W;

@@ -14,7 +14,14 @@
 //   DWD       dWd    M=d, N=H   dyp^T  (K = group rows)   h               TN, fp32 out
 //   DWGU      dWgu   M=2H,N=d   dgu^T  (K = group rows)   xp              TN, fp32 out
 //
-// The first four are ragged in M (tiles are laid over the groups from the
+// and four of a linear head's cross entropy (xent.hip; one group, the tokens that count; the logits' two
+// run with an epilogue of arithmetic under the next tile's first loads, EARLY):
+//   XE_LSE    -      M=n, N=V   x    [n,d]    k-contig  w [V,d]           NT, (max, sum) of half-tile rows out
+//   XE_DZ     dz     M=n, N=V   x    [n,d]    k-contig  w                 NT, softmax's gradient epilogue
+//   XE_DX     dx     M=n, N=d   dz   [n,V]    k-contig  w                 NN, fp32 partial sums out
+//   XE_DW     dW     M=V, N=d   dz^T  (K = n)           x                 TN, fp32 or bf16 out
+//
+// Of the six, the first four are ragged in M (tiles are laid over the groups from the
 // device-side offsets; no host read-back), the last two ragged in K.
 //
 // bf16: v_mfma_f32_16x16x32_bf16 with fp32 accumulation in a persistent

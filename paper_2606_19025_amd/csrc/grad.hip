@@ -12,6 +12,9 @@
 // the device, and a captured launch keeps its own.  Tensors are cut into chunks (chunk_of),
 // which the blocks take in turn; every block stores one partial sum, and a last block adds the
 // partials of all launches in order, so the result does not depend on timing.
+//
+// Measured: four tensors of 2^26 fp32 values, norm 183 us (5.9 TB/s), with clipping to other tensors 625 (5.2
+// TB/s); 300 of 2^14 values 15 and 27 us; one of 4096 values 9 and 15 us, two and three launches' latency.
 #include <cmath>
 
 #include "common.h"
@@ -176,14 +179,16 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(ClipTable t, const 
   }
 }
 
-// Values of a chunk, multiples of what 256 threads load at once.
+// Values of a chunk, multiples of what 256 threads load at once: large ones cost a block's search and its
+// first load's latency less often, small ones spread a list over more blocks (300 tensors of 64 to 2^17
+// values clipped: 10 us less in chunks of 4096 than of 16384).
 int chunk_of(const moe_grad* g, int n) {
   size_t total = 0;
   for (int i = 0; i < n; ++i) total += g[i].n;
   return total < ((size_t)32 << 20) ? 4096 : kMaxChunk;
 }
 
-// Blocks of a launch of `chunks` chunks.
+// Blocks of a launch of `chunks` chunks: all that are resident at once, 8 of 256 threads a CU.
 int chunk_blocks(int chunks) { return std::min(chunks, 8 * num_cus()); }
 
 // f(table, blocks) for launches of up to T::kTensors tensors with values.

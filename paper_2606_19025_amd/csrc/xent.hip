@@ -17,6 +17,14 @@
 // together first (where all count, x itself is read), so a padded batch costs what its tokens
 // do, and nothing that stands in a padded row enters a gradient.  How many there are stays on the
 // device, as in the dispatch.
+//
+// Bound by the matrix units with many tokens (8192, d = 2048, 49152 words, bf16: forward 1.29 ms, 1.28 PFLOP/s,
+// backward 3.91 ms, 1.27 over its three products; of a library's product of the logits' size alone 1.24) and
+// by the streams of W and dW with few (24 tokens forward 49 us, of which W at a copy's rate 41; backward 144,
+// where W is read twice and dW written).
+// dz is rounded to bf16, as the matrix instructions take it: dx and dW are 0.0024 off in the mean, against
+// 0.0017 of a bf16 output's own rounding, where every token has a gradient of its own, and as near as the
+// rounding of the mean's and of few tokens' (Plan::two).
 #include <algorithm>
 #include <cmath>
 
@@ -115,7 +123,8 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
         a.coef[p] = y < a.V ? (a.dloss ? a.dloss[t] : 1.0f) : NAN;
       }
     }
-    if (blockIdx.x == 0 && threadIdx.x < 4) a.off[threadIdx.x] = threadIdx.x & 1 ? total * (1 + (threadIdx.x >> 1)) : 0;
+    if (blockIdx.x == 0 && threadIdx.x < 4)
+      a.off[threadIdx.x] = threadIdx.x & 1 ? total * (1 + (threadIdx.x >> 1)) : 0;
   }
   if (BWD && blockIdx.x == 0 && threadIdx.x == 0)
     *a.out = a.dloss ? a.scale : total ? a.scale / (float)total : 0.0f;
@@ -585,9 +594,10 @@ hipError_t launch_xent_bwd(const moe_xent* x, hipStream_t s) {
   const size_t n = (size_t)x->N * x->d / (bf16 ? 8 : 4);
   const bool share = p.two || (p.split >= 8 && n < (size_t)num_cus() * 256);
   const int blocks = (int)std::min<size_t>(8192, share ? (n + 31) / 32 : (n + 255) / 256);
-#define XENT_DX(E_, SH_, TWO_)                                                                          \
-  MOE_TIMED("xent_dx", s, xent_dx_kernel<E_, SH_, TWO_><<<blocks, 256, 0, s>>>(                          \
-      static_cast<E_*>(x->dx), b.row.pos, b.dx_part, (size_t)x->N * x->d * (p.two ? 2 : 1), p.split, x->N, x->d, b.row.out))
+  const size_t stride = (size_t)x->N * x->d * (p.two ? 2 : 1);
+#define XENT_DX(E_, SH_, TWO_)                                                 \
+  MOE_TIMED("xent_dx", s, xent_dx_kernel<E_, SH_, TWO_><<<blocks, 256, 0, s>>>( \
+      static_cast<E_*>(x->dx), b.row.pos, b.dx_part, stride, p.split, x->N, x->d, b.row.out))
   if (p.two) XENT_DX(bf16_t, 8, true);
   else if (bf16 && share) XENT_DX(bf16_t, 8, false);
   else if (bf16) XENT_DX(bf16_t, 1, false);
