@@ -466,12 +466,13 @@ int moe_block_norm_bwd(const moe_block_norm* p, hipStream_t stream);
  *   dx[t,:] = sum_v dz[t,v] w[v,:]                (dtype)
  *   dw[v,:] (+)= sum_t dz[t,v] x[t,:]             (dw_dtype: MOE_F32, or dtype)
  * dz without the scale and the mean's 1 / n is rounded once to dtype (bf16 and N <= 32: kept in two
- * values, to 2^-16 of it); sums are fp32, dx is rounded once, dw is added to where accumulate_dw != 0
+ * values, to 2^-16 of it; bf16, N > 32 and dloss given: dz without dloss, and for dw the row of x with
+ * it); sums are fp32, dx is rounded once, dw is added to where accumulate_dw != 0
  * and rounded after the sum.  loss and total are not read.
  * ws: device workspace (256-byte aligned) of at least moe_xent_fwd_workspace_size(p) or
  * moe_xent_bwd_workspace_size(p) bytes (which depend on the sizes and types alone and on the
  * current device's compute-unit count; the backward's holds dz of 256 MiB, or of 256 words, at most, up
- * to 256 MiB of partial sums, a copy of x and one of dx in fp32); its contents on entry are ignored.
+ * to 256 MiB of partial sums, two copies of x and one of dx in fp32); its contents on entry are ignored.
  * Two calls may share it only if they are ordered on a stream.
  * Limits: 0 <= N < 2^23, N d below 2^31 - 16 (rows are addressed with 32-bit byte offsets), 1 <= V < 2^30,
  * d <= 2^16, bf16: d % 64 == 0, fp32: d % 8 == 0; scale finite and not 0, z_coef finite; x, w, dx and dw

@@ -22,9 +22,9 @@
 // backward 3.91 ms, 1.27 over its three products; of a library's product of the logits' size alone 1.24) and
 // by the streams of W and dW with few (24 tokens forward 49 us, of which W at a copy's rate 41; backward 144,
 // where W is read twice and dW written).
-// dz is rounded to bf16, as the matrix instructions take it: dx and dW are 0.0024 off in the mean, against
-// 0.0017 of a bf16 output's own rounding, where every token has a gradient of its own, and as near as the
-// rounding of the mean's and of few tokens' (Plan::two).
+// dz is rounded to bf16, as the matrix instructions take it; what of it is a token's, and not its words', stays
+// out of that where it can (above, Plan::two and Plan::fold): dx is off by 0.0017 of its norm, a bf16
+// output's own rounding, dW by that for a mean and for few tokens, and by 0.0024 for gradients of the tokens' own.
 #include <algorithm>
 #include <cmath>
 
@@ -52,6 +52,11 @@ struct RowArgs {
   int* pos;            // [N] row of a token among those that count, or -1
   int* off;            // {0, tokens that count, 0, twice them}
   int two;             // backward: a token's row is copied twice, in any case
+  int fold;            // backward: the gradients dloss go into xs and factor (Plan::fold)
+  const void* w;       // (fold)
+  float z2;
+  void* xs;
+  float* factor;       // of a row of dx, by row
   int* row_label;      // the rest by row
   float* row_lse;      // backward
   float* coef;
@@ -88,6 +93,8 @@ template <bool BWD, int R>
 __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
   __shared__ int buf[4];
   __shared__ int row[R];
+  __shared__ int word[BWD ? R : 1];
+  __shared__ float2 given[BWD ? R : 1];  // lse and dloss
   const int t0 = blockIdx.x * R;
   // tokens that count before this block's, and all of them
   int before = 0, total = 0;
@@ -122,7 +129,10 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
       if constexpr (BWD) {
         a.row_lse[p] = a.lse[t];
         // (a label that is no word of the vocabulary makes what it enters NaN)
-        a.coef[p] = y < a.V ? (a.dloss ? a.dloss[t] : 1.0f) : NAN;
+        const float g = a.dloss ? a.dloss[t] : 1.0f;
+        if (!a.fold) a.coef[p] = y < a.V ? g : NAN;
+        word[threadIdx.x] = y;
+        given[threadIdx.x] = float2{a.lse[t], g};
       }
     }
     if (blockIdx.x == 0 && threadIdx.x < 4)
@@ -132,13 +142,51 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
     *a.out = a.dloss ? a.scale : total ? a.scale / (float)total : 0.0f;
   if (BWD && blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.n_counters; i += 256) a.counters[i] = 0;
-  if (total == a.N && !a.two) return;  // x itself is read
+  if (total == a.N && !a.two && !a.fold) return;  // x itself is read
   __syncthreads();
   // 256 / R threads to a row, so that all rows' loads are in flight
   const int chunks = a.d * a.size / 16;
   const int r = threadIdx.x / (256 / R), p = row[r];
   if (p < 0) return;
   const u32x4_t* src = static_cast<const u32x4_t*>(a.x) + (size_t)(t0 + r) * chunks;
+  if constexpr (BWD) {
+    if (a.fold) {
+      // the label's entry of dz, but for the gradient: q = (1 + 2 z_coef lse) exp(z - lse) - 1
+      const int y = word[r];
+      const float lse = given[r].x, g = given[r].y;
+      const bf16_t* x = static_cast<const bf16_t*>(a.x) + (size_t)(t0 + r) * a.d;
+      const bf16_t* w = static_cast<const bf16_t*>(a.w) + (size_t)(y < a.V ? y : 0) * a.d;
+      float dot = 0.0f;
+#pragma unroll 2
+      for (int c = threadIdx.x % (256 / R); c < chunks; c += 256 / R) {
+        float u[8], v[8];
+        load16_f32(x + 8 * c, u);
+        load16_f32(w + 8 * c, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot += u[e] * v[e];
+      }
+#pragma unroll
+      for (int o = 128 / R; o > 0; o >>= 1) dot += __shfl_xor(dot, o, 64);
+      float q = (1.0f + a.z2 * lse) * expf(a.scale * dot - lse) - 1.0f;
+      if (!(fabsf(q) >= 0x1p-8f && fabsf(q) <= 0x1p8f)) q = 1.0f;  // (any factor is right)
+      if (threadIdx.x % (256 / R) == 0) {
+        a.coef[p] = y < a.V ? 1.0f / q : NAN;
+        a.factor[p] = g * q;
+      }
+      bf16_t* xs = static_cast<bf16_t*>(a.xs) + (size_t)p * a.d;
+      bf16_t* xc = static_cast<bf16_t*>(a.xc) + (size_t)p * a.d;
+#pragma unroll 2
+      for (int c = threadIdx.x % (256 / R); c < chunks; c += 256 / R) {
+        float u[8];
+        load16_f32(x + 8 * c, u);
+        if (total < a.N) store16_f32(xc + 8 * c, u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] *= g * q;
+        store16_f32(xs + 8 * c, u);
+      }
+      return;
+    }
+  }
   u32x4_t* dst = static_cast<u32x4_t*>(a.xc) + (size_t)(a.two ? 2 * p : p) * chunks;
   u32x4_t* again = dst + (a.two ? chunks : 0);
 #pragma unroll 4
@@ -235,7 +283,8 @@ __global__ __launch_bounds__(256) void xent_clear_kernel(u32x4_t* p, size_t n) {
 // 768, 192 partials 8 us, with eight 5).
 template <class E, int SH, bool TWO>
 __global__ __launch_bounds__(256) void xent_dx_kernel(E* dx, const int* pos, const float* part, size_t stride,
-                                                      int S, int N, int d, const float* out) {
+                                                      int S, int N, int d, const float* out,
+                                                      const float* factor) {
   constexpr int V = Vec16<E>::N, AT = 256 / SH;
   __shared__ float sum[SH > 1 ? SH : 1][SH > 1 ? AT : 1][V + 4];
   const int chunks = d / V, sh = threadIdx.x / AT, l = threadIdx.x % AT;
@@ -270,7 +319,7 @@ __global__ __launch_bounds__(256) void xent_dx_kernel(E* dx, const int* pos, con
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] += sum[k][l][j];
     }
-    const float f = *out;
+    const float f = *out * (factor && p >= 0 ? factor[p] : 1.0f);
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] *= f;
     if (i < n) store16_f32(dx + (size_t)t * d + c, v);
@@ -292,6 +341,11 @@ struct Plan {
   // output's own rounding).  A k-step of 64 rows of dW holds both: 5 tokens of d = 768 take as long, 32 of 1024 4 %
   // and 24 of 2048 7 % longer, but 64 tokens of d = 2048 14 %, 128 30 %.
   bool two;
+  // bf16, more tokens than that, each with a gradient g of its own: dz is left without g and with 1 in its
+  // label's entry, q, the rest of which goes with g into the rows of x for dW (rounded once) and of dx (in
+  // fp32).  In dz, which is rounded, g q is off alike in all products of the token that matter: dx by 1.45
+  // times a bf16 output's own rounding (now 1.0), dW by 1.43 to 1.50 times it (now 1.41).
+  bool fold;
   int parts;           // partials of a row, at most
 };
 
@@ -372,6 +426,7 @@ Plan plan_of(const moe_xent& x, bool bwd) {
   if (!bwd) return p;
   p.two = bf16 && x.N <= kTwo;
   if (p.two && p.logits == TILE_256x256) p.logits = TILE_64x128;  // (which write both)
+  p.fold = bf16 && !p.two && x.dloss;
   dx.cap = dw.cap = p.two ? 2 * x.N : x.N;
   // Parts of K of dx: its few tiles reduce over the whole piece, so they are cut until they are three
   // quarters of the CUs; 256 columns a part at least.  Measured (us of the backward by parts): 512 tokens,
@@ -459,6 +514,11 @@ Buffers buffers(const moe_xent& x, const Plan& p, bool bwd, void* ws) {
     r.row_lse = w.take<float>(N);
     r.coef = w.take<float>(N);
     r.out = w.take<float>(1);
+    if (x.dtype == MOE_BF16 && !p.two) {  // (whether dloss is given or not: sizes do not depend on it)
+      r.xs = w.take<char>(N * x.d * s);
+      r.factor = w.take<float>(N);
+    }
+    r.fold = p.fold; r.w = x.w; r.z2 = 2.0f * x.z_coef;
     b.dz = w.take<char>(M * p.piece * s);
     b.dx_part = w.take<float>((size_t)p.split * M * x.d);
     r.n_counters = ceil_div(x.V, p.piece) * kXcdCounters;
@@ -579,6 +639,7 @@ hipError_t launch_xent_bwd(const moe_xent* x, hipStream_t s) {
     dx.accumulate = v0 > 0;
     dw.A = b.dz; dw.lda = ld;
     dw.B = b.row.xc; dw.ldb = x->d;
+    if (p.fold) dw.B = dw.xe.x_all = b.row.xs;
     dw.C = static_cast<char*>(x->dw) + (size_t)v0 * x->d * ws; dw.ldc = x->d;
     dw.M = ld; dw.N = x->d;
     dw.accumulate = x->accumulate_dw;
@@ -599,7 +660,8 @@ hipError_t launch_xent_bwd(const moe_xent* x, hipStream_t s) {
   const size_t stride = (size_t)x->N * x->d * (p.two ? 2 : 1);
 #define XENT_DX(E_, SH_, TWO_)                                                 \
   MOE_TIMED("xent_dx", s, xent_dx_kernel<E_, SH_, TWO_><<<blocks, 256, 0, s>>>( \
-      static_cast<E_*>(x->dx), b.row.pos, b.dx_part, stride, p.split, x->N, x->d, b.row.out))
+      static_cast<E_*>(x->dx), b.row.pos, b.dx_part, stride, p.split, x->N, x->d, b.row.out, \
+      p.fold ? b.row.factor : nullptr))
   if (p.two) XENT_DX(bf16_t, 8, true);
   else if (bf16 && share) XENT_DX(bf16_t, 8, false);
   else if (bf16) XENT_DX(bf16_t, 1, false);

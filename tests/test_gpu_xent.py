@@ -6,7 +6,8 @@ instructions choose: off by at most (d + 1) u sum |x w|, and by 2 u |z| of the s
 Exponentials have about one ulp (2 u) and the rounding of their argument (4 u |z - lse|); a row's sum
 passes at most 64 additions in a lane, 2 across lanes, P / 16 partials of a thread and 16 of the
 threads (each with two exponentials), P pieces of at least 32 columns.  The backward is held to the
-forward's own lse; dz is rounded by h (bf16, up to 32 tokens: its two values leave h^2), sums over n terms have n u of the magnitudes.
+forward's own lse; dz is rounded by h (bf16, up to 32 tokens: its two values leave h^2; more, with gradients of
+their own: x with them by h too), sums over n terms have n u of the magnitudes.
 """
 import math
 
@@ -91,6 +92,7 @@ def check_backward(L, t, scale, z_coef, dloss, add=0.0):
     # the relative error of p, the few products' and the difference's, then dz's own rounding
     e = cf.abs() * (zf * p).abs() * (ze + 4 * U * (z - lse).abs().clamp(max=200) + 10 * U) + 6 * U * cf.abs() * one
     hz = 2 * U if L.dtype != torch.bfloat16 else h * h if N <= 32 else h
+    e = e + 6 * U * dz.abs()  # the factors that dz is taken out of and put back into: three products each
     e = e + hz * dz.abs() + 3 * U * dz.abs() + 1e-37
     x, w = t["x"].double(), t["w"].double()
     dx = dz @ w
@@ -98,7 +100,9 @@ def check_backward(L, t, scale, z_coef, dloss, add=0.0):
     check("dx", L.dx, dx, (tol + h * dx.abs()) * (1 + 2 * h) + 1e-37)
     xk = torch.where(keep[:, None], x, 0.0)
     dw = dz.T @ xk + add
-    tol = e.T @ xk.abs() + (N + 8) * U * (dz.abs().T @ xk.abs()) + 2 * U * abs(add)
+    # (bf16, more than 32 tokens, gradients given: x comes with them, rounded by h beside dz)
+    hx = h * (1 + h) if L.dtype == torch.bfloat16 and N > 32 and dloss is not None else 0.0
+    tol = e.T @ xk.abs() + ((N + 8) * U + hx) * (dz.abs().T @ xk.abs()) + 2 * U * abs(add)
     check("dw", L.dw, dw, (tol + half(L.dw_dtype) * dw.abs()) * (1 + 2 * h) + 1e-37)
     assert (L.dx[~keep] == 0).all()
 
