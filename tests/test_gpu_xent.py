@@ -295,6 +295,82 @@ def test_xent_on_a_stream_and_in_a_graph(gpu_lib):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,d,V,lean", [(20, 64, 300, 30.0), (300, 128, 700, 6.0), (300, 128, 700, 40.0),
+                                        (1300, 512, 4000, 12.0)])
+def test_gradients_of_uneven_size(gpu_lib, dtype, N, d, V, lean):
+    """Gradients from 1e-20 to 1e10, zeros, and no number where a token does not count; tokens that are
+    nearly sure of their label, some of them of a probability that rounds to one."""
+    t = inputs(N, d, V, dtype, 12, 0.2)
+    y = t["labels"].long()
+    lean = lean * torch.rand(N, 1, device="cuda")
+    t["x"] = (t["x"].float() + lean * t["w"][y.clamp(min=0)].float()).to(DT[dtype])
+    g = torch.randn(N, device="cuda") * 10.0 ** torch.linspace(-20, 10, N, device="cuda")
+    g[::7] = 0.0
+    g[y < 0] = float("nan")
+    for scale, z_coef in ((1.0, 0.0), (1.5, 1e-2)):
+        L = LinearCrossEntropy(N, d, V, dtype=DT[dtype], scale=scale, z_coef=z_coef)
+        L.forward(t["x"], t["w"], t["labels"])
+        L.backward(t["x"], t["w"], t["labels"], dloss=g)
+        check_backward(L, t, scale, z_coef, torch.where(y < 0, 0.0, g))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N", [20, 300])
+def test_given_gradients_in_a_graph(gpu_lib, N):
+    """A captured backward with other gradients, tokens and labels at each replay."""
+    d, V = 128, 900
+    sets = [inputs(N, d, V, "bf16", s, p) for s, p in ((1, 0), (2, 0.4), (3, 0))]
+    w, L = sets[0]["w"], LinearCrossEntropy(N, d, V)
+
+    def both(t):
+        L.forward(t["x"], w, t["labels"])
+        L.backward(t["x"], w, t["labels"], dloss=t["dloss"])
+
+    def outs():
+        torch.cuda.synchronize()
+        return [v.clone() for v in (L.loss, L.total, L.dx, L.dw)]
+
+    refs = []
+    for t in sets:
+        both(t)
+        refs.append(outs())
+    live = {k: sets[0][k].clone() for k in ("x", "labels", "dloss")}
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both(live)
+    for i in (1, 0, 2, 1):
+        for k in live:
+            live[k].copy_(sets[i][k])
+        g.replay()
+        assert all(torch.equal(a, b) for a, b in zip(outs(), refs[i])), i
+        both(sets[2 - i])
+        assert all(torch.equal(a, b) for a, b in zip(outs(), refs[2 - i])), i
+
+
+@pytest.mark.gpu
+def test_two_heads_at_once(gpu_lib):
+    """Two objects on two streams, their launches beside each other."""
+    N, d, V = 700, 256, 3000
+    sets = [inputs(N, d, V, "bf16", s, 0.2) for s in (1, 2)]
+    heads = [LinearCrossEntropy(N, d, V) for _ in sets]
+    outs = lambda: [v.clone() for L in heads for v in (L.loss, L.lse, L.total, L.dx, L.dw)]
+    for L, t in zip(heads, sets):
+        L.forward(t["x"], t["w"], t["labels"])
+        L.backward(t["x"], t["w"], t["labels"])
+    torch.cuda.synchronize()
+    ref, streams = outs(), [torch.cuda.Stream() for _ in sets]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(4):
+        for call in ("forward", "backward"):
+            for L, t, s in zip(heads, sets, streams):
+                getattr(L, call)(t["x"], t["w"], t["labels"], stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs(), ref))
+
+
+@pytest.mark.gpu
 def test_xent_gradients_against_differences(gpu_lib):
     """<dx, ex> + <dw, ew> against a central difference in 64 bits of the weighted losses."""
     N, d, V, scale, zc = 9, 64, 70, 0.7, 0.02
