@@ -38,7 +38,7 @@ namespace {
 constexpr int kCountRows = 1024;  // tokens of a counting block
 constexpr int kDirect = 8192;     // up to here every block counts all labels itself
 constexpr int kLossThreads = 1024;
-constexpr int kFew = 128;         // up to here the forward leaves out no row
+constexpr int kFew = 256;         // up to here, a large tile's rows, the forward leaves out none
 constexpr int kTwo = 32;          // up to here the backward keeps dz in two values (Plan::two)
 
 struct RowArgs {
@@ -579,8 +579,8 @@ hipError_t launch_xent_fwd(const moe_xent* x, hipStream_t s) {
     MOE_TIMED("xent_none", s, xent_none_kernel<<<1, 64, 0, s>>>(x->total));
     return hipGetLastError();
   }
-  // Few tokens: every row as it is (rows are independent here, and the weights' stream sets the time: 24
-  // tokens 55 -> 51 us)
+  // Few tokens: every row as it is (rows are independent here, and leaving some out saves no tile of 256 or
+  // little of W's stream: 24 tokens 55 -> 51 us, 256 of d = 2048 65 -> 62, half of them left out or none)
   const bool as_is = x->N <= kFew;
   if (!as_is && (e = rows<false>(b, s)) != hipSuccess) return e;
   const int width = tile_cols(p.logits) / 2;  // of a partial: half a tile's columns

@@ -185,7 +185,7 @@ def test_xent_adds_to_dw(gpu_lib, dtype, low):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("N", [20, 200])
+@pytest.mark.parametrize("N", [20, 200, 300])
 def test_what_does_not_count_enters_nothing(gpu_lib, dtype, N):
     """Infinities and NaN in rows of tokens that do not count; their outputs are zeros."""
     t = inputs(N, 128, 300, dtype, 4, 0.5)
@@ -204,7 +204,7 @@ def test_what_does_not_count_enters_nothing(gpu_lib, dtype, N):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("N", [20, 200])
+@pytest.mark.parametrize("N", [20, 200, 300])
 def test_a_label_that_is_no_word(gpu_lib, N):
     """V and more: the loss is NaN, and what the token enters in the backward."""
     V = 300
