@@ -79,6 +79,10 @@ def parse():
     ap.add_argument("--clip", type=float, default=None, metavar="NORM",
                     help="with --optimizer: clip the step's gradients to this norm together (the "
                          "resident and the shared experts'), and update all of them by one call")
+    ap.add_argument("--head", type=int, default=None, metavar="WORDS",
+                    help="with --optimizer: the layer as a Peri-LN block under an output head of "
+                         "that many words; the loss's gradient takes the place of the drawn dy, "
+                         "and the head and the norms are updated with the experts")
     ap.add_argument("--placement", choices=["fixed", "random"], default="fixed",
                     help="with --optimizer: random placement (Alg. 1) redraws the worker's "
                          "resident set every --reshuffle-every rounds and migrates weights and "
@@ -230,6 +234,15 @@ def optimizer_work(n_step_params, n_round_params, n_peers):
             "replica_mean": ("byte", 4.0 * (n_peers + 2) * n_round_params)}
 
 
+def head_work(T, d, V):
+    """Per-step work of the block's norms and the head's loss: its products' flops (the backward
+    takes the logits again), the norms' bytes."""
+    out = {}
+    for name, products in (("gemm_xe_lse", 1), ("gemm_xe_dz", 1), ("gemm_xe_dx_dw", 2)):
+        out[name] = out[name + "_tile"] = ("flop", 2.0 * products * T * d * V)
+    return {**out, "block_norm_fwd": ("byte", 8.0 * T * d), "block_norm_bwd": ("byte", 10.0 * T * d)}
+
+
 def ghost_sweep(args):
     """Step time of the mid-size layer at 16, 12, 8 and 4 resident experts of
     16: skip-token (unpartitioned router, ghost routes skipped) and the
@@ -311,8 +324,8 @@ def main():
 
     from paper_2606_19025_amd import binding as B
     from paper_2606_19025_amd import inputs as I
-    from paper_2606_19025_amd.layer import ResidentMoELayer, expert_delta
-    from paper_2606_19025_amd.train import AdamW, GradClipper
+    from paper_2606_19025_amd.layer import BlockNorm, ResidentMoELayer, expert_delta
+    from paper_2606_19025_amd.train import AdamW, GradClipper, LinearCrossEntropy
 
     B.lib()
     wl = args.workload
@@ -324,6 +337,9 @@ def main():
     dt = torch.bfloat16 if cfg["dtype"] == "bf16" else torch.float32
     if args.clip is not None and not (args.optimizer and dt == torch.bfloat16):
         sys.exit("--clip needs --optimizer and a bf16 workload")
+    if args.head is not None and not (args.optimizer and dt == torch.bfloat16
+                                      and args.placement == "fixed" and args.head > 0):
+        sys.exit("--head needs --optimizer, a bf16 workload and --placement fixed")
     s_bytes = 2 if dt == torch.bfloat16 else 4
     dev = lambda a, t=dt: None if a is None else torch.from_numpy(
         np.ascontiguousarray(a, np.float32)).cuda().to(t)
@@ -389,6 +405,20 @@ def main():
         log(f"[bench] optimiser state: AdamW m, v and outer momentum of {n_params / 1e6:.1f} M "
             f"expert params" + (f" (+{(r1 + 1) * Hs * d / 1e6:.1f} M shared)" if Hs else ""))
 
+    head = None
+    if args.head is not None:
+        V, g = args.head, torch.Generator(device="cuda").manual_seed(args.seed)
+        f32 = lambda *shape, std=0.02, mean=0.0: torch.empty(*shape, device="cuda").normal_(
+            mean, std, generator=g)
+        master = f32(V, d)
+        head = dict(master=master, words=master.to(dt),
+                    labels=torch.randint(0, V, (T,), device="cuda", dtype=torch.int32, generator=g),
+                    norms=dict(post_weight=f32(d, mean=1.0), post_bias=f32(d), gate=f32(d, mean=1.0),
+                               pre_weight=f32(d, mean=1.0), pre_bias=f32(d)),
+                    block=BlockNorm(T, d, dtype=dt, gate="channel"),
+                    loss=LinearCrossEntropy(T, d, V, dtype=dt))
+        log(f"[bench] output head: {V} words, {V * d / 1e6:.1f} M params")
+
     def part_view(t, p):
         b, e, row = opt["rows"][p]
         return t[b:e].view(Er, row)
@@ -430,8 +460,8 @@ def main():
         o = opt
         o["t"] += 1
         lr = 3e-4
-        if args.clip is not None:
-            clipped_update(lr)
+        if args.clip is not None or head is not None:
+            update_together(lr)
         else:
             update(lr)
         if (i + 1) % args.round_every == 0:
@@ -442,8 +472,8 @@ def main():
             if args.placement == "random" and ((i + 1) // args.round_every) % args.reshuffle_every == 0:
                 reshuffle()
 
-    def clipped_update(lr):
-        """AdamW with the norm of all the step's gradients limited to --clip."""
+    def update_together(lr):
+        """AdamW on all tensors, the norm of all the step's gradients limited to --clip."""
         o = opt
         if args.placement == "random":  # (steps and rates by expert: the gradients are clipped in place)
             if "clipper" not in o:
@@ -457,13 +487,20 @@ def main():
             cut = lambda t, n: [t[:n], t[n:]]
             shared = lambda k: cut(o[k], n_sg) if Hs else []
             flat = lambda g: g.view(-1)
-            o["adamw"] = AdamW(
-                [o["gu"], o["down"]] + shared("s_master"),
-                [flat(L.dw_gate_up), flat(L.dw_down)]
-                + ([flat(L.s_dw_gate_up), flat(L.s_dw_down)] if Hs else []),
-                cut(o["m"], n_gu) + shared("s_m"), cut(o["v"], n_gu) + shared("s_v"),
-                theta_bf16=cut(o["lp"], n_gu) + shared("s_lp"),
-                max_norm=args.clip)
+            theta = [o["gu"], o["down"]] + shared("s_master")
+            grads = [flat(L.dw_gate_up), flat(L.dw_down)]
+            grads += [flat(L.s_dw_gate_up), flat(L.s_dw_down)] if Hs else []
+            low = cut(o["lp"], n_gu) + shared("s_lp")
+            if head is not None:
+                names = list(head["norms"])
+                more = [head["master"]] + [head["norms"][n] for n in names]
+                theta += more
+                grads += [head["loss"].dw] + [getattr(head["block"], "d_" + n) for n in names]
+                low += [head["words"]] + [None] * len(names)
+            zeros = lambda: [torch.zeros_like(t) for t in more] if head is not None else []
+            o["adamw"] = AdamW(theta, grads, cut(o["m"], n_gu) + shared("s_m") + zeros(),
+                               cut(o["v"], n_gu) + shared("s_v") + zeros(), theta_bf16=low,
+                               max_norm=args.clip)
         o["adamw"].step(o["t"], lr)
 
     def update(lr):
@@ -493,9 +530,17 @@ def main():
             B.moe_adamw_step(o["s_master"][n_sg:], L.s_dw_down, o["s_m"][n_sg:], o["s_v"][n_sg:],
                              Hs * d, o["t"], lr, theta_bf16=o["s_lp"][n_sg:])
 
+    def head_step():
+        """The block's norms, the head's loss and their backward: the gradient of the layer's y."""
+        h, w = head, head["norms"]
+        _, u = h["block"].forward(x, L.y, **w)
+        h["loss"].forward(u, h["words"], h["labels"])
+        du = h["loss"].backward(u, h["words"], h["labels"])
+        return h["block"].backward(du, L.y, w["post_weight"], w["post_bias"], w["gate"], w["pre_weight"])[1]
+
     def step(i):
         L.forward(x, wr, wgu, wd, bias, sgu, sd)
-        L.backward(dy, x, wr, wgu, wd, sgu, sd)
+        L.backward(dy if head is None else head_step(), x, wr, wgu, wd, sgu, sd)
         if opt is not None:
             optimizer_step(i)
         elif (i + 1) % args.round_every == 0:
@@ -567,7 +612,10 @@ def main():
         n_delta = args.steps // args.round_every
         work["expert_delta"] = ("byte", 4.0 * n_params * (3 + len(peers)))
         if opt is not None:
-            work.update(optimizer_work(n_params + (r1 + 1) * Hs * d, n_params, len(peers)))
+            n_head = (args.head or 0) * d
+            work.update(optimizer_work(n_params + (r1 + 1) * Hs * d + n_head, n_params, len(peers)))
+            if head is not None:
+                work.update(head_work(T, d, args.head))
             if args.placement == "random":
                 # bytes of the timed pass's migration copies, spread per step
                 work["copy_expert_rows"] = ("byte", opt["copy_bytes_timed"] / args.steps)
@@ -734,7 +782,8 @@ def main():
 
     out = {
         "metric": ("MoE layer training step (fwd+bwd+AdamW) tokens/s (1 GPU)" if opt is not None
-                   else "MoE layer fwd+bwd tokens/s (1 GPU)"),
+                   and head is None else "MoE block and head training step tokens/s (1 GPU)"
+                   if head is not None else "MoE layer fwd+bwd tokens/s (1 GPU)"),
         "value": round(value, 1),
         "unit": "tokens/s",
         "n_gpus": 1,
@@ -753,6 +802,7 @@ def main():
                    "optimizer": "adamw+outer-nesterov" if opt is not None else None,
                    "placement": args.placement if opt is not None else None,
                    **({"clip": args.clip} if opt is not None and args.clip is not None else {}),
+                   **({"head_words": args.head} if head is not None else {}),
                    "expert": args.expert},
         "roofline": roofline,
         "cpu_baseline": cpu,
