@@ -456,8 +456,8 @@ int moe_block_norm_bwd(const moe_block_norm* p, hipStream_t stream);
  *   loss[t] = lse[t] - z[t,labels[t]] + z_coef lse[t]^2
  *   total   = {sum_t loss[t], the number of tokens that count}
  * A token whose label is negative does not count: loss and lse are 0, its dx is 0, nothing of its
- * row of x is used, and its products are left out (forward, up to 256 tokens: made and dropped).  A label of V or more makes the loss NaN, and in
- * the backward its dx and dw.
+ * row of x is used, and its products are left out (forward, up to 256 tokens: made and dropped).
+ * A label of V or more makes the loss NaN, and in the backward its dx and dw.
  * x [N,d], w [V,d] dtype; labels [N] int32; loss, lse [N], total [2] fp32.
  *
  * moe_xent_bwd, from the forward's lse and the gradients dloss [N] of the losses (NULL: those of
