@@ -17,8 +17,8 @@
 // that four sums do for five gradients; a block keeps them in registers, stores one partial
 // row of 4 d and a second launch adds the partials in a fixed order.
 //
-// Measured (bf16, a gate per channel; second launch included): 8192 x 2048 forward 35 us, backward 48; 16384 x
-// 4096 120 and 155 us (4.5 and 5.2 TB/s); 8192 x 1024 16 and 31; fp32 8192 x 2048 55 and 80 (4.9, 5.0 TB/s).
+// Measured (bf16, a gate per channel; second launch included): 8192 x 2048 forward 29 us, backward 48; 16384 x
+// 4096 109 and 155 us (4.9 and 5.2 TB/s); 8192 x 1024 14 and 31; fp32 8192 x 2048 53 and 80 (5.1, 5.0 TB/s).
 #include "common.h"
 #include "kernels.h"
 #include "norm_rows.h"
@@ -99,15 +99,146 @@ DEVI void center(const BlockArgs& a, float (&v)[NV][R::VE], float (*buf)[W], int
   r = 1.0f / sqrtf(s[0] * a.inv_d + a.p.eps);
 }
 
-template <class E, int W, int NV>
-__global__ __launch_bounds__(64 * block_waves(W)) void block_norm_fwd_kernel(BlockArgs a) {
+// The lane's pieces of a row of `bytes` bytes at base -> LDS at dst + 1024 i + 16 lane (dst of the
+// wave's own, base wave-uniform); zeros past the row's end.  The asm sets m0 and leaves the one
+// wait state that an LDS DMA needs after it.
+template <int W, int NV>
+DEVI void dma_row(const void* base, int bytes, int wave, char* dst) {
+  const uint64_t b = (uint64_t)(uintptr_t)base;
+  const u32x4_t r = {(unsigned)__builtin_amdgcn_readfirstlane((unsigned)b),
+                     (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(b >> 32) & 0xFFFFu),
+                     (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00020000u};
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const unsigned off = (unsigned)(((i * W + wave) * 64 + (int)(threadIdx.x & 63)) * 16);
+    const unsigned m0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void_t*)(dst + i * 1024));
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(r), "s"(m0)
+                 : "m0", "memory");
+  }
+}
+
+// Waves of a block: kBlockWaves / W groups of W waves take a row each.
+constexpr int kBlockWaves = 8;
+constexpr int row_block_waves(int W) { return W > kBlockWaves ? W : kBlockWaves; }
+
+// Rows of up to 8 values a lane.  A block's groups of W waves take rows in turn, in step with each other; the
+// next rows' f and x come by DMA into LDS while these are worked on, each wave reading what its own lanes
+// asked for, so that no barrier is needed for them.  Weights stay in registers.  Three blocks of eight waves
+// a CU (two or four: 4096 x 2048 15.4 or 15.5 us and not 14.4, 20000 x 2056 91 or 87 and not 80; 8192 x 2048
+// 28.9 or 31 and 29.5), one of sixteen (4096 x 8192 56 us, with two 60).  64 registers for four spill: 60 us
+// at 8192 x 2048.  Instead of this, a wave or a block for each row: 8192 x 2048 34 us, 16384 x 4096 118 (now
+// 109), 65536 x 256 46 (34); better at 9000 x 1032 alone, 21 (23), where half the lanes hold nothing.
+// PRE, POST: the norms that there are.
+template <class E, int W, int NV, bool PRE, bool POST>
+__global__ __launch_bounds__(64 * row_block_waves(W), 4) void block_norm_fwd_kernel(BlockArgs a) {
   using R = Row<E, W, NV>;
-  constexpr int VE = R::VE;
+  constexpr int VE = R::VE, BW = row_block_waves(W), GROUPS = BW / W, WAVE = 2 * NV * 1024;
+  constexpr int STORES = NV * (1 + PRE), STATS = 2 * (PRE + POST);
+  __shared__ __attribute__((aligned(16))) char ring[2][BW][WAVE];
+  __shared__ float buf[GROUPS][2][W];
+  const moe_block_norm& p = a.p;
+  const bool channel = p.gate_kind == MOE_BLOCK_GATE_CHANNEL;
+  const bool token = p.gate_kind == MOE_BLOCK_GATE_TOKEN;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int group = wave / W, wr = wave % W;
+  const int step = gridDim.x * GROUPS;
+  const bool full = ((NV - 1) * W + wr) * 64 * VE < p.d;  // the wave's every vector holds values of the row
+  float wpre[NV][VE], bpre[NV][VE], wpost[NV][VE], bpost[NV][VE], g[NV][VE];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      wpre[i][j] = bpre[i][j] = wpost[i][j] = bpost[i][j] = 0.f;
+      g[i][j] = 1.f;
+    }
+    if (R::col(i) < p.d) {
+      if (PRE) R::load_f32(p.pre_weight, R::col(i), wpre[i]);
+      if (PRE && p.pre_bias) R::load_f32(p.pre_bias, R::col(i), bpre[i]);
+      if (POST) R::load_f32(p.post_weight, R::col(i), wpost[i]);
+      if (POST && p.post_bias) R::load_f32(p.post_bias, R::col(i), bpost[i]);
+      if (channel) R::load_f32(p.gate, R::col(i), g[i]);
+    }
+  }
+  const int bytes = p.d * (int)sizeof(E);
+  float ng = 1.f;
+  auto fetch = [&](int t, char* dst) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (what was there has been read)
+    const int n = t < p.T ? bytes : 0;
+    const size_t at = t < p.T ? (size_t)t * p.d : 0;
+    dma_row<W, NV>(static_cast<const E*>(p.f) + at, n, wr, dst);
+    dma_row<W, NV>(static_cast<const E*>(p.x) + at, n, wr, dst + NV * 1024);
+    if (token) ng = p.gate[min(t, p.T - 1)];
+  };
+  auto read = [&](const char* src, int k, int i, float* out) {
+    R::unpack(*reinterpret_cast<const u32x4_t*>(src + (k * NV + i) * 1024 + lane * 16), out);
+  };
+  int flip = 0, cur = 0;
+  float (*sums)[W] = buf[group];
+  const int first = blockIdx.x * GROUPS;
+  if (first < p.T) fetch(first + group, ring[0][wave]);
+  for (int t0 = first; t0 < p.T; t0 += step) {  // (as often in all waves)
+    const int t = t0 + group;
+    const bool there = t < p.T;
+    // These rows have landed: memory operations of a wave end in order, and the last rows' stores (none
+    // of vectors past the row's end, statistics of a group's first wave alone) are newer.
+    if (!full) asm volatile("s_waitcnt vmcnt(0)" : "+v"(ng)::"memory");
+    else if (wr == 0) asm volatile("s_waitcnt vmcnt(%1)" : "+v"(ng) : "n"(STORES + STATS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%1)" : "+v"(ng) : "n"(STORES) : "memory");
+    if (t0 == first) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (no stores yet)
+    const float ag = p.scale * ng;
+    const char* src = ring[cur][wave];
+    cur ^= 1;
+    if (t0 + step < p.T) fetch(t + step, ring[cur][wave]);
+    float n[NV][VE], mu, r = 1.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) read(src, 0, i, n[i]);
+    if constexpr (POST) {
+      center<R, W, NV>(a, n, sums, flip, mu, r);
+      if (there && wr == 0 && lane == 0) {
+        p.post_mean[t] = mu;
+        p.post_rstd[t] = r;
+      }
+    }
+    E* xo = static_cast<E*>(p.x_out) + (size_t)t * p.d;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float x[VE];
+      read(src, 1, i, x);
+      const bool in = R::col(i) < p.d;
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        // (past the row's end x' is a zero)
+        const float v = POST ? n[i][j] * r * wpost[i][j] + bpost[i][j] : n[i][j];
+        n[i][j] = in ? (float)from_f32<E>(x[j] + ag * (v * g[i][j])) : 0.f;
+      }
+      if (there && in) store16_f32(xo + R::col(i), n[i]);
+    }
+    if constexpr (PRE) {
+      center<R, W, NV>(a, n, sums, flip, mu, r);
+      if (there && wr == 0 && lane == 0) {
+        p.pre_mean[t] = mu;
+        p.pre_rstd[t] = r;
+      }
+      E* u = static_cast<E*>(p.u) + (size_t)t * p.d;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+#pragma unroll
+        for (int j = 0; j < VE; ++j) n[i][j] = n[i][j] * r * wpre[i][j] + bpre[i][j];
+        if (there && R::col(i) < p.d) store16_f32(u + R::col(i), n[i]);
+      }
+    }
+  }
+}
+
+// Wide rows, 16 values a lane of a block of sixteen waves for each row.
+template <class E>
+__global__ __launch_bounds__(1024) void block_norm_fwd_wide_kernel(BlockArgs a) {
+  constexpr int W = 16, VE = Vec16<E>::N, NV = 16 / VE;
+  using R = Row<E, W, NV>;
   __shared__ float buf[2][W];
   const moe_block_norm& p = a.p;
-  const int t = blockIdx.x * (block_waves(W) / W) + (int)threadIdx.x / R::TPR;
-  if (W == 1 && t >= p.T) return;  // (W > 1: the grid has one block per row)
-  const bool first = threadIdx.x % R::TPR == 0;
+  const int t = blockIdx.x;
+  const bool first = threadIdx.x == 0;
   u32x4_t rf[NV], rx[NV];
   R::load(p.f, t, p.d, rf);
   R::load(p.x, t, p.d, rx);
@@ -166,41 +297,17 @@ __global__ __launch_bounds__(64 * block_waves(W)) void block_norm_fwd_kernel(Blo
   }
 }
 
-// The lane's pieces of a row of `bytes` bytes at base -> LDS at dst + 1024 i + 16 lane (dst of the
-// wave's own, base wave-uniform); zeros past the row's end.  The asm sets m0 and leaves the one
-// wait state that an LDS DMA needs after it.
-template <int W, int NV>
-DEVI void dma_row(const void* base, int bytes, int wave, char* dst) {
-  const uint64_t b = (uint64_t)(uintptr_t)base;
-  const u32x4_t r = {(unsigned)__builtin_amdgcn_readfirstlane((unsigned)b),
-                     (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(b >> 32) & 0xFFFFu),
-                     (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00020000u};
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const unsigned off = (unsigned)(((i * W + wave) * 64 + (int)(threadIdx.x & 63)) * 16);
-    const unsigned m0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void_t*)(dst + i * 1024));
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(r), "s"(m0)
-                 : "m0", "memory");
-  }
-}
-
-// Waves of a block of the backward: kBwdWaves / W groups of W waves take a row each.
-constexpr int kBwdWaves = 8;
-constexpr int bwd_waves(int W) { return W > kBwdWaves ? W : kBwdWaves; }
-
-// Rows of up to 8 values a lane.  A block's groups take rows in turn, in step with each other; the
-// next rows' arrays come by DMA into LDS while this one's are worked on (16 KB of bf16 a row of 2048,
-// no registers), each wave reading what its own lanes asked for, so that no barrier is needed for
-// them (where LDS holds one round alone, fp32 rows past 4096: once it has been read).  Weights stay in
+// Rows of up to 8 values a lane, backward.  A block's groups take rows as in the forward; the
+// next rows' arrays come by DMA into LDS (16 KB of bf16 a row of 2048, no registers; where LDS holds one round alone, fp32 rows past 4096: once it has been read).  Weights stay in
 // registers: a load of them in the loop would wait for the DMA before it.
 // One block a CU (a second one's partial rows cost more than it hides: 8192 x 2048 48 -> 55 us).
 // Instead of this, a block of four waves for each row, the next one's loads in registers: 8192 x 2048 58
 // us, 16384 x 4096 188 (now 155).
 // PRE, POST: the norms that there are.
 template <class E, int W, int NV, bool PRE, bool POST>
-__global__ __launch_bounds__(64 * bwd_waves(W), 4) void block_norm_bwd_kernel(BlockArgs a) {
+__global__ __launch_bounds__(64 * row_block_waves(W), 4) void block_norm_bwd_kernel(BlockArgs a) {
   using R = Row<E, W, NV>;
-  constexpr int VE = R::VE, BW = bwd_waves(W), GROUPS = BW / W, WAVE = 4 * NV * 1024;
+  constexpr int VE = R::VE, BW = row_block_waves(W), GROUPS = BW / W, WAVE = 4 * NV * 1024;
   constexpr int DEPTH = BW * WAVE > 65536 ? 1 : 2;
   __shared__ __attribute__((aligned(16))) char ring[DEPTH][BW][WAVE];
   __shared__ float buf[GROUPS][6][W];
@@ -261,7 +368,7 @@ __global__ __launch_bounds__(64 * bwd_waves(W), 4) void block_norm_bwd_kernel(Bl
   for (int t0 = first; t0 < p.T; t0 += step) {  // (the same rounds in all waves)
     const int t = t0 + group;
     const bool there = t < p.T;
-    // This round's arrays have landed: memory operations of a wave end in order, and the last round's 2 NV
+    // These rows have landed: memory operations of a wave end in order, and the last rows' 2 NV
     // stores (none of vectors past the row's end) and at least one statistic are newer.
     if (!full) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("s_waitcnt vmcnt(%5)"
@@ -333,7 +440,7 @@ __global__ __launch_bounds__(64 * bwd_waves(W), 4) void block_norm_bwd_kernel(Bl
         }
       }
     }
-    if (DEPTH == 1 && t0 + step < p.T) fetch(t + step, ring[0][wave]);  // (all of this round's is read)
+    if (DEPTH == 1 && t0 + step < p.T) fetch(t + step, ring[0][wave]);  // (all of these rows is read)
     // (two buffers in turn: the pre-norm's sums took the first)
     if (token) all_sums<W>(q, sums, flip);
     else if (POST) all_sums<W>(reinterpret_cast<float (&)[2]>(q), sums, flip);
@@ -585,63 +692,46 @@ __global__ __launch_bounds__(16 * kDwShares) void block_norm_dw_kernel(BlockArgs
   }
 }
 
-// Waves per row.  Forward: one where the rows are many and a lane then holds at most four vectors, else
-// so many that it holds 8 values, or sixteen.  Measured (us, 1 / 4 / 8 / 16 waves): bf16 8192 x 1024 16 /
-// 18 / 26 / 46, 8192 x 2048 35 / 36 / 38 / 58, 16384 x 4096 - / 142 / 122 / 147, 4096 x 8192 - / 72 / 64 /
-// 64; fp32 8192 x 512 13 / 17 / 24 / 45, 8192 x 2048 - / 55 / 55 / 70.
-int waves_fwd(int T, int d, int ve) {
-  if (T >= 4096 && vectors(d, ve, 1) <= 4) return 1;
-  for (int W : {4, 8})
-    if (vectors(d, ve, W) * ve <= 8) return W;
-  return 16;
-}
-// Backward: the fewest with a vector in each lane (more rows in a block, and fewer barriers between waves),
-// two of fp32 past sixteen waves' reach; 32: the wide kernel.
-int waves_bwd(int d, int ve) {
+// Waves per row: the fewest with a vector in each lane (more rows in a block, and fewer barriers between
+// waves), two of fp32 past sixteen waves' reach; 32: the wide kernels.
+int row_waves(int d, int ve) {
   for (int W : {1, 2, 4, 8, 16})
     if (vectors(d, ve, W) <= 1) return W;
   return vectors(d, ve, 16) * ve <= 8 ? 16 : 32;
 }
 
 int blocks_bwd(int T, int d, int ve) {
-  const int W = waves_bwd(d, ve), rows = W > 16 ? 1 : bwd_waves(W) / W;
+  const int W = row_waves(d, ve), rows = W > 16 ? 1 : row_block_waves(W) / W;
   return std::min(ceil_div(T, rows), num_cus());
 }
 
-template <class E>
-void fwd_rows(const BlockArgs& a, int W, hipStream_t s) {
+template <class E, bool PRE, bool POST>
+void fwd(const BlockArgs& a, int W, hipStream_t s) {
   constexpr int VE = Vec16<E>::N;
-  const int nv = vectors(a.p.d, VE, W);
-#define BLOCK_FWD(W_, NV_)                                                                \
-  MOE_TIMED("block_norm_fwd", s, block_norm_fwd_kernel<E, W_, NV_>                        \
-            <<<ceil_div(a.p.T, block_waves(W_) / W_), 64 * block_waves(W_), 0, s>>>(a))
-  if (W == 1) {
-    if (nv == 1) BLOCK_FWD(1, 1);
-    else if (nv == 2) BLOCK_FWD(1, 2);
-    else BLOCK_FWD(1, 4);
-  } else if (W == 4) {
-    if (nv == 1) BLOCK_FWD(4, 1);
-    else if constexpr (VE == 4) BLOCK_FWD(4, 2);
-  } else if (W == 8) {
-    BLOCK_FWD(8, 8 / VE);
-  } else {
-    // (what eight waves do not reach)
-    if constexpr (VE == 8) {
-      if (nv == 1) BLOCK_FWD(16, 1);
-      else BLOCK_FWD(16, 2);
-    } else {
-      if (nv == 2) BLOCK_FWD(16, 2);
-      else BLOCK_FWD(16, 4);
-    }
-  }
+  const int blocks = std::min(ceil_div(a.p.T, row_block_waves(W) / W), (W == 16 ? 1 : 3) * num_cus());
+#define BLOCK_FWD(W_, NV_)                                                    \
+  MOE_TIMED("block_norm_fwd", s, block_norm_fwd_kernel<E, W_, NV_, PRE, POST> \
+            <<<blocks, 64 * row_block_waves(W_), 0, s>>>(a))
+  if (W == 1) BLOCK_FWD(1, 1);
+  else if (W == 2) BLOCK_FWD(2, 1);
+  else if (W == 4) BLOCK_FWD(4, 1);
+  else if (W == 8) BLOCK_FWD(8, 1);
+  else if (vectors(a.p.d, VE, 16) == 1) BLOCK_FWD(16, 1);
+  else if constexpr (VE == 4) BLOCK_FWD(16, 2);
 #undef BLOCK_FWD
 }
 
 template <class E>
 hipError_t fwd(const BlockArgs& a, hipStream_t s) {
   const moe_block_norm& p = a.p;
-  const int W = waves_fwd(p.T, p.d, Vec16<E>::N), most = rows_per_launch(W);
-  for (int t = 0; t < p.T; t += most) {
+  const int W = row_waves(p.d, Vec16<E>::N), most = rows_per_launch(16);
+  if (p.T > 0 && W <= 16) {
+    if (!p.pre_weight) fwd<E, false, true>(a, W, s);
+    else if (p.post_weight) fwd<E, true, true>(a, W, s);
+    else fwd<E, true, false>(a, W, s);
+    return hipGetLastError();
+  }
+  for (int t = 0; t < p.T; t += most) {  // (wide rows: a block each)
     BlockArgs part = a;
     moe_block_norm& q = part.p;
     const size_t at = (size_t)t * p.d;
@@ -653,7 +743,7 @@ hipError_t fwd(const BlockArgs& a, hipStream_t s) {
       if (*v) *v += t;
     if (p.gate && p.gate_kind == MOE_BLOCK_GATE_TOKEN) q.gate += t;
     q.T = std::min(p.T - t, most);
-    fwd_rows<E>(part, W, s);
+    MOE_TIMED("block_norm_fwd", s, block_norm_fwd_wide_kernel<E><<<q.T, 1024, 0, s>>>(part));
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -662,10 +752,10 @@ hipError_t fwd(const BlockArgs& a, hipStream_t s) {
 template <class E, bool PRE, bool POST>
 void bwd(const BlockArgs& a, int blocks, hipStream_t s) {
   constexpr int VE = Vec16<E>::N;
-  const int W = waves_bwd(a.p.d, VE);
+  const int W = row_waves(a.p.d, VE);
 #define BLOCK_BWD(W_, NV_)                                                    \
   MOE_TIMED("block_norm_bwd", s, block_norm_bwd_kernel<E, W_, NV_, PRE, POST> \
-            <<<blocks, 64 * bwd_waves(W_), 0, s>>>(a))
+            <<<blocks, 64 * row_block_waves(W_), 0, s>>>(a))
   if (W == 1) BLOCK_BWD(1, 1);
   else if (W == 2) BLOCK_BWD(2, 1);
   else if (W == 4) BLOCK_BWD(4, 1);

@@ -87,7 +87,7 @@ _SYMBOLS = [
     (r"copy_expert_rows_kernel", lambda m: "copy_expert_rows"),
     (r"mx_gemm_kernel(?:<|ILi)(\d)", lambda m: "mx_gemm_" + ("gu", "up", "down")[int(m.group(1))]),
     (r"few_logits_(?:bf16|f32)_kernel", lambda m: "few_logits"),
-    (r"block_norm_bwd_wide_kernel", lambda m: "block_norm_bwd"),
+    (r"(block_norm_[fb]wd)_wide_kernel", lambda m: m.group(1)),
     (r"(block_norm_fwd|block_norm_bwd|block_norm_dw|grad_norm_sum|grad_norm|grad_clip|adamw_steps|"
      r"xent_count|xent_rows|xent_loss|xent_none|xent_clear|xent_dx)_kernel",
      lambda m: m.group(1)),

@@ -15,7 +15,8 @@ from .test_gpu_norm import COLS, DT, SUM, U, check, check_forward, half
 
 # (T, d): one to sixteen waves a row, several rows for each; ragged widths; the ends of the ranges
 SHAPES = [(600, 4104), (300, 8208), (700, 600), (2100, 1024), (530, 2056), (1, 8), (1, 2048), (3, 520), (7, 4104), (2, 16384), (5, 8200), (1023, 72), (300, 1032),
-          (4099, 512), (4100, 264), (4096, 8), (1030, 4096), (3001, 520)]
+          (4099, 512), (4100, 264), (4096, 8), (1030, 4096), (3001, 520), (20001, 264), (13001, 520),
+          (9001, 1032), (3001, 2056), (2001, 4168)]
 # (post, pre, gate, bias)
 FORMS = [(True, True, None, True), (True, True, "channel", True), (True, True, "token", False),
          (False, True, "channel", False), (False, True, "token", True), (True, False, None, True),
