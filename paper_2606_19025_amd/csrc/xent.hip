@@ -429,13 +429,15 @@ Plan plan_of(const moe_xent& x, bool bwd) {
   p.fold = bf16 && !p.two && x.dloss;
   dx.cap = dw.cap = p.two ? 2 * x.N : x.N;
   // Parts of K of dx: its few tiles reduce over the whole piece, so they are cut until they are three
-  // quarters of the CUs; 256 columns a part at least.  Measured (us of the backward by parts): 512 tokens,
-  // d = 2048, 32768 words 1 698, 2 394, 4 253, 8 212, 14 212, 28 242; 1531 tokens, d = 768, 50003 words
-  // 1055, 590, 365, 283, 284, 309.
+  // quarters of the CUs (fp32, several of whose tiles share a CU: one and a half times them); 256 columns a
+  // part at least.  Measured (us of the backward by parts): 512 tokens, d = 2048, 32768 words 1 698, 2 394, 4
+  // 253, 8 212, 14 212, 28 242; 1531 tokens, d = 768, 50003 words 1055, 590, 365, 283, 284, 309; fp32, dx with
+  // dW of 1000 tokens, d = 256, 30000 words 473 at three quarters, 279, and 281 at three times the CUs.
   const double most = (double)(((size_t)256 << 20) / ((size_t)std::max(1, dx.cap) * x.d * 4));
   auto split_of = [&](TileSize t) {
     const double tiles = (double)ceil_div(dx.cap, tile_rows(t)) * ceil_div(x.d, tile_cols(t));
-    return (int)std::max(1.0, std::min({0.75 * num_cus() / std::max(tiles, 1.0), p.piece / 256.0, most}));
+    const double fill = (bf16 ? 0.75 : 1.5) * num_cus();
+    return (int)std::max(1.0, std::min({fill / std::max(tiles, 1.0), p.piece / 256.0, most}));
   };
   const size_t most_dz = std::max<size_t>(kPad, kDzBytes / (std::max(1, x.N) * s) / kPad * kPad);
   const int pieces = (int)((width + std::min(most_w, most_dz) - 1) / std::min(most_w, most_dz));
