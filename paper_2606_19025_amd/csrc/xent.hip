@@ -390,6 +390,17 @@ double ends(int cus, long na, double a, long nb, double b) {
   return std::max(best, found);
 }
 
+// Estimate (us) of dx, in `split` parts, with dW in fp32: the tiles' k-steps of 32 and their ends on the CUs.
+// Large tiles are taken where it is a tenth less for them, also with fewer of them than six a CU (400 tokens,
+// d = 1024, 8000 words 138 us against 152, 787 of 640 on 15290 285 against 306, and where it is not, 1500 of
+// 128 on 30000 226 against 215, 4000 of 512 on 5000 417 against 363).
+double f32_pair_us(const GemmArgs& dx, const GemmArgs& dw, TileSize t, int split) {
+  const double step = t == TILE_32x64 ? 0.33 : 1.05, end = t == TILE_32x64 ? 0.6 : 2.0;
+  const long cols = ceil_div(dx.N, tile_cols(t));
+  return ends(num_cus(), ceil_div(dx.cap, tile_rows(t)) * cols * split, ceil_div(dx.K, 32 * split) * step + end,
+              ceil_div(dw.M, tile_rows(t)) * cols, ceil_div(dw.cap, 32) * step + end);
+}
+
 // Estimate (us) of the backward in 256 x 256 tiles, by pieces of `piece` columns and `split` parts of K of
 // dx: rounds of the logits' tiles; the longest XCD of dx with dW, whose tiles are dealt by the XCD; the
 // partial sums' and, where dz leaves the last-level cache, its own traffic.  On eleven heads of 1500 to
@@ -450,6 +461,9 @@ Plan plan_of(const moe_xent& x, bool bwd) {
     p.pair = xent_pair_tiles(dx, dw, split);
   } else {
     p.pair = f32_tiles((double)ceil_div(x.d, 128) * (ceil_div(x.N, 64) + ceil_div(dw.M, 64)));
+    if (p.pair == TILE_32x64 && f32_pair_us(dx, dw, TILE_64x128, split_of(TILE_64x128)) <
+                                    0.9 * f32_pair_us(dx, dw, TILE_32x64, split_of(TILE_32x64)))
+      p.pair = TILE_64x128;
   }
   p.split = split_of(p.pair);
   if (p.pair != TILE_256x256 || p.logits != TILE_256x256) return p;
