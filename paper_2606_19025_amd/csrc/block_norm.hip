@@ -133,7 +133,6 @@ template <class E, int W, int NV, bool PRE, bool POST>
 __global__ __launch_bounds__(64 * row_block_waves(W), 4) void block_norm_fwd_kernel(BlockArgs a) {
   using R = Row<E, W, NV>;
   constexpr int VE = R::VE, BW = row_block_waves(W), GROUPS = BW / W, WAVE = 2 * NV * 1024;
-  constexpr int STORES = NV * (1 + PRE), STATS = 2 * (PRE + POST);
   __shared__ __attribute__((aligned(16))) char ring[2][BW][WAVE];
   __shared__ float buf[GROUPS][2][W];
   const moe_block_norm& p = a.p;
@@ -142,7 +141,6 @@ __global__ __launch_bounds__(64 * row_block_waves(W), 4) void block_norm_fwd_ker
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int group = wave / W, wr = wave % W;
   const int step = gridDim.x * GROUPS;
-  const bool full = ((NV - 1) * W + wr) * 64 * VE < p.d;  // the wave's every vector holds values of the row
   float wpre[NV][VE], bpre[NV][VE], wpost[NV][VE], bpost[NV][VE], g[NV][VE];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -179,12 +177,9 @@ __global__ __launch_bounds__(64 * row_block_waves(W), 4) void block_norm_fwd_ker
   for (int t0 = first; t0 < p.T; t0 += step) {  // (as often in all waves)
     const int t = t0 + group;
     const bool there = t < p.T;
-    // These rows have landed: memory operations of a wave end in order, and the last rows' stores (none
-    // of vectors past the row's end, statistics of a group's first wave alone) are newer.
-    if (!full) asm volatile("s_waitcnt vmcnt(0)" : "+v"(ng)::"memory");
-    else if (wr == 0) asm volatile("s_waitcnt vmcnt(%1)" : "+v"(ng) : "n"(STORES + STATS) : "memory");
-    else asm volatile("s_waitcnt vmcnt(%1)" : "+v"(ng) : "n"(STORES) : "memory");
-    if (t0 == first) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (no stores yet)
+    // These rows have landed (the last rows' stores too: the loads that the compiler tracks, of a token's gate,
+    // make it wait for all in any case, so no count of what is newer than the DMA would let them pass)
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(ng)::"memory");
     const float ag = p.scale * ng;
     const char* src = ring[cur][wave];
     cur ^= 1;
@@ -317,7 +312,6 @@ __global__ __launch_bounds__(64 * row_block_waves(W), 4) void block_norm_bwd_ker
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int group = wave / W, wr = wave % W;
   const int step = gridDim.x * GROUPS;
-  const bool full = ((NV - 1) * W + wr) * 64 * VE < p.d;  // the wave's every vector holds values of the row
   float s[kSums][NV][VE], wpre[NV][VE], wpost[NV][VE], bpost[NV][VE], g[NV][VE];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -368,13 +362,9 @@ __global__ __launch_bounds__(64 * row_block_waves(W), 4) void block_norm_bwd_ker
   for (int t0 = first; t0 < p.T; t0 += step) {  // (the same rounds in all waves)
     const int t = t0 + group;
     const bool there = t < p.T;
-    // These rows have landed: memory operations of a wave end in order, and the last rows' 2 NV
-    // stores (none of vectors past the row's end) and at least one statistic are newer.
-    if (!full) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    asm volatile("s_waitcnt vmcnt(%5)"
-                 : "+v"(nmx), "+v"(nrx), "+v"(nmf), "+v"(nrf), "+v"(ng)
-                 : "n"(2 * NV + 1)
-                 : "memory");
+    // These rows have landed, and their statistics: all that the wave has in flight, with the last rows' stores,
+    // as how many of them are newer than the DMA goes by the form, the ring's depth and the round
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(nmx), "+v"(nrx), "+v"(nmf), "+v"(nrf), "+v"(ng)::"memory");
     const float mx = nmx, rx = nrx, mf = nmf, rf = nrf, ag = p.scale * ng;
     const char* src = ring[cur][wave];
     if constexpr (DEPTH == 2) {
