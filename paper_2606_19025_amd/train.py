@@ -114,13 +114,9 @@ class LinearCrossEntropy:
         return self.dx
 
 
-class GradClipper:
-    """The norm of the given gradients together, and clipping by it: moe_grad_norm, moe_grad_clip.
-
-    grads: contiguous fp32 or bf16 tensors, read where they lie at every call (a layer's gradient
-    buffers).  max_norm: infinite measures alone.  out: where the clipped gradients go, tensors like
-    grads (None: in place).  ``norm`` holds the norm and the scale min(1, max_norm / norm) of the last
-    call, on the GPU; a norm that is not finite has the scale NaN and clips nothing."""
+class _GradNorm:
+    """The norm of the given gradients together, and the scale that limits it: moe_grad_norm.  One that
+    is given twice counts twice.  out: where a clipper writes (None: nowhere)."""
 
     def __init__(self, grads, max_norm, out=None):
         grads = list(grads)
@@ -128,21 +124,19 @@ class GradClipper:
         self.max_norm = float(max_norm)
         if not self.max_norm > 0:
             raise ValueError(f"max_norm must be positive, got {max_norm}")
-        out = grads if out is None else list(out)
-        if len(out) != len(grads):
+        if out is not None and len(out) != len(grads):
             raise ValueError(f"{len(out)} outputs for {len(grads)} gradients")
-        for i, (g, o) in enumerate(zip(grads, out)):
+        for i, g in enumerate(grads):
             if g.dtype not in (torch.float32, torch.bfloat16):
                 raise ValueError(f"gradient {i} has dtype {g.dtype}: float32 or bfloat16")
             _check_tensor(f"gradient {i}", g, g.shape, g.dtype, self.device, "clipper")
-            _check_tensor(f"output {i}", o, g.shape, g.dtype, self.device, "clipper")
-        _disjoint("outputs", out)
-        _apart("output", out, grads)
+            if out is not None:
+                _check_tensor(f"output {i}", out[i], g.shape, g.dtype, self.device, "clipper")
         self._held = grads, out  # (the library keeps addresses only)
         self.n = len(grads)
         self._grads = (B.moe_grad * self.n)(*[
-            B.moe_grad(g.data_ptr(), o.data_ptr(), g.numel(), B.dtype_code(g))
-            for g, o in zip(grads, out)])
+            B.moe_grad(g.data_ptr(), B._ptr(out and out[i]), g.numel(), B.dtype_code(g))
+            for i, g in enumerate(grads)])
         self.ws_bytes = B.moe_grad_norm_workspace_size(self._grads, self.n)
         self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
         self.norm = torch.empty(2, dtype=torch.float32, device=self.device)
@@ -152,6 +146,23 @@ class GradClipper:
         _check_current(self.device, "clipper")
         B.moe_grad_norm(self._grads, self.n, self.max_norm, self.norm, self.ws, self.ws_bytes, stream)
         return self.norm
+
+
+class GradClipper(_GradNorm):
+    """The norm of the given gradients together, and clipping by it: moe_grad_norm, moe_grad_clip.
+
+    grads: contiguous fp32 or bf16 tensors, read where they lie at every call (a layer's gradient
+    buffers).  max_norm: infinite measures alone.  out: where the clipped gradients go, tensors like
+    grads (None: in place), none of which may overlap another or another's gradient.  ``norm`` holds the
+    norm and the scale min(1, max_norm / norm) of the last call, on the GPU; a norm that is not finite
+    has the scale NaN and clips nothing."""
+
+    def __init__(self, grads, max_norm, out=None):
+        grads = list(grads)
+        out = grads if out is None else list(out)
+        super().__init__(grads, max_norm, out)
+        _disjoint("outputs", out)
+        _apart("output", out, grads)
 
     def clip(self, stream=None):
         """[norm, scale], and the gradients clipped."""
@@ -165,7 +176,7 @@ class AdamW:
     (max_norm; None: as they are).
 
     theta, m, v: lists of fp32 tensors, updated in place; grads: fp32 or bf16, read where they lie
-    at every step; theta_bf16: a list of bf16 tensors (or of None among them) that receive the
+    at every step (one that is given to several parameters counts as often in the norm); theta_bf16: a list of bf16 tensors (or of None among them) that receive the
     updated parameters.  weight_decay and lr_scale: a number, or one for each tensor.  ``norm`` holds
     the last step's [norm, scale]; a step whose norm is not finite changes nothing."""
 
@@ -196,8 +207,8 @@ class AdamW:
         _disjoint("tensors", theta + self.m + self.v + low)
         _apart("tensor", theta + self.m + self.v + low, [None] * (4 * n) + grads)
         self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
-        self._clipper = None if max_norm is None else GradClipper(grads, max_norm)
-        self.norm = None if max_norm is None else self._clipper.norm
+        self._measured = None if max_norm is None else _GradNorm(grads, max_norm)
+        self.norm = None if max_norm is None else self._measured.norm
         self._held = theta, grads, low  # (the library keeps addresses only)
         p = B._ptr
         self._tensors = (B.moe_adamw_tensor * n)(*[
@@ -208,8 +219,8 @@ class AdamW:
     def step(self, t, lr, stream=None):
         """Step t (1 for the first) at rate lr; returns [norm, scale] (None without max_norm)."""
         _check_current(self.device, "optimiser")
-        if self._clipper is not None:
-            self._clipper.measure(stream)
+        if self._measured is not None:
+            self._measured.measure(stream)
         B.moe_adamw_steps(self._tensors, self.n, int(t), float(lr), *self.betas, self.eps, self.norm,
                           stream)
         return self.norm
