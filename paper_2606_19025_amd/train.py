@@ -176,9 +176,11 @@ class AdamW:
     (max_norm; None: as they are).
 
     theta, m, v: lists of fp32 tensors, updated in place; grads: fp32 or bf16, read where they lie
-    at every step (one that is given to several parameters counts as often in the norm); theta_bf16: a list of bf16 tensors (or of None among them) that receive the
-    updated parameters.  weight_decay and lr_scale: a number, or one for each tensor.  ``norm`` holds
-    the last step's [norm, scale]; a step whose norm is not finite changes nothing."""
+    at every step (one that is given to several parameters counts as often in the norm); theta_bf16:
+    a list of bf16 tensors (or of None among them) that receive the updated parameters.  All are
+    16-byte aligned (``GradClipper`` takes gradients as they lie).  weight_decay and lr_scale: a
+    number, or one for each tensor.  ``norm`` holds the last step's [norm, scale]; a step whose norm
+    is not finite changes nothing."""
 
     def __init__(self, theta, grads, m=None, v=None, theta_bf16=None, max_norm=None,
                  betas=(0.9, 0.95), eps=1e-8, weight_decay=0.0, lr_scale=1.0):
@@ -204,6 +206,10 @@ class AdamW:
                 _check_tensor(f"gradient {i}", g, t.shape, torch.bfloat16, dev, "optimiser")
             if low[i] is not None:
                 _check_tensor(f"theta_bf16 {i}", low[i], t.shape, torch.bfloat16, dev, "optimiser")
+            for name, u in (("parameter", t), ("gradient", g), ("m", self.m[i]), ("v", self.v[i]),
+                            ("theta_bf16", low[i])):
+                if u is not None and u.data_ptr() % 16:
+                    raise ValueError(f"{name} {i} must be 16-byte aligned")
         _disjoint("tensors", theta + self.m + self.v + low)
         _apart("tensor", theta + self.m + self.v + low, [None] * (4 * n) + grads)
         self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)

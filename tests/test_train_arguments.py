@@ -31,3 +31,21 @@ def test_a_gradient_given_to_several_parameters_counts_as_often(gpu_lib, dtype):
     # the norm's rounding to fp32 over its fp64 sum
     ref = math.sqrt(2 * float((grad.double() ** 2).sum()))
     assert abs(n[0].item() - ref) <= 1.001 * 2.0 ** -24 * ref
+
+
+def test_misaligned_tensors_are_refused_at_construction():
+    """All that the optimiser reads and writes is 16-byte aligned; a list that is not is no list for it."""
+    at = lambda dtype, k: torch.zeros(16, dtype=dtype)[k:k + 8]
+    good = lambda: dict(theta=[at(F32, 0), at(F32, 4)], grads=[at(F32, 8), at(BF, 8)],
+                        m=[at(F32, 4), at(F32, 0)], v=[at(F32, 0), at(F32, 0)], theta_bf16=[None, at(BF, 0)])
+    AdamW(**good())
+    for name, dtype, k in (("theta", F32, 1), ("theta", F32, 2), ("grads", F32, 3), ("grads", BF, 4),
+                           ("grads", BF, 1), ("m", F32, 1), ("v", F32, 6), ("theta_bf16", BF, 2)):
+        for max_norm in (None, 1.0):
+            bad = good()
+            bad[name][1] = at(dtype, k)
+            with pytest.raises(ValueError):
+                AdamW(**bad, max_norm=max_norm)
+    empty = torch.zeros(16)[1:1]  # (no values: nothing is read)
+    assert empty.numel() == 0
+    AdamW([empty], [empty])
