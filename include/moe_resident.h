@@ -471,8 +471,10 @@ int moe_block_norm_bwd(const moe_block_norm* p, hipStream_t stream);
  * and rounded after the sum.  loss and total are not read.
  * ws: device workspace (256-byte aligned) of at least moe_xent_fwd_workspace_size(p) or
  * moe_xent_bwd_workspace_size(p) bytes (which depend on the sizes and types alone and on the
- * current device's compute-unit count; the backward's holds dz of 256 MiB, or of 256 words, at most, up
- * to 256 MiB of partial sums, two copies of x and one of dx in fp32); its contents on entry are ignored.
+ * current device's compute-unit count; the forward's holds a copy of x, and 8 bytes for each token and half a
+ * tile's words: V / 128 halves in the largest tiles, V / 32 in the smallest; the backward's dz of 256 MiB, or of
+ * 256 words, at most, up to 256 MiB of partial sums, two copies of x and one of dx in fp32); its contents on
+ * entry are ignored.
  * Two calls may share it only if they are ordered on a stream.
  * Limits: 0 <= N < 2^23, N d below 2^31 - 16 (rows are addressed with 32-bit byte offsets), 1 <= V < 2^30,
  * d <= 2^16, bf16: d % 64 == 0, fp32: d % 8 == 0; scale finite and not 0, z_coef finite; x, w, dx and dw

@@ -346,7 +346,7 @@ struct Plan {
   // fp32).  In dz, which is rounded, g q is off alike in all products of the token that matter: dx by 1.45
   // times a bf16 output's own rounding (now 1.0), dW by 1.43 to 1.50 times it (now 1.41).
   bool fold;
-  int parts;           // partials of a row, at most
+  int parts;           // partials of a row of the forward: two of each tile of columns
 };
 
 constexpr size_t kDzBytes = (size_t)256 << 20;  // dz of a piece, at most (or of kPad columns)
@@ -428,12 +428,12 @@ Plan plan_of(const moe_xent& x, bool bwd) {
       std::max<size_t>(kPad, std::min(((size_t)2 << 30) / ((size_t)x.d * 4),
                                       ((size_t)1 << 23) / (size_t)std::max(1, ceil_div(x.N, 32)) * 64) / kPad * kPad);
   p.fwd_piece = (int)std::min<size_t>(most_w, (size_t)width);
-  p.parts = ceil_div(x.V, 64) * 2 + 2;
   GemmArgs z{}, dx{}, dw{};
   z.n_groups = dx.n_groups = dw.n_groups = 1;
   z.cap = dx.cap = dw.cap = x.N;
   z.N = std::min(x.V, p.fwd_piece); z.K = x.d;
   p.logits = bf16 ? xent_logit_tiles(z) : f32_tiles((double)ceil_div(x.N, 64) * ceil_div(z.N, 128));
+  p.parts = ceil_div(x.V, tile_cols(p.logits)) * 2;  // (pieces are whole tiles)
   if (!bwd) return p;
   p.two = bf16 && x.N <= kTwo;
   if (p.two && p.logits == TILE_256x256) p.logits = TILE_64x128;  // (which write both)
