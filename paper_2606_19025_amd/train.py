@@ -104,10 +104,12 @@ class LinearCrossEntropy:
             _check_tensor("dloss", dloss, (self.N,), torch.float32, self.device, "loss")
         if self.ws_bwd is None:
             with _on(stream):
-                self.ws_bwd, self.ws_bwd_bytes = self._workspace(B.moe_xent_bwd_workspace_size, a)
-                self.dx = torch.empty(self.N, self.d, dtype=self.dtype, device=self.device)
-                self.dw = torch.zeros(self.V, self.d, dtype=self.dw_dtype, device=self.device)
-            a.dx, a.dw = self.dx.data_ptr(), self.dw.data_ptr()
+                ws, n = self._workspace(B.moe_xent_bwd_workspace_size, a)
+                dx = torch.empty(self.N, self.d, dtype=self.dtype, device=self.device)
+                dw = torch.zeros(self.V, self.d, dtype=self.dw_dtype, device=self.device)
+            # (all of them or none: a call without memory for one leaves the object as it was)
+            self.dx, self.dw, self.ws_bwd, self.ws_bwd_bytes = dx, dw, ws, n
+            a.dx, a.dw = dx.data_ptr(), dw.data_ptr()
         a.dloss, a.accumulate_dw = B._ptr(dloss), int(accumulate_dw)
         a.ws, a.ws_bytes = self.ws_bwd.data_ptr(), self.ws_bwd_bytes
         B.moe_xent_bwd(a, stream)
