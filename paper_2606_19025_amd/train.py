@@ -55,7 +55,8 @@ class LinearCrossEntropy:
     lse, returns ``dx`` with ``dw`` beside it, fp32 or of the weights' type (dw_dtype).  The buffers
     are the object's own and are reused by the next call: calls on different streams need one each,
     and a call on another stream than the one current at construction has to be ordered behind it.
-    dw and the workspaces are made by the first call that needs them, dw as zeros."""
+    dx, dw and the workspaces are made by the first call that needs them, dw as zeros where that call
+    adds to it; one that is captured may not be the first and add."""
 
     def __init__(self, N, d, V, dtype=torch.bfloat16, scale=1.0, z_coef=0.0, dw_dtype=torch.float32,
                  device="cuda"):
@@ -106,7 +107,11 @@ class LinearCrossEntropy:
             with _on(stream):
                 ws, n = self._workspace(B.moe_xent_bwd_workspace_size, a)
                 dx = torch.empty(self.N, self.d, dtype=self.dtype, device=self.device)
-                dw = torch.zeros(self.V, self.d, dtype=self.dw_dtype, device=self.device)
+                if accumulate_dw and torch.cuda.is_current_stream_capturing():
+                    # (the graph would set dw to zero again at each replay)
+                    raise ValueError("a captured backward adds to a dw that an earlier call has made")
+                make = torch.zeros if accumulate_dw else torch.empty
+                dw = make(self.V, self.d, dtype=self.dw_dtype, device=self.device)
             # (all of them or none: a call without memory for one leaves the object as it was)
             self.dx, self.dw, self.ws_bwd, self.ws_bwd_bytes = dx, dw, ws, n
             a.dx, a.dw = dx.data_ptr(), dw.data_ptr()
