@@ -26,6 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxChunk = 16384;
+constexpr int kMostChunks = 1 << 30;  // of a launch: those of the largest tensor
 
 // Tensors of a launch: their pointers, the chunks before each, and the values of each one's last
 // chunk less one, with the type in the top bit (14 or 22 bytes a tensor, so that a launch takes as
@@ -200,9 +201,10 @@ hipError_t for_tables(const moe_grad* g, int n, F&& f) {
   t.first[0] = 0;
   for (int i = 0; i <= n; ++i) {
     const bool end = i == n;
-    // (a launch's chunks are counted in 31 bits: a tensor that does not fit opens the next)
+    // (a launch's chunks, and a block's steps past the last of them, are counted in 31 bits: a tensor that
+    // does not fit opens the next)
     const int64_t chunks = end ? 0 : (int64_t)((g[i].n + t.chunk - 1) / t.chunk);
-    if (t.count > 0 && (end || t.count == T::kTensors || t.first[t.count] + chunks > INT32_MAX)) {
+    if (t.count > 0 && (end || t.count == T::kTensors || t.first[t.count] + chunks > kMostChunks)) {
       if (const hipError_t e = f(t, chunk_blocks(t.first[t.count])); e != hipSuccess) return e;
       t.count = 0;
     }

@@ -256,9 +256,10 @@ hipError_t launch_adamw_steps(const moe_adamw_tensor* p, int n, float lr, float 
   t.first[0] = 0;
   for (int i = 0; i <= n; ++i) {
     const bool end = i == n;
-    // (a launch's chunks are counted in 31 bits: a tensor that does not fit opens the next)
+    // (a launch's chunks, and a block's steps past the last of them, are counted in 31 bits: a tensor that
+    // does not fit opens the next)
     const int64_t chunks = end ? 0 : (int64_t)((p[i].n + t.chunk - 1) / t.chunk);
-    if (t.count > 0 && (end || t.count == kAdamTensors || t.first[t.count] + chunks > INT32_MAX)) {
+    if (t.count > 0 && (end || t.count == kAdamTensors || t.first[t.count] + chunks > 1 << 30)) {
       const int blocks = std::min(t.first[t.count], few ? 2 * num_cus() : 8192);
       MOE_TIMED("adamw_steps", s, adamw_steps_kernel<<<blocks, 256, 0, s>>>(t, norm));
       if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
