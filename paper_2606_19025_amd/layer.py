@@ -480,11 +480,13 @@ class PeriNormMoELayer:
 
     forward returns (x', u'), which the next block takes (u': None with ``pre=False``, behind the
     last block); backward takes their gradients (du', dres) and returns those of u and x, which the
-    block before takes as its own.  ``layer`` and ``norm`` hold the outputs and gradients."""
+    block before takes as its own.  ``layer`` and ``norm`` hold the outputs and gradients.  gate is the
+    block's (``BlockNorm``); router_gate is the layer's own argument of that name."""
 
     def __init__(self, T, d, E, k, H, resident, dtype=torch.bfloat16, pre=True, gate=None,
-                 norm_bias=True, scale=1.0, eps=1e-5, device="cuda", **kw):
-        self.layer = ResidentMoELayer(T, d, E, k, H, resident, dtype=dtype, device=device, **kw)
+                 norm_bias=True, scale=1.0, eps=1e-5, device="cuda", router_gate="softmax_topk", **kw):
+        self.layer = ResidentMoELayer(T, d, E, k, H, resident, dtype=dtype, device=device,
+                                      gate=router_gate, **kw)
         self.norm = BlockNorm(T, d, dtype=dtype, pre=pre, gate=gate, bias=norm_bias, scale=scale,
                               eps=eps, device=device)
 
