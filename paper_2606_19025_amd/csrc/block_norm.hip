@@ -293,8 +293,9 @@ __global__ __launch_bounds__(1024) void block_norm_fwd_wide_kernel(BlockArgs a) 
 }
 
 // Rows of up to 8 values a lane, backward.  A block's groups take rows as in the forward; the
-// next rows' arrays come by DMA into LDS (16 KB of bf16 a row of 2048, no registers; where LDS holds one round alone, fp32 rows past 4096: once it has been read).  Weights stay in
-// registers: a load of them in the loop would wait for the DMA before it.
+// next rows' arrays come by DMA into LDS (16 KB of bf16 a row of 2048, no registers; where LDS holds one
+// round alone, fp32 rows past 4096: once it has been read).  Weights stay in registers: a load of them in the
+// loop would wait for the DMA before it.
 // One block a CU (a second one's partial rows cost more than it hides: 8192 x 2048 48 -> 55 us).
 // Instead of this, a block of four waves for each row, the next one's loads in registers: 8192 x 2048 58
 // us, 16384 x 4096 188 (now 155).

@@ -474,8 +474,9 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
   static_assert(Cfg<KA>::LDS == Cfg<KB>::LDS, "one LDS ring size per launch");
   constexpr int NW = 8, MI = Cfg<KA>::MI, NJ = Cfg<KA>::NJ, WM = Cfg<KA>::WM;
   // The logits' kinds spend their epilogue on arithmetic and leave the ring alone, so that the next
-  // tile's first k-steps are loaded under it; what their rows need (label, lse, coefficient) comes with
-  // those, and dz is staged in 2 KB of a wave's own, 16 rows by 64 columns at a time.
+  // tile's first k-steps are loaded under it; what their rows need (label, lse, coefficient) is asked for
+  // ahead of those (of the label the waves that load it wait for at once, as v0 is taken from it: a memory
+  // latency at each tile), and dz is staged in 2 KB of a wave's own, 16 rows by 64 columns at a time.
   constexpr bool EARLY = KA == XE_LSE || KA == XE_DZ;
   constexpr int SETS = EARLY ? 1 : kMaxSets;
   __shared__ __attribute__((aligned(1024))) char lds[Cfg<KA>::LDS];
@@ -916,7 +917,9 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_kernel(GemmLaunch L) {
       // in 200 instead of 148 us in about half of the calls.)
       if (dyn && threadIdx.x == 0) nxt = atomicAdd(L.counters + xcd, 1);
 
-      // (every wave passed the last k-step's barrier, after which none reads the ring)
+      // (every wave passed the last k-step's barrier: all that it needs of the ring it has read.  What the last
+      // k32-step reads behind that barrier, a next k-step's fragments, may race with these loads and is never
+      // used: a tile's first fragments are read behind its own barrier)
       if constexpr (EARLY) {
         if (i + per_xcd < total) {
           make_ctx(i + per_xcd, early);

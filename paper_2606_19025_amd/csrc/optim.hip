@@ -19,7 +19,6 @@
 // results are reproducible bit for bit by any fp32 evaluation of the same
 // formulas.  The bf16 working copy that the grouped GEMMs read is written in
 // the same pass (round to nearest even).
-
 #include "common.h"
 #include "kernels.h"
 #include "timing.h"

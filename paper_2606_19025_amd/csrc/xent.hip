@@ -13,10 +13,10 @@
 // vocabulary after the other: the logits again, which end as dz in dtype, then dx and dW of the
 // piece in one launch.  dx is summed over pieces (and parts of K) in fp32 and rounded once.
 //
-// Tokens that do not count (label < 0) are left out of every product: the others' rows are copied
-// together first (where all count, x itself is read), so a padded batch costs what its tokens
-// do, and nothing that stands in a padded row enters a gradient.  How many there are stays on the
-// device, as in the dispatch.
+// Tokens that do not count (label < 0) are left out of every product (but the forward's of up to kFew
+// tokens): the others' rows are copied together first (where all count, x itself is read), so a padded
+// batch costs what its tokens do, and nothing that stands in a padded row enters a gradient.  How many there
+// are stays on the device, as in the dispatch.
 //
 // Bound by the matrix units with many tokens (8192, d = 2048, 49152 words, bf16: forward 1.29 ms, 1.28 PFLOP/s,
 // backward 3.91 ms, 1.27 over its three products; of a library's product of the logits' size alone 1.24) and
@@ -595,8 +595,11 @@ hipError_t launch_xent_fwd(const moe_xent* x, hipStream_t s) {
     MOE_TIMED("xent_none", s, xent_none_kernel<<<1, 64, 0, s>>>(x->total));
     return hipGetLastError();
   }
-  // Few tokens: every row as it is (rows are independent here, and leaving some out saves no tile of 256 or
-  // little of W's stream: 24 tokens 55 -> 51 us, 256 of d = 2048 65 -> 62, half of them left out or none)
+  // Few tokens: every row as it is (rows are independent here).  In bf16 leaving some out saves no tile of 256 and
+  // little of W's stream, less than its launch takes: 24 tokens 55 -> 51 us, 256 of d = 2048 on 49152 words 59 ->
+  // 55, half of them left out 57 -> 54.  In fp32 that holds of small heads (256 of d = 64 on 1000 words 14 -> 11 us,
+  // 512 on 8000 32 -> 29) and of tokens that all count (256 of 2048 on 49152 388 -> 384); the products bound
+  // large ones, whose left-out tokens cost what others do (half of those 256: 384 us, and 210 without them).
   const bool as_is = x->N <= kFew;
   if (!as_is && (e = rows<false>(b, s)) != hipSuccess) return e;
   const int width = tile_cols(p.logits) / 2;  // of a partial: half a tile's columns

@@ -162,7 +162,9 @@ class GradClipper(_GradNorm):
     buffers).  max_norm: infinite measures alone.  out: where the clipped gradients go, tensors like
     grads (None: in place), none of which may overlap another or another's gradient.  ``norm`` holds the
     norm and the scale min(1, max_norm / norm) of the last call, on the GPU; a norm that is not finite
-    has the scale NaN and clips nothing."""
+    has the scale NaN and clips nothing.  The workspace is the object's own: calls on different streams
+    need one each, and a call on another stream than the one current at construction has to be ordered
+    behind it."""
 
     def __init__(self, grads, max_norm, out=None):
         grads = list(grads)
@@ -187,7 +189,8 @@ class AdamW:
     a list of bf16 tensors (or of None among them) that receive the updated parameters.  All are
     16-byte aligned (``GradClipper`` takes gradients as they lie).  weight_decay and lr_scale: a
     number, or one for each tensor.  ``norm`` holds the last step's [norm, scale]; a step whose norm
-    is not finite changes nothing."""
+    is not finite changes nothing.  A step on another stream than the one current at construction,
+    where m and v are set to zero, has to be ordered behind it."""
 
     def __init__(self, theta, grads, m=None, v=None, theta_bf16=None, max_norm=None,
                  betas=(0.9, 0.95), eps=1e-8, weight_decay=0.0, lr_scale=1.0):
